@@ -70,7 +70,7 @@ typedef enum dte_status {
 #define DTE_DEV_OVERFLOW 1u /* more changed elements than `capacity`; lists not produced   */
 #define DTE_DEV_BOUNDS 2u   /* apply met an offset >= numel of its shard, an entry for a NULL
                                shard, or a canonical index outside its tensor; entry skipped */
-#define DTE_DEV_TIMEOUT 4u  /* dte_push_wait gave up; no other kernel of this library waits   */
+#define DTE_DEV_TIMEOUT 4u  /* dte_push_wait gave up, or a matrix kernel's wait for its own copies did */
 #define DTE_DEV_CORRUPT 8u  /* unpack rejected a chunk (header or checksum); lists have holes */
 
 /* Source tensor p of the canonical training-side space: fp32, row-major.  ndim is 1 or 2;
@@ -411,6 +411,124 @@ DTE_API dte_status dte_extract_delta_host(const dte_layout* layout, const float*
                                   void* workspace, uint64_t workspace_bytes, const dte_delta* out,
                                   uint32_t* offsets_h, uint16_t* values_h, uint64_t* list_ptr_h,
                                   uint64_t* counters_h, void* cuda_stream);
+
+/* ---- Operators at the two ends of the model -----------------------------------------------------
+ * The transfer moves what one training step changed; these are the parts of that step that own the
+ * two vocabulary tensors and the norm weights, and the parts a receiver needs to score tokens with
+ * the shards it holds: embedding lookup, layer / RMS norm, and the softmax cross entropy of a linear
+ * head over a large vocabulary whose logits are never stored, each with its gradient.
+ *
+ * Conventions of this section
+ *   - A matrix is row-major with unit column stride; row r starts at data + r * ld elements.  Inputs
+ *     may have any ld (0: one row broadcast to all); outputs need ld >= cols, and may overlap neither
+ *     the inputs nor each other.  Any alignment of the element type is accepted unless stated
+ *     otherwise; 16-byte aligned data with rows a multiple of 16 bytes apart takes the vector path.
+ *   - Element types: DTE_F32 and DTE_BF16 for numbers, DTE_I32 and DTE_I64 for token ids.  Sums,
+ *     softmax statistics and norm statistics are fp32 whatever the types; results are rounded once.
+ *   - Every operator enqueues kernels (and memsets) only: no allocation, no synchronisation, no state
+ *     kept between calls, so a call can be captured into a CUDA graph.  Scratch is the caller's
+ *     `workspace` (device memory, 256-byte aligned); its contents do not matter before a call and mean
+ *     nothing after it, and one workspace must not serve two calls that can overlap.
+ *   - Deterministic: no sum depends on the order in which threads run.
+ *   - `device` is the CUDA device of all pointers and of the stream.
+ *   - flags: optional device word; DTE_DEV_BOUNDS is OR-ed in if an id or target is >= `vocab`
+ *     (it is then treated as belonging to no shard), DTE_DEV_TIMEOUT if a kernel's internal wait ran
+ *     out (the outputs are then not usable).  The caller clears it.
+ *   - Vocabulary-parallel use: a call works on rows [row_start, row_start + rows) of a vocabulary of
+ *     `vocab` entries, as a receiver's shard holds them; ids outside the range belong to another rank. */
+#define DTE_F32 0u
+#define DTE_BF16 1u
+#define DTE_I32 2u
+#define DTE_I64 3u
+
+typedef struct dte_matrix {
+    void* data;
+    uint64_t rows, cols, ld;
+    uint32_t dtype;
+    uint32_t reserved;
+} dte_matrix;
+
+typedef struct dte_ids {
+    const void* data;
+    uint64_t count;
+    uint32_t dtype;
+    uint32_t reserved;
+} dte_ids;
+
+/* out[n] = scale * table[ids[n] - row_start]; a zero row where the id is negative (padding) or not in
+ * this shard.  table.cols == out.cols, out.rows == ids.count; table and out types are independent. */
+DTE_API dte_status dte_embedding_forward(const dte_matrix* table, const dte_ids* ids, uint64_t row_start,
+                                         uint64_t vocab, double scale, const dte_matrix* out, uint64_t* flags,
+                                         int device, void* cuda_stream);
+
+/* dtable[v] = scale * sum of dout[n] over the n with ids[n] == row_start + v, added up in order of n in
+ * blocks (dout rows of padding and of other shards are not read).  accumulate != 0 adds to what
+ * dtable holds, and rows without a token are not touched; otherwise every row is written, zeros
+ * included.  ids.count < 2^31, dtable.rows < 2^31. */
+DTE_API uint64_t dte_embedding_backward_workspace_bytes(uint64_t n_ids, uint64_t hidden);
+DTE_API dte_status dte_embedding_backward(const dte_matrix* dout, const dte_ids* ids, uint64_t row_start,
+                                          uint64_t vocab, double scale, int accumulate, const dte_matrix* dtable,
+                                          void* workspace, uint64_t workspace_bytes, uint64_t* flags, int device,
+                                          void* cuda_stream);
+
+/* Norm over the columns of each row.
+ *   DTE_NORM_LAYER: y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   DTE_NORM_RMS  : y = x * rstd * weight + bias,          rstd = 1 / sqrt(mean(x^2) + eps)
+ * weight (NULL: ones) and bias (NULL: none) hold x.cols values of type param_dtype.  out has x's type.
+ * mean (DTE_NORM_LAYER only) and rstd, one fp32 per row, are what the backward pass reads; either may
+ * be NULL. */
+#define DTE_NORM_LAYER 0u
+#define DTE_NORM_RMS 1u
+DTE_API dte_status dte_norm_forward(const dte_matrix* x, const void* weight, const void* bias, uint32_t param_dtype,
+                                    uint32_t kind, double eps, const dte_matrix* out, float* mean, float* rstd,
+                                    int device, void* cuda_stream);
+
+/* Gradients of dte_norm_forward from dout and the saved statistics, with g = dout * weight and
+ * xhat = (x - mean) * rstd:
+ *   dx = rstd * (g - [DTE_NORM_LAYER: mean(g)] - xhat * mean(g * xhat))
+ *   dweight = sum over rows of dout * xhat,  dbias = sum over rows of dout      (fp32, x.cols values)
+ * dx (x's type), dweight and dbias may be NULL when not wanted; accumulate != 0 adds to dweight and
+ * dbias.  dout and dx have x's type. */
+DTE_API uint64_t dte_norm_backward_workspace_bytes(uint64_t rows, uint64_t hidden);
+DTE_API dte_status dte_norm_backward(const dte_matrix* dout, const dte_matrix* x, const void* weight,
+                                     uint32_t param_dtype, uint32_t kind, const float* mean, const float* rstd,
+                                     int accumulate, const dte_matrix* dx, float* dweight, float* dbias,
+                                     void* workspace, uint64_t workspace_bytes, int device, void* cuda_stream);
+
+/* Softmax cross entropy of z = logit_scale * x . weight^T without storing z.  x: tokens x hidden,
+ * weight: rows [vocab_start, vocab_start + weight.rows) of the head, both BF16; hidden a multiple of 8,
+ * weight.data 16-byte aligned and weight.ld a multiple of 8 (>= cols): its rows go through the tensor memory
+ * accelerator.  logit_scale > 0.  targets: one id per token; a negative one (ignored token) gives
+ * lse = target_logit = loss = 0 and no gradient, and that row of x is never read.
+ *   lse[n] = log sum_v exp z[n][v] over this shard's rows
+ *   target_logit[n] = z[n][target], 0 where the target belongs to another shard
+ *   loss[n] = lse[n] - target_logit[n]       (the loss itself when the shard is the whole vocabulary;
+ *             else combine: lse = log sum over ranks of exp(lse), target_logit = sum over ranks)
+ * All three fp32, one per token; target_logit and loss may be NULL. */
+DTE_API uint64_t dte_linear_ce_forward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden);
+DTE_API dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets,
+                                         uint64_t vocab_start, uint64_t vocab, double logit_scale, float* lse,
+                                         float* target_logit, float* loss, void* workspace, uint64_t workspace_bytes,
+                                         uint64_t* flags, int device, void* cuda_stream);
+
+/* Gradients for a given dloss[n] (fp32), with lse over the WHOLE vocabulary (all ranks combined) and
+ * p = exp(z - lse):
+ *   dx[n]      = logit_scale * dloss[n] * (sum_v p[n][v] weight[v] - weight[target])        (BF16; with a
+ *                vocabulary shard: this rank's share, to be summed over ranks)
+ *   dweight[v] = logit_scale * (sum_n dloss[n] p[n][v] x[n] - sum over target[n] == v of dloss[n] x[n])
+ * dx or dweight may be NULL.  dweight: BF16 or FP32; accumulate != 0 adds to it.  The logits are recomputed
+ * in pieces of the vocabulary; a piece's dloss * p is kept in the workspace as BF16, the operand type of
+ * the two products that consume it, and the target terms stay fp32.  dx and dweight rows need 16-byte
+ * alignment (data and ld).  A workspace of dte_linear_ce_backward_workspace_bytes holds pieces of the
+ * size that measured best; any workspace from dte_linear_ce_backward_workspace_min_bytes up is accepted
+ * and gives smaller pieces. */
+DTE_API uint64_t dte_linear_ce_backward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden);
+DTE_API uint64_t dte_linear_ce_backward_workspace_min_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden);
+DTE_API dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets,
+                                          uint64_t vocab_start, uint64_t vocab, double logit_scale, const float* lse,
+                                          const float* dloss, int accumulate, const dte_matrix* dx,
+                                          const dte_matrix* dweight, void* workspace, uint64_t workspace_bytes,
+                                          uint64_t* flags, int device, void* cuda_stream);
 
 /* Static strings. */
 DTE_API const char* dte_status_string(dte_status s);

@@ -29,6 +29,10 @@ SYMBOLS = [
     "dte_op_counts", "dte_layout_num_ops", "dte_chunk_count_bound", "dte_chunk_bytes_bound",
     "dte_pack_chunks", "dte_unpack_chunks", "dte_apply_canonical", "dte_extract_delta_push",
     "dte_push_wait", "dte_layout_num_receivers", "dte_layout_receiver_num_ops",
+    "dte_embedding_forward", "dte_embedding_backward", "dte_embedding_backward_workspace_bytes",
+    "dte_norm_forward", "dte_norm_backward", "dte_norm_backward_workspace_bytes",
+    "dte_linear_ce_forward", "dte_linear_ce_forward_workspace_bytes", "dte_linear_ce_backward",
+    "dte_linear_ce_backward_workspace_bytes", "dte_linear_ce_backward_workspace_min_bytes",
 ]
 
 
@@ -128,6 +132,21 @@ def lib() -> C.CDLL:
         L.dte_extract_delta_host.argtypes = [vp, vp, vp, vp, i64, dbl, dbl, dbl, dbl, dbl, vp, u64,
                                              vp, vp, vp, vp, vp, vp]
         L.dte_extract_delta_host.restype = C.c_int
+        i, u32 = C.c_int, C.c_uint32
+        L.dte_embedding_forward.argtypes = [vp, vp, u64, u64, dbl, vp, vp, i, vp]
+        L.dte_embedding_backward.argtypes = [vp, vp, u64, u64, dbl, i, vp, vp, u64, vp, i, vp]
+        L.dte_norm_forward.argtypes = [vp, vp, vp, u32, u32, dbl, vp, vp, vp, i, vp]
+        L.dte_norm_backward.argtypes = [vp, vp, vp, u32, u32, vp, vp, i, vp, vp, vp, vp, u64, i, vp]
+        L.dte_linear_ce_forward.argtypes = [vp, vp, vp, u64, u64, dbl, vp, vp, vp, vp, u64, vp, i, vp]
+        L.dte_linear_ce_backward.argtypes = [vp, vp, vp, u64, u64, dbl, vp, vp, i, vp, vp, vp, u64, vp, i, vp]
+        for name in ("dte_embedding_forward", "dte_embedding_backward", "dte_norm_forward", "dte_norm_backward",
+                     "dte_linear_ce_forward", "dte_linear_ce_backward"):
+            getattr(L, name).restype = i
+        for name, n_args in (("dte_embedding_backward_workspace_bytes", 2), ("dte_norm_backward_workspace_bytes", 2),
+                             ("dte_linear_ce_forward_workspace_bytes", 3), ("dte_linear_ce_backward_workspace_bytes", 3),
+                             ("dte_linear_ce_backward_workspace_min_bytes", 3)):
+            getattr(L, name).argtypes = [u64] * n_args
+            getattr(L, name).restype = u64
         L.dte_status_string.argtypes = [C.c_int]
         L.dte_status_string.restype = C.c_char_p
         L.dte_last_error.argtypes = []

@@ -1,0 +1,1014 @@
+// Softmax cross entropy of a linear head over a large vocabulary, without storing the logits, and its
+// gradient.  z = s x W^T;  lse = log sum_v exp z_v;  with p = exp(z - lse), f = s * dloss:
+//   dx = f (p W - W[target]),   dW = (f p)^T x - (rows of f x, added up by target).
+//
+// Bound by the tensor cores (2 tokens V hidden operations forward, 6 backward: the logits are made
+// again rather than kept) for more than a few hundred tokens, by reading W for a few.  One persistent
+// tcgen05 kernel serves all four products; what differs is how its operands lie in memory and what its
+// epilogue does with a finished tile of accumulators:
+//   kLse   logits tile -> per row the maximum and the sum of exponentials of its columns (registers only)
+//   kProb  logits tile -> f p as bf16, for one piece of the vocabulary
+//   kDx    piece of f p times W: adds to fp32 sums over pieces
+//   kDw    (f p)^T x: complete for the piece's vocabulary rows, less the target term, rounded and written
+// Tokens without a target are dropped before the first product: the rows that count are copied together,
+// so prompts cost nothing and what their rows hold (NaN included) reaches no sum.  The target term
+// stays out of the bf16 operand f p: it is the largest entry of its row by far, and its rounding would
+// be most of the gradient's error; both gradients take it in fp32 instead.
+#include <atomic>
+
+#include "dte_mma.cuh"
+#include "dte_ops.cuh"
+
+namespace dte {
+
+enum CeKind { kLse = 0, kProb = 1, kDx = 2, kDw = 3 };
+
+constexpr uint32_t kTileM = 128;                 // accumulator rows of one CTA: the 128 lanes of tensor memory
+constexpr uint32_t kTileK = 64;                  // 128 bytes of bf16: one swizzle row
+constexpr uint32_t kMaxTileN = 256;
+constexpr uint32_t kCeThreads = 192;             // TMA warp, MMA warp, four epilogue warps
+constexpr uint32_t kStageBytesA = kTileM * kTileK * 2;
+constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one is filled while the other is drained
+constexpr uint64_t kPadRows = 256;               // token rows are padded to this, with zero rows
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+// Work is split for this many SMs whatever the device has, so that results do not depend on it.
+constexpr uint32_t kSplitSms = 148;
+
+template <int CTAS>
+struct CeStage {
+    static constexpr uint32_t kBytesB = kMaxTileN / CTAS * kTileK * 2;
+    static constexpr uint32_t kBytes = kStageBytesA + kBytesB;
+    static constexpr uint32_t kStages = CTAS == 2 ? 6 : 4;
+    static constexpr uint32_t kSmem = kStages * kBytes + 1024 + 256;
+};
+
+struct CeParams {
+    uint32_t m, n, k;            // extents; the one that counts tokens is replaced by *tokens
+    const uint32_t* tokens;      // tokens that count
+    uint32_t tile_n, splits;
+    uint32_t w_row;              // first row of W of this piece
+    uint64_t* flags;
+    // kLse, kProb
+    float k2;                    // logit_scale * log2(e): accumulators -> base-2 exponents
+    float scale;
+    const int32_t* target;       // row of this shard, or -1
+    float2* stats;               // kLse: (maximum, sum) per tile of columns and token
+    uint64_t stats_ld;
+    float* target_logit;
+    const float* f;              // kProb: logit_scale * dloss per token
+    const float* neg_lse2;       //        -lse * log2(e)
+    __nv_bfloat16* prob;         //        tokens x prob_ld
+    uint64_t prob_ld;
+    // kDx
+    float* dx_sum;               // splits x padded tokens x hidden
+    uint64_t dx_split;           // elements of one split's part
+    bool add;
+    // kDw
+    void* dweight;
+    uint64_t dweight_ld;
+    bool dweight_bf16, accumulate;
+    const uint32_t* slot;
+    const float* target_sum;
+};
+
+// Position of a tile in the order in which CTAs take them: groups of `group` rows of tiles, and inside a
+// group the row index runs fastest, so that the CTAs at work share few rows and few columns in L2.
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t group, uint32_t* split,
+                                        uint32_t* tm, uint32_t* tn) {
+    const uint32_t per_split = tiles_m * tiles_n;
+    *split = t / per_split;
+    t -= *split * per_split;
+    const uint32_t g = t / (group * tiles_n);
+    t -= g * group * tiles_n;
+    const uint32_t rows = min(group, tiles_m - g * group);
+    *tm = g * group + t % rows;
+    *tn = t / rows;
+}
+
+__device__ __forceinline__ void load_tile(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    tmem_load32(addr, r);
+    tmem_load_wait(r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+template <int KIND>
+__device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, uint32_t row, uint32_t tn, uint32_t split,
+                                            uint32_t tokens, bool empty) {
+    const uint32_t n0 = tn * p.tile_n;
+    if (KIND == kLse) {
+        const bool valid = row < tokens;
+        const int64_t tcol = valid ? (int64_t)p.target[row] - n0 : -1;
+        float top = -INFINITY, sum = 0.f;
+        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+            if (n0 + c >= p.n) break;
+            float v[32];
+            load_tile(tmem + c, v);
+            const bool mine = tcol >= (int64_t)c && tcol < (int64_t)c + 32;
+            if (__any_sync(0xFFFFFFFFu, mine)) {
+                float at = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) at = tcol == (int64_t)(c + j) ? v[j] : at;
+                if (mine) p.target_logit[row] = at * p.scale;
+            }
+            const uint32_t left = p.n - (n0 + c);
+            if (left < 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j >= (int)left) v[j] = -INFINITY;
+            }
+            float peak = v[0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) peak = fmaxf(peak, v[j]);
+            const float now = fmaxf(top, peak * p.k2);
+            // nothing but -inf so far: keep the exponents at -inf instead of forming inf - inf
+            const float from = now == -INFINITY ? 0.f : now;
+            float part = 0.f, part2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                part += exp2_fast(fmaf(v[j], p.k2, -from));
+                part2 += exp2_fast(fmaf(v[j + 1], p.k2, -from));
+            }
+            sum = fmaf(sum, exp2_fast(top - from), part + part2);
+            top = now;
+        }
+        if (valid) p.stats[(uint64_t)tn * p.stats_ld + row] = make_float2(top, sum);
+    } else if (KIND == kProb) {
+        const float f = p.f[row], nl = p.neg_lse2[row];     // zero for padding rows
+        __nv_bfloat16* out = p.prob + (uint64_t)row * p.prob_ld + n0;
+        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+            float v[32];
+            load_tile(tmem + c, v);
+            const uint32_t left = p.n > n0 + c ? p.n - (n0 + c) : 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = f * exp2_fast(fmaf(v[j], p.k2, nl));
+            if (left < 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j >= (int)left) v[j] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 16) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = row < tokens ? pack_bf16(v[j + 2 * i], v[j + 2 * i + 1]) : 0u;
+                store32(out + c + j, w);
+            }
+        }
+    } else if (KIND == kDx) {
+        float* out = p.dx_sum + split * p.dx_split + (uint64_t)row * p.n + n0;
+        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+            if (n0 + c >= p.n) break;
+            float v[32];
+            load_tile(tmem + c, v);
+            if (row < tokens) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    if (n0 + c + j >= p.n) break;
+                    uint32_t w[8];
+                    if (p.add) load32(out + c + j, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float x = empty ? 0.f : v[j + i];
+                        if (p.add) x += __uint_as_float(w[i]);
+                        w[i] = __float_as_uint(x);
+                    }
+                    store32(out + c + j, w);
+                }
+            }
+        }
+    } else {
+        const uint64_t vrow = (uint64_t)p.w_row + row;
+        const bool valid = row < p.m;
+        const uint32_t at = valid ? p.slot[vrow] : kNone;
+        const float* term = p.target_sum + (uint64_t)(at == kNone ? 0 : at) * p.n + n0;
+        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+            if (n0 + c >= p.n) break;
+            float v[32];
+            load_tile(tmem + c, v);
+            if (valid) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    if (n0 + c + j >= p.n) break;
+                    float o[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = empty ? 0.f : v[j + i];
+                    if (at != kNone) {
+                        uint32_t w[8];
+                        load32(term + c + j, w);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) o[i] -= __uint_as_float(w[i]);
+                    }
+                    const uint64_t off = vrow * p.dweight_ld + n0 + c + j;
+                    if (p.dweight_bf16) {
+                        __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.dweight) + off;
+                        Raw8<__nv_bfloat16> r;
+                        if (p.accumulate) {
+                            float old[8];
+                            r.load(d);
+                            r.get(old);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] += old[i];
+                        }
+                        r.set(o);
+                        r.store(d);
+                    } else {
+                        float* d = static_cast<float*>(p.dweight) + off;
+                        Raw8<float> r;
+                        if (p.accumulate) {
+                            float old[8];
+                            r.load(d);
+                            r.get(old);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] += old[i];
+                        }
+                        r.set(o);
+                        r.store(d);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// One CTA (CTAS == 1) or a pair of CTAs on neighbouring SMs (CTAS == 2) per tile of 128 * CTAS rows.  Of a
+// pair, each CTA holds its own 128 rows of A and half of B; the leader's MMA reads both halves, so every byte
+// of B is loaded and stored once per pair.  Barriers: full (leader: both CTAs' loads), empty (each: the stage
+// has been multiplied), done (each: the tile's accumulators are complete), drained (leader: both CTAs'
+// epilogues have read them).
+template <int KIND, int CTAS>
+__global__ void __launch_bounds__(kCeThreads, 1)
+    ce_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CeParams p) {
+    using S = CeStage<CTAS>;
+    constexpr bool kAmn = KIND == kDw, kBmn = KIND == kDx || KIND == kDw;
+    extern __shared__ uint8_t ce_smem_raw[];
+    __shared__ __align__(8) uint64_t s_bar[2 * S::kStages + 5];
+    __shared__ uint32_t s_tmem, s_gave_up;
+
+    const uint32_t stage0 = (smem_addr(ce_smem_raw) + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_addr(s_bar);
+    auto full = [&](uint32_t i) { return bar0 + 8 * i; };
+    auto empty = [&](uint32_t i) { return bar0 + 8 * (S::kStages + i); };
+    auto done = [&](uint32_t i) { return bar0 + 8 * (2 * S::kStages + i); };
+    auto drained = [&](uint32_t i) { return bar0 + 8 * (2 * S::kStages + 2 + i); };
+    const uint32_t last_bar = bar0 + 8 * (2 * S::kStages + 4);
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
+    const bool leader = rank == 0;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&map_a);
+        tma_prefetch_map(&map_b);
+        for (uint32_t i = 0; i < S::kStages; ++i) {
+            mbar_init(full(i), 1);
+            mbar_init(empty(i), 1);
+        }
+        for (uint32_t i = 0; i < 2; ++i) {
+            mbar_init(done(i), 1);
+            mbar_init(drained(i), 4 * CTAS);
+        }
+        mbar_init(last_bar, 1);
+        s_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<CTAS>(smem_addr(&s_tmem), kTmemColumns);
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
+    volatile uint32_t* gave_up = &s_gave_up;
+
+    const uint32_t tokens = *p.tokens;
+    const uint32_t m = KIND == kDw ? p.m : tokens, k = KIND == kDw ? tokens : p.k;
+    const uint32_t tiles_m = (m + kTileM * CTAS - 1) / (kTileM * CTAS), tiles_n = (p.n + p.tile_n - 1) / p.tile_n;
+    const uint32_t total = tiles_m * tiles_n * p.splits;
+    const uint32_t group = 16 / CTAS;
+    const uint32_t blocks_k = (k + kTileK - 1) / kTileK;
+    const uint32_t first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    const uint32_t part_n = p.tile_n / CTAS;             // columns of B in this CTA
+
+    if (warp == 0 && lane == 0) {
+        // ---- loads ----
+        uint32_t stage = 0, phase = 0, issued = 0;
+        bool ok = true;
+        for (uint32_t t = first; t < total && ok; t += step) {
+            uint32_t split, tm, tn;
+            tile_at(t, tiles_m, tiles_n, group, &split, &tm, &tn);
+            const int m0 = (int)((tm * CTAS + rank) * kTileM), n0 = (int)(tn * p.tile_n + rank * part_n);
+            const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
+            for (uint32_t kb = kb0; kb < kb1; ++kb) {
+                if (!(ok = mbar_wait(empty(stage), phase ^ 1, gave_up))) break;
+                const uint32_t a = stage0 + stage * S::kBytes, b = a + kStageBytesA;
+                const uint32_t bar = CTAS == 2 ? cluster_map(full(stage), 0) : full(stage);
+                if (leader) mbar_expect_tx(full(stage), CTAS * (kStageBytesA + part_n * kTileK * 2));
+                const int k0 = (int)(kb * kTileK);
+                if (kAmn) {
+                    tma_load_2d<CTAS>(a, &map_a, m0, k0, bar);
+                    tma_load_2d<CTAS>(a + kStageBytesA / 2, &map_a, m0 + 64, k0, bar);
+                } else {
+                    tma_load_2d<CTAS>(a, &map_a, k0, m0, bar);
+                }
+                if (kBmn) {
+                    for (uint32_t j = 0; j < part_n; j += 64)
+                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, n0 + (int)j, k0 + (int)p.w_row * (KIND == kDx), bar);
+                } else {
+                    tma_load_2d<CTAS>(b, &map_b, k0, n0 + (int)p.w_row, bar);
+                }
+                ++issued;
+                if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+            }
+        }
+        if (!ok && leader) {
+            // a wait ran out: let the copies in flight land (again with a limit) before shared memory goes away
+            for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
+                const uint32_t s = (stage + S::kStages - 1 - i) % S::kStages;
+                const uint32_t ph = s < stage ? phase : phase ^ 1;
+                for (uint32_t tries = 0; tries < kSpinLimit && !mbar_try_wait(full(s), ph); ++tries) {}
+            }
+        }
+    } else if (warp == 1 && lane == 0 && leader) {
+        // ---- matrix products ----
+        const uint32_t desc = mma_desc(kTileM * CTAS, p.tile_n, kAmn, kBmn);
+        const uint32_t chunk = kTileK * 128;              // MN-major: 64 columns x 64 k
+        uint32_t stage = 0, phase = 0, use = 0;
+        bool ok = true;
+        for (uint32_t t = first; t < total && ok; t += step, ++use) {
+            const uint32_t split = t / (tiles_m * tiles_n);
+            const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
+            const uint32_t buf = use & 1, acc = tmem + buf * kMaxTileN;
+            if (!(ok = mbar_wait(drained(buf), ((use >> 1) & 1) ^ 1, gave_up))) break;
+            tc_fence_after();
+            for (uint32_t kb = kb0; kb < kb1; ++kb) {
+                if (!(ok = mbar_wait(full(stage), phase, gave_up))) break;
+                tc_fence_after();
+                const uint32_t a = stage0 + stage * S::kBytes, b = a + kStageBytesA;
+                uint64_t da = operand_desc(a, kAmn ? chunk : 16), db = operand_desc(b, kBmn ? chunk : 16);
+#pragma unroll
+                for (uint32_t i = 0; i < kTileK / 16; ++i) {
+                    mma_bf16<CTAS>(acc, da, db, desc, kb != kb0 || i != 0);
+                    da += kAmn ? 2048 >> 4 : 32 >> 4;      // 16 further along K
+                    db += kBmn ? 2048 >> 4 : 32 >> 4;
+                }
+                mma_commit<CTAS>(empty(stage));
+                if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+            }
+            if (ok) mma_commit<CTAS>(done(buf));
+        }
+        if (!ok) {
+            mma_commit<CTAS>(last_bar);
+            for (uint32_t tries = 0; tries < kSpinLimit && !mbar_try_wait(last_bar, 0); ++tries) {}
+        }
+    } else if (warp >= 2) {
+        // ---- epilogue: warp w may read the quarter w % 4 of tensor memory's lanes ----
+        const uint32_t quarter = warp & 3;
+        uint32_t use = 0;
+        for (uint32_t t = first; t < total; t += step, ++use) {
+            uint32_t split, tm, tn;
+            tile_at(t, tiles_m, tiles_n, group, &split, &tm, &tn);
+            const uint32_t buf = use & 1;
+            const bool ok = mbar_wait(done(buf), (use >> 1) & 1, gave_up);
+            if (__any_sync(0xFFFFFFFFu, !ok)) break;
+            tc_fence_after();
+            const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
+            const uint32_t row = (tm * CTAS + rank) * kTileM + quarter * 32 + lane;
+            ce_epilogue<KIND>(p, tmem + buf * kMaxTileN + (quarter * 32 << 16), row, tn, split, tokens, kb0 == kb1);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(cluster_map(drained(buf), 0));
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();     // the peer may still signal barriers here, or read this CTA's operands
+    tc_fence_after();
+    if (warp == 1) tmem_free<CTAS>(tmem, kTmemColumns);
+    if (threadIdx.x == 0 && *gave_up && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
+}
+
+// ---- before and after the products --------------------------------------------------------------------------
+struct RowsParams {
+    const void* targets;
+    uint32_t targets_dtype, n;
+    int64_t vocab_start, vocab;
+    uint32_t vocab_rows;
+    uint32_t* count;         // tokens that count
+    int32_t* source;         // [i] = token of compact row i
+    int32_t* target;         // [i] = its target as a row of this shard, or -1
+    int32_t* place;          // [token] = compact row or -1 (NULL: not wanted)
+    float *lse, *target_logit, *loss;   // forward: zero for ignored tokens
+    uint64_t* flags;
+};
+
+constexpr int kRowsThreads = 1024;
+
+// Numbers the tokens that count, in order.  One CTA: the list is short next to everything else.
+__global__ void __launch_bounds__(kRowsThreads) ce_rows_kernel(const RowsParams p) {
+    __shared__ uint32_t s_warp[32];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    uint32_t base = 0;
+    bool bad = false;
+    for (uint64_t i0 = 0; i0 < p.n; i0 += kRowsThreads) {
+        const uint64_t i = i0 + threadIdx.x;
+        const int64_t id = i < p.n ? load_id(p.targets, p.targets_dtype, i) : -1;
+        const bool counts = id >= 0;
+        bad |= id >= p.vocab;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts);
+        if (lane == 0) s_warp[warp] = __popc(mask);
+        __syncthreads();
+        uint32_t before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < 32; ++w) {
+            const uint32_t c = s_warp[w];
+            before += w < (int)warp ? c : 0;
+            all += c;
+        }
+        const uint32_t at = base + before + __popc(mask & ((1u << lane) - 1));
+        if (counts) {
+            const uint64_t row = (uint64_t)id - (uint64_t)p.vocab_start;
+            p.source[at] = (int32_t)i;
+            p.target[at] = row < p.vocab_rows ? (int32_t)row : -1;
+        } else if (i < p.n) {
+            if (p.lse) p.lse[i] = 0.f;
+            if (p.target_logit) p.target_logit[i] = 0.f;
+            if (p.loss) p.loss[i] = 0.f;
+        }
+        if (p.place && i < p.n) p.place[i] = counts ? (int32_t)at : -1;
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *p.count = base;
+    if (bad && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
+}
+
+struct GatherRowsParams {
+    const uint32_t* count;
+    const int32_t* source;
+    const __nv_bfloat16* x;
+    uint64_t x_ld;
+    uint32_t hidden;
+    bool vec;
+    __nv_bfloat16* rows;     // padded tokens x hidden
+    float* target_logit;     // forward: cleared (compact order)
+    // backward
+    const float* dloss;
+    const float* lse;
+    float scale;
+    float* f;
+    float* neg_lse2;
+};
+
+// Copies the rows that count together and clears the padding rows up to the next multiple of kPadRows.
+__global__ void __launch_bounds__(256) ce_gather_kernel(const GatherRowsParams p) {
+    const uint32_t count = *p.count, i = blockIdx.x;
+    const uint32_t padded = (uint32_t)((count + kPadRows - 1) / kPadRows * kPadRows);
+    if (i >= padded) return;
+    const bool live = i < count;
+    const uint32_t src = live ? (uint32_t)p.source[i] : 0;
+    __nv_bfloat16* out = p.rows + (uint64_t)i * p.hidden;
+    const __nv_bfloat16* in = p.x + (uint64_t)src * p.x_ld;
+    for (uint32_t c = threadIdx.x * 8; c < p.hidden; c += 256 * 8) {
+        Raw8<__nv_bfloat16> r;
+        if (!live) {
+            r.zero();
+        } else if (p.vec) {
+            r.load(in + c);
+        } else {
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = to_f(in[c + j]);
+            r.set(f);
+        }
+        r.store(out + c);
+    }
+    if (threadIdx.x == 0) {
+        if (p.target_logit) p.target_logit[i] = 0.f;
+        if (p.f) {
+            p.f[i] = live ? p.scale * p.dloss[src] : 0.f;
+            p.neg_lse2[i] = live ? -p.lse[src] * kLog2e : 0.f;
+        }
+    }
+}
+
+struct CombineParams {
+    const uint32_t* count;
+    const int32_t* source;
+    const float2* stats;
+    uint64_t stats_ld;
+    uint32_t tiles;
+    const float* row_target_logit;
+    float *lse, *target_logit, *loss;
+};
+
+// log-sum-exp of a token from its tiles' statistics: 32 tokens per CTA, 32 threads per token.
+__global__ void __launch_bounds__(1024) ce_combine_kernel(const CombineParams p) {
+    __shared__ float s_top[32][33], s_sum[32][33];
+    const uint32_t count = *p.count, lane = threadIdx.x & 31, part = threadIdx.x / 32;
+    const uint32_t i0 = blockIdx.x * 32;
+    if (i0 >= count) return;
+    float top = -INFINITY, sum = 0.f;
+    auto join = [](float& top, float& sum, float t2, float s2) {
+        const float now = fmaxf(top, t2), from = now == -INFINITY ? 0.f : now;
+        sum = sum * exp2_fast(top - from) + s2 * exp2_fast(t2 - from);
+        top = now;
+    };
+    if (i0 + lane < count) {
+#pragma unroll 4
+        for (uint32_t t = part; t < p.tiles; t += 32) {
+            const float2 v = p.stats[(uint64_t)t * p.stats_ld + i0 + lane];
+            join(top, sum, v.x, v.y);
+        }
+    }
+    s_top[part][lane] = top;
+    s_sum[part][lane] = sum;
+    __syncthreads();
+    top = s_top[lane][part];
+    sum = s_sum[lane][part];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        join(top, sum, t2, s2);
+    }
+    const uint32_t i = i0 + part;
+    if (lane == 0 && i < count) {
+        const float lse = (top + log2f(sum)) * kLn2, at = p.row_target_logit[i];
+        const uint32_t n = (uint32_t)p.source[i];
+        p.lse[n] = lse;
+        if (p.target_logit) p.target_logit[n] = at;
+        if (p.loss) p.loss[n] = lse - at;
+    }
+}
+
+struct DxParams {
+    const int32_t* place;
+    const int32_t* target;
+    const float* f;
+    const float* sums;
+    uint64_t split_elems;
+    uint32_t splits, hidden;
+    const __nv_bfloat16* weight;
+    uint64_t weight_ld;
+    __nv_bfloat16* dx;
+    uint64_t dx_ld;
+};
+
+// dx of every token: its splits' sums less the target's row; zero for ignored tokens.
+__global__ void __launch_bounds__(256) ce_dx_kernel(const DxParams p) {
+    const int32_t i = p.place[blockIdx.x];
+    __nv_bfloat16* out = p.dx + (uint64_t)blockIdx.x * p.dx_ld;
+    const int32_t target = i >= 0 ? p.target[i] : -1;
+    const float f = i >= 0 ? p.f[i] : 0.f;
+    for (uint32_t c = threadIdx.x * 8; c < p.hidden; c += 256 * 8) {
+        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (i >= 0) {
+            for (uint32_t s = 0; s < p.splits; ++s) {
+                Raw8<float> r;
+                float v[8];
+                r.load(p.sums + s * p.split_elems + (uint64_t)i * p.hidden + c);
+                r.get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] += v[j];
+            }
+            if (target >= 0) {
+                Raw8<__nv_bfloat16> r;
+                float w[8];
+                r.load(p.weight + (uint64_t)target * p.weight_ld + c);
+                r.get(w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = fmaf(-f, w[j], o[j]);
+            }
+        }
+        Raw8<__nv_bfloat16> r;
+        r.set(o);
+        r.store(out + c);
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------
+static int pair_of(uint64_t tokens) { return tokens > kTileM ? 2 : 1; }
+
+struct CeShape {
+    uint64_t padded, piece, pieces;
+    int ctas;
+    uint32_t splits;       // of kDx's long axis
+};
+
+constexpr uint64_t kProbBytes = 256ull << 20;    // f p of one piece
+constexpr uint64_t kMinPiece = 2048;
+
+static CeShape ce_shape(uint64_t tokens, uint64_t vocab, uint64_t hidden, uint64_t prob_bytes) {
+    CeShape s;
+    s.padded = align_up(tokens ? tokens : 1, kPadRows);
+    s.ctas = pair_of(tokens);
+    uint64_t piece = prob_bytes / (2 * s.padded) / kMaxTileN * kMaxTileN;
+    if (piece < kMinPiece) piece = kMinPiece;
+    const uint64_t all = align_up(vocab ? vocab : 1, kMaxTileN);
+    if (piece > all) piece = all;
+    s.pieces = (all + piece - 1) / piece;
+    s.piece = align_up((all + s.pieces - 1) / s.pieces, kMaxTileN);
+    s.pieces = (all + s.piece - 1) / s.piece;
+    // few tiles: cut the long axis so that the GPU is full, in parts of at least 4 blocks
+    const uint64_t tiles = s.padded / kPadRows * ((hidden + kMaxTileN - 1) / kMaxTileN);
+    uint64_t splits = (kSplitSms / s.ctas) / (tiles ? tiles : 1);
+    const uint64_t most = s.piece / kTileK / 4;
+    if (splits > most) splits = most;
+    if (splits > 32) splits = 32;
+    s.splits = (uint32_t)(splits ? splits : 1);
+    return s;
+}
+
+// Offsets of everything in a workspace.
+struct CeLayout {
+    uint64_t count, source, target, place, rows, scalar0, scalar1, stats, prob, dx_sum, target_sum, slot, sort, total;
+};
+
+static uint64_t take(uint64_t& at, uint64_t bytes) {
+    const uint64_t here = at;
+    at += align_up(bytes, kWorkspaceAlign);
+    return here;
+}
+
+static uint32_t lse_tile_n(uint64_t tokens, uint64_t vocab) {
+    (void)tokens;
+    (void)vocab;
+    return kMaxTileN;
+}
+
+static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded, uint64_t& at) {
+    CeLayout l = {};
+    l.count = take(at, 4);
+    l.source = take(at, padded * 4);
+    l.target = take(at, padded * 4);
+    l.place = take(at, padded * 4);
+    l.rows = take(at, padded * hidden * 2);
+    l.scalar0 = take(at, padded * 4);
+    l.scalar1 = take(at, padded * 4);
+    (void)tokens;
+    return l;
+}
+
+static CeLayout forward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden) {
+    const CeShape s = ce_shape(tokens, vocab, hidden, kProbBytes);
+    uint64_t at = 0;
+    CeLayout l = common_layout(tokens, hidden, s.padded, at);
+    const uint64_t tn = lse_tile_n(tokens, vocab);
+    l.stats = take(at, (vocab + tn - 1) / tn * s.padded * sizeof(float2));
+    l.total = at;
+    return l;
+}
+
+static CeLayout backward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden, const CeShape& s) {
+    uint64_t at = 0;
+    CeLayout l = common_layout(tokens, hidden, s.padded, at);
+    l.prob = take(at, s.padded * s.piece * 2);
+    l.dx_sum = take(at, s.splits * s.padded * hidden * 4);
+    l.target_sum = take(at, s.padded * hidden * 4);
+    l.slot = take(at, align_up(vocab, kMaxTileN) * 4);
+    l.sort = take(at, sorted_sum_workspace_bytes(s.padded, hidden));
+    l.total = at;
+    return l;
+}
+
+// The driver's tensor-map encoder, found through the runtime: no link against libcuda.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static dte_status encoder(EncodeTiled* out) {
+    static std::atomic<void*> known{nullptr};
+    void* f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        cudaDriverEntryPointQueryResult r;
+        DTE_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r));
+        if (r != cudaDriverEntryPointSuccess || !f) return op_fail(DTE_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+        known.store(f, std::memory_order_relaxed);
+    }
+    *out = reinterpret_cast<EncodeTiled>(f);
+    return DTE_OK;
+}
+
+// bf16 matrix rows x cols with row stride ld, read in boxes of 64 columns x box_rows
+static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
+    EncodeTiled f;
+    dte_status s = encoder(&f);
+    if (s != DTE_OK) return s;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {kTileK, box_rows};
+    const cuuint32_t unit[2] = {1, 1};
+    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, unit,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return op_fail(DTE_ERR_CUDA, "cuTensorMapEncodeTiled refused a matrix");
+    return DTE_OK;
+}
+
+template <int KIND, int CTAS>
+static dte_status launch_ce_as(const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t most_tiles, int sms, cudaStream_t st) {
+    using S = CeStage<CTAS>;
+    DTE_CUDA(cudaFuncSetAttribute(ce_kernel<KIND, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
+    cudaLaunchConfig_t cfg = {};
+    const uint64_t teams = (uint64_t)(sms / CTAS);
+    cfg.gridDim = dim3((unsigned)((most_tiles < teams ? most_tiles : teams) * CTAS));
+    cfg.blockDim = dim3(kCeThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CTAS;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    DTE_CUDA(cudaLaunchKernelEx(&cfg, ce_kernel<KIND, CTAS>, a, b, p));
+    return DTE_OK;
+}
+
+template <int KIND>
+static dte_status launch_ce(int ctas, const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t rows, int sms, cudaStream_t st) {
+    const uint64_t tiles = (rows + kTileM * ctas - 1) / (kTileM * ctas) * ((p.n + p.tile_n - 1) / p.tile_n) * p.splits;
+    return ctas == 2 ? launch_ce_as<KIND, 2>(a, b, p, tiles, sms, st) : launch_ce_as<KIND, 1>(a, b, p, tiles, sms, st);
+}
+
+static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets, uint64_t vocab_start,
+                             uint64_t vocab, double logit_scale, const uint64_t* flags) {
+    dte_status s;
+    if ((s = check_matrix(x, "x is null", false)) != DTE_OK) return s;
+    if ((s = check_matrix(weight, "weight is null", false)) != DTE_OK) return s;
+    if ((s = check_ids(targets)) != DTE_OK) return s;
+    if (x->dtype != DTE_BF16 || weight->dtype != DTE_BF16) return op_fail(DTE_ERR_INVALID_ARG, "x and weight must be BF16");
+    if (x->cols != weight->cols || x->rows != targets->count)
+        return op_fail(DTE_ERR_INVALID_ARG, "x must be targets.count x weight.cols");
+    if (weight->rows == 0) return op_fail(DTE_ERR_INVALID_ARG, "weight has no rows");
+    if (x->cols % 8) return op_fail(DTE_ERR_INVALID_ARG, "hidden must be a multiple of 8");
+    if (((uintptr_t)weight->data & 15u) || weight->ld % 8 || (weight->rows > 1 && weight->ld < weight->cols))
+        return op_fail(DTE_ERR_INVALID_ARG, "weight must be 16-byte aligned with ld >= cols, a multiple of 8");
+    if ((s = check_range(vocab_start, weight->rows, vocab)) != DTE_OK) return s;
+    if (!(logit_scale > 0) || !std::isfinite(logit_scale)) return op_fail(DTE_ERR_INVALID_ARG, "logit_scale must be finite and > 0");
+    if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
+    if (targets->count > (1u << 24) || weight->rows > (1u << 30) || x->cols > (1u << 20))
+        return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^30 vocabulary rows and 2^20 hidden");
+    return DTE_OK;
+}
+
+static bool ce_sizes_ok(uint64_t tokens, uint64_t vocab, uint64_t hidden) {
+    return tokens <= (1u << 24) && vocab <= (1u << 30) && hidden <= (1u << 20);
+}
+
+static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix* x, const dte_ids* targets, uint64_t vocab_start,
+                               uint64_t vocab, uint64_t vocab_rows, uint64_t padded, float scale, float* lse, float* target_logit,
+                               float* loss, const float* lse_in, const float* dloss, uint64_t* flags, cudaStream_t st) {
+    RowsParams r = {};
+    r.targets = targets->data;
+    r.targets_dtype = targets->dtype;
+    r.n = (uint32_t)targets->count;
+    r.vocab_start = (int64_t)vocab_start;
+    r.vocab = (int64_t)vocab;
+    r.vocab_rows = (uint32_t)vocab_rows;
+    r.count = reinterpret_cast<uint32_t*>(ws + l.count);
+    r.source = reinterpret_cast<int32_t*>(ws + l.source);
+    r.target = reinterpret_cast<int32_t*>(ws + l.target);
+    r.place = dloss ? reinterpret_cast<int32_t*>(ws + l.place) : nullptr;
+    r.lse = lse;
+    r.target_logit = target_logit;
+    r.loss = loss;
+    r.flags = flags;
+    ce_rows_kernel<<<1, kRowsThreads, 0, st>>>(r);
+    DTE_CUDA(cudaGetLastError());
+    GatherRowsParams g = {};
+    g.count = r.count;
+    g.source = r.source;
+    g.x = static_cast<const __nv_bfloat16*>(x->data);
+    g.x_ld = x->ld;
+    g.hidden = (uint32_t)x->cols;
+    g.vec = vec8_ok(x);
+    g.rows = reinterpret_cast<__nv_bfloat16*>(ws + l.rows);
+    if (dloss) {
+        g.dloss = dloss;
+        g.lse = lse_in;
+        g.scale = scale;
+        g.f = reinterpret_cast<float*>(ws + l.scalar0);
+        g.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
+    } else {
+        g.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
+    }
+    ce_gather_kernel<<<(unsigned)padded, 256, 0, st>>>(g);
+    DTE_CUDA(cudaGetLastError());
+    return DTE_OK;
+}
+
+}  // namespace dte
+
+using namespace dte;
+
+extern "C" uint64_t dte_linear_ce_forward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden) {
+    if (!ce_sizes_ok(tokens, vocab_rows, hidden)) return UINT64_MAX;     // refused by the call
+    return forward_layout(tokens, vocab_rows, hidden).total;
+}
+
+extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets, uint64_t vocab_start,
+                                            uint64_t vocab, double logit_scale, float* lse, float* target_logit, float* loss,
+                                            void* workspace, uint64_t workspace_bytes, uint64_t* flags, int device,
+                                            void* cuda_stream) {
+    dte_status s;
+    if ((s = check_head(x, weight, targets, vocab_start, vocab, logit_scale, flags)) != DTE_OK) return s;
+    if (targets->count && !lse) return op_fail(DTE_ERR_INVALID_ARG, "lse is null");
+    if (((uintptr_t)lse | (uintptr_t)target_logit | (uintptr_t)loss) & 3u)
+        return op_fail(DTE_ERR_INVALID_ARG, "lse, target_logit and loss must be 4-byte aligned");
+    const uint64_t n = targets->count, V = weight->rows, H = x->cols;
+    const CeLayout l = forward_layout(n, V, H);
+    if ((s = check_workspace(workspace, workspace_bytes, l.total)) != DTE_OK) return s;
+    if (n == 0) return DTE_OK;
+    OpDeviceGuard g(device);
+    int sms = 0;
+    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const CeShape sh = ce_shape(n, V, H, kProbBytes);
+    if ((s = prepare_rows(l, ws, x, targets, vocab_start, vocab, V, sh.padded, (float)logit_scale, lse, target_logit, loss, nullptr,
+                          nullptr, flags, st)) != DTE_OK)
+        return s;
+    const uint32_t tn = lse_tile_n(n, V);
+    CeParams p = {};
+    p.n = (uint32_t)V;
+    p.k = (uint32_t)H;
+    p.tokens = reinterpret_cast<uint32_t*>(ws + l.count);
+    p.tile_n = tn;
+    p.splits = 1;
+    p.flags = flags;
+    p.scale = (float)logit_scale;
+    p.k2 = (float)(logit_scale * 1.4426950408889634);
+    p.target = reinterpret_cast<int32_t*>(ws + l.target);
+    p.stats = reinterpret_cast<float2*>(ws + l.stats);
+    p.stats_ld = sh.padded;
+    p.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
+    CUtensorMap ma, mb;
+    if ((s = encode(&ma, ws + l.rows, sh.padded, H, H, kTileM)) != DTE_OK) return s;
+    if ((s = encode(&mb, weight->data, V, H, weight->ld, tn / sh.ctas)) != DTE_OK) return s;
+    if ((s = launch_ce<kLse>(sh.ctas, ma, mb, p, n, sms, st)) != DTE_OK) return s;
+    CombineParams c = {};
+    c.count = p.tokens;
+    c.source = reinterpret_cast<int32_t*>(ws + l.source);
+    c.stats = p.stats;
+    c.stats_ld = p.stats_ld;
+    c.tiles = (uint32_t)((V + tn - 1) / tn);
+    c.row_target_logit = p.target_logit;
+    c.lse = lse;
+    c.target_logit = target_logit;
+    c.loss = loss;
+    ce_combine_kernel<<<(unsigned)((n + 31) / 32), 1024, 0, st>>>(c);
+    DTE_CUDA(cudaGetLastError());
+    return DTE_OK;
+}
+
+extern "C" uint64_t dte_linear_ce_backward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden) {
+    if (!ce_sizes_ok(tokens, vocab_rows, hidden)) return UINT64_MAX;     // refused by the call
+    return backward_layout(tokens, vocab_rows, hidden, ce_shape(tokens, vocab_rows, hidden, kProbBytes)).total;
+}
+
+extern "C" uint64_t dte_linear_ce_backward_workspace_min_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden) {
+    if (!ce_sizes_ok(tokens, vocab_rows, hidden)) return UINT64_MAX;
+    return backward_layout(tokens, vocab_rows, hidden, ce_shape(tokens, vocab_rows, hidden, 0)).total;
+}
+
+extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets, uint64_t vocab_start,
+                                             uint64_t vocab, double logit_scale, const float* lse, const float* dloss, int accumulate,
+                                             const dte_matrix* dx, const dte_matrix* dweight, void* workspace, uint64_t workspace_bytes,
+                                             uint64_t* flags, int device, void* cuda_stream) {
+    dte_status s;
+    if ((s = check_head(x, weight, targets, vocab_start, vocab, logit_scale, flags)) != DTE_OK) return s;
+    const uint64_t n = targets->count, V = weight->rows, H = x->cols;
+    if (n && (!lse || !dloss)) return op_fail(DTE_ERR_INVALID_ARG, "lse / dloss is null");
+    if (((uintptr_t)lse | (uintptr_t)dloss) & 3u) return op_fail(DTE_ERR_INVALID_ARG, "lse and dloss must be 4-byte aligned");
+    if (dx) {
+        if ((s = check_matrix(dx, "dx is null", true)) != DTE_OK) return s;
+        if (dx->dtype != DTE_BF16 || dx->rows != n || dx->cols != H) return op_fail(DTE_ERR_INVALID_ARG, "dx must have x's shape, BF16");
+        if (!vec8_ok(dx)) return op_fail(DTE_ERR_INVALID_ARG, "dx rows must be 16-byte aligned");
+    }
+    if (dweight) {
+        if ((s = check_matrix(dweight, "dweight is null", true)) != DTE_OK) return s;
+        if (dweight->rows != V || dweight->cols != H) return op_fail(DTE_ERR_INVALID_ARG, "dweight must have weight's shape");
+        if (!vec8_ok(dweight)) return op_fail(DTE_ERR_INVALID_ARG, "dweight rows must be 16-byte aligned");
+    }
+    // the largest piece this workspace holds
+    uint64_t budget = kProbBytes;
+    CeShape sh = ce_shape(n, V, H, budget);
+    CeLayout l = backward_layout(n, V, H, sh);
+    while (l.total > workspace_bytes && budget) {
+        budget = budget > (1u << 20) ? budget / 2 : 0;
+        sh = ce_shape(n, V, H, budget);
+        l = backward_layout(n, V, H, sh);
+    }
+    if ((s = check_workspace(workspace, workspace_bytes, l.total)) != DTE_OK) return s;
+    if (!dx && !dweight) return DTE_OK;
+    if (n == 0 && (!dweight || accumulate)) return DTE_OK;
+    OpDeviceGuard g(device);
+    int sms = 0;
+    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (n == 0) {
+        DTE_CUDA(cudaMemset2DAsync(dweight->data, dweight->ld * elem_size(dweight->dtype), 0, H * elem_size(dweight->dtype), V, st));
+        return DTE_OK;
+    }
+    if ((s = prepare_rows(l, ws, x, targets, vocab_start, vocab, V, sh.padded, (float)logit_scale, nullptr, nullptr, nullptr, lse, dloss,
+                          flags, st)) != DTE_OK)
+        return s;
+    const uint32_t* count = reinterpret_cast<uint32_t*>(ws + l.count);
+    const float* f = reinterpret_cast<float*>(ws + l.scalar0);
+    const int32_t* target = reinterpret_cast<int32_t*>(ws + l.target);
+    uint32_t* slot = reinterpret_cast<uint32_t*>(ws + l.slot);
+    float* target_sum = reinterpret_cast<float*>(ws + l.target_sum);
+    if (dweight) {
+        DTE_CUDA(cudaMemsetAsync(slot, 0xFF, align_up(V, kMaxTileN) * 4, st));
+        SortedSum q = {};
+        q.ids = target;
+        q.ids_dtype = DTE_I32;
+        q.n = (uint32_t)n;
+        q.n_dev = count;
+        q.row_start = 0;
+        q.vocab = V;
+        q.rows = (uint32_t)V;
+        q.src = ws + l.rows;
+        q.src_dtype = DTE_BF16;
+        q.src_ld = H;
+        q.weight = f;
+        q.hidden = (uint32_t)H;
+        q.scale = 1.f;
+        q.out = target_sum;
+        q.out_dtype = DTE_F32;
+        q.out_ld = H;
+        q.slot = slot;
+        if ((s = launch_sorted_sum(q, true, ws + l.sort, sms, st)) != DTE_OK) return s;
+    }
+    CeParams p = {};
+    p.tokens = count;
+    p.flags = flags;
+    p.scale = (float)logit_scale;
+    p.k2 = (float)(logit_scale * 1.4426950408889634);
+    p.target = target;
+    p.f = f;
+    p.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
+    p.prob = reinterpret_cast<__nv_bfloat16*>(ws + l.prob);
+    p.prob_ld = sh.piece;
+    p.dx_sum = reinterpret_cast<float*>(ws + l.dx_sum);
+    p.dx_split = sh.padded * H;
+    if (dweight) {
+        p.dweight = dweight->data;
+        p.dweight_ld = dweight->ld;
+        p.dweight_bf16 = dweight->dtype == DTE_BF16;
+    }
+    p.accumulate = accumulate != 0;
+    p.slot = slot;
+    p.target_sum = target_sum;
+    CUtensorMap x_k, w_k, g_k, w_n, g_m, x_n;
+    const uint32_t bn = kMaxTileN;
+    if ((s = encode(&x_k, ws + l.rows, sh.padded, H, H, kTileM)) != DTE_OK) return s;
+    if ((s = encode(&w_k, weight->data, V, H, weight->ld, bn / sh.ctas)) != DTE_OK) return s;
+    if ((s = encode(&g_k, ws + l.prob, sh.padded, sh.piece, sh.piece, kTileM)) != DTE_OK) return s;
+    if ((s = encode(&w_n, weight->data, V, H, weight->ld, kTileK)) != DTE_OK) return s;
+    if ((s = encode(&g_m, ws + l.prob, sh.padded, sh.piece, sh.piece, kTileK)) != DTE_OK) return s;
+    if ((s = encode(&x_n, ws + l.rows, sh.padded, H, H, kTileK)) != DTE_OK) return s;
+    for (uint64_t piece = 0; piece < sh.pieces; ++piece) {
+        const uint64_t v0 = piece * sh.piece, vc = V - v0 < sh.piece ? V - v0 : sh.piece;
+        p.w_row = (uint32_t)v0;
+        p.tile_n = bn;
+        p.splits = 1;
+        p.n = (uint32_t)vc;
+        p.k = (uint32_t)H;
+        if ((s = launch_ce<kProb>(sh.ctas, x_k, w_k, p, n, sms, st)) != DTE_OK) return s;
+        if (dx) {
+            p.n = (uint32_t)H;
+            p.k = (uint32_t)vc;
+            p.splits = sh.splits;
+            p.add = piece > 0;
+            if ((s = launch_ce<kDx>(sh.ctas, g_k, w_n, p, n, sms, st)) != DTE_OK) return s;
+        }
+        if (dweight) {
+            p.m = (uint32_t)vc;
+            p.n = (uint32_t)H;
+            p.splits = 1;
+            if ((s = launch_ce<kDw>(sh.ctas, g_m, x_n, p, vc, sms, st)) != DTE_OK) return s;
+        }
+    }
+    if (dx) {
+        DxParams d = {};
+        d.place = reinterpret_cast<int32_t*>(ws + l.place);
+        d.target = target;
+        d.f = f;
+        d.sums = p.dx_sum;
+        d.split_elems = p.dx_split;
+        d.splits = sh.splits;
+        d.hidden = (uint32_t)H;
+        d.weight = static_cast<const __nv_bfloat16*>(weight->data);
+        d.weight_ld = weight->ld;
+        d.dx = static_cast<__nv_bfloat16*>(dx->data);
+        d.dx_ld = dx->ld;
+        ce_dx_kernel<<<(unsigned)n, 256, 0, st>>>(d);
+        DTE_CUDA(cudaGetLastError());
+    }
+    return DTE_OK;
+}

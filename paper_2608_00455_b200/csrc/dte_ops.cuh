@@ -1,0 +1,208 @@
+// Shared by the operators at the two ends of the model (embedding, norm, linear cross entropy):
+// argument checks on the host, typed vector access and reductions on the device, and the sorted-token
+// sum that the embedding gradient and the head's gradient both need.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include <cmath>
+
+#include "dte_internal.cuh"
+
+namespace dte {
+
+constexpr uint64_t kWorkspaceAlign = 256;
+
+inline uint64_t align_up(uint64_t n, uint64_t a) { return (n + a - 1) / a * a; }
+
+// ---- host: argument checks ------------------------------------------------------------------------
+inline dte_status op_fail(dte_status s, const char* msg) {
+    set_error(msg);
+    return s;
+}
+
+struct OpDeviceGuard {
+    int prev = -1;
+    explicit OpDeviceGuard(int dev) {
+        cudaGetDevice(&prev);
+        if (prev != dev) cudaSetDevice(dev); else prev = -1;
+    }
+    ~OpDeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+inline uint32_t elem_size(uint32_t dtype) { return dtype == DTE_BF16 ? 2u : dtype == DTE_I64 ? 8u : 4u; }
+
+// Multiplications and the vector kernels' index arithmetic stay far below 2^63 with these limits.
+constexpr uint64_t kMaxDim = 1ull << 31;
+
+inline dte_status check_matrix(const dte_matrix* m, const char* null_msg, bool output) {
+    if (!m) return op_fail(DTE_ERR_INVALID_ARG, null_msg);
+    if (m->dtype != DTE_F32 && m->dtype != DTE_BF16) return op_fail(DTE_ERR_INVALID_ARG, "matrix dtype must be DTE_F32 or DTE_BF16");
+    if (m->cols == 0 || m->cols >= kMaxDim || m->rows >= kMaxDim || m->ld >= (1ull << 40))
+        return op_fail(DTE_ERR_INVALID_ARG, "matrix needs 1 <= cols < 2^31, rows < 2^31 and ld < 2^40");
+    if (m->rows && !m->data) return op_fail(DTE_ERR_INVALID_ARG, null_msg);
+    if ((uintptr_t)m->data & (elem_size(m->dtype) - 1)) return op_fail(DTE_ERR_INVALID_ARG, "matrix data is not aligned to its element type");
+    if (output && m->rows > 1 && m->ld < m->cols) return op_fail(DTE_ERR_INVALID_ARG, "output rows overlap: ld < cols");
+    return DTE_OK;
+}
+
+inline dte_status check_ids(const dte_ids* t) {
+    if (!t || (t->count && !t->data)) return op_fail(DTE_ERR_INVALID_ARG, "ids are null");
+    if (t->dtype != DTE_I32 && t->dtype != DTE_I64) return op_fail(DTE_ERR_INVALID_ARG, "ids must be DTE_I32 or DTE_I64");
+    if ((uintptr_t)t->data & (elem_size(t->dtype) - 1)) return op_fail(DTE_ERR_INVALID_ARG, "ids are not aligned to their type");
+    if (t->count >= kMaxDim) return op_fail(DTE_ERR_INVALID_ARG, "ids.count must be < 2^31");
+    return DTE_OK;
+}
+
+inline dte_status check_range(uint64_t start, uint64_t rows, uint64_t vocab) {
+    if (vocab >= (1ull << 62) || start > vocab || rows > vocab - start)
+        return op_fail(DTE_ERR_INVALID_ARG, "the shard's rows do not lie inside the vocabulary");
+    return DTE_OK;
+}
+
+inline dte_status check_workspace(const void* ws, uint64_t have, uint64_t need) {
+    if (have < need) return op_fail(DTE_ERR_CAPACITY, "workspace is too small; see the operator's workspace_bytes");
+    if (need && !ws) return op_fail(DTE_ERR_INVALID_ARG, "workspace is null");
+    if ((uintptr_t)ws & (kWorkspaceAlign - 1)) return op_fail(DTE_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    return DTE_OK;
+}
+
+// 16-byte accesses of whole rows: data and every row start aligned, columns a multiple of 8 elements.
+inline bool vec8_ok(const dte_matrix* m) {
+    const uint64_t unit = 16 / elem_size(m->dtype);
+    return !((uintptr_t)m->data & 15u) && (m->cols % 8 == 0) && (m->rows <= 1 || m->ld % unit == 0);
+}
+
+dte_status device_sms(int device, int* sms);   // multiprocessor count, cached per device
+
+// ---- sorted-token sums ----------------------------------------------------------------------------
+// out[key] = scale * sum over entries with that key of weight[entry] * src[row of entry]
+// Entries are ordered by a stable radix sort of their keys, so every sum has one fixed order.
+struct SortedSum {
+    // keys: ids minus row_start where that lies in [0, rows), else the entry is dropped
+    const void* ids;
+    uint32_t ids_dtype;
+    uint32_t n;               // entries (upper bound when n_dev is set)
+    const uint32_t* n_dev;    // device: actual number of entries; NULL: n
+    int64_t row_start;
+    uint64_t vocab;
+    uint32_t rows;
+    const void* src;          // n x hidden
+    uint32_t src_dtype;
+    uint64_t src_ld;
+    const float* weight;      // per entry, or NULL
+    uint32_t hidden;
+    float scale;
+    // dense form (slot == NULL): out is rows x hidden of out_dtype, accumulate or write all rows.
+    // compact form: out is fp32 n x hidden; row i holds the sum of the run that starts at sorted
+    // position i, and slot[key] = i (slot must hold 0xFFFFFFFF everywhere before).
+    void* out;
+    uint32_t out_dtype;
+    uint64_t out_ld;
+    bool accumulate;
+    uint32_t* slot;
+    uint64_t* flags;
+};
+uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t hidden);
+dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, int sms, cudaStream_t st);
+
+#ifdef __CUDACC__
+// ---- device: typed access --------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ float to_f(T v);
+template <>
+__device__ __forceinline__ float to_f<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_f(float v);
+template <>
+__device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Eight consecutive elements as they lie in memory (16 or 32 bytes), loaded now, converted later.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load_cs(const __nv_bfloat16* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float* f) const {
+        f[0] = bf16_lo(a.x); f[1] = bf16_hi(a.x); f[2] = bf16_lo(a.y); f[3] = bf16_hi(a.y);
+        f[4] = bf16_lo(a.z); f[5] = bf16_hi(a.z); f[6] = bf16_lo(a.w); f[7] = bf16_hi(a.w);
+    }
+    __device__ __forceinline__ void set(const float* f) {
+        a = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = a; }
+    __device__ __forceinline__ void store_cs(__nv_bfloat16* p) const { __stcs(reinterpret_cast<uint4*>(p), a); }
+};
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = reinterpret_cast<const float4*>(p)[0];
+        b = reinterpret_cast<const float4*>(p)[1];
+    }
+    __device__ __forceinline__ void load_cs(const float* p) {
+        a = __ldcs(reinterpret_cast<const float4*>(p));
+        b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float* f) const {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+    __device__ __forceinline__ void set(const float* f) {
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    __device__ __forceinline__ void store(float* p) const {
+        reinterpret_cast<float4*>(p)[0] = a;
+        reinterpret_cast<float4*>(p)[1] = b;
+    }
+    __device__ __forceinline__ void store_cs(float* p) const {
+        __stcs(reinterpret_cast<float4*>(p), a);
+        __stcs(reinterpret_cast<float4*>(p) + 1, b);
+    }
+};
+
+// V consecutive elements: V == 8 through Raw8, V == 1 one element of any alignment.
+template <typename T, int V>
+struct Vec;
+template <typename T>
+struct Vec<T, 8> : Raw8<T> {};
+template <typename T>
+struct Vec<T, 1> {
+    T a;
+    __device__ __forceinline__ void load(const T* p) { a = *p; }
+    __device__ __forceinline__ void load_cs(const T* p) { a = *p; }
+    __device__ __forceinline__ void zero() { a = from_f<T>(0.f); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = to_f<T>(a); }
+    __device__ __forceinline__ void set(const float* f) { a = from_f<T>(f[0]); }
+    __device__ __forceinline__ void store(T* p) const { *p = a; }
+    __device__ __forceinline__ void store_cs(T* p) const { *p = a; }
+};
+
+__device__ __forceinline__ int64_t load_id(const void* ids, uint32_t dtype, uint64_t i) {
+    return dtype == DTE_I64 ? (int64_t) static_cast<const long long*>(ids)[i] : (int64_t) static_cast<const int*>(ids)[i];
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+#endif  // __CUDACC__
+
+}  // namespace dte

@@ -1,0 +1,255 @@
+"""Embedding lookup, layer / RMS norm and the linear head's cross entropy, with their gradients: argument
+marshalling for the operators of the C ABI (include/dte.h says what each computes).
+
+Tensors are CUDA tensors the caller owns; every call enqueues on `stream` (default: the current stream of the
+tensors' device) and returns.  A tensor that belongs to another stream is the caller's to order and to
+keep alive (torch.Tensor.record_stream), as for every other call of this package.  A refused argument raises
+DteError and enqueues nothing.
+
+Matrices may have any shape whose last dimension is contiguous and whose other dimensions can be flattened to
+rows a fixed stride apart.  Workspaces are uint8 tensors of at least the bytes the operator's
+*_workspace_bytes function gives for the same sizes.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+from .binding import DTE_OK, DteError, _check, lib
+
+DTE_F32, DTE_BF16, DTE_I32, DTE_I64 = 0, 1, 2, 3
+DTE_NORM_LAYER, DTE_NORM_RMS = 0, 1
+_INVALID_ARG = 1
+
+_NUMBERS = {torch.float32: DTE_F32, torch.bfloat16: DTE_BF16}
+_IDS = {torch.int32: DTE_I32, torch.int64: DTE_I64}
+
+
+class MatrixDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("ld", C.c_uint64),
+                ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class IdsDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("count", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+def _refuse(msg: str):
+    raise DteError(_INVALID_ARG, msg)
+
+
+def _device(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name} must be a tensor")
+    if not t.is_cuda:
+        _refuse(f"{name} is not on a CUDA device; there is no CPU fallback")
+    return t.get_device()
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(rows, stride between rows) of a tensor seen as a matrix of its last dimension."""
+    shape, stride = t.shape, t.stride()
+    n, ld = 1, None
+    for d in range(t.dim() - 2, -1, -1):
+        if shape[d] == 1:
+            continue
+        if ld is None:
+            ld = stride[d]
+        elif stride[d] != ld * n and shape[d] * n > 0:
+            _refuse(f"{name}: the leading dimensions cannot be flattened to rows a fixed stride apart")
+        n *= shape[d]
+    return n, shape[-1] if ld is None else ld
+
+
+def _matrix(t: torch.Tensor, name: str, device: int) -> MatrixDesc:
+    if _device(t, name) != device:
+        _refuse(f"{name} is on another device")
+    dtype = _NUMBERS.get(t.dtype)
+    if dtype is None:
+        _refuse(f"{name} must be float32 or bfloat16")
+    dim = t.dim()
+    if dim == 0:
+        _refuse(f"{name} needs at least one dimension")
+    cols = t.shape[-1]
+    if cols != 1 and t.stride(-1) != 1:
+        _refuse(f"{name}: the last dimension must be contiguous")
+    if dim == 2:
+        rows, ld = t.shape[0], t.stride(0)
+        if rows == 1:
+            ld = cols
+    else:
+        rows, ld = _rows(t, name)
+    return MatrixDesc(t.data_ptr(), rows, cols, ld, dtype, 0)
+
+
+def _ids(t: torch.Tensor, name: str, device: int) -> IdsDesc:
+    if _device(t, name) != device:
+        _refuse(f"{name} is on another device")
+    dtype = _IDS.get(t.dtype)
+    if dtype is None:
+        _refuse(f"{name} must be int32 or int64")
+    if not t.is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    return IdsDesc(t.data_ptr(), t.numel(), dtype, 0)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, device: int, count: int, dtypes=(torch.float32,)):
+    """Address of a contiguous vector of `count` values, or None."""
+    if t is None:
+        return None
+    if _device(t, name) != device:
+        _refuse(f"{name} is on another device")
+    if t.dtype not in dtypes:
+        _refuse(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in dtypes)}")
+    if t.numel() != count or not t.is_contiguous():
+        _refuse(f"{name} must be contiguous with {count} values")
+    return t.data_ptr()
+
+
+def _workspace(t: Optional[torch.Tensor], device: int):
+    if t is None:
+        return None, 0
+    if _device(t, "workspace") != device:
+        _refuse("workspace is on another device")
+    if not t.is_contiguous():
+        _refuse("workspace must be contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _flags(t: Optional[torch.Tensor], device: int):
+    if t is None:
+        return None
+    if _device(t, "flags") != device:
+        _refuse("flags is on another device")
+    if t.dtype != torch.int64 or t.numel() < 1:
+        _refuse("flags must be int64")
+    return t.data_ptr()
+
+
+def _stream(stream, device: int) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def _number(v, name: str) -> int:
+    if v < 0:
+        _refuse(f"{name} must not be negative")
+    return int(v)
+
+
+def _done(status: int) -> None:
+    if status != DTE_OK:
+        _check(status)
+
+
+_PARAM_TYPES = (torch.float32, torch.bfloat16)
+
+
+def _params(weight, bias, device: int, cols: int):
+    w = _vector(weight, "weight", device, cols, _PARAM_TYPES)
+    b = _vector(bias, "bias", device, cols, _PARAM_TYPES)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        _refuse("weight and bias must have one type")
+    kept = weight if weight is not None else bias
+    return w, b, DTE_F32 if kept is None else _NUMBERS[kept.dtype]
+
+
+def dte_embedding_forward(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, row_start: int = 0,
+                          vocab: Optional[int] = None, flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out[n] = scale * table[ids[n] - row_start], zero for negative ids and ids of other shards."""
+    device = _device(table, "table")
+    m, o, i = _matrix(table, "table", device), _matrix(out, "out", device), _ids(ids, "ids", device)
+    _done(lib().dte_embedding_forward(C.byref(m), C.byref(i), _number(row_start, "row_start"),
+                                      row_start + m.rows if vocab is None else _number(vocab, "vocab"), scale, C.byref(o),
+                                      _flags(flags, device), device, _stream(stream, device)))
+
+
+def dte_embedding_backward_workspace_bytes(n_ids: int, hidden: int) -> int:
+    return lib().dte_embedding_backward_workspace_bytes(n_ids, hidden)
+
+
+def dte_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                           row_start: int = 0, vocab: Optional[int] = None, accumulate: bool = False,
+                           flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dtable[v] (+)= scale * sum of dout[n] over the tokens with ids[n] == row_start + v."""
+    device = _device(dtable, "dtable")
+    d, m, i = _matrix(dout, "dout", device), _matrix(dtable, "dtable", device), _ids(ids, "ids", device)
+    ws, size = _workspace(workspace, device)
+    _done(lib().dte_embedding_backward(C.byref(d), C.byref(i), _number(row_start, "row_start"),
+                                       row_start + m.rows if vocab is None else _number(vocab, "vocab"), scale, bool(accumulate),
+                                       C.byref(m), ws, size, _flags(flags, device), device, _stream(stream, device)))
+
+
+def dte_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
+                     mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], eps: float, rms: bool = False, stream=None) -> None:
+    """Layer norm (rms: RMS norm) of every row of x; mean and rstd keep the statistics for the backward pass."""
+    device = _device(x, "x")
+    m, o = _matrix(x, "x", device), _matrix(out, "out", device)
+    w, b, dtype = _params(weight, bias, device, m.cols)
+    _done(lib().dte_norm_forward(C.byref(m), w, b, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER, eps, C.byref(o),
+                                 _vector(mean, "mean", device, m.rows), _vector(rstd, "rstd", device, m.rows), device,
+                                 _stream(stream, device)))
+
+
+def dte_norm_backward_workspace_bytes(rows: int, hidden: int) -> int:
+    return lib().dte_norm_backward_workspace_bytes(rows, hidden)
+
+
+def dte_norm_backward(dout: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: Optional[torch.Tensor],
+                      rstd: torch.Tensor, dx: Optional[torch.Tensor], dweight: Optional[torch.Tensor], dbias: Optional[torch.Tensor],
+                      workspace: Optional[torch.Tensor], accumulate: bool = False, rms: bool = False, stream=None) -> None:
+    """Gradients of dte_norm_forward; dweight and dbias are float32 (accumulate: added to)."""
+    device = _device(x, "x")
+    d, m = _matrix(dout, "dout", device), _matrix(x, "x", device)
+    o = None if dx is None else _matrix(dx, "dx", device)
+    w, _, dtype = _params(weight, None, device, m.cols)
+    ws, size = _workspace(workspace, device)
+    _done(lib().dte_norm_backward(C.byref(d), C.byref(m), w, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER,
+                                  _vector(mean, "mean", device, m.rows), _vector(rstd, "rstd", device, m.rows), bool(accumulate),
+                                  None if o is None else C.byref(o), _vector(dweight, "dweight", device, m.cols),
+                                  _vector(dbias, "dbias", device, m.cols), ws, size, device, _stream(stream, device)))
+
+
+def dte_linear_ce_forward_workspace_bytes(tokens: int, vocab_rows: int, hidden: int) -> int:
+    return lib().dte_linear_ce_forward_workspace_bytes(tokens, vocab_rows, hidden)
+
+
+def dte_linear_ce_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                          target_logit: Optional[torch.Tensor], loss: Optional[torch.Tensor], workspace: torch.Tensor,
+                          logit_scale: float = 1.0, vocab_start: int = 0, vocab: Optional[int] = None,
+                          flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """lse, target logit and loss of every token for the head rows [vocab_start, vocab_start + rows)."""
+    device = _device(x, "x")
+    m, w, t = _matrix(x, "x", device), _matrix(weight, "weight", device), _ids(targets, "targets", device)
+    ws, size = _workspace(workspace, device)
+    _done(lib().dte_linear_ce_forward(C.byref(m), C.byref(w), C.byref(t), _number(vocab_start, "vocab_start"),
+                                      vocab_start + w.rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+                                      _vector(lse, "lse", device, t.count), _vector(target_logit, "target_logit", device, t.count),
+                                      _vector(loss, "loss", device, t.count), ws, size, _flags(flags, device), device,
+                                      _stream(stream, device)))
+
+
+def dte_linear_ce_backward_workspace_bytes(tokens: int, vocab_rows: int, hidden: int) -> int:
+    return lib().dte_linear_ce_backward_workspace_bytes(tokens, vocab_rows, hidden)
+
+
+def dte_linear_ce_backward_workspace_min_bytes(tokens: int, vocab_rows: int, hidden: int) -> int:
+    return lib().dte_linear_ce_backward_workspace_min_bytes(tokens, vocab_rows, hidden)
+
+
+def dte_linear_ce_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                           dx: Optional[torch.Tensor], dweight: Optional[torch.Tensor], workspace: torch.Tensor,
+                           logit_scale: float = 1.0, vocab_start: int = 0, vocab: Optional[int] = None, accumulate: bool = False,
+                           flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx and dweight for a given dloss per token; lse over the whole vocabulary."""
+    device = _device(x, "x")
+    m, w, t = _matrix(x, "x", device), _matrix(weight, "weight", device), _ids(targets, "targets", device)
+    d = None if dx is None else _matrix(dx, "dx", device)
+    g = None if dweight is None else _matrix(dweight, "dweight", device)
+    ws, size = _workspace(workspace, device)
+    _done(lib().dte_linear_ce_backward(C.byref(m), C.byref(w), C.byref(t), _number(vocab_start, "vocab_start"),
+                                       vocab_start + w.rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+                                       _vector(lse, "lse", device, t.count), _vector(dloss, "dloss", device, t.count),
+                                       bool(accumulate), None if d is None else C.byref(d), None if g is None else C.byref(g), ws,
+                                       size, _flags(flags, device), device, _stream(stream, device)))
