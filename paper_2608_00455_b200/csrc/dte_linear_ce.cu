@@ -26,7 +26,8 @@ enum CeKind { kLse = 0, kProb = 1, kDx = 2, kDw = 3 };
 constexpr uint32_t kTileM = 128;                 // accumulator rows of one CTA: the 128 lanes of tensor memory
 constexpr uint32_t kTileK = 64;                  // 128 bytes of bf16: one swizzle row
 constexpr uint32_t kMaxTileN = 256;
-constexpr uint32_t kCeThreads = 192;             // TMA warp, MMA warp, four epilogue warps
+constexpr uint32_t kEpilogueWarps = 8;           // two for each quarter of tensor memory's lanes, half a tile's columns each
+constexpr uint32_t kCeThreads = 64 + 32 * kEpilogueWarps;   // TMA warp, MMA warp, epilogue
 constexpr uint32_t kStageBytesA = kTileM * kTileK * 2;
 constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one is filled while the other is drained
 constexpr uint64_t kPadRows = 256;               // token rows are padded to this, with zero rows
@@ -55,7 +56,7 @@ struct CeParams {
     const int32_t* target;       // row of this shard, or -1
     float2* stats;               // kLse: (maximum, sum) per tile of columns and token
     uint64_t stats_ld;
-    float* target_logit;
+    float* target_logit;         // kLse: the target's logit as the tensor cores added it up
     const float* f;              // kProb: logit_scale * dloss per token
     const float* neg_lse2;       //        -lse * log2(e)
     __nv_bfloat16* prob;         //        tokens x prob_ld
@@ -94,34 +95,35 @@ __device__ __forceinline__ void load_tile(uint32_t addr, float (&v)[32]) {
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
 }
 
+// The 128 columns from c0 (half a tile) of row `row`; lane_row: the row within the CTA's 128.
 template <int KIND>
-__device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, uint32_t row, uint32_t tn, uint32_t split,
-                                            uint32_t tokens, bool empty) {
-    const uint32_t n0 = tn * p.tile_n;
+__device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, uint32_t row, uint32_t lane_row, uint32_t half, uint32_t use,
+                                            uint32_t tn, uint32_t split, uint32_t tokens, bool empty, float2 (*s_stat)[kTileM]) {
+    const uint32_t n0 = tn * p.tile_n, c0 = half * (kMaxTileN / 2), c1 = min(c0 + kMaxTileN / 2, p.tile_n);
     if (KIND == kLse) {
         const bool valid = row < tokens;
         const int64_t tcol = valid ? (int64_t)p.target[row] - n0 : -1;
         float top = -INFINITY, sum = 0.f;
-        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+        for (uint32_t c = c0; c < c1; c += 32) {
             if (n0 + c >= p.n) break;
             float v[32];
             load_tile(tmem + c, v);
-            const bool mine = tcol >= (int64_t)c && tcol < (int64_t)c + 32;
+            const uint32_t left = min(p.n - (n0 + c), c1 - c);      // a tile is a multiple of 16 columns wide
+            const bool mine = tcol >= (int64_t)c && tcol < (int64_t)c + 32 && tcol < (int64_t)(c + left);
             if (__any_sync(0xFFFFFFFFu, mine)) {
                 float at = 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) at = tcol == (int64_t)(c + j) ? v[j] : at;
                 if (mine) p.target_logit[row] = at * p.scale;
             }
-            const uint32_t left = p.n - (n0 + c);
             if (left < 32) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
                     if (j >= (int)left) v[j] = -INFINITY;
             }
-            float peak = v[0];
+            float peak = fmaxf(v[0], v[1]);
 #pragma unroll
-            for (int j = 1; j < 32; ++j) peak = fmaxf(peak, v[j]);
+            for (int j = 2; j < 32; j += 2) peak = fmaxf(peak, fmaxf(v[j], v[j + 1]));
             const float now = fmaxf(top, peak * p.k2);
             // nothing but -inf so far: keep the exponents at -inf instead of forming inf - inf
             const float from = now == -INFINITY ? 0.f : now;
@@ -134,11 +136,18 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
             sum = fmaf(sum, exp2_fast(top - from), part + part2);
             top = now;
         }
-        if (valid) p.stats[(uint64_t)tn * p.stats_ld + row] = make_float2(top, sum);
+        // the two halves of a row meet in shared memory (two buffers: the next tile may begin before this one is read)
+        if (half) s_stat[use & 1][lane_row] = make_float2(top, sum);
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + lane_row / 32) : "memory");
+        if (!half && valid) {
+            const float2 o = s_stat[use & 1][lane_row];
+            const float now = fmaxf(top, o.x), from = now == -INFINITY ? 0.f : now;
+            p.stats[(uint64_t)tn * p.stats_ld + row] = make_float2(now, sum * exp2_fast(top - from) + o.y * exp2_fast(o.x - from));
+        }
     } else if (KIND == kProb) {
         const float f = p.f[row], nl = p.neg_lse2[row];     // zero for padding rows
         __nv_bfloat16* out = p.prob + (uint64_t)row * p.prob_ld + n0;
-        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+        for (uint32_t c = c0; c < c1; c += 32) {
             float v[32];
             load_tile(tmem + c, v);
             const uint32_t left = p.n > n0 + c ? p.n - (n0 + c) : 0;
@@ -159,23 +168,29 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
         }
     } else if (KIND == kDx) {
         float* out = p.dx_sum + split * p.dx_split + (uint64_t)row * p.n + n0;
-        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+        const bool add = p.add && row < tokens;
+        for (uint32_t c = c0; c < c1; c += 32) {
             if (n0 + c >= p.n) break;
+            uint32_t old[4][8];
+            if (add) {                                      // in flight while the tile is read
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (n0 + c + 8 * j < p.n) load32(out + c + 8 * j, old[j]);
+            }
             float v[32];
             load_tile(tmem + c, v);
             if (row < tokens) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    if (n0 + c + j >= p.n) break;
+                for (int j = 0; j < 4; ++j) {
+                    if (n0 + c + 8 * j >= p.n) break;
                     uint32_t w[8];
-                    if (p.add) load32(out + c + j, w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        float x = empty ? 0.f : v[j + i];
-                        if (p.add) x += __uint_as_float(w[i]);
+                        float x = empty ? 0.f : v[8 * j + i];
+                        if (add) x += __uint_as_float(old[j][i]);
                         w[i] = __float_as_uint(x);
                     }
-                    store32(out + c + j, w);
+                    store32(out + c + 8 * j, w);
                 }
             }
         }
@@ -183,25 +198,36 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
         const uint64_t vrow = (uint64_t)p.w_row + row;
         const bool valid = row < p.m;
         const uint32_t at = valid ? p.slot[vrow] : kNone;
-        const float* term = p.target_sum + (uint64_t)(at == kNone ? 0 : at) * p.n + n0;
-        for (uint32_t c = 0; c < p.tile_n; c += 32) {
+        const bool hit = at != kNone;                       // a token has this row as its target
+        const float* term = p.target_sum + (uint64_t)(hit ? at : 0) * p.n + n0;
+        // few rows are hit, but most warps hold one: its terms are loaded a step ahead
+        uint32_t w[4][8], ahead[4][8];
+        auto fetch = [&](uint32_t c, uint32_t (&to)[4][8]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[j][i] = 0u;
+                if (hit && c < c1 && n0 + c + 8 * j < p.n) load32(term + c + 8 * j, to[j]);
+            }
+        };
+        fetch(c0, ahead);
+        for (uint32_t c = c0; c < c1; c += 32) {
             if (n0 + c >= p.n) break;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[j][i] = ahead[j][i];
+            fetch(c + 32, ahead);
             float v[32];
             load_tile(tmem + c, v);
             if (valid) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    if (n0 + c + j >= p.n) break;
+                for (int j = 0; j < 4; ++j) {
+                    if (n0 + c + 8 * j >= p.n) break;
                     float o[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = empty ? 0.f : v[j + i];
-                    if (at != kNone) {
-                        uint32_t w[8];
-                        load32(term + c + j, w);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] -= __uint_as_float(w[i]);
-                    }
-                    const uint64_t off = vrow * p.dweight_ld + n0 + c + j;
+                    for (int i = 0; i < 8; ++i) o[i] = (empty ? 0.f : v[8 * j + i]) - __uint_as_float(w[j][i]);
+                    const uint64_t off = vrow * p.dweight_ld + n0 + c + 8 * j;
                     if (p.dweight_bf16) {
                         __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.dweight) + off;
                         Raw8<__nv_bfloat16> r;
@@ -246,6 +272,8 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     extern __shared__ uint8_t ce_smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S::kStages + 5];
     __shared__ uint32_t s_tmem, s_gave_up;
+    __shared__ uint32_t s_ok[2][2][4];
+    __shared__ float2 s_stat[KIND == kLse ? 2 : 1][kTileM];
 
     const uint32_t stage0 = (smem_addr(ce_smem_raw) + 1023u) & ~1023u;
     const uint32_t bar0 = smem_addr(s_bar);
@@ -258,6 +286,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
     const bool leader = rank == 0;
 
+    let_next_start();      // the next kernel sets up its barriers and tensor memory on the SMs that this one leaves first
     if (threadIdx.x == 0) {
         tma_prefetch_map(&map_a);
         tma_prefetch_map(&map_b);
@@ -267,7 +296,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
         }
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(done(i), 1);
-            mbar_init(drained(i), 4 * CTAS);
+            mbar_init(drained(i), kEpilogueWarps * CTAS);
         }
         mbar_init(last_bar, 1);
         s_gave_up = 0;
@@ -279,6 +308,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     __syncthreads();
     if (CTAS == 2) cluster_sync_all();
     tc_fence_after();
+    wait_for_earlier();
     const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
     volatile uint32_t* gave_up = &s_gave_up;
 
@@ -364,18 +394,26 @@ __global__ void __launch_bounds__(kCeThreads, 1)
         }
     } else if (warp >= 2) {
         // ---- epilogue: warp w may read the quarter w % 4 of tensor memory's lanes ----
-        const uint32_t quarter = warp & 3;
+        const uint32_t quarter = warp & 3, half = (warp - 2) / 4;
         uint32_t use = 0;
         for (uint32_t t = first; t < total; t += step, ++use) {
             uint32_t split, tm, tn;
             tile_at(t, tiles_m, tiles_n, group, &split, &tm, &tn);
             const uint32_t buf = use & 1;
-            const bool ok = mbar_wait(done(buf), (use >> 1) & 1, gave_up);
-            if (__any_sync(0xFFFFFFFFu, !ok)) break;
+            bool ok = mbar_wait(done(buf), (use >> 1) & 1, gave_up);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            if (KIND == kLse) {
+                // the two warps of a quarter go on or stop together: they meet again inside the epilogue
+                if (lane == 0) s_ok[use & 1][half][quarter] = ok;
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+                ok = s_ok[use & 1][0][quarter] && s_ok[use & 1][1][quarter];
+            }
+            if (!ok) break;
             tc_fence_after();
             const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
-            const uint32_t row = (tm * CTAS + rank) * kTileM + quarter * 32 + lane;
-            ce_epilogue<KIND>(p, tmem + buf * kMaxTileN + (quarter * 32 << 16), row, tn, split, tokens, kb0 == kb1);
+            const uint32_t lane_row = quarter * 32 + lane;
+            ce_epilogue<KIND>(p, tmem + buf * kMaxTileN + (quarter * 32 << 16), (tm * CTAS + rank) * kTileM + lane_row, lane_row, half, use, tn,
+                              split, tokens, kb0 == kb1, s_stat);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(cluster_map(drained(buf), 0));
@@ -405,39 +443,61 @@ struct RowsParams {
 };
 
 constexpr int kRowsThreads = 1024;
+constexpr int kRowsPer = 8;      // consecutive tokens of a thread
 
 // Numbers the tokens that count, in order.  One CTA: the list is short next to everything else.
 __global__ void __launch_bounds__(kRowsThreads) ce_rows_kernel(const RowsParams p) {
     __shared__ uint32_t s_warp[32];
+    let_next_start();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     uint32_t base = 0;
     bool bad = false;
-    for (uint64_t i0 = 0; i0 < p.n; i0 += kRowsThreads) {
-        const uint64_t i = i0 + threadIdx.x;
-        const int64_t id = i < p.n ? load_id(p.targets, p.targets_dtype, i) : -1;
-        const bool counts = id >= 0;
-        bad |= id >= p.vocab;
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, counts);
-        if (lane == 0) s_warp[warp] = __popc(mask);
-        __syncthreads();
-        uint32_t before = 0, all = 0;
+    for (uint64_t i0 = 0; i0 < p.n; i0 += kRowsThreads * kRowsPer) {
+        int64_t id[kRowsPer];
+        uint32_t mine = 0;
 #pragma unroll
-        for (int w = 0; w < 32; ++w) {
-            const uint32_t c = s_warp[w];
-            before += w < (int)warp ? c : 0;
-            all += c;
+        for (int j = 0; j < kRowsPer; ++j) {
+            const uint64_t i = i0 + threadIdx.x * kRowsPer + j;
+            id[j] = i < p.n ? load_id(p.targets, p.targets_dtype, i) : -1;
         }
-        const uint32_t at = base + before + __popc(mask & ((1u << lane) - 1));
-        if (counts) {
-            const uint64_t row = (uint64_t)id - (uint64_t)p.vocab_start;
-            p.source[at] = (int32_t)i;
-            p.target[at] = row < p.vocab_rows ? (int32_t)row : -1;
-        } else if (i < p.n) {
-            if (p.lse) p.lse[i] = 0.f;
-            if (p.target_logit) p.target_logit[i] = 0.f;
-            if (p.loss) p.loss[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kRowsPer; ++j) {
+            mine += id[j] >= 0;
+            bad |= id[j] >= p.vocab;
         }
-        if (p.place && i < p.n) p.place[i] = counts ? (int32_t)at : -1;
+        uint32_t inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            if (lane >= (uint32_t)o) inc += v;
+        }
+        if (lane == 31) s_warp[warp] = inc;
+        __syncthreads();
+        const uint32_t total = s_warp[lane];
+        uint32_t before = lane < warp ? total : 0, all = total;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+            all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+        }
+        uint32_t at = base + before + inc - mine;
+#pragma unroll
+        for (int j = 0; j < kRowsPer; ++j) {
+            const uint64_t i = i0 + threadIdx.x * kRowsPer + j;
+            if (i >= p.n) break;
+            const bool counts = id[j] >= 0;
+            if (p.place) p.place[i] = counts ? (int32_t)at : -1;
+            if (counts) {
+                const uint64_t row = (uint64_t)id[j] - (uint64_t)p.vocab_start;
+                p.source[at] = (int32_t)i;
+                p.target[at] = row < p.vocab_rows ? (int32_t)row : -1;
+                ++at;
+            } else {
+                if (p.lse) p.lse[i] = 0.f;
+                if (p.target_logit) p.target_logit[i] = 0.f;
+                if (p.loss) p.loss[i] = 0.f;
+            }
+        }
         base += all;
         __syncthreads();
     }
@@ -453,7 +513,12 @@ struct GatherRowsParams {
     uint32_t hidden;
     bool vec;
     __nv_bfloat16* rows;     // padded tokens x hidden
-    float* target_logit;     // forward: cleared (compact order)
+    // forward: the target's logit, added up in fp32 here and, later, by the tensor cores (compact order)
+    const int32_t* target;
+    const __nv_bfloat16* weight;
+    uint64_t weight_ld;
+    float* exact_logit;
+    float* target_logit;     // cleared
     // backward
     const float* dloss;
     const float* lse;
@@ -464,82 +529,116 @@ struct GatherRowsParams {
 
 // Copies the rows that count together and clears the padding rows up to the next multiple of kPadRows.
 __global__ void __launch_bounds__(256) ce_gather_kernel(const GatherRowsParams p) {
+    __shared__ float s_part[8];
+    wait_for_earlier();
+    let_next_start();
     const uint32_t count = *p.count, i = blockIdx.x;
     const uint32_t padded = (uint32_t)((count + kPadRows - 1) / kPadRows * kPadRows);
     if (i >= padded) return;
     const bool live = i < count;
     const uint32_t src = live ? (uint32_t)p.source[i] : 0;
+    const int32_t target = live && p.exact_logit ? p.target[i] : -1;
     __nv_bfloat16* out = p.rows + (uint64_t)i * p.hidden;
     const __nv_bfloat16* in = p.x + (uint64_t)src * p.x_ld;
+    float dot = 0.f;
     for (uint32_t c = threadIdx.x * 8; c < p.hidden; c += 256 * 8) {
-        Raw8<__nv_bfloat16> r;
+        Raw8<__nv_bfloat16> r, w;
+        if (target >= 0) w.load(p.weight + (uint64_t)target * p.weight_ld + c);
+        float f[8];
         if (!live) {
             r.zero();
         } else if (p.vec) {
             r.load(in + c);
         } else {
-            float f[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] = to_f(in[c + j]);
             r.set(f);
         }
         r.store(out + c);
-    }
-    if (threadIdx.x == 0) {
-        if (p.target_logit) p.target_logit[i] = 0.f;
-        if (p.f) {
-            p.f[i] = live ? p.scale * p.dloss[src] : 0.f;
-            p.neg_lse2[i] = live ? -p.lse[src] * kLog2e : 0.f;
+        if (target >= 0) {
+            float g[8];
+            r.get(f);
+            w.get(g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dot = fmaf(f[j], g[j], dot);
         }
+    }
+    if (p.exact_logit) {
+        dot = warp_sum(dot);
+        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x / 32] = dot;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int w = 1; w < 8; ++w) dot += s_part[w];
+            p.exact_logit[i] = target >= 0 ? dot * p.scale : 0.f;
+            p.target_logit[i] = 0.f;
+        }
+    } else if (threadIdx.x == 0) {
+        p.f[i] = live ? p.scale * p.dloss[src] : 0.f;
+        p.neg_lse2[i] = live ? -p.lse[src] * kLog2e : 0.f;
     }
 }
 
 struct CombineParams {
     const uint32_t* count;
     const int32_t* source;
+    const int32_t* target;
     const float2* stats;
     uint64_t stats_ld;
     uint32_t tiles;
     const float* row_target_logit;
+    const float* exact_logit;
     float *lse, *target_logit, *loss;
 };
 
-// log-sum-exp of a token from its tiles' statistics: 32 tokens per CTA, 32 threads per token.
-__global__ void __launch_bounds__(1024) ce_combine_kernel(const CombineParams p) {
-    __shared__ float s_top[32][33], s_sum[32][33];
-    const uint32_t count = *p.count, lane = threadIdx.x & 31, part = threadIdx.x / 32;
-    const uint32_t i0 = blockIdx.x * 32;
-    if (i0 >= count) return;
-    float top = -INFINITY, sum = 0.f;
+constexpr int kCombineRows = 8;      // tokens of a CTA: their statistics of one tile fill two sectors
+constexpr int kCombineThreads = 512;
+
+// log-sum-exp of a token from its tiles' statistics.  The tensor cores add a logit's products up with
+// truncation (4e-6 of its size at 4096 products), which matters for one logit, the target's: it is taken from the
+// fp32 sum, and lse is moved by what that changes in the sum of exponentials, so that a loss near zero stays exact.
+__global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const CombineParams p) {
+    __shared__ float s_top[kCombineThreads / 32][kCombineRows], s_sum[kCombineThreads / 32][kCombineRows];
+    wait_for_earlier();
+    const uint32_t count = *p.count, r = threadIdx.x % kCombineRows, part = threadIdx.x / kCombineRows;
+    constexpr uint32_t kParts = kCombineThreads / kCombineRows;
+    const uint32_t i = blockIdx.x * kCombineRows + r;
+    if (blockIdx.x * kCombineRows >= count) return;
     auto join = [](float& top, float& sum, float t2, float s2) {
         const float now = fmaxf(top, t2), from = now == -INFINITY ? 0.f : now;
         sum = sum * exp2_fast(top - from) + s2 * exp2_fast(t2 - from);
         top = now;
     };
-    if (i0 + lane < count) {
-#pragma unroll 4
-        for (uint32_t t = part; t < p.tiles; t += 32) {
-            const float2 v = p.stats[(uint64_t)t * p.stats_ld + i0 + lane];
+    float top = -INFINITY, sum = 0.f;
+    if (i < count) {
+#pragma unroll 8
+        for (uint32_t t = part; t < p.tiles; t += kParts) {
+            const float2 v = p.stats[(uint64_t)t * p.stats_ld + i];
             join(top, sum, v.x, v.y);
         }
     }
-    s_top[part][lane] = top;
-    s_sum[part][lane] = sum;
-    __syncthreads();
-    top = s_top[lane][part];
-    sum = s_sum[lane][part];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
+    for (int o = kCombineRows; o < 32; o <<= 1) {
         const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         join(top, sum, t2, s2);
     }
-    const uint32_t i = i0 + part;
-    if (lane == 0 && i < count) {
-        const float lse = (top + log2f(sum)) * kLn2, at = p.row_target_logit[i];
+    if ((threadIdx.x & 31) < kCombineRows) {
+        s_top[threadIdx.x / 32][r] = top;
+        s_sum[threadIdx.x / 32][r] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < kCombineRows && i < count) {
+        for (int w = 1; w < kCombineThreads / 32; ++w) join(top, sum, s_top[w][r], s_sum[w][r]);
+        float lse = (top + log2f(sum)) * kLn2;
+        const float made = p.row_target_logit[i], exact = p.exact_logit[i];
         const uint32_t n = (uint32_t)p.source[i];
+        if (p.target[i] >= 0 && made != exact) {
+            const float move = exp2_fast((made - lse) * kLog2e) * expm1f(exact - made);
+            if (fabsf(move) < 0.5f) lse += log1pf(move);      // else the logits are not finite or beyond fp32's reach
+        }
         p.lse[n] = lse;
-        if (p.target_logit) p.target_logit[n] = at;
-        if (p.loss) p.loss[n] = lse - at;
+        if (p.target_logit) p.target_logit[n] = exact;
+        if (p.loss) p.loss[n] = lse - exact;
     }
 }
 
@@ -558,6 +657,7 @@ struct DxParams {
 
 // dx of every token: its splits' sums less the target's row; zero for ignored tokens.
 __global__ void __launch_bounds__(256) ce_dx_kernel(const DxParams p) {
+    wait_for_earlier();
     const int32_t i = p.place[blockIdx.x];
     __nv_bfloat16* out = p.dx + (uint64_t)blockIdx.x * p.dx_ld;
     const int32_t target = i >= 0 ? p.target[i] : -1;
@@ -632,10 +732,21 @@ static uint64_t take(uint64_t& at, uint64_t bytes) {
     return here;
 }
 
+// Columns of a tile of kLse.  More than 128 tokens: 256, the widest.  Up to 128 tokens there is one row of tiles and
+// reading W is all the time there is: the width that gives every SM the same share of W's rows
+// (151936 rows: 208, five tiles for each of 148 SMs, 195 us; 256 gives 5 tiles to two of them and 4 to the others, 209 us).
 static uint32_t lse_tile_n(uint64_t tokens, uint64_t vocab) {
-    (void)tokens;
-    (void)vocab;
-    return kMaxTileN;
+    if (pair_of(tokens) == 2) return kMaxTileN;
+    uint32_t best = kMaxTileN;
+    uint64_t best_rows = UINT64_MAX;
+    for (uint32_t n = kMaxTileN; n >= 128; n -= 16) {
+        const uint64_t tiles = (vocab + n - 1) / n, rows = (tiles + kSplitSms - 1) / kSplitSms * n;
+        if (rows < best_rows) {
+            best_rows = rows;
+            best = n;
+        }
+    }
+    return best;
 }
 
 static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded, uint64_t& at) {
@@ -707,30 +818,36 @@ static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint
 }
 
 template <int KIND, int CTAS>
-static dte_status launch_ce_as(const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t most_tiles, int sms, cudaStream_t st) {
+static dte_status launch_ce_as(const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t most_tiles, int device, cudaStream_t st) {
     using S = CeStage<CTAS>;
-    DTE_CUDA(cudaFuncSetAttribute(ce_kernel<KIND, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
+    static std::atomic<uint64_t> ready{0};
+    dte_status s = allow_smem(ce_kernel<KIND, CTAS>, S::kSmem, device, ready);
+    if (s != DTE_OK) return s;
+    int sms = 0;
+    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
     cudaLaunchConfig_t cfg = {};
     const uint64_t teams = (uint64_t)(sms / CTAS);
     cfg.gridDim = dim3((unsigned)((most_tiles < teams ? most_tiles : teams) * CTAS));
     cfg.blockDim = dim3(kCeThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CTAS;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // as launch_after
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CTAS;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     DTE_CUDA(cudaLaunchKernelEx(&cfg, ce_kernel<KIND, CTAS>, a, b, p));
     return DTE_OK;
 }
 
 template <int KIND>
-static dte_status launch_ce(int ctas, const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t rows, int sms, cudaStream_t st) {
+static dte_status launch_ce(int ctas, const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t rows, int device, cudaStream_t st) {
     const uint64_t tiles = (rows + kTileM * ctas - 1) / (kTileM * ctas) * ((p.n + p.tile_n - 1) / p.tile_n) * p.splits;
-    return ctas == 2 ? launch_ce_as<KIND, 2>(a, b, p, tiles, sms, st) : launch_ce_as<KIND, 1>(a, b, p, tiles, sms, st);
+    return ctas == 2 ? launch_ce_as<KIND, 2>(a, b, p, tiles, device, st) : launch_ce_as<KIND, 1>(a, b, p, tiles, device, st);
 }
 
 static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets, uint64_t vocab_start,
@@ -758,8 +875,8 @@ static bool ce_sizes_ok(uint64_t tokens, uint64_t vocab, uint64_t hidden) {
     return tokens <= (1u << 24) && vocab <= (1u << 30) && hidden <= (1u << 20);
 }
 
-static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix* x, const dte_ids* targets, uint64_t vocab_start,
-                               uint64_t vocab, uint64_t vocab_rows, uint64_t padded, float scale, float* lse, float* target_logit,
+static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets,
+                               uint64_t vocab_start, uint64_t vocab, uint64_t padded, float scale, float* lse, float* target_logit,
                                float* loss, const float* lse_in, const float* dloss, uint64_t* flags, cudaStream_t st) {
     RowsParams r = {};
     r.targets = targets->data;
@@ -767,7 +884,7 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     r.n = (uint32_t)targets->count;
     r.vocab_start = (int64_t)vocab_start;
     r.vocab = (int64_t)vocab;
-    r.vocab_rows = (uint32_t)vocab_rows;
+    r.vocab_rows = (uint32_t)weight->rows;
     r.count = reinterpret_cast<uint32_t*>(ws + l.count);
     r.source = reinterpret_cast<int32_t*>(ws + l.source);
     r.target = reinterpret_cast<int32_t*>(ws + l.target);
@@ -786,17 +903,20 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     g.hidden = (uint32_t)x->cols;
     g.vec = vec8_ok(x);
     g.rows = reinterpret_cast<__nv_bfloat16*>(ws + l.rows);
+    g.scale = scale;
     if (dloss) {
         g.dloss = dloss;
         g.lse = lse_in;
-        g.scale = scale;
         g.f = reinterpret_cast<float*>(ws + l.scalar0);
         g.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     } else {
+        g.target = r.target;
+        g.weight = static_cast<const __nv_bfloat16*>(weight->data);
+        g.weight_ld = weight->ld;
         g.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
+        g.exact_logit = reinterpret_cast<float*>(ws + l.scalar1);
     }
-    ce_gather_kernel<<<(unsigned)padded, 256, 0, st>>>(g);
-    DTE_CUDA(cudaGetLastError());
+    DTE_CUDA(launch_after(ce_gather_kernel, dim3((unsigned)padded), 256, 0, st, g));
     return DTE_OK;
 }
 
@@ -824,11 +944,11 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     if (n == 0) return DTE_OK;
     OpDeviceGuard g(device);
     int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    if ((s = device_sms(device, &sms)) != DTE_OK) return s;             // also checks the ordinal
     cudaStream_t st = (cudaStream_t)cuda_stream;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const CeShape sh = ce_shape(n, V, H, kProbBytes);
-    if ((s = prepare_rows(l, ws, x, targets, vocab_start, vocab, V, sh.padded, (float)logit_scale, lse, target_logit, loss, nullptr,
+    if ((s = prepare_rows(l, ws, x, weight, targets, vocab_start, vocab, sh.padded, (float)logit_scale, lse, target_logit, loss, nullptr,
                           nullptr, flags, st)) != DTE_OK)
         return s;
     const uint32_t tn = lse_tile_n(n, V);
@@ -848,19 +968,20 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     CUtensorMap ma, mb;
     if ((s = encode(&ma, ws + l.rows, sh.padded, H, H, kTileM)) != DTE_OK) return s;
     if ((s = encode(&mb, weight->data, V, H, weight->ld, tn / sh.ctas)) != DTE_OK) return s;
-    if ((s = launch_ce<kLse>(sh.ctas, ma, mb, p, n, sms, st)) != DTE_OK) return s;
+    if ((s = launch_ce<kLse>(sh.ctas, ma, mb, p, n, device, st)) != DTE_OK) return s;
     CombineParams c = {};
     c.count = p.tokens;
     c.source = reinterpret_cast<int32_t*>(ws + l.source);
     c.stats = p.stats;
     c.stats_ld = p.stats_ld;
     c.tiles = (uint32_t)((V + tn - 1) / tn);
+    c.target = p.target;
     c.row_target_logit = p.target_logit;
+    c.exact_logit = reinterpret_cast<float*>(ws + l.scalar1);
     c.lse = lse;
     c.target_logit = target_logit;
     c.loss = loss;
-    ce_combine_kernel<<<(unsigned)((n + 31) / 32), 1024, 0, st>>>(c);
-    DTE_CUDA(cudaGetLastError());
+    DTE_CUDA(launch_after(ce_combine_kernel, dim3((unsigned)((n + kCombineRows - 1) / kCombineRows)), kCombineThreads, 0, st, c));
     return DTE_OK;
 }
 
@@ -907,14 +1028,15 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     if (n == 0 && (!dweight || accumulate)) return DTE_OK;
     OpDeviceGuard g(device);
     int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    if ((s = device_sms(device, &sms)) != DTE_OK) return s;             // also checks the ordinal
     cudaStream_t st = (cudaStream_t)cuda_stream;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (n == 0) {
         DTE_CUDA(cudaMemset2DAsync(dweight->data, dweight->ld * elem_size(dweight->dtype), 0, H * elem_size(dweight->dtype), V, st));
         return DTE_OK;
     }
-    if ((s = prepare_rows(l, ws, x, targets, vocab_start, vocab, V, sh.padded, (float)logit_scale, nullptr, nullptr, nullptr, lse, dloss,
+    if (dweight) DTE_CUDA(cudaMemsetAsync(ws + l.slot, 0xFF, align_up(V, kMaxTileN) * 4, st));
+    if ((s = prepare_rows(l, ws, x, weight, targets, vocab_start, vocab, sh.padded, (float)logit_scale, nullptr, nullptr, nullptr, lse, dloss,
                           flags, st)) != DTE_OK)
         return s;
     const uint32_t* count = reinterpret_cast<uint32_t*>(ws + l.count);
@@ -923,7 +1045,6 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     uint32_t* slot = reinterpret_cast<uint32_t*>(ws + l.slot);
     float* target_sum = reinterpret_cast<float*>(ws + l.target_sum);
     if (dweight) {
-        DTE_CUDA(cudaMemsetAsync(slot, 0xFF, align_up(V, kMaxTileN) * 4, st));
         SortedSum q = {};
         q.ids = target;
         q.ids_dtype = DTE_I32;
@@ -942,7 +1063,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         q.out_dtype = DTE_F32;
         q.out_ld = H;
         q.slot = slot;
-        if ((s = launch_sorted_sum(q, true, ws + l.sort, sms, st)) != DTE_OK) return s;
+        if ((s = launch_sorted_sum(q, true, ws + l.sort, device, st)) != DTE_OK) return s;
     }
     CeParams p = {};
     p.tokens = count;
@@ -979,19 +1100,19 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         p.splits = 1;
         p.n = (uint32_t)vc;
         p.k = (uint32_t)H;
-        if ((s = launch_ce<kProb>(sh.ctas, x_k, w_k, p, n, sms, st)) != DTE_OK) return s;
+        if ((s = launch_ce<kProb>(sh.ctas, x_k, w_k, p, n, device, st)) != DTE_OK) return s;
         if (dx) {
             p.n = (uint32_t)H;
             p.k = (uint32_t)vc;
             p.splits = sh.splits;
             p.add = piece > 0;
-            if ((s = launch_ce<kDx>(sh.ctas, g_k, w_n, p, n, sms, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDx>(sh.ctas, g_k, w_n, p, n, device, st)) != DTE_OK) return s;
         }
         if (dweight) {
             p.m = (uint32_t)vc;
             p.n = (uint32_t)H;
             p.splits = 1;
-            if ((s = launch_ce<kDw>(sh.ctas, g_m, x_n, p, vc, sms, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDw>(sh.ctas, g_m, x_n, p, vc, device, st)) != DTE_OK) return s;
         }
     }
     if (dx) {
@@ -1007,8 +1128,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         d.weight_ld = weight->ld;
         d.dx = static_cast<__nv_bfloat16*>(dx->data);
         d.dx_ld = dx->ld;
-        ce_dx_kernel<<<(unsigned)n, 256, 0, st>>>(d);
-        DTE_CUDA(cudaGetLastError());
+        DTE_CUDA(launch_after(ce_dx_kernel, dim3((unsigned)n), 256, 0, st, d));
     }
     return DTE_OK;
 }

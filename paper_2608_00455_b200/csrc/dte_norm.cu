@@ -30,12 +30,24 @@ struct NormParams {
     float eps, inv_cols;
     float* mean;
     float* rstd;
+    bool want_bias;           // backward: dbias is wanted
     float* partial;           // backward: teams' sums, grid x 2 x cols (NULL: no weight gradient wanted)
 };
 
 __device__ __forceinline__ float load_param(const void* p, uint32_t dtype, uint32_t i, float none) {
     if (!p) return none;
     return dtype == DTE_BF16 ? to_f(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+
+__device__ __forceinline__ float f2_sum(F2 a) {
+    float lo, hi;
+    f2_get(a, lo, hi);
+    return lo + hi;
+}
+__device__ __forceinline__ float f2_at(const F2* a, int j) {
+    float lo, hi;
+    f2_get(a[j / 2], lo, hi);
+    return j & 1 ? hi : lo;
 }
 
 // The eight columns of thread t of a team of n threads.  VEC: 16-byte accesses (8 consecutive bf16, or
@@ -50,9 +62,11 @@ struct RowPart<__nv_bfloat16, true> {
     __device__ __forceinline__ void load(const __nv_bfloat16* p, uint32_t t, uint32_t, uint32_t cols) {
         a = t * 8 < cols ? __ldcs(reinterpret_cast<const uint4*>(p + t * 8)) : make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ void get(float* f) const {
-        f[0] = bf16_lo(a.x); f[1] = bf16_hi(a.x); f[2] = bf16_lo(a.y); f[3] = bf16_hi(a.y);
-        f[4] = bf16_lo(a.z); f[5] = bf16_hi(a.z); f[6] = bf16_lo(a.w); f[7] = bf16_hi(a.w);
+    __device__ __forceinline__ void get(F2* f) const {
+        f[0] = f2(bf16_lo(a.x), bf16_hi(a.x));
+        f[1] = f2(bf16_lo(a.y), bf16_hi(a.y));
+        f[2] = f2(bf16_lo(a.z), bf16_hi(a.z));
+        f[3] = f2(bf16_lo(a.w), bf16_hi(a.w));
     }
     static __device__ __forceinline__ void put(__nv_bfloat16* p, uint32_t t, uint32_t, uint32_t cols, const float* f) {
         if (t * 8 < cols)
@@ -69,8 +83,11 @@ struct RowPart<float, true> {
         a = t * 4 < cols ? __ldcs(reinterpret_cast<const float4*>(p + t * 4)) : z;
         b = (n + t) * 4 < cols ? __ldcs(reinterpret_cast<const float4*>(p + (n + t) * 4)) : z;
     }
-    __device__ __forceinline__ void get(float* f) const {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    __device__ __forceinline__ void get(F2* f) const {
+        f[0] = f2(a.x, a.y);
+        f[1] = f2(a.z, a.w);
+        f[2] = f2(b.x, b.y);
+        f[3] = f2(b.z, b.w);
     }
     static __device__ __forceinline__ void put(float* p, uint32_t t, uint32_t n, uint32_t cols, const float* f) {
         if (t * 4 < cols) *reinterpret_cast<float4*>(p + t * 4) = make_float4(f[0], f[1], f[2], f[3]);
@@ -85,9 +102,9 @@ struct RowPart<T, false> {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) a[j] = t + j * n < cols ? p[t + j * n] : from_f<T>(0.f);
     }
-    __device__ __forceinline__ void get(float* f) const {
+    __device__ __forceinline__ void get(F2* f) const {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) f[j] = to_f<T>(a[j]);
+        for (int j = 0; j < kPer / 2; ++j) f[j] = f2(to_f<T>(a[2 * j]), to_f<T>(a[2 * j + 1]));
     }
     static __device__ __forceinline__ void put(T* p, uint32_t t, uint32_t n, uint32_t cols, const float* f) {
 #pragma unroll
@@ -128,12 +145,20 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
     const uint32_t me = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
     const T* x = static_cast<const T*>(p.x);
     T* y = static_cast<T*>(p.out);
-    float w[kPer], b[kPer];
+    F2 w[kPer / 2], b[kPer / 2], in[kPer / 2];            // in: 1 for columns of the row, 0 past its end
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = RowPart<T, VEC>::col(t, n, j);
-        w[j] = c < p.cols ? load_param(p.weight, p.param_dtype, c, 1.f) : 0.f;
-        b[j] = c < p.cols ? load_param(p.bias, p.param_dtype, c, 0.f) : 0.f;
+    for (int j = 0; j < kPer / 2; ++j) {
+        float u[2], v[2], q[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t c = RowPart<T, VEC>::col(t, n, 2 * j + i);
+            q[i] = c < p.cols ? 1.f : 0.f;
+            u[i] = c < p.cols ? load_param(p.weight, p.param_dtype, c, 1.f) : 0.f;
+            v[i] = c < p.cols ? load_param(p.bias, p.param_dtype, c, 0.f) : 0.f;
+        }
+        w[j] = f2(u[0], u[1]);
+        b[j] = f2(v[0], v[1]);
+        in[j] = f2(q[0], q[1]);
     }
     RowPart<T, VEC> next;
     if (me < p.rows) next.load(x + (uint64_t)me * p.x_ld, t, n, p.cols);
@@ -142,26 +167,30 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
     for (uint32_t k = 0; k < rounds; ++k) {
         const uint64_t row = (uint64_t)k * teams + me;
         if (TEAM > 32 && row >= p.rows) break;
-        float f[kPer];
+        F2 f[kPer / 2];
         next.get(f);
         if (row + teams < p.rows) next.load(x + (row + teams) * p.x_ld, t, n, p.cols);
         float mean = 0.f;
         if (KIND == DTE_NORM_LAYER) {
-            float s[1] = {((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]))};
+            float s[1] = {f2_sum(f2_add(f2_add(f[0], f[1]), f2_add(f[2], f[3])))};
             team_sum<TEAM, 1>(s, buf[0]);
             mean = s[0] * p.inv_cols;
+            const F2 m = f2(-mean, -mean);
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) f[j] = RowPart<T, VEC>::col(t, n, j) < p.cols ? f[j] - mean : 0.f;
+            for (int j = 0; j < kPer / 2; ++j) f[j] = f2_fma(in[j], m, f[j]);
         }
-        float q[1] = {0.f};
+        F2 q2 = f2_mul(f[0], f[0]);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) q[0] = fmaf(f[j], f[j], q[0]);
+        for (int j = 1; j < kPer / 2; ++j) q2 = f2_fma(f[j], f[j], q2);
+        float q[1] = {f2_sum(q2)};
         team_sum<TEAM, 1>(q, KIND == DTE_NORM_LAYER ? buf[1] : buf[k & 1]);
         const float rstd = 1.f / sqrtf(q[0] * p.inv_cols + p.eps);
         if (row < p.rows) {
+            const F2 r = f2(rstd, rstd);
+            float o[kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) f[j] = fmaf(f[j] * rstd, w[j], b[j]);
-            RowPart<T, VEC>::put(y + row * p.out_ld, t, n, p.cols, f);
+            for (int j = 0; j < kPer / 2; ++j) f2_get(f2_fma(f2_mul(f[j], r), w[j], b[j]), o[2 * j], o[2 * j + 1]);
+            RowPart<T, VEC>::put(y + row * p.out_ld, t, n, p.cols, o);
             if (t == 0) {
                 if (KIND == DTE_NORM_LAYER && p.mean) p.mean[row] = mean;
                 if (p.rstd) p.rstd[row] = rstd;
@@ -180,12 +209,17 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
     const T* x = static_cast<const T*>(p.x);
     const T* dy = static_cast<const T*>(p.dout);
     T* dx = static_cast<T*>(p.out);
-    float w[kPer], dw[kPer], db[kPer];
+    F2 w[kPer / 2], dw[kPer / 2], db[kPer / 2];
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const uint32_t c = RowPart<T, VEC>::col(t, n, j);
-        w[j] = c < p.cols ? load_param(p.weight, p.param_dtype, c, 1.f) : 0.f;
-        dw[j] = db[j] = 0.f;
+    for (int j = 0; j < kPer / 2; ++j) {
+        float u[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t c = RowPart<T, VEC>::col(t, n, 2 * j + i);
+            u[i] = c < p.cols ? load_param(p.weight, p.param_dtype, c, 1.f) : 0.f;
+        }
+        w[j] = f2(u[0], u[1]);
+        dw[j] = db[j] = f2(0.f, 0.f);
     }
     RowPart<T, VEC> nx, ny;
     float nmean = 0.f, nrstd = 0.f;
@@ -200,31 +234,47 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
     for (uint32_t k = 0; k < rounds; ++k) {
         const uint64_t row = (uint64_t)k * teams + me;
         if (TEAM > 32 && row >= p.rows) break;
-        float xh[kPer], g[kPer];
+        F2 xh[kPer / 2], g[kPer / 2];
         nx.get(xh);
         ny.get(g);
         const float mean = nmean, rstd = nrstd;
         if (row + teams < p.rows) fetch(row + teams);
-        float s[2] = {0.f, 0.f};
         const bool live = row < p.rows;
+        const F2 r = f2(rstd, rstd), m = f2(-mean * rstd, -mean * rstd);
+        F2 s2 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            // columns past the end hold zero in g and w, so they add nothing whatever xh is; it stays finite
-            xh[j] = (KIND == DTE_NORM_LAYER ? xh[j] - mean : xh[j]) * rstd;
+        for (int j = 0; j < kPer / 2; ++j) {
+            // columns past the end hold zero in g and w, so they add nothing: xh is finite there
+            xh[j] = KIND == DTE_NORM_LAYER ? f2_fma(xh[j], r, m) : f2_mul(xh[j], r);
             if (live) {
-                dw[j] = fmaf(g[j], xh[j], dw[j]);
-                db[j] += g[j];
+                dw[j] = f2_fma(g[j], xh[j], dw[j]);
+                if (KIND == DTE_NORM_LAYER || p.want_bias) db[j] = f2_add(db[j], g[j]);
             }
-            g[j] *= w[j];
-            s[0] = fmaf(g[j], xh[j], s[0]);
-            s[1] += g[j];
+            g[j] = f2_mul(g[j], w[j]);
+            s2 = f2_fma(g[j], xh[j], s2);
+            if (KIND == DTE_NORM_LAYER) s1 = f2_add(s1, g[j]);
         }
-        team_sum<TEAM, 2>(s, buf[k & 1]);
+        float c1 = 0.f, c2;
+        if (KIND == DTE_NORM_LAYER) {
+            float s[2] = {f2_sum(s2), f2_sum(s1)};
+            team_sum<TEAM, 2>(s, buf[k & 1]);
+            c2 = s[0];
+            c1 = s[1];
+        } else {
+            float s[1] = {f2_sum(s2)};
+            team_sum<TEAM, 1>(s, buf[k & 1]);
+            c2 = s[0];
+        }
         if (live && dx) {
-            const float c2 = s[0] * p.inv_cols, c1 = KIND == DTE_NORM_LAYER ? s[1] * p.inv_cols : 0.f;
+            // rstd * (g - c1 - xh * c2)
+            c2 *= -p.inv_cols * rstd;
+            c1 *= -p.inv_cols * rstd;
+            const F2 a = f2(c2, c2), b = f2(c1, c1);
+            float o[kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) g[j] = rstd * (fmaf(-xh[j], c2, g[j]) - c1);
-            RowPart<T, VEC>::put(dx + row * p.out_ld, t, n, p.cols, g);
+            for (int j = 0; j < kPer / 2; ++j)
+                f2_get(f2_fma(xh[j], a, KIND == DTE_NORM_LAYER ? f2_fma(g[j], r, b) : f2_mul(g[j], r)), o[2 * j], o[2 * j + 1]);
+            RowPart<T, VEC>::put(dx + row * p.out_ld, t, n, p.cols, o);
         }
     }
     if (!p.partial) return;
@@ -235,8 +285,8 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const uint32_t c = RowPart<T, VEC>::col(t, n, j);
-            sums[0][(threadIdx.x / n) * (n * kPer) + c] = dw[j];
-            sums[1][(threadIdx.x / n) * (n * kPer) + c] = db[j];
+            sums[0][(threadIdx.x / n) * (n * kPer) + c] = f2_at(dw, j);
+            sums[1][(threadIdx.x / n) * (n * kPer) + c] = f2_at(db, j);
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 2 * p.cols; i += kTeamThreads) {
@@ -251,8 +301,8 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
         for (int j = 0; j < kPer; ++j) {
             const uint32_t c = RowPart<T, VEC>::col(t, n, j);
             if (c < p.cols) {
-                o[c] = dw[j];
-                o[p.cols + c] = db[j];
+                o[c] = f2_at(dw, j);
+                o[p.cols + c] = f2_at(db, j);
             }
         }
     }
@@ -262,6 +312,7 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
 __global__ void __launch_bounds__(1024) norm_sums_kernel(const float* partial, uint32_t parts, uint32_t cols, bool accumulate,
                                                          float* dweight, float* dbias) {
     __shared__ float sums[32][33];
+    wait_for_earlier();
     float* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
     const uint32_t lane = threadIdx.x & 31, part = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
@@ -523,6 +574,7 @@ extern "C" dte_status dte_norm_backward(const dte_matrix* dout, const dte_matrix
     p.inv_cols = (float)(1.0 / (double)x->cols);
     p.mean = const_cast<float*>(mean);
     p.rstd = const_cast<float*>(rstd);
+    p.want_bias = dbias != nullptr;
     p.partial = want ? static_cast<float*>(workspace) : nullptr;
     const NormShape sh = norm_shape(x->rows, x->cols, sms, 1024);
     cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -531,9 +583,8 @@ extern "C" dte_status dte_norm_backward(const dte_matrix* dout, const dte_matrix
         DTE_CUDA(cudaGetLastError());
     }
     if (want) {
-        norm_sums_kernel<<<dim3((p.cols + 31) / 32, 2), 1024, 0, st>>>(p.partial, x->rows ? sh.ctas : 0, p.cols,
-                                                                      accumulate != 0, dweight, dbias);
-        DTE_CUDA(cudaGetLastError());
+        DTE_CUDA(launch_after(norm_sums_kernel, dim3((p.cols + 31) / 32, 2), 1024, 0, st, p.partial, x->rows ? sh.ctas : 0, p.cols,
+                              accumulate != 0, dweight, dbias));
     }
     return DTE_OK;
 }

@@ -5,6 +5,7 @@
 
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "dte_internal.cuh"
@@ -75,6 +76,16 @@ inline bool vec8_ok(const dte_matrix* m) {
 
 dte_status device_sms(int device, int* sms);   // multiprocessor count, cached per device
 
+// Raises a kernel's dynamic shared memory limit, once per device.
+template <typename Kernel>
+inline dte_status allow_smem(Kernel* kernel, size_t bytes, int device, std::atomic<uint64_t>& done) {
+    const uint64_t bit = 1ull << device;                 // device < kMaxDevices = 64: checked by device_sms
+    if (done.load(std::memory_order_relaxed) & bit) return DTE_OK;
+    DTE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return DTE_OK;
+}
+
 // ---- sorted-token sums ----------------------------------------------------------------------------
 // out[key] = scale * sum over entries with that key of weight[entry] * src[row of entry]
 // Entries are ordered by a stable radix sort of their keys, so every sum has one fixed order.
@@ -90,7 +101,7 @@ struct SortedSum {
     const void* src;          // n x hidden
     uint32_t src_dtype;
     uint64_t src_ld;
-    const float* weight;      // per entry, or NULL
+    const float* weight;      // per entry, or NULL; with weights: src bf16, compact form, vector path
     uint32_t hidden;
     float scale;
     // dense form (slot == NULL): out is rows x hidden of out_dtype, accumulate or write all rows.
@@ -104,9 +115,32 @@ struct SortedSum {
     uint64_t* flags;
 };
 uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t hidden);
-dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, int sms, cudaStream_t st);
+dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, int device, cudaStream_t st);
 
 #ifdef __CUDACC__
+// ---- dependent launches ------------------------------------------------------------------------------
+// A kernel launched with launch_after may start while the one before it in the stream still runs (its launch
+// costs nothing then); it calls wait_for_earlier before it touches memory, which returns when all earlier
+// work is complete and visible.  Used only inside a call, between its own kernels.
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the kernel behind this one start now, as far as there is room.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... KernelArgs, typename... Args>
+inline cudaError_t launch_after(void (*kernel)(KernelArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, KernelArgs(args)...);
+}
+
 // ---- device: typed access --------------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ float to_f(T v);
@@ -196,6 +230,32 @@ struct Vec<T, 1> {
 
 __device__ __forceinline__ int64_t load_id(const void* ids, uint32_t dtype, uint64_t i) {
     return dtype == DTE_I64 ? (int64_t) static_cast<const long long*>(ids)[i] : (int64_t) static_cast<const int*>(ids)[i];
+}
+
+// Two floats in one 64-bit register pair: the packed instructions do two operations per issue slot.
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f2_get(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

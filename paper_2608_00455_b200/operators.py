@@ -12,7 +12,7 @@ rows a fixed stride apart.  Workspaces are uint8 tensors of at least the bytes t
 """
 from __future__ import annotations
 
-import ctypes as C
+import struct
 from typing import Optional
 
 import torch
@@ -27,13 +27,11 @@ _NUMBERS = {torch.float32: DTE_F32, torch.bfloat16: DTE_BF16}
 _IDS = {torch.int32: DTE_I32, torch.int64: DTE_I64}
 
 
-class MatrixDesc(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("ld", C.c_uint64),
-                ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
-
-
-class IdsDesc(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("count", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+# dte_matrix and dte_ids of the C ABI as packed bytes (natural alignment, no padding): cheaper to make per call than
+# a ctypes structure
+_pack_matrix = struct.Struct("=QQQQII").pack
+_pack_ids = struct.Struct("=QQII").pack
+assert struct.calcsize("=QQQQII") == 40 and struct.calcsize("=QQII") == 24
 
 
 def _refuse(msg: str):
@@ -43,9 +41,16 @@ def _refuse(msg: str):
 def _device(t: torch.Tensor, name: str) -> int:
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0 or not t.is_cuda:
         _refuse(f"{name} is not on a CUDA device; there is no CPU fallback")
-    return t.get_device()
+    return device
+
+
+def _same_device(t: torch.Tensor, name: str, device: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        if _device(t, name) != device:
+            _refuse(f"{name} is on another device")
 
 
 def _rows(t: torch.Tensor, name: str):
@@ -63,44 +68,45 @@ def _rows(t: torch.Tensor, name: str):
     return n, shape[-1] if ld is None else ld
 
 
-def _matrix(t: torch.Tensor, name: str, device: int) -> MatrixDesc:
-    if _device(t, name) != device:
-        _refuse(f"{name} is on another device")
+def _matrix(t: torch.Tensor, name: str, device: int):
+    """(packed dte_matrix, rows, columns)."""
+    _same_device(t, name, device)
     dtype = _NUMBERS.get(t.dtype)
     if dtype is None:
         _refuse(f"{name} must be float32 or bfloat16")
-    dim = t.dim()
-    if dim == 0:
-        _refuse(f"{name} needs at least one dimension")
-    cols = t.shape[-1]
-    if cols != 1 and t.stride(-1) != 1:
-        _refuse(f"{name}: the last dimension must be contiguous")
-    if dim == 2:
-        rows, ld = t.shape[0], t.stride(0)
+    shape = t.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        ld, unit = t.stride()
         if rows == 1:
             ld = cols
-    else:
+    elif shape:
+        cols, unit = shape[-1], t.stride(-1)
         rows, ld = _rows(t, name)
-    return MatrixDesc(t.data_ptr(), rows, cols, ld, dtype, 0)
+    else:
+        _refuse(f"{name} needs at least one dimension")
+    if unit != 1 and cols != 1:
+        _refuse(f"{name}: the last dimension must be contiguous")
+    return _pack_matrix(t.data_ptr(), rows, cols, ld, dtype, 0), rows, cols
 
 
-def _ids(t: torch.Tensor, name: str, device: int) -> IdsDesc:
-    if _device(t, name) != device:
-        _refuse(f"{name} is on another device")
+def _ids(t: torch.Tensor, name: str, device: int):
+    """(packed dte_ids, count)."""
+    _same_device(t, name, device)
     dtype = _IDS.get(t.dtype)
     if dtype is None:
         _refuse(f"{name} must be int32 or int64")
     if not t.is_contiguous():
         _refuse(f"{name} must be contiguous")
-    return IdsDesc(t.data_ptr(), t.numel(), dtype, 0)
+    count = t.numel()
+    return _pack_ids(t.data_ptr(), count, dtype, 0), count
 
 
 def _vector(t: Optional[torch.Tensor], name: str, device: int, count: int, dtypes=(torch.float32,)):
     """Address of a contiguous vector of `count` values, or None."""
     if t is None:
         return None
-    if _device(t, name) != device:
-        _refuse(f"{name} is on another device")
+    _same_device(t, name, device)
     if t.dtype not in dtypes:
         _refuse(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in dtypes)}")
     if t.numel() != count or not t.is_contiguous():
@@ -111,8 +117,7 @@ def _vector(t: Optional[torch.Tensor], name: str, device: int, count: int, dtype
 def _workspace(t: Optional[torch.Tensor], device: int):
     if t is None:
         return None, 0
-    if _device(t, "workspace") != device:
-        _refuse("workspace is on another device")
+    _same_device(t, "workspace", device)
     if not t.is_contiguous():
         _refuse("workspace must be contiguous")
     return t.data_ptr(), t.numel() * t.element_size()
@@ -121,8 +126,7 @@ def _workspace(t: Optional[torch.Tensor], device: int):
 def _flags(t: Optional[torch.Tensor], device: int):
     if t is None:
         return None
-    if _device(t, "flags") != device:
-        _refuse("flags is on another device")
+    _same_device(t, "flags", device)
     if t.dtype != torch.int64 or t.numel() < 1:
         _refuse("flags must be int64")
     return t.data_ptr()
@@ -159,9 +163,11 @@ def dte_embedding_forward(table: torch.Tensor, ids: torch.Tensor, out: torch.Ten
                           vocab: Optional[int] = None, flags: Optional[torch.Tensor] = None, stream=None) -> None:
     """out[n] = scale * table[ids[n] - row_start], zero for negative ids and ids of other shards."""
     device = _device(table, "table")
-    m, o, i = _matrix(table, "table", device), _matrix(out, "out", device), _ids(ids, "ids", device)
-    _done(lib().dte_embedding_forward(C.byref(m), C.byref(i), _number(row_start, "row_start"),
-                                      row_start + m.rows if vocab is None else _number(vocab, "vocab"), scale, C.byref(o),
+    m, rows, _ = _matrix(table, "table", device)
+    o, _, _ = _matrix(out, "out", device)
+    i, _ = _ids(ids, "ids", device)
+    _done(lib().dte_embedding_forward(m, i, _number(row_start, "row_start"),
+                                      row_start + rows if vocab is None else _number(vocab, "vocab"), scale, o,
                                       _flags(flags, device), device, _stream(stream, device)))
 
 
@@ -174,21 +180,24 @@ def dte_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.
                            flags: Optional[torch.Tensor] = None, stream=None) -> None:
     """dtable[v] (+)= scale * sum of dout[n] over the tokens with ids[n] == row_start + v."""
     device = _device(dtable, "dtable")
-    d, m, i = _matrix(dout, "dout", device), _matrix(dtable, "dtable", device), _ids(ids, "ids", device)
+    d, _, _ = _matrix(dout, "dout", device)
+    m, rows, _ = _matrix(dtable, "dtable", device)
+    i, _ = _ids(ids, "ids", device)
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_embedding_backward(C.byref(d), C.byref(i), _number(row_start, "row_start"),
-                                       row_start + m.rows if vocab is None else _number(vocab, "vocab"), scale, bool(accumulate),
-                                       C.byref(m), ws, size, _flags(flags, device), device, _stream(stream, device)))
+    _done(lib().dte_embedding_backward(d, i, _number(row_start, "row_start"),
+                                       row_start + rows if vocab is None else _number(vocab, "vocab"), scale, bool(accumulate),
+                                       m, ws, size, _flags(flags, device), device, _stream(stream, device)))
 
 
 def dte_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
                      mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], eps: float, rms: bool = False, stream=None) -> None:
     """Layer norm (rms: RMS norm) of every row of x; mean and rstd keep the statistics for the backward pass."""
     device = _device(x, "x")
-    m, o = _matrix(x, "x", device), _matrix(out, "out", device)
-    w, b, dtype = _params(weight, bias, device, m.cols)
-    _done(lib().dte_norm_forward(C.byref(m), w, b, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER, eps, C.byref(o),
-                                 _vector(mean, "mean", device, m.rows), _vector(rstd, "rstd", device, m.rows), device,
+    m, rows, cols = _matrix(x, "x", device)
+    o, _, _ = _matrix(out, "out", device)
+    w, b, dtype = _params(weight, bias, device, cols)
+    _done(lib().dte_norm_forward(m, w, b, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER, eps, o,
+                                 _vector(mean, "mean", device, rows), _vector(rstd, "rstd", device, rows), device,
                                  _stream(stream, device)))
 
 
@@ -201,14 +210,14 @@ def dte_norm_backward(dout: torch.Tensor, x: torch.Tensor, weight: Optional[torc
                       workspace: Optional[torch.Tensor], accumulate: bool = False, rms: bool = False, stream=None) -> None:
     """Gradients of dte_norm_forward; dweight and dbias are float32 (accumulate: added to)."""
     device = _device(x, "x")
-    d, m = _matrix(dout, "dout", device), _matrix(x, "x", device)
-    o = None if dx is None else _matrix(dx, "dx", device)
-    w, _, dtype = _params(weight, None, device, m.cols)
+    d, _, _ = _matrix(dout, "dout", device)
+    m, rows, cols = _matrix(x, "x", device)
+    o = None if dx is None else _matrix(dx, "dx", device)[0]
+    w, _, dtype = _params(weight, None, device, cols)
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_norm_backward(C.byref(d), C.byref(m), w, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER,
-                                  _vector(mean, "mean", device, m.rows), _vector(rstd, "rstd", device, m.rows), bool(accumulate),
-                                  None if o is None else C.byref(o), _vector(dweight, "dweight", device, m.cols),
-                                  _vector(dbias, "dbias", device, m.cols), ws, size, device, _stream(stream, device)))
+    _done(lib().dte_norm_backward(d, m, w, dtype, DTE_NORM_RMS if rms else DTE_NORM_LAYER,
+                                  _vector(mean, "mean", device, rows), _vector(rstd, "rstd", device, rows), bool(accumulate),
+                                  o, _vector(dweight, "dweight", device, cols), _vector(dbias, "dbias", device, cols), ws, size, device, _stream(stream, device)))
 
 
 def dte_linear_ce_forward_workspace_bytes(tokens: int, vocab_rows: int, hidden: int) -> int:
@@ -221,12 +230,14 @@ def dte_linear_ce_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.
                           flags: Optional[torch.Tensor] = None, stream=None) -> None:
     """lse, target logit and loss of every token for the head rows [vocab_start, vocab_start + rows)."""
     device = _device(x, "x")
-    m, w, t = _matrix(x, "x", device), _matrix(weight, "weight", device), _ids(targets, "targets", device)
+    m, _, _ = _matrix(x, "x", device)
+    w, rows, _ = _matrix(weight, "weight", device)
+    t, n = _ids(targets, "targets", device)
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_linear_ce_forward(C.byref(m), C.byref(w), C.byref(t), _number(vocab_start, "vocab_start"),
-                                      vocab_start + w.rows if vocab is None else _number(vocab, "vocab"), logit_scale,
-                                      _vector(lse, "lse", device, t.count), _vector(target_logit, "target_logit", device, t.count),
-                                      _vector(loss, "loss", device, t.count), ws, size, _flags(flags, device), device,
+    _done(lib().dte_linear_ce_forward(m, w, t, _number(vocab_start, "vocab_start"),
+                                      vocab_start + rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+                                      _vector(lse, "lse", device, n), _vector(target_logit, "target_logit", device, n),
+                                      _vector(loss, "loss", device, n), ws, size, _flags(flags, device), device,
                                       _stream(stream, device)))
 
 
@@ -244,12 +255,14 @@ def dte_linear_ce_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch
                            flags: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx and dweight for a given dloss per token; lse over the whole vocabulary."""
     device = _device(x, "x")
-    m, w, t = _matrix(x, "x", device), _matrix(weight, "weight", device), _ids(targets, "targets", device)
-    d = None if dx is None else _matrix(dx, "dx", device)
-    g = None if dweight is None else _matrix(dweight, "dweight", device)
+    m, _, _ = _matrix(x, "x", device)
+    w, rows, _ = _matrix(weight, "weight", device)
+    t, n = _ids(targets, "targets", device)
+    d = None if dx is None else _matrix(dx, "dx", device)[0]
+    g = None if dweight is None else _matrix(dweight, "dweight", device)[0]
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_linear_ce_backward(C.byref(m), C.byref(w), C.byref(t), _number(vocab_start, "vocab_start"),
-                                       vocab_start + w.rows if vocab is None else _number(vocab, "vocab"), logit_scale,
-                                       _vector(lse, "lse", device, t.count), _vector(dloss, "dloss", device, t.count),
-                                       bool(accumulate), None if d is None else C.byref(d), None if g is None else C.byref(g), ws,
+    _done(lib().dte_linear_ce_backward(m, w, t, _number(vocab_start, "vocab_start"),
+                                       vocab_start + rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+                                       _vector(lse, "lse", device, n), _vector(dloss, "dloss", device, n),
+                                       bool(accumulate), d, g, ws,
                                        size, _flags(flags, device), device, _stream(stream, device)))
