@@ -464,7 +464,7 @@ DTE_API dte_status dte_embedding_forward(const dte_matrix* table, const dte_ids*
 /* dtable[v] = scale * sum of dout[n] over the n with ids[n] == row_start + v, added up in order of n in
  * blocks (dout rows of padding and of other shards are not read).  accumulate != 0 adds to what
  * dtable holds, and rows without a token are not touched; otherwise every row is written, zeros
- * included.  ids.count < 2^31, dtable.rows < 2^31. */
+ * included.  ids.count < 2^31, dtable.rows < 2^21. */
 DTE_API uint64_t dte_embedding_backward_workspace_bytes(uint64_t n_ids, uint64_t hidden);
 DTE_API dte_status dte_embedding_backward(const dte_matrix* dout, const dte_ids* ids, uint64_t row_start,
                                           uint64_t vocab, double scale, int accumulate, const dte_matrix* dtable,

@@ -4,13 +4,9 @@
 // Backward: dtable[v] = s * sum_{n: id_n = v} dout[n].  What it cannot do without: the rows of dout once,
 // the gradient once (all of it, zeros included, in the non-accumulating form: for one micro-batch over
 // a full vocabulary that is most of the bytes).  Adding rows with float atomics would make the sum's
-// order, and with it the weights, differ from run to run; so the tokens are ordered first by a stable
-// radix sort and every sum runs in a fixed order.
-#include <cooperative_groups.h>
-
+// order, and with it the weights, differ from run to run; so the tokens are grouped by row first, in the
+// order of the tokens, and every sum runs in a fixed order.
 #include "dte_ops.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace dte {
 
@@ -74,31 +70,140 @@ static void lookup_types(const LookupParams& q, bool vec, cudaStream_t st) {
     else lookup_kernel<TI, TO, 1><<<(unsigned)ctas, kLookupThreads, 0, st>>>(p);
 }
 
-// ---- stable radix sort of (key, position) -------------------------------------------------------------
-// One thread-block cluster sorts: it can synchronise in hardware and read each other's histograms
-// through distributed shared memory, so all passes are one launch.  Each warp owns a contiguous stretch of
-// the entries, which together with the order of lanes (match mask below the lane) makes the sort stable.
-// The kernel that writes the gradient's zeros starts beside it and takes far longer.
-constexpr int kSortCtas = 8;
-constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kMaxDigitBits = 9;
-constexpr int kMaxBins = 1 << kMaxDigitBits;
-constexpr size_t kSortSmem = ((size_t)kSortWarps * kMaxBins + 2 * kMaxBins + 64) * sizeof(uint32_t);
+// ---- tokens grouped by row ------------------------------------------------------------------------------
+// The rows are cut into ranges, one CTA each.  Every CTA reads all ids (they stay in L2: 16384 ids are 128 KB),
+// counts those of its range per row and those of smaller rows in all, and so knows where its entries start
+// without hearing from any other CTA: one launch, no communication.  Each warp owns a contiguous stretch of the ids
+// and a histogram of its own, which together with the order of the lanes makes the grouping stable: entries of
+// a row are in the order of the tokens.  (A radix sort in one thread-block cluster took 22 us for 16384
+// ids and 152 k rows.)
+constexpr int kGroupThreads = 1024;
+constexpr int kGroupWarps = kGroupThreads / 32;
+constexpr uint32_t kMaxBins = 1536;            // rows of a CTA: 32 histograms of this many words fill 192 KB
+constexpr uint32_t kGroupCtas = 148;           // ranges to aim for: one per SM
+constexpr int kGroupUnroll = 16;               // ids of a lane in flight: 16384 ids are one round
 
-struct SortParams {
+struct GroupParams {
     const void* ids;
     uint32_t ids_dtype, n;
     const uint32_t* n_dev;
     int64_t row_start, vocab;
-    uint32_t rows, passes, digit_bits;
-    uint32_t* key[2];
-    uint32_t* pos[2];
+    uint32_t rows, bins;
+    uint32_t* first;           // rows + 1: where each row's entries start
+    uint32_t* key;             // entries: row ...
+    uint32_t* pos;             // ... and token
+    uint32_t* counters;        // cleared for the kernel behind
+    uint32_t n_counters;
     uint64_t* flags;
 };
 
-// Zeros, in small pieces in the order of their addresses: a front of a few MB moving through memory writes
-// 7.5 TB/s (2.5 GB in 330 us), while 148 or 296 CTAs that each walk the whole array reach 6.2.
+__global__ void __launch_bounds__(kGroupThreads, 1) group_kernel(const GroupParams p) {
+    extern __shared__ uint32_t group_hist[];    // kGroupWarps x bins
+    __shared__ uint32_t s_warp[32];
+    __shared__ uint32_t s_below;
+    wait_for_earlier();
+    let_next_start();
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid & 31, below_lanes = (1u << lane) - 1;
+    const uint32_t n = p.n_dev ? *p.n_dev : p.n;
+    const uint32_t r0 = blockIdx.x * p.bins, count = min(p.bins, p.rows - r0);
+    const uint32_t share = (n + kGroupWarps * 32 - 1) / (kGroupWarps * 32) * 32;
+    const uint64_t begin = (uint64_t)warp * share, end = begin + share < n ? begin + share : n;
+    uint32_t* h = group_hist + warp * p.bins;
+    for (uint32_t i = tid; i < kGroupWarps * p.bins; i += kGroupThreads) group_hist[i] = 0;
+    for (uint32_t i = blockIdx.x * kGroupThreads + tid; i < p.n_counters; i += gridDim.x * kGroupThreads) p.counters[i] = 0;
+    if (tid == 0) s_below = 0;
+    __syncthreads();
+
+    // calls f(index, row - r0, mask of lanes with the same row) for the entries of this range, in order
+    uint32_t below = 0;
+    bool bad = false;
+    auto scan = [&](bool first_time, auto&& f) {
+        for (uint64_t i0 = begin; i0 < end; i0 += 32 * kGroupUnroll) {
+            int64_t id[kGroupUnroll];
+#pragma unroll
+            for (int u = 0; u < kGroupUnroll; ++u) {
+                const uint64_t i = i0 + u * 32 + lane;
+                id[u] = i < end ? load_id(p.ids, p.ids_dtype, i) : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < kGroupUnroll; ++u) {
+                const uint64_t row = (uint64_t)id[u] - (uint64_t)p.row_start;
+                const bool valid = id[u] >= 0 && row < p.rows;
+                const bool mine = valid && (uint32_t)row - r0 < count;
+                if (first_time) {
+                    below += valid && row < r0;
+                    bad |= id[u] >= p.vocab;
+                }
+                if (__any_sync(0xFFFFFFFFu, mine)) {
+                    const uint32_t bin = mine ? (uint32_t)row - r0 : kNone;
+                    const uint32_t same = __match_any_sync(0xFFFFFFFFu, bin);
+                    f(i0 + u * 32 + lane, mine, bin, same);
+                    __syncwarp();
+                }
+            }
+        }
+    };
+    scan(true, [&](uint64_t, bool mine, uint32_t bin, uint32_t same) {
+        if (mine && !(same & below_lanes)) h[bin] += __popc(same);
+    });
+#pragma unroll
+    for (int o = 16; o; o >>= 1) below += __shfl_xor_sync(0xFFFFFFFFu, below, o);
+    if (lane == 0) atomicAdd(&s_below, below);
+    __syncthreads();
+    // thread t: bins 2t and 2t + 1
+    uint32_t total[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t bin = 2 * tid + j;
+        if (bin < count)
+            for (int w = 0; w < kGroupWarps; ++w) {
+                const uint32_t v = group_hist[w * p.bins + bin];
+                group_hist[w * p.bins + bin] = total[j];
+                total[j] += v;
+            }
+    }
+    uint32_t inc = total[0] + total[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+        if (lane >= (uint32_t)o) inc += v;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    uint32_t off = lane < warp ? s_warp[lane] : 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) off += __shfl_xor_sync(0xFFFFFFFFu, off, o);
+    uint32_t at = s_below + off + inc - total[0] - total[1];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t bin = 2 * tid + j;
+        if (bin < count) {
+            p.first[r0 + bin] = at;
+            if (r0 + bin + 1 == p.rows) p.first[p.rows] = at + total[j];
+            if (total[j])
+                for (int w = 0; w < kGroupWarps; ++w) group_hist[w * p.bins + bin] += at;
+            at += total[j];
+        }
+    }
+    __syncthreads();
+    scan(false, [&](uint64_t i, bool mine, uint32_t bin, uint32_t same) {
+        uint32_t to = 0;
+        if (mine) to = h[bin] + __popc(same & below_lanes);
+        __syncwarp();
+        if (mine) {
+            if (!(same & below_lanes)) h[bin] += __popc(same);
+            p.key[to] = r0 + bin;
+            p.pos[to] = (uint32_t)i;
+        }
+    });
+    if (bad && blockIdx.x == 0 && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
+}
+
+// ---- zeros ---------------------------------------------------------------------------------------------------
+// Written beside the grouping, in small pieces in the order of their addresses: such a front of a few MB moving
+// through memory writes 7.5 TB/s (2.5 GB in 330 us), while 148 or 296 CTAs that each walk the whole array reach 6.2.
+// Rows with entries are written twice; to look up first which rows have none cost each small CTA more
+// (2.5 GB in 515 us) than the second write.
 constexpr int kFillThreads = 256;
 constexpr uint64_t kFillBytes = kFillThreads * 64;   // of one CTA
 
@@ -118,142 +223,49 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillParams p) 
         if (i < vecs) reinterpret_cast<uint4*>(d)[i] = make_uint4(0, 0, 0, 0);
     }
     for (uint64_t i = vecs * 16 + threadIdx.x * 2; i < n; i += kFillThreads * 2) *reinterpret_cast<uint16_t*>(d + i) = 0;
-    // the sort runs beside this kernel: whoever follows this kernel must find both complete
+    // the grouping runs beside this kernel: whoever follows this kernel must find both complete
     if (blockIdx.x == gridDim.x - 1) wait_for_earlier();
 }
 
-__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads, 1) sort_kernel(const SortParams p) {
-    extern __shared__ uint32_t sort_smem[];
-    let_next_start();
-    cg::cluster_group cluster = cg::this_cluster();
-    uint32_t* hist = sort_smem;                          // kSortWarps x kMaxBins
-    uint32_t* cta_total = hist + kSortWarps * kMaxBins;  // kMaxBins, read by the other CTAs
-    uint32_t* base = cta_total + kMaxBins;               // kMaxBins
-    uint32_t* scan = base + kMaxBins;                    // 32
-    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid & 31;
-    const uint32_t rank = blockIdx.x;
-    const uint32_t n = p.n_dev ? *p.n_dev : p.n;
-    const uint32_t bins = 1u << p.digit_bits, dmask = bins - 1;
-    const uint64_t share = ((uint64_t)(n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) / 32 * 32;
-    const uint64_t begin = (uint64_t)(rank * kSortWarps + warp) * share;
-    const uint64_t end = begin + share < n ? begin + share : n;
-    uint32_t* h = hist + warp * kMaxBins;
-    bool bad = false;
-
-    for (uint32_t pass = 0; pass < p.passes; ++pass) {
-        const uint32_t shift = pass * p.digit_bits;
-        const uint32_t* in_key = p.key[(pass & 1) ^ 1];
-        const uint32_t* in_pos = p.pos[(pass & 1) ^ 1];
-        uint32_t* out_key = p.key[pass & 1];
-        uint32_t* out_pos = p.pos[pass & 1];
-        auto read_key = [&](uint64_t i) -> uint32_t {
-            if (pass) return __ldcg(in_key + i);     // written by other SMs of the cluster: L2
-            const int64_t id = load_id(p.ids, p.ids_dtype, i);
-            const uint64_t row = (uint64_t)id - (uint64_t)p.row_start;
-            bad |= id >= p.vocab;
-            return id >= 0 && row < p.rows ? (uint32_t)row : p.rows;
-        };
-        for (uint32_t d = lane; d < bins; d += 32) h[d] = 0;
-        __syncwarp();
-        for (uint64_t i0 = begin; i0 < end; i0 += 32) {
-            const bool live = i0 + lane < end;
-            const uint32_t digit = live ? (read_key(i0 + lane) >> shift) & dmask : kNone;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-            if (live && lane == (uint32_t)(__ffs(same) - 1)) h[digit] += __popc(same);
-            __syncwarp();
-        }
-        __syncthreads();
-        // hist[w][d] := entries of digit d in earlier warps of this CTA
-        if (tid < bins) {
-            uint32_t sum = 0;
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t v = hist[w * kMaxBins + tid];
-                hist[w * kMaxBins + tid] = sum;
-                sum += v;
-            }
-            cta_total[tid] = sum;
-        }
-        cluster.sync();
-        // base[d] := entries of smaller digits anywhere + of digit d in earlier CTAs
-        uint32_t all = 0, before = 0;
-        if (tid < bins) {
-            for (uint32_t c = 0; c < kSortCtas; ++c) {
-                const uint32_t v = cluster.map_shared_rank(cta_total, c)[tid];
-                if (c < rank) before += v;
-                all += v;
-            }
-        }
-        uint32_t inc = all;
-        if (tid < kMaxBins) {
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-                if (lane >= (uint32_t)o) inc += v;
-            }
-            if (lane == 31) scan[warp] = inc;
-        }
-        __syncthreads();
-        if (tid < bins) {
-            uint32_t off = 0;
-            for (uint32_t w = 0; w < warp; ++w) off += scan[w];
-            base[tid] = off + inc - all + before;
-        }
-        __syncthreads();
-        for (uint32_t d = lane; d < bins; d += 32) h[d] += base[d];
-        __syncwarp();
-        for (uint64_t i0 = begin; i0 < end; i0 += 32) {
-            const bool live = i0 + lane < end;
-            const uint32_t key = live ? read_key(i0 + lane) : 0;
-            const uint32_t digit = live ? (key >> shift) & dmask : kNone;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-            uint32_t to = 0;
-            if (live) to = h[digit] + __popc(same & ((1u << lane) - 1));
-            __syncwarp();
-            if (live) {
-                if (lane == (uint32_t)(__ffs(same) - 1)) h[digit] += __popc(same);
-                __stcg(out_key + to, key);
-                __stcg(out_pos + to, pass ? __ldcg(in_pos + i0 + lane) : (uint32_t)(i0 + lane));
-            }
-            __syncwarp();
-        }
-        __threadfence();
-        cluster.sync();      // the pass's output is complete, and cta_total may be reused
-    }
-    if (bad && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
-}
-
-// ---- sums over runs of equal keys ------------------------------------------------------------------------
-// The sorted entries are cut into blocks of kSumBlock, whatever the runs are, so a token that makes up
-// a tenth of the batch costs no more than rare ones.  A warp sums one block's runs over one stretch of columns;
-// a run inside the block is finished there, the ends of runs that cross blocks are left as fp32 partial sums
-// (at most two per block: [0] the run that comes in, [1] the run that goes out and began here), which
-// the second kernel adds up in order.
-constexpr int kSumBlock = 16;          // entries of a warp: two batches of kSumUnroll loads in flight
+// ---- sums over the entries of a row -------------------------------------
+// The grouped entries are cut into blocks of kSumBlock, whatever the rows are, so a token that makes up a tenth of
+// the batch costs no more than rare ones.  A warp sums one block's runs of equal rows over one stretch of columns; a
+// run inside the block is finished there.  Of a run that crosses blocks each block leaves an fp32 partial sum (at most
+// two per block: [0] of the run that comes in, [1] of the run that began here and goes on), and the warp that leaves
+// the last of them adds them up, in the order of the blocks whoever it is.
+constexpr int kSumBlock = 16;          // entries of a warp
 constexpr int kSumThreads = 128;
-constexpr int kSumUnroll = 8;
 
 struct SumParams {
+    const uint32_t* first;
     const uint32_t* key;
     const uint32_t* pos;
-    uint32_t n, rows, hidden, chunks;
-    const uint32_t* n_dev;
+    uint32_t rows, hidden, chunks;
     const void* src;
     uint64_t src_ld;
     const float* weight;
     float scale;
     void* out;
     uint64_t out_ld;
-    bool accumulate;
-    uint32_t* slot;
-    float* partial;      // blocks x 2 x hidden
+    bool accumulate, compact;
+    float* partial;          // blocks x 2 x hidden
+    uint32_t* counters;      // blocks x chunks: partial sums left of the run that begins in the block and goes on
 };
 
+template <int V>
+__device__ __forceinline__ void load_partial(const float* p, float* f) {       // written by other SMs: from L2
+    if constexpr (V == 8) {
+        const float4 a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+        f[0] = __ldcg(p);
+    }
+}
+
 template <typename TO, int V>
-__device__ __forceinline__ void write_sum(const SumParams& p, uint32_t key, uint32_t at, uint32_t col, bool active,
-                                          float* acc) {
-    if (p.slot && col == 0) p.slot[key] = at;
+__device__ __forceinline__ void write_sum(const SumParams& p, uint32_t row, uint32_t col, bool active, float* acc) {
     if (!active) return;
-    TO* o = static_cast<TO*>(p.out) + (uint64_t)(p.slot ? at : key) * p.out_ld + col;
+    TO* o = static_cast<TO*>(p.out) + row * p.out_ld + col;
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] *= p.scale;
     Vec<TO, V> v;
@@ -268,168 +280,177 @@ __device__ __forceinline__ void write_sum(const SumParams& p, uint32_t key, uint
     v.store(o);
 }
 
+// Leaves this block's share of a run that crosses blocks; the last to do so finishes the run.
+template <typename TO, int V>
+__device__ __forceinline__ void leave_partial(const SumParams& p, uint64_t block, uint32_t chunk, uint32_t key, uint32_t col, bool active,
+                                              float* acc) {
+    const uint32_t begin = p.first[key], end = p.first[key + 1];
+    const uint64_t b0 = begin / kSumBlock, b1 = (end - 1) / kSumBlock;
+    if (active) {
+        Vec<float, V> v;
+        v.set(acc);
+        v.store(p.partial + (block * 2 + (block == b0)) * p.hidden + col);
+    }
+    __threadfence();
+    __syncwarp();
+    uint32_t last = 0;
+    if ((threadIdx.x & 31) == 0) last = atomicAdd(p.counters + b0 * p.chunks + chunk, 1u) == (uint32_t)(b1 - b0);
+    if (!__shfl_sync(0xFFFFFFFFu, last, 0)) return;
+    __threadfence();
+    if (active) {
+        const float* part = p.partial + col;
+        float sum[V];
+        load_partial<V>(part + (b0 * 2 + 1) * p.hidden, sum);
+#pragma unroll 2
+        for (uint64_t b = b0 + 1; b <= b1; ++b) {
+            float x[V];
+            load_partial<V>(part + b * 2 * p.hidden, x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[j] += x[j];
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = sum[j];
+    }
+    write_sum<TO, V>(p, p.compact ? begin : key, col, active, acc);
+}
+
 template <typename TS, typename TO, int V, bool WEIGHTED>
-__global__ void __launch_bounds__(kSumThreads) sum_runs_kernel(const SumParams p) {
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
+    constexpr int kSumUnroll = sizeof(TS) == 2 ? 8 : 4;     // 32 registers of loads in flight
     wait_for_earlier();
-    const uint64_t w = (uint64_t)blockIdx.x * (kSumThreads / 32) + threadIdx.x / 32;
-    const uint32_t lane = threadIdx.x & 31;
-    const uint64_t block = w / p.chunks, first = block * kSumBlock;
-    const uint32_t n = p.n_dev ? *p.n_dev : p.n;
+    const uint32_t w = blockIdx.x * (kSumThreads / 32) + threadIdx.x / 32, lane = threadIdx.x & 31;
+    const uint32_t block = w / p.chunks, chunk = w % p.chunks, first = block * kSumBlock;
+    const uint32_t n = p.first[p.rows];                      // entries of this shard
     if (first >= n) return;
-    const uint32_t col = (uint32_t)(w % p.chunks) * (32 * V) + lane * V;
+    const uint32_t col = chunk * (32 * V) + lane * V;
     const bool active = col < p.hidden;
     const bool mine = lane < kSumBlock && first + lane < n;
-    const uint32_t key = mine ? p.key[first + lane] : p.rows;
+    const uint32_t key = mine ? p.key[first + lane] : kNone;
     const uint32_t pos = mine ? p.pos[first + lane] : 0;
     const uint32_t prev = first ? p.key[first - 1] : kNone;
     const uint32_t next = first + kSumBlock < n ? p.key[first + kSumBlock] : kNone;
-    const float wt = WEIGHTED && key < p.rows ? p.weight[pos] : 1.f;
+    const float wt = WEIGHTED && mine ? p.weight[pos] : 1.f;
     const TS* src = static_cast<const TS*>(p.src) + col;
-    float* part = p.partial + block * 2 * p.hidden + col;
 
     float acc[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
     uint32_t cur = __shfl_sync(0xFFFFFFFFu, key, 0), start = 0;
     bool incoming = cur == prev;
-    for (uint32_t i0 = 0; i0 < kSumBlock && cur < p.rows; i0 += kSumUnroll) {
+    for (uint32_t i0 = 0; i0 < kSumBlock && first + i0 < n; i0 += kSumUnroll) {
         Vec<TS, V> r[kSumUnroll];
 #pragma unroll
         for (int u = 0; u < kSumUnroll; ++u) {
-            const uint32_t k = __shfl_sync(0xFFFFFFFFu, key, i0 + u), q = __shfl_sync(0xFFFFFFFFu, pos, i0 + u);
-            if (k < p.rows && active) r[u].load_cs(src + (uint64_t)q * p.src_ld); else r[u].zero();
+            const uint32_t q = __shfl_sync(0xFFFFFFFFu, pos, i0 + u);
+            if (first + i0 + u < n && active) r[u].load_cs(src + q * p.src_ld); else r[u].zero();
         }
 #pragma unroll
         for (int u = 0; u < kSumUnroll; ++u) {
             const uint32_t k = __shfl_sync(0xFFFFFFFFu, key, i0 + u);
             const float f = WEIGHTED ? __shfl_sync(0xFFFFFFFFu, wt, i0 + u) : 1.f;
-            if (cur < p.rows && k != cur) {              // uniform over the warp
-                if (incoming) {
-                    if (active) {
-                        Vec<float, V> v;
-                        v.set(acc);
-                        v.store(part);
-                    }
-                } else {
-                    write_sum<TO, V>(p, cur, (uint32_t)first + start, col, active, acc);
-                }
+            if (k == kNone) break;                           // uniform over the warp, like the next one
+            if (k != cur) {
+                if (incoming) leave_partial<TO, V>(p, block, chunk, cur, col, active, acc);
+                else write_sum<TO, V>(p, p.compact ? first + start : cur, col, active, acc);
 #pragma unroll
                 for (int j = 0; j < V; ++j) acc[j] = 0.f;
                 cur = k;
                 start = i0 + u;
                 incoming = false;
             }
-            if (k < p.rows) {
-                float x[V];
-                r[u].get(x);
+            float x[V];
+            r[u].get(x);
 #pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] = WEIGHTED ? fmaf(f, x[j], acc[j]) : acc[j] + x[j];
-            }
+            for (int j = 0; j < V; ++j) acc[j] = WEIGHTED ? fmaf(f, x[j], acc[j]) : acc[j] + x[j];
         }
     }
-    if (cur >= p.rows) return;
-    if (incoming || next == cur) {
-        if (active) {
-            Vec<float, V> v;
-            v.set(acc);
-            v.store(part + (incoming ? 0 : p.hidden));
-        }
-    } else {
-        write_sum<TO, V>(p, cur, (uint32_t)first + start, col, active, acc);
-    }
+    if (incoming || next == cur) leave_partial<TO, V>(p, block, chunk, cur, col, active, acc);
+    else write_sum<TO, V>(p, p.compact ? first + start : cur, col, active, acc);
 }
 
-template <typename TO, int V>
-__global__ void __launch_bounds__(kSumThreads) sum_crossing_kernel(const SumParams p) {
-    wait_for_earlier();
-    const uint64_t w = (uint64_t)blockIdx.x * (kSumThreads / 32) + threadIdx.x / 32;
-    const uint32_t lane = threadIdx.x & 31;
-    const uint64_t block = w / p.chunks, first = block * kSumBlock;
-    const uint32_t n = p.n_dev ? *p.n_dev : p.n;
-    if (first + kSumBlock >= n) return;                       // nothing goes out of the last block
-    // lane l: key of entry first - 1 + l, so that one load answers all questions about this block's last run
-    const uint32_t at = lane <= kSumBlock + 1 ? lane : kSumBlock + 1;
-    const uint32_t key = first + at >= 1 ? p.key[first + at - 1] : kNone;
-    const uint32_t last = __shfl_sync(0xFFFFFFFFu, key, kSumBlock);
-    if (last >= p.rows || __shfl_sync(0xFFFFFFFFu, key, kSumBlock + 1) != last) return;
-    const uint32_t same = __ballot_sync(0xFFFFFFFFu, key == last);
-    if ((same & 3u) == 3u) return;                            // an earlier block began this run
-    const uint32_t start = __ffs(same & ~1u) - 2;
-    // the block in which the run ends: the first behind this one whose last entry is another key
-    uint64_t last_block = block + 1;
-    while (true) {
-        const uint64_t e = (last_block + lane) * kSumBlock + kSumBlock - 1;
-        const uint32_t ends = __ballot_sync(0xFFFFFFFFu, e >= n || p.key[e] != last);
-        if (ends) {
-            last_block += __ffs(ends) - 1;
-            // a run that fills its last full block exactly ends there although that block's last key is the same
-            if (last_block * kSumBlock >= n || p.key[last_block * kSumBlock] != last) --last_block;
-            break;
-        }
-        last_block += 32;
-    }
-    const uint32_t col = (uint32_t)(w % p.chunks) * (32 * V) + lane * V;
-    const bool active = col < p.hidden;
-    float acc[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = 0.f;
-    if (active) {
-        const float* part = p.partial + col;
-        Vec<float, V> v;
-        v.load(part + (block * 2 + 1) * p.hidden);
-        v.get(acc);
-#pragma unroll 4
-        for (uint64_t b = block + 1; b <= last_block; ++b) {
-            float x[V];
-            v.load(part + b * 2 * p.hidden);
-            v.get(x);
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += x[j];
-        }
-    }
-    write_sum<TO, V>(p, last, (uint32_t)first + start, col, active, acc);
+static uint64_t sum_chunks(uint64_t hidden, bool vec) { return (hidden + (vec ? 255 : 31)) / (vec ? 256 : 32); }
+
+struct SumLayout {
+    uint64_t first, key, pos, counters, partial, total;
+};
+
+static SumLayout sum_layout(uint64_t n, uint64_t rows, uint64_t hidden) {
+    const uint64_t blocks = (n + kSumBlock - 1) / kSumBlock;
+    SumLayout l;
+    l.first = 0;
+    l.key = l.first + align_up((rows + 1) * 4, kWorkspaceAlign);
+    l.pos = l.key + align_up(n * 4, kWorkspaceAlign);
+    l.counters = l.pos + align_up(n * 4, kWorkspaceAlign);
+    l.partial = l.counters + align_up(blocks * sum_chunks(hidden, false) * 4, kWorkspaceAlign);
+    l.total = l.partial + align_up(blocks * 2 * hidden * 4, kWorkspaceAlign);
+    return l;
+}
+
+uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t rows, uint64_t hidden) { return sum_layout(n, rows, hidden).total; }
+
+const uint32_t* sorted_sum_first(const void* workspace) { return static_cast<const uint32_t*>(workspace); }
+
+bool sorted_sum_fits(uint64_t n, uint64_t rows, uint64_t hidden, uint32_t out_dtype) {
+    const uint64_t sums = (n / kSumBlock + 1) * sum_chunks(hidden, false);
+    const uint64_t fills = rows * (hidden * elem_size(out_dtype) / kFillBytes + 1);
+    return sums < (1ull << 31) && fills < (1ull << 31) && sums + fills < (1ull << 31);
 }
 
 template <typename TS, typename TO, int V, bool WEIGHTED = false>
-static dte_status launch_sums(const SumParams& p, cudaStream_t st) {
-    const uint64_t blocks = ((uint64_t)p.n + kSumBlock - 1) / kSumBlock;
-    const unsigned ctas = (unsigned)((blocks * p.chunks + kSumThreads / 32 - 1) / (kSumThreads / 32));
-    DTE_CUDA(launch_after(sum_runs_kernel<TS, TO, V, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
-    if (p.n > kSumBlock) DTE_CUDA(launch_after(sum_crossing_kernel<TO, V>, dim3(ctas), kSumThreads, 0, st, p));
+static dte_status launch_sums(const SumParams& p, unsigned ctas, cudaStream_t st) {
+    DTE_CUDA(launch_after(sum_kernel<TS, TO, V, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
     return DTE_OK;
 }
 
-uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t hidden) {
-    const uint64_t blocks = (n + kSumBlock - 1) / kSumBlock;
-    return 4 * align_up(n * 4, kWorkspaceAlign) + align_up(blocks * 2 * hidden * 4, kWorkspaceAlign);
-}
-
-dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, int device, cudaStream_t st) {
+dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool after, int device, cudaStream_t st) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const uint64_t arr = align_up((uint64_t)q.n * 4, kWorkspaceAlign);
-    SortParams s = {};
-    s.ids = q.ids;
-    s.ids_dtype = q.ids_dtype;
-    s.n = q.n;
-    s.n_dev = q.n_dev;
-    s.row_start = q.row_start;
-    s.vocab = (int64_t)q.vocab;
-    s.rows = q.rows;
-    uint32_t bits = 1;                                   // keys 0 .. rows (rows: dropped entries)
-    while (bits < 32 && (q.rows >> bits)) ++bits;
-    s.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
-    s.digit_bits = (bits + s.passes - 1) / s.passes;
-    s.key[0] = reinterpret_cast<uint32_t*>(ws);
-    s.key[1] = reinterpret_cast<uint32_t*>(ws + arr);
-    s.pos[0] = reinterpret_cast<uint32_t*>(ws + 2 * arr);
-    s.pos[1] = reinterpret_cast<uint32_t*>(ws + 3 * arr);
-    s.flags = q.flags;
-    static std::atomic<uint64_t> sort_ready{0};
-    dte_status status = allow_smem(sort_kernel, kSortSmem, device, sort_ready);
-    if (status != DTE_OK) return status;
-    sort_kernel<<<kSortCtas, kSortThreads, kSortSmem, st>>>(s);
-    DTE_CUDA(cudaGetLastError());
-    if (!q.slot && !q.accumulate) {
+    const SumLayout l = sum_layout(q.n, q.rows, q.hidden);
+    const uint64_t blocks = ((uint64_t)q.n + kSumBlock - 1) / kSumBlock, chunks = sum_chunks(q.hidden, vec);
+    GroupParams g = {};
+    g.ids = q.ids;
+    g.ids_dtype = q.ids_dtype;
+    g.n = q.n;
+    g.n_dev = q.n_dev;
+    g.row_start = q.row_start;
+    g.vocab = (int64_t)q.vocab;
+    g.rows = q.rows;
+    g.bins = (q.rows + kGroupCtas - 1) / kGroupCtas;
+    if (g.bins > kMaxBins) g.bins = kMaxBins;
+    g.first = reinterpret_cast<uint32_t*>(ws + l.first);
+    g.key = reinterpret_cast<uint32_t*>(ws + l.key);
+    g.pos = reinterpret_cast<uint32_t*>(ws + l.pos);
+    g.counters = reinterpret_cast<uint32_t*>(ws + l.counters);
+    g.n_counters = (uint32_t)(blocks * chunks);
+    g.flags = q.flags;
+    static std::atomic<uint64_t> ready{0};
+    dte_status s = allow_smem(group_kernel, (size_t)kGroupWarps * kMaxBins * 4, device, ready);
+    if (s != DTE_OK) return s;
+    const unsigned ranges = (q.rows + g.bins - 1) / g.bins;
+    const size_t smem = (size_t)kGroupWarps * g.bins * 4;
+    if (after) {
+        DTE_CUDA(launch_after(group_kernel, dim3(ranges), kGroupThreads, smem, st, g));
+    } else {
+        group_kernel<<<ranges, kGroupThreads, smem, st>>>(g);
+        DTE_CUDA(cudaGetLastError());
+    }
+    SumParams p = {};
+    p.first = g.first;
+    p.key = g.key;
+    p.pos = g.pos;
+    p.rows = q.rows;
+    p.hidden = q.hidden;
+    p.chunks = (uint32_t)chunks;
+    p.src = q.src;
+    p.src_ld = q.src_ld;
+    p.weight = q.weight;
+    p.scale = q.scale;
+    p.out = q.out;
+    p.out_ld = q.out_ld;
+    p.accumulate = q.accumulate;
+    p.compact = q.compact;
+    p.partial = reinterpret_cast<float*>(ws + l.partial);
+    p.counters = g.counters;
+    if (!q.compact && !q.accumulate) {
         const uint32_t es = elem_size(q.out_dtype);
         FillParams f;
         f.data = static_cast<uint8_t*>(q.out);
@@ -444,35 +465,19 @@ dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, int 
         DTE_CUDA(launch_after(fill_kernel, dim3((unsigned)(f.rows * f.pieces)), kFillThreads, 0, st, f));
     }
     if (q.n == 0) return DTE_OK;
-    SumParams p = {};
-    p.key = s.key[(s.passes & 1) ^ 1];
-    p.pos = s.pos[(s.passes & 1) ^ 1];
-    p.n = q.n;
-    p.n_dev = q.n_dev;
-    p.rows = q.rows;
-    p.hidden = q.hidden;
-    p.chunks = (q.hidden + (vec ? 256 : 32) - 1) / (vec ? 256 : 32);
-    p.src = q.src;
-    p.src_ld = q.src_ld;
-    p.weight = q.weight;
-    p.scale = q.scale;
-    p.out = q.out;
-    p.out_ld = q.out_ld;
-    p.accumulate = q.accumulate;
-    p.slot = q.slot;
-    p.partial = reinterpret_cast<float*>(ws + 4 * arr);
+    const unsigned ctas = (unsigned)((blocks * chunks + kSumThreads / 32 - 1) / (kSumThreads / 32));
     const bool sb = q.src_dtype == DTE_BF16, ob = q.out_dtype == DTE_BF16;
-    if (p.weight) return launch_sums<__nv_bfloat16, float, 8, true>(p, st);      // the head's gradient
+    if (p.weight) return launch_sums<__nv_bfloat16, float, 8, true>(p, ctas, st);      // the head's gradient
     if (vec) {
-        if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 8>(p, st);
-        if (sb) return launch_sums<__nv_bfloat16, float, 8>(p, st);
-        if (ob) return launch_sums<float, __nv_bfloat16, 8>(p, st);
-        return launch_sums<float, float, 8>(p, st);
+        if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 8>(p, ctas, st);
+        if (sb) return launch_sums<__nv_bfloat16, float, 8>(p, ctas, st);
+        if (ob) return launch_sums<float, __nv_bfloat16, 8>(p, ctas, st);
+        return launch_sums<float, float, 8>(p, ctas, st);
     }
-    if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 1>(p, st);
-    if (sb) return launch_sums<__nv_bfloat16, float, 1>(p, st);
-    if (ob) return launch_sums<float, __nv_bfloat16, 1>(p, st);
-    return launch_sums<float, float, 1>(p, st);
+    if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 1>(p, ctas, st);
+    if (sb) return launch_sums<__nv_bfloat16, float, 1>(p, ctas, st);
+    if (ob) return launch_sums<float, __nv_bfloat16, 1>(p, ctas, st);
+    return launch_sums<float, float, 1>(p, ctas, st);
 }
 
 dte_status device_sms(int device, int* sms) {
@@ -533,9 +538,12 @@ extern "C" dte_status dte_embedding_forward(const dte_matrix* table, const dte_i
     return DTE_OK;
 }
 
+// The workspace helper does not know the table: it leaves room for the row index of the largest one (8 MB).
+constexpr uint64_t kMaxTableRows = (1u << 21) - 1;
+
 extern "C" uint64_t dte_embedding_backward_workspace_bytes(uint64_t n_ids, uint64_t hidden) {
     if (n_ids >= kMaxDim || hidden >= kMaxDim) return UINT64_MAX;   // refused by the call
-    return sorted_sum_workspace_bytes(n_ids, hidden);
+    return sorted_sum_workspace_bytes(n_ids, kMaxTableRows, hidden);
 }
 
 extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_ids* ids, uint64_t row_start,
@@ -551,13 +559,11 @@ extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_i
     if (dtable->cols != dout->cols || dout->rows != ids->count)
         return op_fail(DTE_ERR_INVALID_ARG, "dout must be ids.count x dtable.cols");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
-    if ((s = check_workspace(workspace, workspace_bytes, sorted_sum_workspace_bytes(ids->count, dout->cols))) != DTE_OK) return s;
+    if ((s = check_workspace(workspace, workspace_bytes, sorted_sum_workspace_bytes(ids->count, kMaxTableRows, dout->cols))) != DTE_OK) return s;
     const bool vec = vec8_ok(dout) && vec8_ok(dtable);
-    const uint64_t chunks = (dout->cols + (vec ? 255 : 31)) / (vec ? 256 : 32);
-    if ((ids->count / kSumBlock + 1) * chunks >= (1ull << 32))
-        return op_fail(DTE_ERR_INVALID_ARG, "ids.count x hidden is too large for one call");
-    const uint64_t row_bytes = dtable->cols * elem_size(dtable->dtype);
-    if (dtable->rows * (row_bytes / kFillBytes + 1) >= (1ull << 31)) return op_fail(DTE_ERR_INVALID_ARG, "dtable is too large for one call");
+    if (dtable->rows > kMaxTableRows) return op_fail(DTE_ERR_INVALID_ARG, "at most 2097151 rows of a table");
+    if (!sorted_sum_fits(ids->count, dtable->rows, dout->cols, dtable->dtype))
+        return op_fail(DTE_ERR_INVALID_ARG, "ids.count x hidden or dtable is too large for one call");
     if (dtable->rows == 0) return DTE_OK;
     OpDeviceGuard g(device);
     int sms = 0;
@@ -579,5 +585,5 @@ extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_i
     q.out_ld = dtable->ld;
     q.accumulate = accumulate != 0;
     q.flags = flags;
-    return launch_sorted_sum(q, vec, workspace, device, (cudaStream_t)cuda_stream);
+    return launch_sorted_sum(q, vec, workspace, false, device, (cudaStream_t)cuda_stream);
 }

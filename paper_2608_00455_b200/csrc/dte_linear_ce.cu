@@ -69,7 +69,7 @@ struct CeParams {
     void* dweight;
     uint64_t dweight_ld;
     bool dweight_bf16, accumulate;
-    const uint32_t* slot;
+    const uint32_t* first;       // per vocabulary row: where its target term lies, if the next row's lies further on
     const float* target_sum;
 };
 
@@ -197,8 +197,8 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
     } else {
         const uint64_t vrow = (uint64_t)p.w_row + row;
         const bool valid = row < p.m;
-        const uint32_t at = valid ? p.slot[vrow] : kNone;
-        const bool hit = at != kNone;                       // a token has this row as its target
+        const uint32_t at = valid ? p.first[vrow] : 0;
+        const bool hit = valid && p.first[vrow + 1] > at;   // a token has this row as its target
         const float* term = p.target_sum + (uint64_t)(hit ? at : 0) * p.n + n0;
         // few rows are hit, but most warps hold one: its terms are loaded a step ahead
         uint32_t w[4][8], ahead[4][8];
@@ -723,7 +723,7 @@ static CeShape ce_shape(uint64_t tokens, uint64_t vocab, uint64_t hidden, uint64
 
 // Offsets of everything in a workspace.
 struct CeLayout {
-    uint64_t count, source, target, place, rows, scalar0, scalar1, stats, prob, dx_sum, target_sum, slot, sort, total;
+    uint64_t count, source, target, place, rows, scalar0, scalar1, stats, prob, dx_sum, target_sum, sums, total;
 };
 
 static uint64_t take(uint64_t& at, uint64_t bytes) {
@@ -778,8 +778,7 @@ static CeLayout backward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden
     l.prob = take(at, s.padded * s.piece * 2);
     l.dx_sum = take(at, s.splits * s.padded * hidden * 4);
     l.target_sum = take(at, s.padded * hidden * 4);
-    l.slot = take(at, align_up(vocab, kMaxTileN) * 4);
-    l.sort = take(at, sorted_sum_workspace_bytes(s.padded, hidden));
+    l.sums = take(at, sorted_sum_workspace_bytes(s.padded, vocab, hidden));
     l.total = at;
     return l;
 }
@@ -866,13 +865,13 @@ static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, cons
     if ((s = check_range(vocab_start, weight->rows, vocab)) != DTE_OK) return s;
     if (!(logit_scale > 0) || !std::isfinite(logit_scale)) return op_fail(DTE_ERR_INVALID_ARG, "logit_scale must be finite and > 0");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
-    if (targets->count > (1u << 24) || weight->rows > (1u << 30) || x->cols > (1u << 20))
-        return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^30 vocabulary rows and 2^20 hidden");
+    if (targets->count > (1u << 24) || weight->rows > (1u << 24) || x->cols > (1u << 20))
+        return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^24 vocabulary rows and 2^20 hidden");
     return DTE_OK;
 }
 
 static bool ce_sizes_ok(uint64_t tokens, uint64_t vocab, uint64_t hidden) {
-    return tokens <= (1u << 24) && vocab <= (1u << 30) && hidden <= (1u << 20);
+    return tokens <= (1u << 24) && vocab <= (1u << 24) && hidden <= (1u << 20);
 }
 
 static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets,
@@ -1035,14 +1034,12 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         DTE_CUDA(cudaMemset2DAsync(dweight->data, dweight->ld * elem_size(dweight->dtype), 0, H * elem_size(dweight->dtype), V, st));
         return DTE_OK;
     }
-    if (dweight) DTE_CUDA(cudaMemsetAsync(ws + l.slot, 0xFF, align_up(V, kMaxTileN) * 4, st));
     if ((s = prepare_rows(l, ws, x, weight, targets, vocab_start, vocab, sh.padded, (float)logit_scale, nullptr, nullptr, nullptr, lse, dloss,
                           flags, st)) != DTE_OK)
         return s;
     const uint32_t* count = reinterpret_cast<uint32_t*>(ws + l.count);
     const float* f = reinterpret_cast<float*>(ws + l.scalar0);
     const int32_t* target = reinterpret_cast<int32_t*>(ws + l.target);
-    uint32_t* slot = reinterpret_cast<uint32_t*>(ws + l.slot);
     float* target_sum = reinterpret_cast<float*>(ws + l.target_sum);
     if (dweight) {
         SortedSum q = {};
@@ -1062,8 +1059,8 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         q.out = target_sum;
         q.out_dtype = DTE_F32;
         q.out_ld = H;
-        q.slot = slot;
-        if ((s = launch_sorted_sum(q, true, ws + l.sort, device, st)) != DTE_OK) return s;
+        q.compact = true;
+        if ((s = launch_sorted_sum(q, true, ws + l.sums, true, device, st)) != DTE_OK) return s;
     }
     CeParams p = {};
     p.tokens = count;
@@ -1083,7 +1080,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         p.dweight_bf16 = dweight->dtype == DTE_BF16;
     }
     p.accumulate = accumulate != 0;
-    p.slot = slot;
+    p.first = sorted_sum_first(ws + l.sums);
     p.target_sum = target_sum;
     CUtensorMap x_k, w_k, g_k, w_n, g_m, x_n;
     const uint32_t bn = kMaxTileN;

@@ -4,20 +4,28 @@
 // its statistics are reduced there (the variance from the centred values, not as E[x^2] - E[x]^2) and
 // the result is written.  CTAs are persistent over rows: the weights, and in the backward pass the
 // running sums of the weight's gradient, belong to columns and so stay in the same thread's
-// registers for all its rows, and the next row is loaded before the current row's reduction, which
-// hides the reduction's latency behind the loads.
+// registers for all its rows.  The rows to come are on their way into shared memory meanwhile: every thread copies
+// its own columns of the next rows (asynchronous 16-byte copies) and reads back what it copied, so the
+// ring needs no barrier.  One row ahead in registers keeps 32 KB per SM in flight and reached 4.1 TB/s.
 //
-// A row is held by a team: 8, 16 or 32 lanes of a warp for up to 256 columns (a head's norm: several
-// rows per warp, reductions by shuffles alone), else one CTA of ceil(columns / 8) threads, eight columns
-// per thread, up to 8192 columns.  Longer rows take the kernels that pass over the row from memory again.
+// A row is held by a team: 8, 16 or 32 lanes of a warp for up to 512 columns (a head's norm: several
+// rows per warp, reductions by shuffles alone), else one CTA of ceil(columns / 16) threads, sixteen columns
+// per thread, up to 16384 columns.  Sixteen, because what a warp spends on a row beside its columns (reduction,
+// addresses, statistics) was half of its instructions at eight.  Longer rows take the kernels that pass over the
+// row from memory again.
 #include "dte_ops.cuh"
 
 namespace dte {
 
-constexpr int kPer = 8;                  // columns per thread
+constexpr int kPer = 16;                 // columns per thread
 constexpr int kTeamThreads = 256;        // CTA size when teams are parts of a warp
 constexpr uint32_t kMaxRegCols = 1024 * kPer;
 constexpr int kLongThreads = 512;
+// Shared memory of a thread's rows in flight and threads per SM, measured together (us, layer norm 8191 x 4096
+// fp32 / its gradient 16384 x 4096 bf16): these 45 / 88; half the ring 53 / 99; 768 threads 51 / 105; 1024
+// threads 46 / 101.  More rows in flight than 64 KB (forward) per SM make the memory slower, not faster.
+constexpr int kRingForward = 128, kRingBackward = 256;
+constexpr unsigned kSmThreadsForward = 512, kSmThreadsBackward = 512;
 
 struct NormParams {
     const void* x;
@@ -50,48 +58,59 @@ __device__ __forceinline__ float f2_at(const F2* a, int j) {
     return j & 1 ? hi : lo;
 }
 
-// The eight columns of thread t of a team of n threads.  VEC: 16-byte accesses (8 consecutive bf16, or
-// two groups of 4 consecutive floats n threads apart); else element by element, n columns apart.
+// 16 bytes into shared memory, asynchronously; zeros where `live` is false (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool live) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int AHEAD>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory"); }
+__device__ __forceinline__ uint4 shared16(uint32_t from) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from));
+    return v;
+}
+
+// The columns of thread t of a team of n threads.  VEC: 16-byte pieces, n pieces apart; else element by element,
+// n columns apart.
 template <typename T, bool VEC>
 struct RowPart;
 
-template <>
-struct RowPart<__nv_bfloat16, true> {
-    uint4 a;
-    static __device__ __forceinline__ uint32_t col(uint32_t t, uint32_t, int j) { return t * 8 + j; }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, uint32_t t, uint32_t, uint32_t cols) {
-        a = t * 8 < cols ? __ldcs(reinterpret_cast<const uint4*>(p + t * 8)) : make_uint4(0, 0, 0, 0);
+template <typename T>
+struct RowPart<T, true> {
+    static constexpr int kPiece = 16 / sizeof(T), kPieces = kPer / kPiece;
+    static __device__ __forceinline__ uint32_t col(uint32_t t, uint32_t n, int j) { return ((j / kPiece) * n + t) * kPiece + j % kPiece; }
+    // shared memory: piece i of the thread lies i * step bytes behind `at`
+    static __device__ __forceinline__ void copy(uint32_t at, uint32_t step, const T* p, uint32_t t, uint32_t n, uint32_t cols) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) copy16(at + i * step, p + col(t, n, i * kPiece), col(t, n, i * kPiece) < cols);
     }
-    __device__ __forceinline__ void get(F2* f) const {
-        f[0] = f2(bf16_lo(a.x), bf16_hi(a.x));
-        f[1] = f2(bf16_lo(a.y), bf16_hi(a.y));
-        f[2] = f2(bf16_lo(a.z), bf16_hi(a.z));
-        f[3] = f2(bf16_lo(a.w), bf16_hi(a.w));
+    static __device__ __forceinline__ void get(uint32_t at, uint32_t step, F2* f) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint4 a = shared16(at + i * step);
+            if (sizeof(T) == 2) {
+                f[4 * i] = f2(bf16_lo(a.x), bf16_hi(a.x));
+                f[4 * i + 1] = f2(bf16_lo(a.y), bf16_hi(a.y));
+                f[4 * i + 2] = f2(bf16_lo(a.z), bf16_hi(a.z));
+                f[4 * i + 3] = f2(bf16_lo(a.w), bf16_hi(a.w));
+            } else {
+                f[2 * i] = f2(__uint_as_float(a.x), __uint_as_float(a.y));
+                f[2 * i + 1] = f2(__uint_as_float(a.z), __uint_as_float(a.w));
+            }
+        }
     }
-    static __device__ __forceinline__ void put(__nv_bfloat16* p, uint32_t t, uint32_t, uint32_t cols, const float* f) {
-        if (t * 8 < cols)
-            *reinterpret_cast<uint4*>(p + t * 8) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
-                                                              pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-    }
-};
-template <>
-struct RowPart<float, true> {
-    float4 a, b;
-    static __device__ __forceinline__ uint32_t col(uint32_t t, uint32_t n, int j) { return (j / 4) * 4 * n + t * 4 + j % 4; }
-    __device__ __forceinline__ void load(const float* p, uint32_t t, uint32_t n, uint32_t cols) {
-        const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-        a = t * 4 < cols ? __ldcs(reinterpret_cast<const float4*>(p + t * 4)) : z;
-        b = (n + t) * 4 < cols ? __ldcs(reinterpret_cast<const float4*>(p + (n + t) * 4)) : z;
-    }
-    __device__ __forceinline__ void get(F2* f) const {
-        f[0] = f2(a.x, a.y);
-        f[1] = f2(a.z, a.w);
-        f[2] = f2(b.x, b.y);
-        f[3] = f2(b.z, b.w);
-    }
-    static __device__ __forceinline__ void put(float* p, uint32_t t, uint32_t n, uint32_t cols, const float* f) {
-        if (t * 4 < cols) *reinterpret_cast<float4*>(p + t * 4) = make_float4(f[0], f[1], f[2], f[3]);
-        if ((n + t) * 4 < cols) *reinterpret_cast<float4*>(p + (n + t) * 4) = make_float4(f[4], f[5], f[6], f[7]);
+    static __device__ __forceinline__ void put(T* p, uint32_t t, uint32_t n, uint32_t cols, const F2* f) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            if (col(t, n, i * kPiece) >= cols) break;
+            uint4 a;
+            if (sizeof(T) == 2)
+                a = make_uint4(pack_bf16(f[4 * i]), pack_bf16(f[4 * i + 1]), pack_bf16(f[4 * i + 2]), pack_bf16(f[4 * i + 3]));
+            else
+                a = make_uint4((uint32_t)f[2 * i].v, (uint32_t)(f[2 * i].v >> 32), (uint32_t)f[2 * i + 1].v, (uint32_t)(f[2 * i + 1].v >> 32));
+            *reinterpret_cast<uint4*>(p + col(t, n, i * kPiece)) = a;
+        }
     }
 };
 template <typename T>
@@ -106,44 +125,122 @@ struct RowPart<T, false> {
 #pragma unroll
         for (int j = 0; j < kPer / 2; ++j) f[j] = f2(to_f<T>(a[2 * j]), to_f<T>(a[2 * j + 1]));
     }
-    static __device__ __forceinline__ void put(T* p, uint32_t t, uint32_t n, uint32_t cols, const float* f) {
+    static __device__ __forceinline__ void put(T* p, uint32_t t, uint32_t n, uint32_t cols, const F2* f) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
-            if (t + j * n < cols) p[t + j * n] = from_f<T>(f[j]);
+            if (t + j * n < cols) p[t + j * n] = from_f<T>(f2_at(f, j));
     }
 };
 
-// Sum of v[0..N) over the team; every member gets the result.  TEAM > 32: the whole CTA, of at most TEAM
-// threads (buf: N x 32 floats, not reused before the CTA has passed another barrier).
+// How many rows a team works on at once, so that their reductions share shuffles and barriers, and how many are on
+// their way or at work, in shared memory.
+template <typename T, bool VEC, int INPUTS, int TEAM>
+struct Rows {
+    static constexpr int kMost = INPUTS == 1 ? kRingForward : TEAM > 512 ? 128 : kRingBackward;   // an SM has 227 KB
+    static constexpr int kRowBytes = kPer * sizeof(T) * INPUTS;      // of a thread
+    static constexpr int kBatch = VEC && sizeof(T) * INPUTS <= 4 && kMost >= 2 * kRowBytes ? 2 : 1;
+    static constexpr int kRing = VEC ? kMost / kRowBytes : kBatch;
+    static constexpr int kBytes = VEC ? kRing * kRowBytes : 0;
+    static_assert(kRing % kBatch == 0 && kRing >= kBatch, "batches must not wrap around the ring");
+};
+
+// A thread's columns of row after row of INPUTS matrices: round k is row me + k * teams.
+template <typename T, bool VEC, int INPUTS, int TEAM>
+struct Feed {
+    using R = Rows<T, VEC, INPUTS, TEAM>;
+    static constexpr uint32_t kPieces = VEC ? kPer * sizeof(T) / 16 : 1;
+    RowPart<T, VEC> next[INPUTS];                 // !VEC: one row ahead, in registers
+    const T* from[INPUTS];                        // of the round to ask for next
+    uint64_t step[INPUTS];
+    uint32_t asked, rounds;                       // rounds asked for, rounds that have a row
+    uint32_t t, n, cols, begin, end, at;          // shared memory of the ring; the oldest round
+    __device__ __forceinline__ Feed(const NormParams& p, uint32_t smem, uint32_t me, uint32_t teams, uint32_t t_, uint32_t n_)
+        : asked(0), rounds(me < p.rows ? (p.rows - me + teams - 1) / teams : 0), t(t_), n(n_), cols(p.cols), begin(smem + threadIdx.x * 16) {
+        end = begin + R::kRing * INPUTS * kPieces * blockDim.x * 16;
+        at = begin;
+        from[0] = static_cast<const T*>(p.x) + me * p.x_ld;
+        step[0] = teams * p.x_ld;
+        if constexpr (INPUTS == 2) {
+            from[1] = static_cast<const T*>(p.dout) + me * p.dout_ld;
+            step[1] = teams * p.dout_ld;
+        }
+#pragma unroll
+        for (int k = 0; k < R::kRing; ++k) ask();
+    }
+    // asks for the next round's row; a round without a row asks for nothing
+    __device__ __forceinline__ void ask() {
+        const bool live = asked < rounds;
+        if constexpr (VEC) {
+            if (live)
+#pragma unroll
+                for (int i = 0; i < INPUTS; ++i)
+                    RowPart<T, true>::copy(at + i * kPieces * blockDim.x * 16, blockDim.x * 16, from[i], t, n, cols);
+            copy_commit();
+            at += INPUTS * kPieces * blockDim.x * 16;
+            if (at == end) at = begin;
+        } else if (live) {
+#pragma unroll
+            for (int i = 0; i < INPUTS; ++i) next[i].load(from[i], t, n, cols);
+        }
+        ++asked;
+#pragma unroll
+        for (int i = 0; i < INPUTS; ++i) from[i] += step[i];
+    }
+    // waits for the oldest kBatch rounds asked for and not done
+    __device__ __forceinline__ void wait() {
+        if constexpr (VEC) copy_wait<R::kRing - R::kBatch>();
+    }
+    // row j of those, matrix i
+    __device__ __forceinline__ void get(int j, int i, F2 (&f)[kPer / 2]) const {
+        if constexpr (VEC) RowPart<T, true>::get(at + (j * INPUTS + i) * kPieces * blockDim.x * 16, blockDim.x * 16, f);
+        else next[i].get(f);
+    }
+};
+
+// Sums of v[0..N) over the team, N a power of two; every member gets them.  Lanes first trade values, so that
+// each goes on with half of them (4 sums take 6 shuffles, not 20).  TEAM > 32: the whole CTA, of at most TEAM threads
+// (buf: N x 32 floats, not reused before the CTA has passed another barrier).
 template <int TEAM, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float* buf) {
+    constexpr int kLanes = TEAM < 32 ? TEAM : 32;
+    const uint32_t lane = threadIdx.x & 31;
+    int o = kLanes / 2;
 #pragma unroll
-    for (int o = (TEAM < 32 ? TEAM : 32) / 2; o; o >>= 1)
+    for (int half = N / 2; half; half /= 2, o /= 2) {
+        const bool upper = lane & o;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    if (TEAM > 32) {
-        const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, warps = blockDim.x / 32;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) buf[i * 32 + warp] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = lane < warps ? buf[i * 32 + lane] : 0.f;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+        for (int i = 0; i < half; ++i) {
+            const float give = upper ? v[i] : v[half + i], keep = upper ? v[half + i] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, o);
         }
+    }
+    // now every group of kLanes / N lanes holds a share of one sum: sum i in the i-th group
+    float s = v[0];
+#pragma unroll
+    for (; o; o /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (TEAM > 32) {
+        const uint32_t warp = threadIdx.x / 32, warps = blockDim.x / 32;
+        if (lane % (32 / N) == 0) buf[warp * N + lane / (32 / N)] = s;
+        __syncthreads();
+        s = 0.f;
+        for (uint32_t w = lane / N; w < warps; w += 32 / N) s += buf[w * N + lane % N];
+#pragma unroll
+        for (int q = 16; q >= N; q /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, q);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = N == 1 ? s : __shfl_sync(0xFFFFFFFFu, s, i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = N == 1 ? s : __shfl_sync(0xFFFFFFFFu, s, i * (kLanes / N), kLanes);
     }
 }
 
 template <typename T, bool VEC, int TEAM, uint32_t KIND>
 __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward_kernel(const NormParams p) {
-    __shared__ float buf[2][32];
+    __shared__ float buf[2][64];
     const uint32_t n = TEAM <= 32 ? TEAM : blockDim.x;
     const uint32_t t = TEAM <= 32 ? threadIdx.x % n : threadIdx.x;
     const uint32_t teams = TEAM <= 32 ? gridDim.x * (kTeamThreads / n) : gridDim.x;
     const uint32_t me = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
-    const T* x = static_cast<const T*>(p.x);
     T* y = static_cast<T*>(p.out);
     F2 w[kPer / 2], b[kPer / 2], in[kPer / 2];            // in: 1 for columns of the row, 0 past its end
 #pragma unroll
@@ -160,40 +257,58 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
         b[j] = f2(v[0], v[1]);
         in[j] = f2(q[0], q[1]);
     }
-    RowPart<T, VEC> next;
-    if (me < p.rows) next.load(x + (uint64_t)me * p.x_ld, t, n, p.cols);
+    extern __shared__ __align__(16) uint8_t norm_smem[];
+    Feed<T, VEC, 1, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, teams, t, n);
+    constexpr int B = Rows<T, VEC, 1, TEAM>::kBatch;
     // all lanes of a warp go round together, so that shuffles stay full; a team past the end idles
-    const uint32_t rounds = (p.rows + teams - 1) / teams;
-    for (uint32_t k = 0; k < rounds; ++k) {
-        const uint64_t row = (uint64_t)k * teams + me;
+    const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
+    uint32_t row = me;
+    for (uint32_t k = 0; k < rounds; ++k, row += teams * B) {
         if (TEAM > 32 && row >= p.rows) break;
-        F2 f[kPer / 2];
-        next.get(f);
-        if (row + teams < p.rows) next.load(x + (row + teams) * p.x_ld, t, n, p.cols);
-        float mean = 0.f;
+        F2 f[B][kPer / 2];
+        float mean[B], q[B];
+        feed.wait();
+#pragma unroll
+        for (int j = 0; j < B; ++j) feed.get(j, 0, f[j]);
         if (KIND == DTE_NORM_LAYER) {
-            float s[1] = {f2_sum(f2_add(f2_add(f[0], f[1]), f2_add(f[2], f[3])))};
-            team_sum<TEAM, 1>(s, buf[0]);
-            mean = s[0] * p.inv_cols;
-            const F2 m = f2(-mean, -mean);
 #pragma unroll
-            for (int j = 0; j < kPer / 2; ++j) f[j] = f2_fma(in[j], m, f[j]);
+            for (int j = 0; j < B; ++j) {
+                F2 a = f2_add(f[j][0], f[j][1]);
+#pragma unroll
+                for (int i = 2; i < kPer / 2; i += 2) a = f2_add(a, f2_add(f[j][i], f[j][i + 1]));
+                mean[j] = f2_sum(a);
+            }
+            team_sum<TEAM, B>(mean, buf[0]);
+#pragma unroll
+            for (int j = 0; j < B; ++j) {
+                mean[j] *= p.inv_cols;
+                const F2 m = f2(-mean[j], -mean[j]);
+#pragma unroll
+                for (int i = 0; i < kPer / 2; ++i) f[j][i] = f2_fma(in[i], m, f[j][i]);
+            }
         }
-        F2 q2 = f2_mul(f[0], f[0]);
 #pragma unroll
-        for (int j = 1; j < kPer / 2; ++j) q2 = f2_fma(f[j], f[j], q2);
-        float q[1] = {f2_sum(q2)};
-        team_sum<TEAM, 1>(q, KIND == DTE_NORM_LAYER ? buf[1] : buf[k & 1]);
-        const float rstd = 1.f / sqrtf(q[0] * p.inv_cols + p.eps);
-        if (row < p.rows) {
-            const F2 r = f2(rstd, rstd);
-            float o[kPer];
+        for (int j = 0; j < B; ++j) {
+            F2 q2 = f2_mul(f[j][0], f[j][0]);
 #pragma unroll
-            for (int j = 0; j < kPer / 2; ++j) f2_get(f2_fma(f2_mul(f[j], r), w[j], b[j]), o[2 * j], o[2 * j + 1]);
-            RowPart<T, VEC>::put(y + row * p.out_ld, t, n, p.cols, o);
+            for (int i = 1; i < kPer / 2; ++i) q2 = f2_fma(f[j][i], f[j][i], q2);
+            q[j] = f2_sum(q2);
+        }
+#pragma unroll
+        for (int j = 0; j < B; ++j) feed.ask();              // into the places that these rows have left
+        team_sum<TEAM, B>(q, KIND == DTE_NORM_LAYER ? buf[1] : buf[k & 1]);
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const uint32_t r = row + j * teams;
+            if (r >= p.rows) break;
+            const float rstd = 1.f / sqrtf(q[j] * p.inv_cols + p.eps);
+            const F2 s = f2(rstd, rstd);
+#pragma unroll
+            for (int i = 0; i < kPer / 2; ++i) f[j][i] = f2_fma(f2_mul(f[j][i], s), w[i], b[i]);
+            RowPart<T, VEC>::put(y + r * p.out_ld, t, n, p.cols, f[j]);
             if (t == 0) {
-                if (KIND == DTE_NORM_LAYER && p.mean) p.mean[row] = mean;
-                if (p.rstd) p.rstd[row] = rstd;
+                if (KIND == DTE_NORM_LAYER && p.mean) p.mean[r] = mean[j];
+                if (p.rstd) p.rstd[r] = rstd;
             }
         }
     }
@@ -201,13 +316,11 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
 
 template <typename T, bool VEC, int TEAM, uint32_t KIND>
 __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backward_kernel(const NormParams p) {
-    __shared__ float buf[2][64];
+    __shared__ float buf[2][128];
     const uint32_t n = TEAM <= 32 ? TEAM : blockDim.x;
     const uint32_t t = TEAM <= 32 ? threadIdx.x % n : threadIdx.x;
     const uint32_t teams = TEAM <= 32 ? gridDim.x * (kTeamThreads / n) : gridDim.x;
     const uint32_t me = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
-    const T* x = static_cast<const T*>(p.x);
-    const T* dy = static_cast<const T*>(p.dout);
     T* dx = static_cast<T*>(p.out);
     F2 w[kPer / 2], dw[kPer / 2], db[kPer / 2];
 #pragma unroll
@@ -221,79 +334,95 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
         w[j] = f2(u[0], u[1]);
         dw[j] = db[j] = f2(0.f, 0.f);
     }
-    RowPart<T, VEC> nx, ny;
-    float nmean = 0.f, nrstd = 0.f;
-    auto fetch = [&](uint64_t row) {
-        nx.load(x + row * p.x_ld, t, n, p.cols);
-        ny.load(dy + row * p.dout_ld, t, n, p.cols);
-        if (KIND == DTE_NORM_LAYER) nmean = p.mean[row];
-        nrstd = p.rstd[row];
+    extern __shared__ __align__(16) uint8_t norm_smem[];
+    Feed<T, VEC, 2, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, teams, t, n);
+    constexpr int B = Rows<T, VEC, 2, TEAM>::kBatch, S = KIND == DTE_NORM_LAYER ? 2 : 1;
+    float nmean[B], nrstd[B];                               // statistics of the next rounds
+    auto fetch = [&](uint32_t row) {
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const uint32_t r = row + j * teams;
+            nmean[j] = KIND == DTE_NORM_LAYER && r < p.rows ? p.mean[r] : 0.f;
+            nrstd[j] = r < p.rows ? p.rstd[r] : 0.f;
+        }
     };
-    if (me < p.rows) fetch(me);
-    const uint32_t rounds = (p.rows + teams - 1) / teams;
-    for (uint32_t k = 0; k < rounds; ++k) {
-        const uint64_t row = (uint64_t)k * teams + me;
+    fetch(me);
+    const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
+    uint32_t row = me;
+    for (uint32_t k = 0; k < rounds; ++k, row += teams * B) {
         if (TEAM > 32 && row >= p.rows) break;
-        F2 xh[kPer / 2], g[kPer / 2];
-        nx.get(xh);
-        ny.get(g);
-        const float mean = nmean, rstd = nrstd;
-        if (row + teams < p.rows) fetch(row + teams);
-        const bool live = row < p.rows;
-        const F2 r = f2(rstd, rstd), m = f2(-mean * rstd, -mean * rstd);
-        F2 s2 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
+        float sums[B * S];
+        F2 r[B], m[B];                                      // xhat = x * r + m
 #pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) {
-            // columns past the end hold zero in g and w, so they add nothing: xh is finite there
-            xh[j] = KIND == DTE_NORM_LAYER ? f2_fma(xh[j], r, m) : f2_mul(xh[j], r);
-            if (live) {
-                dw[j] = f2_fma(g[j], xh[j], dw[j]);
-                if (KIND == DTE_NORM_LAYER || p.want_bias) db[j] = f2_add(db[j], g[j]);
+        for (int j = 0; j < B; ++j) {
+            r[j] = f2(nrstd[j], nrstd[j]);
+            m[j] = f2(-nmean[j] * nrstd[j], -nmean[j] * nrstd[j]);
+        }
+        fetch(row + teams * B);
+        feed.wait();
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            F2 xh[kPer / 2], g[kPer / 2];
+            feed.get(j, 0, xh);
+            feed.get(j, 1, g);
+            const bool live = row + j * teams < p.rows;
+            F2 s2 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < kPer / 2; ++i) {
+                // columns past the end hold zero in g and w, so they add nothing: xh is finite there
+                xh[i] = KIND == DTE_NORM_LAYER ? f2_fma(xh[i], r[j], m[j]) : f2_mul(xh[i], r[j]);
+                if (live) {
+                    dw[i] = f2_fma(g[i], xh[i], dw[i]);
+                    if (KIND == DTE_NORM_LAYER || p.want_bias) db[i] = f2_add(db[i], g[i]);
+                }
+                g[i] = f2_mul(g[i], w[i]);
+                s2 = f2_fma(g[i], xh[i], s2);
+                if (KIND == DTE_NORM_LAYER) s1 = f2_add(s1, g[i]);
             }
-            g[j] = f2_mul(g[j], w[j]);
-            s2 = f2_fma(g[j], xh[j], s2);
-            if (KIND == DTE_NORM_LAYER) s1 = f2_add(s1, g[j]);
+            sums[j * S] = f2_sum(s2);
+            if (S == 2) sums[j * S + 1] = f2_sum(s1);
         }
-        float c1 = 0.f, c2;
-        if (KIND == DTE_NORM_LAYER) {
-            float s[2] = {f2_sum(s2), f2_sum(s1)};
-            team_sum<TEAM, 2>(s, buf[k & 1]);
-            c2 = s[0];
-            c1 = s[1];
-        } else {
-            float s[1] = {f2_sum(s2)};
-            team_sum<TEAM, 1>(s, buf[k & 1]);
-            c2 = s[0];
-        }
-        if (live && dx) {
-            // rstd * (g - c1 - xh * c2)
-            c2 *= -p.inv_cols * rstd;
-            c1 *= -p.inv_cols * rstd;
-            const F2 a = f2(c2, c2), b = f2(c1, c1);
-            float o[kPer];
+        team_sum<TEAM, B * S>(sums, buf[k & 1]);
 #pragma unroll
-            for (int j = 0; j < kPer / 2; ++j)
-                f2_get(f2_fma(xh[j], a, KIND == DTE_NORM_LAYER ? f2_fma(g[j], r, b) : f2_mul(g[j], r)), o[2 * j], o[2 * j + 1]);
-            RowPart<T, VEC>::put(dx + row * p.out_ld, t, n, p.cols, o);
+        for (int j = 0; j < B; ++j) {
+            const uint32_t at = row + j * teams;
+            if (at < p.rows && dx) {
+                // rstd * (g - c1 - xh * c2); the row is read from shared memory again: cheaper than its registers
+                float rstd, unused;
+                f2_get(r[j], rstd, unused);
+                const float c2 = -sums[j * S] * p.inv_cols * rstd, c1 = S == 2 ? -sums[j * S + S - 1] * p.inv_cols * rstd : 0.f;
+                const F2 a = f2(c2, c2), b = f2(c1, c1);
+                F2 xh[kPer / 2], g[kPer / 2];
+                feed.get(j, 0, xh);
+                feed.get(j, 1, g);
+#pragma unroll
+                for (int i = 0; i < kPer / 2; ++i) {
+                    xh[i] = KIND == DTE_NORM_LAYER ? f2_fma(xh[i], r[j], m[j]) : f2_mul(xh[i], r[j]);
+                    g[i] = f2_mul(g[i], w[i]);
+                    g[i] = f2_fma(xh[i], a, KIND == DTE_NORM_LAYER ? f2_fma(g[i], r[j], b) : f2_mul(g[i], r[j]));
+                }
+                RowPart<T, VEC>::put(dx + at * p.out_ld, t, n, p.cols, g);
+            }
         }
+#pragma unroll
+        for (int j = 0; j < B; ++j) feed.ask();              // into the places that these rows have left
     }
     if (!p.partial) return;
     if (TEAM <= 32) {
         // the CTA's teams hold sums of the same columns: add them up in order of the teams
-        __shared__ float sums[2][kTeamThreads * kPer];
+        __shared__ float sums[kTeamThreads * kPer];
         constexpr uint32_t kTeams = TEAM <= 32 ? kTeamThreads / TEAM : 1;
+        for (int which = 0; which < 2; ++which) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const uint32_t c = RowPart<T, VEC>::col(t, n, j);
-            sums[0][(threadIdx.x / n) * (n * kPer) + c] = f2_at(dw, j);
-            sums[1][(threadIdx.x / n) * (n * kPer) + c] = f2_at(db, j);
-        }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 2 * p.cols; i += kTeamThreads) {
-            const uint32_t which = i >= p.cols, c = which ? i - p.cols : i;
-            float v = 0.f;
-            for (uint32_t m = 0; m < kTeams; ++m) v += sums[which][m * (n * kPer) + c];
-            p.partial[((uint64_t)blockIdx.x * 2 + which) * p.cols + c] = v;
+            for (int j = 0; j < kPer; ++j)
+                sums[(threadIdx.x / n) * (n * kPer) + RowPart<T, VEC>::col(t, n, j)] = f2_at(which ? db : dw, j);
+            __syncthreads();
+            for (uint32_t c = threadIdx.x; c < p.cols; c += kTeamThreads) {
+                float v = 0.f;
+                for (uint32_t m = 0; m < kTeams; ++m) v += sums[m * (n * kPer) + c];
+                p.partial[((uint64_t)blockIdx.x * 2 + which) * p.cols + c] = v;
+            }
+            __syncthreads();
         }
     } else {
         float* o = p.partial + (uint64_t)blockIdx.x * 2 * p.cols;
@@ -319,7 +448,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const float* partial, u
     float v = 0.f;
     if (c < cols) {
         const float* src = partial + (uint64_t)blockIdx.y * cols + c;
-#pragma unroll 4
+#pragma unroll 10
         for (uint32_t i = part; i < parts; i += 32) v += src[(uint64_t)i * 2 * cols];
     }
     sums[part][lane] = v;
@@ -440,45 +569,65 @@ static NormShape norm_shape(uint64_t rows, uint64_t cols, int sms, unsigned thre
     return s;
 }
 
-template <typename T, bool VEC, uint32_t KIND>
-static void forward_team(const NormParams& p, const NormShape& s, cudaStream_t st) {
-    if (s.team == 8) norm_forward_kernel<T, VEC, 8, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 16) norm_forward_kernel<T, VEC, 16, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 32) norm_forward_kernel<T, VEC, 32, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 512) norm_forward_kernel<T, VEC, 512, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 1024) norm_forward_kernel<T, VEC, 1024, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else norm_forward_long_kernel<T, KIND><<<s.ctas, s.threads, 0, st>>>(p);
+template <typename T, bool VEC, int TEAM, uint32_t KIND>
+static dte_status forward_as(const NormParams& p, const NormShape& s, int device, cudaStream_t st) {
+    constexpr size_t kPerThread = Rows<T, VEC, 1, TEAM>::kBytes;
+    static std::atomic<uint64_t> ready{0};
+    dte_status r = allow_smem(norm_forward_kernel<T, VEC, TEAM, KIND>, kPerThread * (TEAM <= 32 ? kTeamThreads : TEAM), device, ready);
+    if (r != DTE_OK) return r;
+    norm_forward_kernel<T, VEC, TEAM, KIND><<<s.ctas, s.threads, kPerThread * s.threads, st>>>(p);
+    return DTE_OK;
 }
 
 template <typename T, bool VEC, uint32_t KIND>
-static void backward_team(const NormParams& p, const NormShape& s, cudaStream_t st) {
-    if (s.team == 8) norm_backward_kernel<T, VEC, 8, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 16) norm_backward_kernel<T, VEC, 16, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 32) norm_backward_kernel<T, VEC, 32, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 512) norm_backward_kernel<T, VEC, 512, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else if (s.team == 1024) norm_backward_kernel<T, VEC, 1024, KIND><<<s.ctas, s.threads, 0, st>>>(p);
-    else {
+static dte_status forward_team(const NormParams& p, const NormShape& s, int device, cudaStream_t st) {
+    if (s.team == 0) {
+        norm_forward_long_kernel<T, KIND><<<s.ctas, s.threads, 0, st>>>(p);
+        return DTE_OK;
+    }
+    if (s.team == 8) return forward_as<T, VEC, 8, KIND>(p, s, device, st);
+    if (s.team == 16) return forward_as<T, VEC, 16, KIND>(p, s, device, st);
+    if (s.team == 32) return forward_as<T, VEC, 32, KIND>(p, s, device, st);
+    if (s.team == 512) return forward_as<T, VEC, 512, KIND>(p, s, device, st);
+    return forward_as<T, VEC, 1024, KIND>(p, s, device, st);
+}
+
+template <typename T, bool VEC, int TEAM, uint32_t KIND>
+static dte_status backward_as(const NormParams& p, const NormShape& s, int device, cudaStream_t st) {
+    constexpr size_t kPerThread = Rows<T, VEC, 2, TEAM>::kBytes;
+    static std::atomic<uint64_t> ready{0};
+    dte_status r = allow_smem(norm_backward_kernel<T, VEC, TEAM, KIND>, kPerThread * (TEAM <= 32 ? kTeamThreads : TEAM), device, ready);
+    if (r != DTE_OK) return r;
+    norm_backward_kernel<T, VEC, TEAM, KIND><<<s.ctas, s.threads, kPerThread * s.threads, st>>>(p);
+    return DTE_OK;
+}
+
+template <typename T, bool VEC, uint32_t KIND>
+static dte_status backward_team(const NormParams& p, const NormShape& s, int device, cudaStream_t st) {
+    if (s.team == 0) {
         if (p.out) norm_backward_long_kernel<T, KIND><<<s.ctas, s.threads, 0, st>>>(p);
         if (p.partial) norm_columns_long_kernel<T, KIND><<<dim3((p.cols + 255) / 256, s.ctas), 256, 0, st>>>(p);
+        return DTE_OK;
     }
+    if (s.team == 8) return backward_as<T, VEC, 8, KIND>(p, s, device, st);
+    if (s.team == 16) return backward_as<T, VEC, 16, KIND>(p, s, device, st);
+    if (s.team == 32) return backward_as<T, VEC, 32, KIND>(p, s, device, st);
+    if (s.team == 512) return backward_as<T, VEC, 512, KIND>(p, s, device, st);
+    return backward_as<T, VEC, 1024, KIND>(p, s, device, st);
 }
 
-template <bool BACK>
-static void norm_launch(const NormParams& p, const NormShape& s, bool bf16, bool vec, uint32_t kind, cudaStream_t st) {
-#define DTE_NORM_CASE(T, V, K) \
-    if (BACK) backward_team<T, V, K>(p, s, st); else forward_team<T, V, K>(p, s, st)
-    if (kind == DTE_NORM_LAYER) {
-        if (bf16 && vec) { DTE_NORM_CASE(__nv_bfloat16, true, DTE_NORM_LAYER); }
-        else if (bf16) { DTE_NORM_CASE(__nv_bfloat16, false, DTE_NORM_LAYER); }
-        else if (vec) { DTE_NORM_CASE(float, true, DTE_NORM_LAYER); }
-        else { DTE_NORM_CASE(float, false, DTE_NORM_LAYER); }
-    } else {
-        if (bf16 && vec) { DTE_NORM_CASE(__nv_bfloat16, true, DTE_NORM_RMS); }
-        else if (bf16) { DTE_NORM_CASE(__nv_bfloat16, false, DTE_NORM_RMS); }
-        else if (vec) { DTE_NORM_CASE(float, true, DTE_NORM_RMS); }
-        else { DTE_NORM_CASE(float, false, DTE_NORM_RMS); }
-    }
-#undef DTE_NORM_CASE
+template <bool BACK, typename T, bool VEC, uint32_t KIND>
+static dte_status norm_direction(const NormParams& p, const NormShape& s, int device, cudaStream_t st) {
+    if constexpr (BACK) return backward_team<T, VEC, KIND>(p, s, device, st);
+    else return forward_team<T, VEC, KIND>(p, s, device, st);
+}
+
+template <bool BACK, uint32_t KIND>
+static dte_status norm_launch(const NormParams& p, const NormShape& s, bool bf16, bool vec, int device, cudaStream_t st) {
+    if (bf16 && vec) return norm_direction<BACK, __nv_bfloat16, true, KIND>(p, s, device, st);
+    if (bf16) return norm_direction<BACK, __nv_bfloat16, false, KIND>(p, s, device, st);
+    if (vec) return norm_direction<BACK, float, true, KIND>(p, s, device, st);
+    return norm_direction<BACK, float, false, KIND>(p, s, device, st);
 }
 
 static dte_status check_params(const void* w, const void* b, uint32_t dtype) {
@@ -524,8 +673,12 @@ extern "C" dte_status dte_norm_forward(const dte_matrix* x, const void* weight, 
     p.inv_cols = (float)(1.0 / (double)x->cols);
     p.mean = mean;
     p.rstd = rstd;
-    norm_launch<false>(p, norm_shape(x->rows, x->cols, sms, 1024), x->dtype == DTE_BF16, vec8_ok(x) && vec8_ok(out), kind,
-                       (cudaStream_t)cuda_stream);
+    const NormShape sh = norm_shape(x->rows, x->cols, sms, kSmThreadsForward);
+    const bool bf16 = x->dtype == DTE_BF16, vec = vec8_ok(x) && vec8_ok(out);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    s = kind == DTE_NORM_LAYER ? norm_launch<false, DTE_NORM_LAYER>(p, sh, bf16, vec, device, st)
+                               : norm_launch<false, DTE_NORM_RMS>(p, sh, bf16, vec, device, st);
+    if (s != DTE_OK) return s;
     DTE_CUDA(cudaGetLastError());
     return DTE_OK;
 }
@@ -576,10 +729,13 @@ extern "C" dte_status dte_norm_backward(const dte_matrix* dout, const dte_matrix
     p.rstd = const_cast<float*>(rstd);
     p.want_bias = dbias != nullptr;
     p.partial = want ? static_cast<float*>(workspace) : nullptr;
-    const NormShape sh = norm_shape(x->rows, x->cols, sms, 1024);
+    const NormShape sh = norm_shape(x->rows, x->cols, sms, kSmThreadsBackward);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (x->rows) {
-        norm_launch<true>(p, sh, x->dtype == DTE_BF16, vec8_ok(x) && vec8_ok(dout) && (!dx || vec8_ok(dx)), kind, st);
+        const bool bf16 = x->dtype == DTE_BF16, vec = vec8_ok(x) && vec8_ok(dout) && (!dx || vec8_ok(dx));
+        s = kind == DTE_NORM_LAYER ? norm_launch<true, DTE_NORM_LAYER>(p, sh, bf16, vec, device, st)
+                                   : norm_launch<true, DTE_NORM_RMS>(p, sh, bf16, vec, device, st);
+        if (s != DTE_OK) return s;
         DTE_CUDA(cudaGetLastError());
     }
     if (want) {

@@ -62,9 +62,9 @@ inline dte_status check_range(uint64_t start, uint64_t rows, uint64_t vocab) {
 }
 
 inline dte_status check_workspace(const void* ws, uint64_t have, uint64_t need) {
+    if ((uintptr_t)ws & (kWorkspaceAlign - 1)) return op_fail(DTE_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     if (have < need) return op_fail(DTE_ERR_CAPACITY, "workspace is too small; see the operator's workspace_bytes");
     if (need && !ws) return op_fail(DTE_ERR_INVALID_ARG, "workspace is null");
-    if ((uintptr_t)ws & (kWorkspaceAlign - 1)) return op_fail(DTE_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     return DTE_OK;
 }
 
@@ -86,11 +86,10 @@ inline dte_status allow_smem(Kernel* kernel, size_t bytes, int device, std::atom
     return DTE_OK;
 }
 
-// ---- sorted-token sums ----------------------------------------------------------------------------
-// out[key] = scale * sum over entries with that key of weight[entry] * src[row of entry]
-// Entries are ordered by a stable radix sort of their keys, so every sum has one fixed order.
+// ---- sums over the tokens of a row -----------------------------------------------------------------
+// out[row] = scale * sum over the entries with that row of weight[entry] * src[entry], in the order of the entries
 struct SortedSum {
-    // keys: ids minus row_start where that lies in [0, rows), else the entry is dropped
+    // row of an entry: id - row_start where that lies in [0, rows), else the entry is dropped
     const void* ids;
     uint32_t ids_dtype;
     uint32_t n;               // entries (upper bound when n_dev is set)
@@ -101,21 +100,22 @@ struct SortedSum {
     const void* src;          // n x hidden
     uint32_t src_dtype;
     uint64_t src_ld;
-    const float* weight;      // per entry, or NULL; with weights: src bf16, compact form, vector path
+    const float* weight;      // per entry, or NULL; with weights: src bf16, out fp32 compact, vector path
     uint32_t hidden;
     float scale;
-    // dense form (slot == NULL): out is rows x hidden of out_dtype, accumulate or write all rows.
-    // compact form: out is fp32 n x hidden; row i holds the sum of the run that starts at sorted
-    // position i, and slot[key] = i (slot must hold 0xFFFFFFFF everywhere before).
+    // compact: out is fp32, n x hidden, and the sum of a row lies at position first[row] (see
+    // sorted_sum_first) if first[row + 1] > first[row]; else out is rows x hidden of out_dtype, added to or written whole
     void* out;
     uint32_t out_dtype;
     uint64_t out_ld;
-    bool accumulate;
-    uint32_t* slot;
+    bool accumulate, compact;
     uint64_t* flags;
 };
-uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t hidden);
-dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, int device, cudaStream_t st);
+uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t rows, uint64_t hidden);
+const uint32_t* sorted_sum_first(const void* workspace);     // rows + 1 positions, valid behind launch_sorted_sum
+bool sorted_sum_fits(uint64_t n, uint64_t rows, uint64_t hidden, uint32_t out_dtype);
+// after: an earlier kernel of the same call is in front (see launch_after)
+dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, bool after, int device, cudaStream_t st);
 
 #ifdef __CUDACC__
 // ---- dependent launches ------------------------------------------------------------------------------
@@ -242,6 +242,11 @@ __device__ __forceinline__ F2 f2(float lo, float hi) {
     return r;
 }
 __device__ __forceinline__ void f2_get(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ uint32_t pack_bf16(F2 a) {
+    float lo, hi;
+    f2_get(a, lo, hi);
+    return pack_bf16(lo, hi);
+}
 __device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
     F2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
