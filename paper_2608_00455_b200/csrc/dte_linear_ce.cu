@@ -36,11 +36,19 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // Work is split for this many SMs whatever the device has, so that results do not depend on it.
 constexpr uint32_t kSplitSms = 148;
 
+// The two matrices that this file makes itself, the rows that count and f p, are stored in blocks of 64 x 64, row-major
+// inside (8 KB, 128 bytes a row: the swizzled operand tile as TMA writes it).  Every load of them is then 8 KB
+// in one stretch, whether the tile is wanted along its rows or its columns, and one tensor map serves both.
+constexpr uint32_t kBlock = 64;
+__device__ __forceinline__ uint64_t blocked(uint32_t row, uint32_t col, uint32_t blocks) {
+    return ((uint64_t)(row / kBlock) * blocks + col / kBlock) * (kBlock * kBlock) + (row % kBlock) * kBlock + col % kBlock;
+}
+
 template <int CTAS>
 struct CeStage {
     static constexpr uint32_t kBytesB = kMaxTileN / CTAS * kTileK * 2;
     static constexpr uint32_t kBytes = kStageBytesA + kBytesB;
-    static constexpr uint32_t kStages = CTAS == 2 ? 6 : 4;
+    static constexpr uint32_t kStages = 196608 / kBytes;
     static constexpr uint32_t kSmem = kStages * kBytes + 1024 + 256;
 };
 
@@ -48,6 +56,7 @@ struct CeParams {
     uint32_t m, n, k;            // extents; the one that counts tokens is replaced by *tokens
     const uint32_t* tokens;      // tokens that count
     uint32_t tile_n, splits;
+    uint32_t x_blocks, prob_blocks;   // blocks of 64 columns in a row of the blocked matrices
     uint32_t w_row;              // first row of W of this piece
     uint64_t* flags;
     // kLse, kProb
@@ -59,8 +68,7 @@ struct CeParams {
     float* target_logit;         // kLse: the target's logit as the tensor cores added it up
     const float* f;              // kProb: logit_scale * dloss per token
     const float* neg_lse2;       //        -lse * log2(e)
-    __nv_bfloat16* prob;         //        tokens x prob_ld
-    uint64_t prob_ld;
+    __nv_bfloat16* prob;         //        blocked, prob_blocks blocks wide
     // kDx
     float* dx_sum;               // splits x padded tokens x hidden
     uint64_t dx_split;           // elements of one split's part
@@ -97,7 +105,7 @@ __device__ __forceinline__ void load_tile(uint32_t addr, float (&v)[32]) {
 
 // The 128 columns from c0 (half a tile) of row `row`; lane_row: the row within the CTA's 128.
 template <int KIND>
-__device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, uint32_t row, uint32_t lane_row, uint32_t half, uint32_t use,
+__device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, uint32_t row, uint32_t lane_row, uint32_t half, uint32_t buf,
                                             uint32_t tn, uint32_t split, uint32_t tokens, bool empty, float2 (*s_stat)[kTileM]) {
     const uint32_t n0 = tn * p.tile_n, c0 = half * (kMaxTileN / 2), c1 = min(c0 + kMaxTileN / 2, p.tile_n);
     if (KIND == kLse) {
@@ -137,16 +145,15 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
             top = now;
         }
         // the two halves of a row meet in shared memory (two buffers: the next tile may begin before this one is read)
-        if (half) s_stat[use & 1][lane_row] = make_float2(top, sum);
+        if (half) s_stat[buf][lane_row] = make_float2(top, sum);
         asm volatile("bar.sync %0, 64;" ::"r"(1 + lane_row / 32) : "memory");
         if (!half && valid) {
-            const float2 o = s_stat[use & 1][lane_row];
+            const float2 o = s_stat[buf][lane_row];
             const float now = fmaxf(top, o.x), from = now == -INFINITY ? 0.f : now;
             p.stats[(uint64_t)tn * p.stats_ld + row] = make_float2(now, sum * exp2_fast(top - from) + o.y * exp2_fast(o.x - from));
         }
     } else if (KIND == kProb) {
         const float f = p.f[row], nl = p.neg_lse2[row];     // zero for padding rows
-        __nv_bfloat16* out = p.prob + (uint64_t)row * p.prob_ld + n0;
         for (uint32_t c = c0; c < c1; c += 32) {
             float v[32];
             load_tile(tmem + c, v);
@@ -163,7 +170,7 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = row < tokens ? pack_bf16(v[j + 2 * i], v[j + 2 * i + 1]) : 0u;
-                store32(out + c + j, w);
+                store32(p.prob + blocked(row, n0 + c + j, p.prob_blocks), w);
             }
         }
     } else if (KIND == kDx) {
@@ -328,7 +335,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
         for (uint32_t t = first; t < total && ok; t += step) {
             uint32_t split, tm, tn;
             tile_at(t, tiles_m, tiles_n, group, &split, &tm, &tn);
-            const int m0 = (int)((tm * CTAS + rank) * kTileM), n0 = (int)(tn * p.tile_n + rank * part_n);
+            const uint32_t m0 = (tm * CTAS + rank) * kTileM, n0 = tn * p.tile_n + rank * part_n;
             const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
             for (uint32_t kb = kb0; kb < kb1; ++kb) {
                 if (!(ok = mbar_wait(empty(stage), phase ^ 1, gave_up))) break;
@@ -336,17 +343,21 @@ __global__ void __launch_bounds__(kCeThreads, 1)
                 const uint32_t bar = CTAS == 2 ? cluster_map(full(stage), 0) : full(stage);
                 if (leader) mbar_expect_tx(full(stage), CTAS * (kStageBytesA + part_n * kTileK * 2));
                 const int k0 = (int)(kb * kTileK);
-                if (kAmn) {
-                    tma_load_2d<CTAS>(a, &map_a, m0, k0, bar);
-                    tma_load_2d<CTAS>(a + kStageBytesA / 2, &map_a, m0 + 64, k0, bar);
-                } else {
-                    tma_load_2d<CTAS>(a, &map_a, k0, m0, bar);
-                }
-                if (kBmn) {
+                // A: two blocks of a blocked matrix.  Along the rows (K is its columns): 64 rows each; along the columns: 64
+                // columns each.
+                const uint32_t mb = m0 / kBlock, blocks = KIND == kLse || KIND == kProb ? p.x_blocks : p.prob_blocks;
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i)
+                    tma_load_2d<CTAS>(a + i * (kStageBytesA / 2), &map_a, 0,
+                                      (int)((kAmn ? kb * blocks + mb + i : (mb + i) * blocks + kb) * kBlock), bar);
+                if (KIND == kDw) {
+                    for (uint32_t j = 0; j < part_n; j += kBlock)
+                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, 0, (int)((kb * p.x_blocks + (n0 + j) / kBlock) * kBlock), bar);
+                } else if (KIND == kDx) {
                     for (uint32_t j = 0; j < part_n; j += 64)
-                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, n0 + (int)j, k0 + (int)p.w_row * (KIND == kDx), bar);
+                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, (int)(n0 + j), k0 + (int)p.w_row, bar);
                 } else {
-                    tma_load_2d<CTAS>(b, &map_b, k0, n0 + (int)p.w_row, bar);
+                    tma_load_2d<CTAS>(b, &map_b, k0, (int)(n0 + p.w_row), bar);
                 }
                 ++issued;
                 if (++stage == S::kStages) { stage = 0; phase ^= 1; }
@@ -395,6 +406,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     } else if (warp >= 2) {
         // ---- epilogue: warp w may read the quarter w % 4 of tensor memory's lanes ----
         const uint32_t quarter = warp & 3, half = (warp - 2) / 4;
+        const uint32_t lane_row = quarter * 32 + lane;
         uint32_t use = 0;
         for (uint32_t t = first; t < total; t += step, ++use) {
             uint32_t split, tm, tn;
@@ -404,15 +416,14 @@ __global__ void __launch_bounds__(kCeThreads, 1)
             ok = !__any_sync(0xFFFFFFFFu, !ok);
             if (KIND == kLse) {
                 // the two warps of a quarter go on or stop together: they meet again inside the epilogue
-                if (lane == 0) s_ok[use & 1][half][quarter] = ok;
+                if (lane == 0) s_ok[buf][half][quarter] = ok;
                 asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
-                ok = s_ok[use & 1][0][quarter] && s_ok[use & 1][1][quarter];
+                ok = s_ok[buf][0][quarter] && s_ok[buf][1][quarter];
             }
             if (!ok) break;
             tc_fence_after();
             const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
-            const uint32_t lane_row = quarter * 32 + lane;
-            ce_epilogue<KIND>(p, tmem + buf * kMaxTileN + (quarter * 32 << 16), (tm * CTAS + rank) * kTileM + lane_row, lane_row, half, use, tn,
+            ce_epilogue<KIND>(p, tmem + buf * kMaxTileN + (quarter * 32 << 16), (tm * CTAS + rank) * kTileM + lane_row, lane_row, half, buf, tn,
                               split, tokens, kb0 == kb1, s_stat);
             tc_fence_before();
             __syncwarp();
@@ -506,15 +517,18 @@ __global__ void __launch_bounds__(kRowsThreads) ce_rows_kernel(const RowsParams 
 }
 
 struct GatherRowsParams {
-    const uint32_t* count;
-    const int32_t* source;
+    uint32_t* count;
+    int32_t* source;
+    RowsParams rows_of;      // few tokens: every CTA numbers them itself (see kFewTokens)
+    bool few;
     const __nv_bfloat16* x;
     uint64_t x_ld;
     uint32_t hidden;
     bool vec;
-    __nv_bfloat16* rows;     // padded tokens x hidden
+    __nv_bfloat16* rows;     // blocked: padded tokens x blocks of 64
+    uint32_t blocks;
     // forward: the target's logit, added up in fp32 here and, later, by the tensor cores (compact order)
-    const int32_t* target;
+    int32_t* target;
     const __nv_bfloat16* weight;
     uint64_t weight_ld;
     float* exact_logit;
@@ -527,22 +541,103 @@ struct GatherRowsParams {
     float* neg_lse2;
 };
 
+// Up to this many tokens every CTA of ce_gather_kernel numbers the tokens for itself, which takes it a microsecond
+// and saves the launch of ce_rows_kernel in front of it.
+constexpr int kGatherThreads = 256;
+constexpr uint32_t kFewTokens = kGatherThreads * kRowsPer;
+
 // Copies the rows that count together and clears the padding rows up to the next multiple of kPadRows.
-__global__ void __launch_bounds__(256) ce_gather_kernel(const GatherRowsParams p) {
-    __shared__ float s_part[8];
+__global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherRowsParams p) {
+    __shared__ float s_part[kGatherThreads / 32];
+    __shared__ uint32_t s_warp[kGatherThreads / 32];
+    __shared__ int32_t s_mine[2];          // token and target of this CTA's row
     wait_for_earlier();
     let_next_start();
-    const uint32_t count = *p.count, i = blockIdx.x;
+    const uint32_t i = blockIdx.x;
+    uint32_t count, src;
+    int32_t target;
+    if (p.few) {
+        const RowsParams& q = p.rows_of;
+        const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+        int64_t id[kRowsPer];
+        uint32_t mine = 0;
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < kRowsPer; ++j) {
+            const uint32_t t = threadIdx.x * kRowsPer + j;
+            id[j] = t < q.n ? load_id(q.targets, q.targets_dtype, t) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kRowsPer; ++j) {
+            mine += id[j] >= 0;
+            bad |= id[j] >= q.vocab;
+        }
+        uint32_t inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            if (lane >= (uint32_t)o) inc += v;
+        }
+        if (lane == 31) s_warp[warp] = inc;
+        if (threadIdx.x < 2) s_mine[threadIdx.x] = threadIdx.x ? -1 : 0;
+        __syncthreads();
+        uint32_t at = inc - mine;
+        count = 0;
+#pragma unroll
+        for (int w = 0; w < kGatherThreads / 32; ++w) {
+            at += w < (int)warp ? s_warp[w] : 0;
+            count += s_warp[w];
+        }
+        const bool writer = i == 0;        // one CTA leaves the numbering for the kernels behind
+#pragma unroll
+        for (int j = 0; j < kRowsPer; ++j) {
+            const uint32_t t = threadIdx.x * kRowsPer + j;
+            if (t >= q.n) break;
+            const bool counts = id[j] >= 0;
+            const uint64_t row = (uint64_t)id[j] - (uint64_t)q.vocab_start;
+            const int32_t to = counts && row < q.vocab_rows ? (int32_t)row : -1;
+            if (counts && at == i) {
+                s_mine[0] = (int32_t)t;
+                s_mine[1] = to;
+            }
+            if (writer) {
+                if (q.place) q.place[t] = counts ? (int32_t)at : -1;
+                if (counts) {
+                    q.source[at] = (int32_t)t;
+                    q.target[at] = to;
+                } else {
+                    if (q.lse) q.lse[t] = 0.f;
+                    if (q.target_logit) q.target_logit[t] = 0.f;
+                    if (q.loss) q.loss[t] = 0.f;
+                }
+            }
+            at += counts;
+        }
+        if (writer) {
+            if (threadIdx.x == 0) *q.count = count;
+            if (bad && q.flags) atomicOr((unsigned long long*)q.flags, (unsigned long long)DTE_DEV_BOUNDS);
+        }
+        __syncthreads();
+        src = (uint32_t)s_mine[0];
+        target = s_mine[1];
+    } else {
+        count = *p.count;
+        src = i < count ? (uint32_t)p.source[i] : 0;
+        target = i < count ? p.target[i] : -1;
+    }
     const uint32_t padded = (uint32_t)((count + kPadRows - 1) / kPadRows * kPadRows);
     if (i >= padded) return;
     const bool live = i < count;
-    const uint32_t src = live ? (uint32_t)p.source[i] : 0;
-    const int32_t target = live && p.exact_logit ? p.target[i] : -1;
-    __nv_bfloat16* out = p.rows + (uint64_t)i * p.hidden;
+    if (!p.exact_logit) target = -1;
     const __nv_bfloat16* in = p.x + (uint64_t)src * p.x_ld;
     float dot = 0.f;
-    for (uint32_t c = threadIdx.x * 8; c < p.hidden; c += 256 * 8) {
+    for (uint32_t c = threadIdx.x * 8; c < p.blocks * kBlock; c += kGatherThreads * 8) {
         Raw8<__nv_bfloat16> r, w;
+        if (c >= p.hidden) {             // the last block's columns past the row: zeros, they meet zeros of W
+            r.zero();
+            r.store(p.rows + blocked(i, c, p.blocks));
+            continue;
+        }
         if (target >= 0) w.load(p.weight + (uint64_t)target * p.weight_ld + c);
         float f[8];
         if (!live) {
@@ -554,7 +649,7 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const GatherRowsParams p
             for (int j = 0; j < 8; ++j) f[j] = to_f(in[c + j]);
             r.set(f);
         }
-        r.store(out + c);
+        r.store(p.rows + blocked(i, c, p.blocks));
         if (target >= 0) {
             float g[8];
             r.get(f);
@@ -569,7 +664,7 @@ __global__ void __launch_bounds__(256) ce_gather_kernel(const GatherRowsParams p
         __syncthreads();
         if (threadIdx.x == 0) {
 #pragma unroll
-            for (int w = 1; w < 8; ++w) dot += s_part[w];
+            for (int w = 1; w < kGatherThreads / 32; ++w) dot += s_part[w];
             p.exact_logit[i] = target >= 0 ? dot * p.scale : 0.f;
             p.target_logit[i] = 0.f;
         }
@@ -627,12 +722,21 @@ __global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const Combi
         s_sum[threadIdx.x / 32][r] = sum;
     }
     __syncthreads();
-    if (threadIdx.x < kCombineRows && i < count) {
-        for (int w = 1; w < kCombineThreads / 32; ++w) join(top, sum, s_top[w][r], s_sum[w][r]);
+    constexpr uint32_t kWarps = kCombineThreads / 32;      // 16: half a warp per row now
+    if (threadIdx.x >= kCombineRows * kWarps) return;
+    top = s_top[threadIdx.x % kWarps][threadIdx.x / kWarps];
+    sum = s_sum[threadIdx.x % kWarps][threadIdx.x / kWarps];
+#pragma unroll
+    for (int o = kWarps / 2; o; o /= 2) {
+        const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        join(top, sum, t2, s2);
+    }
+    const uint32_t row = blockIdx.x * kCombineRows + threadIdx.x / kWarps;
+    if (threadIdx.x % kWarps == 0 && row < count) {
         float lse = (top + log2f(sum)) * kLn2;
-        const float made = p.row_target_logit[i], exact = p.exact_logit[i];
-        const uint32_t n = (uint32_t)p.source[i];
-        if (p.target[i] >= 0 && made != exact) {
+        const float made = p.row_target_logit[row], exact = p.exact_logit[row];
+        const uint32_t n = (uint32_t)p.source[row];
+        if (p.target[row] >= 0 && made != exact) {
             const float move = exp2_fast((made - lse) * kLog2e) * expm1f(exact - made);
             if (fabsf(move) < 0.5f) lse += log1pf(move);      // else the logits are not finite or beyond fp32's reach
         }
@@ -755,7 +859,7 @@ static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded,
     l.source = take(at, padded * 4);
     l.target = take(at, padded * 4);
     l.place = take(at, padded * 4);
-    l.rows = take(at, padded * hidden * 2);
+    l.rows = take(at, padded * align_up(hidden, kBlock) * 2);
     l.scalar0 = take(at, padded * 4);
     l.scalar1 = take(at, padded * 4);
     (void)tokens;
@@ -816,6 +920,11 @@ static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint
     return DTE_OK;
 }
 
+// a blocked matrix of rows x blocks blocks of 64 columns
+static dte_status encode_blocked(CUtensorMap* map, const void* base, uint64_t rows, uint64_t blocks) {
+    return encode(map, base, rows * blocks, kBlock, kBlock, kBlock);
+}
+
 template <int KIND, int CTAS>
 static dte_status launch_ce_as(const CUtensorMap& a, const CUtensorMap& b, const CeParams& p, uint64_t most_tiles, int device, cudaStream_t st) {
     using S = CeStage<CTAS>;
@@ -867,6 +976,8 @@ static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, cons
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (targets->count > (1u << 24) || weight->rows > (1u << 24) || x->cols > (1u << 20))
         return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^24 vocabulary rows and 2^20 hidden");
+    if (align_up(targets->count, kPadRows) * ((x->cols + kBlock - 1) / kBlock) >= (1ull << 31))
+        return op_fail(DTE_ERR_INVALID_ARG, "tokens x hidden is too large for one call");
     return DTE_OK;
 }
 
@@ -892,9 +1003,9 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     r.target_logit = target_logit;
     r.loss = loss;
     r.flags = flags;
-    ce_rows_kernel<<<1, kRowsThreads, 0, st>>>(r);
-    DTE_CUDA(cudaGetLastError());
     GatherRowsParams g = {};
+    g.rows_of = r;
+    g.few = targets->count <= kFewTokens;
     g.count = r.count;
     g.source = r.source;
     g.x = static_cast<const __nv_bfloat16*>(x->data);
@@ -902,6 +1013,7 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     g.hidden = (uint32_t)x->cols;
     g.vec = vec8_ok(x);
     g.rows = reinterpret_cast<__nv_bfloat16*>(ws + l.rows);
+    g.blocks = (uint32_t)((x->cols + kBlock - 1) / kBlock);
     g.scale = scale;
     if (dloss) {
         g.dloss = dloss;
@@ -909,13 +1021,20 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
         g.f = reinterpret_cast<float*>(ws + l.scalar0);
         g.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     } else {
-        g.target = r.target;
         g.weight = static_cast<const __nv_bfloat16*>(weight->data);
         g.weight_ld = weight->ld;
         g.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
         g.exact_logit = reinterpret_cast<float*>(ws + l.scalar1);
     }
-    DTE_CUDA(launch_after(ce_gather_kernel, dim3((unsigned)padded), 256, 0, st, g));
+    g.target = r.target;
+    if (g.few) {
+        ce_gather_kernel<<<(unsigned)padded, kGatherThreads, 0, st>>>(g);
+    } else {
+        ce_rows_kernel<<<1, kRowsThreads, 0, st>>>(r);
+        DTE_CUDA(cudaGetLastError());
+        DTE_CUDA(launch_after(ce_gather_kernel, dim3((unsigned)padded), kGatherThreads, 0, st, g));
+    }
+    DTE_CUDA(cudaGetLastError());
     return DTE_OK;
 }
 
@@ -964,8 +1083,9 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     p.stats = reinterpret_cast<float2*>(ws + l.stats);
     p.stats_ld = sh.padded;
     p.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
+    p.x_blocks = (uint32_t)((H + kBlock - 1) / kBlock);
     CUtensorMap ma, mb;
-    if ((s = encode(&ma, ws + l.rows, sh.padded, H, H, kTileM)) != DTE_OK) return s;
+    if ((s = encode_blocked(&ma, ws + l.rows, sh.padded, p.x_blocks)) != DTE_OK) return s;
     if ((s = encode(&mb, weight->data, V, H, weight->ld, tn / sh.ctas)) != DTE_OK) return s;
     if ((s = launch_ce<kLse>(sh.ctas, ma, mb, p, n, device, st)) != DTE_OK) return s;
     CombineParams c = {};
@@ -1043,24 +1163,23 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     float* target_sum = reinterpret_cast<float*>(ws + l.target_sum);
     if (dweight) {
         SortedSum q = {};
-        q.ids = target;
-        q.ids_dtype = DTE_I32;
+        q.ids = targets->data;
+        q.ids_dtype = targets->dtype;
         q.n = (uint32_t)n;
-        q.n_dev = count;
-        q.row_start = 0;
-        q.vocab = V;
+        q.row_start = (int64_t)vocab_start;
+        q.vocab = vocab;
         q.rows = (uint32_t)V;
-        q.src = ws + l.rows;
+        q.src = x->data;
         q.src_dtype = DTE_BF16;
-        q.src_ld = H;
-        q.weight = f;
+        q.src_ld = x->ld;
+        q.weight = dloss;
         q.hidden = (uint32_t)H;
-        q.scale = 1.f;
+        q.scale = (float)logit_scale;
         q.out = target_sum;
         q.out_dtype = DTE_F32;
         q.out_ld = H;
         q.compact = true;
-        if ((s = launch_sorted_sum(q, true, ws + l.sums, true, device, st)) != DTE_OK) return s;
+        if ((s = launch_sorted_sum(q, vec8_ok(x), ws + l.sums, true, device, st)) != DTE_OK) return s;
     }
     CeParams p = {};
     p.tokens = count;
@@ -1071,7 +1190,8 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.f = f;
     p.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     p.prob = reinterpret_cast<__nv_bfloat16*>(ws + l.prob);
-    p.prob_ld = sh.piece;
+    p.prob_blocks = (uint32_t)(sh.piece / kBlock);
+    p.x_blocks = (uint32_t)((H + kBlock - 1) / kBlock);
     p.dx_sum = reinterpret_cast<float*>(ws + l.dx_sum);
     p.dx_split = sh.padded * H;
     if (dweight) {
@@ -1082,14 +1202,12 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.accumulate = accumulate != 0;
     p.first = sorted_sum_first(ws + l.sums);
     p.target_sum = target_sum;
-    CUtensorMap x_k, w_k, g_k, w_n, g_m, x_n;
+    CUtensorMap rows, prob, w_k, w_n;
     const uint32_t bn = kMaxTileN;
-    if ((s = encode(&x_k, ws + l.rows, sh.padded, H, H, kTileM)) != DTE_OK) return s;
+    if ((s = encode_blocked(&rows, ws + l.rows, sh.padded, p.x_blocks)) != DTE_OK) return s;
+    if ((s = encode_blocked(&prob, ws + l.prob, sh.padded, p.prob_blocks)) != DTE_OK) return s;
     if ((s = encode(&w_k, weight->data, V, H, weight->ld, bn / sh.ctas)) != DTE_OK) return s;
-    if ((s = encode(&g_k, ws + l.prob, sh.padded, sh.piece, sh.piece, kTileM)) != DTE_OK) return s;
     if ((s = encode(&w_n, weight->data, V, H, weight->ld, kTileK)) != DTE_OK) return s;
-    if ((s = encode(&g_m, ws + l.prob, sh.padded, sh.piece, sh.piece, kTileK)) != DTE_OK) return s;
-    if ((s = encode(&x_n, ws + l.rows, sh.padded, H, H, kTileK)) != DTE_OK) return s;
     for (uint64_t piece = 0; piece < sh.pieces; ++piece) {
         const uint64_t v0 = piece * sh.piece, vc = V - v0 < sh.piece ? V - v0 : sh.piece;
         p.w_row = (uint32_t)v0;
@@ -1097,19 +1215,19 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         p.splits = 1;
         p.n = (uint32_t)vc;
         p.k = (uint32_t)H;
-        if ((s = launch_ce<kProb>(sh.ctas, x_k, w_k, p, n, device, st)) != DTE_OK) return s;
+        if ((s = launch_ce<kProb>(sh.ctas, rows, w_k, p, n, device, st)) != DTE_OK) return s;
         if (dx) {
             p.n = (uint32_t)H;
             p.k = (uint32_t)vc;
             p.splits = sh.splits;
             p.add = piece > 0;
-            if ((s = launch_ce<kDx>(sh.ctas, g_k, w_n, p, n, device, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDx>(sh.ctas, prob, w_n, p, n, device, st)) != DTE_OK) return s;
         }
         if (dweight) {
             p.m = (uint32_t)vc;
             p.n = (uint32_t)H;
             p.splits = 1;
-            if ((s = launch_ce<kDw>(sh.ctas, g_m, x_n, p, vc, device, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDw>(sh.ctas, prob, rows, p, vc, device, st)) != DTE_OK) return s;
         }
     }
     if (dx) {

@@ -100,7 +100,7 @@ struct SortedSum {
     const void* src;          // n x hidden
     uint32_t src_dtype;
     uint64_t src_ld;
-    const float* weight;      // per entry, or NULL; with weights: src bf16, out fp32 compact, vector path
+    const float* weight;      // per entry, or NULL; with weights: src bf16, out fp32 compact
     uint32_t hidden;
     float scale;
     // compact: out is fp32, n x hidden, and the sum of a row lies at position first[row] (see

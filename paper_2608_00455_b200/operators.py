@@ -41,8 +41,8 @@ def _refuse(msg: str):
 def _device(t: torch.Tensor, name: str) -> int:
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
-    device = t.get_device()
-    if device < 0 or not t.is_cuda:
+    device = t.get_device()               # -1 on the CPU
+    if device < 0:
         _refuse(f"{name} is not on a CUDA device; there is no CPU fallback")
     return device
 
@@ -70,18 +70,19 @@ def _rows(t: torch.Tensor, name: str):
 
 def _matrix(t: torch.Tensor, name: str, device: int):
     """(packed dte_matrix, rows, columns)."""
-    _same_device(t, name, device)
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _same_device(t, name, device)
     dtype = _NUMBERS.get(t.dtype)
     if dtype is None:
         _refuse(f"{name} must be float32 or bfloat16")
-    shape = t.shape
-    if len(shape) == 2:
-        rows, cols = shape
-        ld, unit = t.stride()
+    stride = t.stride()
+    if len(stride) == 2:
+        rows, cols = t.shape
+        ld, unit = stride
         if rows == 1:
             ld = cols
-    elif shape:
-        cols, unit = shape[-1], t.stride(-1)
+    elif stride:
+        cols, unit = t.shape[-1], stride[-1]
         rows, ld = _rows(t, name)
     else:
         _refuse(f"{name} needs at least one dimension")
@@ -92,7 +93,8 @@ def _matrix(t: torch.Tensor, name: str, device: int):
 
 def _ids(t: torch.Tensor, name: str, device: int):
     """(packed dte_ids, count)."""
-    _same_device(t, name, device)
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _same_device(t, name, device)
     dtype = _IDS.get(t.dtype)
     if dtype is None:
         _refuse(f"{name} must be int32 or int64")
@@ -106,6 +108,8 @@ def _vector(t: Optional[torch.Tensor], name: str, device: int, count: int, dtype
     """Address of a contiguous vector of `count` values, or None."""
     if t is None:
         return None
+    if t.__class__ is torch.Tensor and t.dtype in dtypes and t.numel() == count and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     _same_device(t, name, device)
     if t.dtype not in dtypes:
         _refuse(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in dtypes)}")
@@ -132,14 +136,21 @@ def _flags(t: Optional[torch.Tensor], device: int):
     return t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it, where this torch has the call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream, device: int) -> int:
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
-def _number(v, name: str) -> int:
-    if v < 0:
-        _refuse(f"{name} must not be negative")
-    return int(v)
+def _range(start: int, rows: int, vocab: Optional[int], name: str):
+    """(first row, vocabulary size) of a shard."""
+    if start < 0 or (vocab is not None and vocab < 0):
+        _refuse(f"{name} and vocab must not be negative")
+    return start, start + rows if vocab is None else vocab
 
 
 def _done(status: int) -> None:
@@ -166,9 +177,8 @@ def dte_embedding_forward(table: torch.Tensor, ids: torch.Tensor, out: torch.Ten
     m, rows, _ = _matrix(table, "table", device)
     o, _, _ = _matrix(out, "out", device)
     i, _ = _ids(ids, "ids", device)
-    _done(lib().dte_embedding_forward(m, i, _number(row_start, "row_start"),
-                                      row_start + rows if vocab is None else _number(vocab, "vocab"), scale, o,
-                                      _flags(flags, device), device, _stream(stream, device)))
+    first, total = _range(row_start, rows, vocab, "row_start")
+    _done(lib().dte_embedding_forward(m, i, first, total, scale, o, _flags(flags, device), device, _stream(stream, device)))
 
 
 def dte_embedding_backward_workspace_bytes(n_ids: int, hidden: int) -> int:
@@ -184,9 +194,9 @@ def dte_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.
     m, rows, _ = _matrix(dtable, "dtable", device)
     i, _ = _ids(ids, "ids", device)
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_embedding_backward(d, i, _number(row_start, "row_start"),
-                                       row_start + rows if vocab is None else _number(vocab, "vocab"), scale, bool(accumulate),
-                                       m, ws, size, _flags(flags, device), device, _stream(stream, device)))
+    first, total = _range(row_start, rows, vocab, "row_start")
+    _done(lib().dte_embedding_backward(d, i, first, total, scale, bool(accumulate), m, ws, size, _flags(flags, device), device,
+                                       _stream(stream, device)))
 
 
 def dte_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
@@ -234,8 +244,8 @@ def dte_linear_ce_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.
     w, rows, _ = _matrix(weight, "weight", device)
     t, n = _ids(targets, "targets", device)
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_linear_ce_forward(m, w, t, _number(vocab_start, "vocab_start"),
-                                      vocab_start + rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+    first, total = _range(vocab_start, rows, vocab, "vocab_start")
+    _done(lib().dte_linear_ce_forward(m, w, t, first, total, logit_scale,
                                       _vector(lse, "lse", device, n), _vector(target_logit, "target_logit", device, n),
                                       _vector(loss, "loss", device, n), ws, size, _flags(flags, device), device,
                                       _stream(stream, device)))
@@ -261,8 +271,8 @@ def dte_linear_ce_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch
     d = None if dx is None else _matrix(dx, "dx", device)[0]
     g = None if dweight is None else _matrix(dweight, "dweight", device)[0]
     ws, size = _workspace(workspace, device)
-    _done(lib().dte_linear_ce_backward(m, w, t, _number(vocab_start, "vocab_start"),
-                                       vocab_start + rows if vocab is None else _number(vocab, "vocab"), logit_scale,
+    first, total = _range(vocab_start, rows, vocab, "vocab_start")
+    _done(lib().dte_linear_ce_backward(m, w, t, first, total, logit_scale,
                                        _vector(lse, "lse", device, n), _vector(dloss, "dloss", device, n),
                                        bool(accumulate), d, g, ws,
                                        size, _flags(flags, device), device, _stream(stream, device)))

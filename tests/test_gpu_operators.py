@@ -428,6 +428,20 @@ def test_head_many_tiles_and_pieces():
         assert_within(dw, ww, bw + U[BF16] * ww.abs() * 1.01, "dweight")
 
 
+@pytest.mark.parametrize("tokens,vocab,hidden", [(1998, 18844, 2040), (9400, 700, 1016)])
+def test_head_many_rounds_of_tiles(tokens, vocab, hidden):
+    # whole rounds of tiles over 148 SMs, with ragged edges: in the logits and dweight, and in dx
+    x, w, t = head_case(tokens, vocab, hidden, 80, 0.01)
+    ref = Head(x, w, t)
+    got = run_forward(x, w, t)
+    ref.check_forward(*got)
+    lse, dloss = got[0], normal(81, (tokens,))
+    wx, bx, ww, bw = ref.gradients(dloss, lse)
+    dx, dw = run_backward(x, w, t, lse, dloss)
+    assert_within(dx, wx, bx + U[BF16] * wx.abs() * 1.01, "dx")
+    assert_within(dw, ww, bw + U[BF16] * ww.abs() * 1.01, "dweight")
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_head_accumulates_into_a_gradient_of_either_type(dtype):
     tokens, vocab, hidden = 200, 900, 136
