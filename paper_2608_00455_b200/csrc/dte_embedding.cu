@@ -86,9 +86,8 @@ constexpr int kGroupUnroll = 16;               // ids of a lane in flight: 16384
 struct GroupParams {
     const void* ids;
     uint32_t ids_dtype, n;
-    const uint32_t* n_dev;
     int64_t row_start, vocab;
-    uint32_t rows, bins;
+    uint32_t rows, bins, warps;    // warps that have entries
     uint32_t* first;           // rows + 1: where each row's entries start
     uint32_t* key;             // entries: row ...
     uint32_t* pos;             // ... and token
@@ -98,18 +97,18 @@ struct GroupParams {
 };
 
 __global__ void __launch_bounds__(kGroupThreads, 1) group_kernel(const GroupParams p) {
-    extern __shared__ uint32_t group_hist[];    // kGroupWarps x bins
+    extern __shared__ uint32_t group_hist[];    // warps x bins
     __shared__ uint32_t s_warp[32];
     __shared__ uint32_t s_below;
-    wait_for_earlier();
+    // reads what the caller passed and writes what no kernel in front of it in this call uses, so it need not wait for them
     let_next_start();
     const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid & 31, below_lanes = (1u << lane) - 1;
-    const uint32_t n = p.n_dev ? *p.n_dev : p.n;
+    const uint32_t n = p.n;
     const uint32_t r0 = blockIdx.x * p.bins, count = min(p.bins, p.rows - r0);
-    const uint32_t share = (n + kGroupWarps * 32 - 1) / (kGroupWarps * 32) * 32;
-    const uint64_t begin = (uint64_t)warp * share, end = begin + share < n ? begin + share : n;
+    const uint64_t share = ((uint64_t)n + p.warps * 32 - 1) / (p.warps * 32) * 32;
+    const uint64_t begin = min(warp * share, (uint64_t)n), end = min(begin + share, (uint64_t)n);
     uint32_t* h = group_hist + warp * p.bins;
-    for (uint32_t i = tid; i < kGroupWarps * p.bins; i += kGroupThreads) group_hist[i] = 0;
+    for (uint32_t i = tid; i < p.warps * p.bins; i += kGroupThreads) group_hist[i] = 0;
     for (uint32_t i = blockIdx.x * kGroupThreads + tid; i < p.n_counters; i += gridDim.x * kGroupThreads) p.counters[i] = 0;
     if (tid == 0) s_below = 0;
     __syncthreads();
@@ -156,7 +155,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_kernel(const GroupPara
     for (int j = 0; j < 2; ++j) {
         const uint32_t bin = 2 * tid + j;
         if (bin < count)
-            for (int w = 0; w < kGroupWarps; ++w) {
+            for (uint32_t w = 0; w < p.warps; ++w) {
                 const uint32_t v = group_hist[w * p.bins + bin];
                 group_hist[w * p.bins + bin] = total[j];
                 total[j] += v;
@@ -181,7 +180,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_kernel(const GroupPara
             p.first[r0 + bin] = at;
             if (r0 + bin + 1 == p.rows) p.first[p.rows] = at + total[j];
             if (total[j])
-                for (int w = 0; w < kGroupWarps; ++w) group_hist[w * p.bins + bin] += at;
+                for (uint32_t w = 0; w < p.warps; ++w) group_hist[w * p.bins + bin] += at;
             at += total[j];
         }
     }
@@ -197,6 +196,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) group_kernel(const GroupPara
         }
     });
     if (bad && blockIdx.x == 0 && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
+    if (blockIdx.x == 0) wait_for_earlier();      // whoever waits for this kernel waits for the ones in front of it, too
 }
 
 // ---- zeros ---------------------------------------------------------------------------------------------------
@@ -228,12 +228,13 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const FillParams p) 
 }
 
 // ---- sums over the entries of a row -------------------------------------
-// The grouped entries are cut into blocks of kSumBlock, whatever the rows are, so a token that makes up a tenth of
+// The grouped entries are cut into blocks, whatever the rows are, so a token that makes up a tenth of
 // the batch costs no more than rare ones.  A warp sums one block's runs of equal rows over one stretch of columns; a
 // run inside the block is finished there.  Of a run that crosses blocks each block leaves an fp32 partial sum (at most
 // two per block: [0] of the run that comes in, [1] of the run that began here and goes on), and the warp that leaves
 // the last of them adds them up, in the order of the blocks whoever it is.
-constexpr int kSumBlock = 16;          // entries of a warp
+constexpr uint32_t kMaxSumBlock = 16;   // entries of a warp, fewer where there are too few to fill the GPU (see sum_block)
+constexpr uint32_t kMinSumBlock = 4;
 constexpr int kSumThreads = 128;
 constexpr int kSumUnroll = 4;          // entries of a batch: with 8 the registers cost more warps than the loads gain (411 -> 393 us)
 
@@ -241,7 +242,7 @@ struct SumParams {
     const uint32_t* first;
     const uint32_t* key;
     const uint32_t* pos;
-    uint32_t rows, hidden, chunks;
+    uint32_t rows, hidden, chunks, block;
     const void* src;
     uint64_t src_ld;
     const float* weight;
@@ -286,7 +287,7 @@ template <typename TO, int V>
 __device__ __forceinline__ void leave_partial(const SumParams& p, uint64_t block, uint32_t chunk, uint32_t key, uint32_t col, bool active,
                                               float* acc) {
     const uint32_t begin = p.first[key], end = p.first[key + 1];
-    const uint64_t b0 = begin / kSumBlock, b1 = (end - 1) / kSumBlock;
+    const uint64_t b0 = begin / p.block, b1 = (end - 1) / p.block;
     if (active) {
         Vec<float, V> v;
         v.set(acc);
@@ -319,16 +320,16 @@ template <typename TS, typename TO, int V, bool WEIGHTED>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
     wait_for_earlier();
     const uint32_t w = blockIdx.x * (kSumThreads / 32) + threadIdx.x / 32, lane = threadIdx.x & 31;
-    const uint32_t block = w / p.chunks, chunk = w % p.chunks, first = block * kSumBlock;
+    const uint32_t block = w / p.chunks, chunk = w % p.chunks, first = block * p.block;
     const uint32_t n = p.first[p.rows];                      // entries of this shard
     if (first >= n) return;
     const uint32_t col = chunk * (32 * V) + lane * V;
     const bool active = col < p.hidden;
-    const bool mine = lane < kSumBlock && first + lane < n;
+    const bool mine = lane < p.block && first + lane < n;
     const uint32_t key = mine ? p.key[first + lane] : kNone;
     const uint32_t pos = mine ? p.pos[first + lane] : 0;
     const uint32_t prev = first ? p.key[first - 1] : kNone;
-    const uint32_t next = first + kSumBlock < n ? p.key[first + kSumBlock] : kNone;
+    const uint32_t next = first + p.block < n ? p.key[first + p.block] : kNone;
     const float wt = WEIGHTED && mine ? p.weight[pos] : 1.f;
     const TS* src = static_cast<const TS*>(p.src) + col;
 
@@ -337,7 +338,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
     uint32_t cur = __shfl_sync(0xFFFFFFFFu, key, 0), start = 0;
     bool incoming = cur == prev;
-    for (uint32_t i0 = 0; i0 < kSumBlock && first + i0 < n; i0 += kSumUnroll) {
+    for (uint32_t i0 = 0; i0 < p.block && first + i0 < n; i0 += kSumUnroll) {
         Vec<TS, V> r[kSumUnroll];
 #pragma unroll
         for (int u = 0; u < kSumUnroll; ++u) {
@@ -374,15 +375,28 @@ struct SumLayout {
     uint64_t first, key, pos, counters, partial, total;
 };
 
+// Entries of a block: the most, unless that leaves the GPU short of warps (6007 x 2048 fp32 of which a quarter is in the shard:
+// 16 entries 62 us, 4 entries 58 us; 16384 x 4096: 16 entries 394 us, 8 entries 405 us).
+static uint32_t sum_block(uint64_t n, uint64_t chunks) {
+    uint32_t block = kMaxSumBlock;
+    while (block > kMinSumBlock && n / block * chunks < kGroupCtas * 32) block /= 2;
+    return block;
+}
+
 static SumLayout sum_layout(uint64_t n, uint64_t rows, uint64_t hidden) {
-    const uint64_t blocks = (n + kSumBlock - 1) / kSumBlock;
+    const uint64_t most = sum_chunks(hidden, false);       // element by element
+    const uint64_t blocks = (n + kMinSumBlock - 1) / kMinSumBlock;
+    // smaller blocks are used only while twice their size gives fewer than kGroupCtas * 32 warps (sum_block)
+    const uint64_t by_most = (n + kMaxSumBlock - 1) / kMaxSumBlock;
+    const uint64_t few = 2 * kGroupCtas * 32 / sum_chunks(hidden, true) + 2;
+    const uint64_t used = by_most > (blocks < few ? blocks : few) ? by_most : (blocks < few ? blocks : few);
     SumLayout l;
     l.first = 0;
     l.key = l.first + align_up((rows + 1) * 4, kWorkspaceAlign);
     l.pos = l.key + align_up(n * 4, kWorkspaceAlign);
     l.counters = l.pos + align_up(n * 4, kWorkspaceAlign);
-    l.partial = l.counters + align_up(blocks * sum_chunks(hidden, false) * 4, kWorkspaceAlign);
-    l.total = l.partial + align_up(blocks * 2 * hidden * 4, kWorkspaceAlign);
+    l.partial = l.counters + align_up(used * most * 4, kWorkspaceAlign);
+    l.total = l.partial + align_up(used * 2 * hidden * 4, kWorkspaceAlign);
     return l;
 }
 
@@ -391,7 +405,7 @@ uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t rows, uint64_t hidden) 
 const uint32_t* sorted_sum_first(const void* workspace) { return static_cast<const uint32_t*>(workspace); }
 
 bool sorted_sum_fits(uint64_t n, uint64_t rows, uint64_t hidden, uint32_t out_dtype) {
-    const uint64_t sums = (n / kSumBlock + 1) * sum_chunks(hidden, false);
+    const uint64_t sums = (n / kMinSumBlock + 1) * sum_chunks(hidden, false);
     const uint64_t fills = rows * (hidden * elem_size(out_dtype) / kFillBytes + 1);
     return sums < (1ull << 31) && fills < (1ull << 31) && sums + fills < (1ull << 31);
 }
@@ -405,17 +419,21 @@ static dte_status launch_sums(const SumParams& p, unsigned ctas, cudaStream_t st
 dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool after, int device, cudaStream_t st) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const SumLayout l = sum_layout(q.n, q.rows, q.hidden);
-    const uint64_t blocks = ((uint64_t)q.n + kSumBlock - 1) / kSumBlock, chunks = sum_chunks(q.hidden, vec);
+    const uint64_t chunks = sum_chunks(q.hidden, vec);
+    const uint32_t block = sum_block(q.n, chunks);
+    const uint64_t blocks = ((uint64_t)q.n + block - 1) / block;
     GroupParams g = {};
     g.ids = q.ids;
     g.ids_dtype = q.ids_dtype;
     g.n = q.n;
-    g.n_dev = q.n_dev;
     g.row_start = q.row_start;
     g.vocab = (int64_t)q.vocab;
     g.rows = q.rows;
     g.bins = (q.rows + kGroupCtas - 1) / kGroupCtas;
     if (g.bins > kMaxBins) g.bins = kMaxBins;
+    // a warp takes at least one round of loads: few entries leave fewer histograms to add up
+    const uint64_t warps = ((uint64_t)q.n + 32 * kGroupUnroll - 1) / (32 * kGroupUnroll);
+    g.warps = (uint32_t)(warps < 1 ? 1 : warps > kGroupWarps ? kGroupWarps : warps);
     g.first = reinterpret_cast<uint32_t*>(ws + l.first);
     g.key = reinterpret_cast<uint32_t*>(ws + l.key);
     g.pos = reinterpret_cast<uint32_t*>(ws + l.pos);
@@ -426,7 +444,7 @@ dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool
     dte_status s = allow_smem(group_kernel, (size_t)kGroupWarps * kMaxBins * 4, device, ready);
     if (s != DTE_OK) return s;
     const unsigned ranges = (q.rows + g.bins - 1) / g.bins;
-    const size_t smem = (size_t)kGroupWarps * g.bins * 4;
+    const size_t smem = (size_t)g.warps * g.bins * 4;
     if (after) {
         DTE_CUDA(launch_after(group_kernel, dim3(ranges), kGroupThreads, smem, st, g));
     } else {
@@ -440,6 +458,7 @@ dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool
     p.rows = q.rows;
     p.hidden = q.hidden;
     p.chunks = (uint32_t)chunks;
+    p.block = block;
     p.src = q.src;
     p.src_ld = q.src_ld;
     p.weight = q.weight;

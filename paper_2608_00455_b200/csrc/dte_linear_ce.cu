@@ -77,6 +77,7 @@ struct CeParams {
     void* dweight;
     uint64_t dweight_ld;
     bool dweight_bf16, accumulate;
+    bool whole_sectors;          // every group of 32 bytes of a row of dweight starts on a sector
     const uint32_t* first;       // per vocabulary row: where its target term lies, if the next row's lies further on
     const float* target_sum;
 };
@@ -101,6 +102,21 @@ __device__ __forceinline__ void load_tile(uint32_t addr, float (&v)[32]) {
     tmem_load_wait(r);
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+// o += the (up to) four groups of 8 columns at d
+template <typename T>
+__device__ __forceinline__ void add_old(const T* d, uint32_t groups, float (&o)[32]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (groups <= (uint32_t)j) break;
+        Raw8<T> r;
+        float old[8];
+        r.load(d + 8 * j);
+        r.get(old);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[8 * j + i] += old[i];
+    }
 }
 
 // The 128 columns from c0 (half a tile) of row `row`; lane_row: the row within the CTA's 128.
@@ -227,38 +243,43 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
             fetch(c + 32, ahead);
             float v[32];
             load_tile(tmem + c, v);
-            if (valid) {
+            if (!valid) continue;
+            const uint64_t off = vrow * p.dweight_ld + n0 + c;
+            const uint32_t left = (p.n - (n0 + c)) / 8;      // groups of 8 columns
+            float o[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = (empty ? 0.f : v[j]) - __uint_as_float(w[j / 8][j % 8]);
+            if (p.dweight_bf16) {
+                __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.dweight) + off;
+                if (p.accumulate) add_old(d, left, o);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t q[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] = pack_bf16(o[16 * j + 2 * i], o[16 * j + 2 * i + 1]);
+                    if (p.whole_sectors && left >= 2u * j + 2) {
+                        store32(d + 16 * j, q);
+                    } else {
+                        uint4* e = reinterpret_cast<uint4*>(d + 16 * j);
+                        if (left > 2u * j) e[0] = make_uint4(q[0], q[1], q[2], q[3]);
+                        if (left > 2u * j + 1) e[1] = make_uint4(q[4], q[5], q[6], q[7]);
+                    }
+                }
+            } else {
+                float* d = static_cast<float*>(p.dweight) + off;
+                if (p.accumulate) add_old(d, left, o);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (n0 + c + 8 * j >= p.n) break;
-                    float o[8];
+                    if (left <= (uint32_t)j) break;
+                    uint32_t q[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = (empty ? 0.f : v[8 * j + i]) - __uint_as_float(w[j][i]);
-                    const uint64_t off = vrow * p.dweight_ld + n0 + c + 8 * j;
-                    if (p.dweight_bf16) {
-                        __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.dweight) + off;
-                        Raw8<__nv_bfloat16> r;
-                        if (p.accumulate) {
-                            float old[8];
-                            r.load(d);
-                            r.get(old);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] += old[i];
-                        }
-                        r.set(o);
-                        r.store(d);
+                    for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(o[8 * j + i]);
+                    if (p.whole_sectors) {
+                        store32(d + 8 * j, q);
                     } else {
-                        float* d = static_cast<float*>(p.dweight) + off;
-                        Raw8<float> r;
-                        if (p.accumulate) {
-                            float old[8];
-                            r.load(d);
-                            r.get(old);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] += old[i];
-                        }
-                        r.set(o);
-                        r.store(d);
+                        uint4* e = reinterpret_cast<uint4*>(d + 8 * j);
+                        e[0] = make_uint4(q[0], q[1], q[2], q[3]);
+                        e[1] = make_uint4(q[4], q[5], q[6], q[7]);
                     }
                 }
             }
@@ -687,7 +708,7 @@ struct CombineParams {
 };
 
 constexpr int kCombineRows = 8;      // tokens of a CTA: their statistics of one tile fill two sectors
-constexpr int kCombineThreads = 512;
+constexpr int kCombineThreads = 1024;
 
 // log-sum-exp of a token from its tiles' statistics.  The tensor cores add a logit's products up with
 // truncation (4e-6 of its size at 4096 products), which matters for one logit, the target's: it is taken from the
@@ -704,6 +725,13 @@ __global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const Combi
         sum = sum * exp2_fast(top - from) + s2 * exp2_fast(t2 - from);
         top = now;
     };
+    // what the last step needs, asked for before the statistics
+    constexpr uint32_t kWarps = kCombineThreads / 32;      // then: kWarps lanes per row
+    const uint32_t row = blockIdx.x * kCombineRows + threadIdx.x / kWarps;
+    const bool writer = threadIdx.x < kCombineRows * kWarps && threadIdx.x % kWarps == 0 && row < count;
+    const float made = writer ? p.row_target_logit[row] : 0.f, exact = writer ? p.exact_logit[row] : 0.f;
+    const uint32_t n = writer ? (uint32_t)p.source[row] : 0;
+    const bool here = writer && p.target[row] >= 0;
     float top = -INFINITY, sum = 0.f;
     if (i < count) {
 #pragma unroll 8
@@ -722,7 +750,6 @@ __global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const Combi
         s_sum[threadIdx.x / 32][r] = sum;
     }
     __syncthreads();
-    constexpr uint32_t kWarps = kCombineThreads / 32;      // 16: half a warp per row now
     if (threadIdx.x >= kCombineRows * kWarps) return;
     top = s_top[threadIdx.x % kWarps][threadIdx.x / kWarps];
     sum = s_sum[threadIdx.x % kWarps][threadIdx.x / kWarps];
@@ -731,12 +758,9 @@ __global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const Combi
         const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         join(top, sum, t2, s2);
     }
-    const uint32_t row = blockIdx.x * kCombineRows + threadIdx.x / kWarps;
-    if (threadIdx.x % kWarps == 0 && row < count) {
+    if (writer) {
         float lse = (top + log2f(sum)) * kLn2;
-        const float made = p.row_target_logit[row], exact = p.exact_logit[row];
-        const uint32_t n = (uint32_t)p.source[row];
-        if (p.target[row] >= 0 && made != exact) {
+        if (here && made != exact) {
             const float move = exp2_fast((made - lse) * kLog2e) * expm1f(exact - made);
             if (fabsf(move) < 0.5f) lse += log1pf(move);      // else the logits are not finite or beyond fp32's reach
         }
@@ -1198,6 +1222,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         p.dweight = dweight->data;
         p.dweight_ld = dweight->ld;
         p.dweight_bf16 = dweight->dtype == DTE_BF16;
+        p.whole_sectors = !(((uintptr_t)dweight->data | dweight->ld * elem_size(dweight->dtype)) & 31u);
     }
     p.accumulate = accumulate != 0;
     p.first = sorted_sum_first(ws + l.sums);

@@ -92,8 +92,7 @@ struct SortedSum {
     // row of an entry: id - row_start where that lies in [0, rows), else the entry is dropped
     const void* ids;
     uint32_t ids_dtype;
-    uint32_t n;               // entries (upper bound when n_dev is set)
-    const uint32_t* n_dev;    // device: actual number of entries; NULL: n
+    uint32_t n;               // entries
     int64_t row_start;
     uint64_t vocab;
     uint32_t rows;
