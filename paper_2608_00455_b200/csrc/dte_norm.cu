@@ -144,7 +144,7 @@ struct Rows {
     static_assert(kRing % kBatch == 0 && kRing >= kBatch, "batches must not wrap around the ring");
 };
 
-// A thread's columns of row after row of INPUTS matrices: round k is row me + k * teams.
+// A thread's columns of row after row of INPUTS matrices: round k is row me + k * apart.
 template <typename T, bool VEC, int INPUTS, int TEAM>
 struct Feed {
     using R = Rows<T, VEC, INPUTS, TEAM>;
@@ -154,15 +154,15 @@ struct Feed {
     uint64_t step[INPUTS];
     uint32_t asked, rounds;                       // rounds asked for, rounds that have a row
     uint32_t t, n, cols, begin, end, at;          // shared memory of the ring; the oldest round
-    __device__ __forceinline__ Feed(const NormParams& p, uint32_t smem, uint32_t me, uint32_t teams, uint32_t t_, uint32_t n_)
-        : asked(0), rounds(me < p.rows ? (p.rows - me + teams - 1) / teams : 0), t(t_), n(n_), cols(p.cols), begin(smem + threadIdx.x * 16) {
+    __device__ __forceinline__ Feed(const NormParams& p, uint32_t smem, uint32_t me, uint32_t apart, uint32_t rounds_, uint32_t t_, uint32_t n_)
+        : asked(0), rounds(rounds_), t(t_), n(n_), cols(p.cols), begin(smem + threadIdx.x * 16) {
         end = begin + R::kRing * INPUTS * kPieces * blockDim.x * 16;
         at = begin;
         from[0] = static_cast<const T*>(p.x) + me * p.x_ld;
-        step[0] = teams * p.x_ld;
+        step[0] = apart * p.x_ld;
         if constexpr (INPUTS == 2) {
             from[1] = static_cast<const T*>(p.dout) + me * p.dout_ld;
-            step[1] = teams * p.dout_ld;
+            step[1] = apart * p.dout_ld;
         }
 #pragma unroll
         for (int k = 0; k < R::kRing; ++k) ask();
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
         in[j] = f2(q[0], q[1]);
     }
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    Feed<T, VEC, 1, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, teams, t, n);
+    Feed<T, VEC, 1, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, teams, me < p.rows ? (p.rows - me + teams - 1) / teams : 0, t, n);
     constexpr int B = Rows<T, VEC, 1, TEAM>::kBatch;
     // all lanes of a warp go round together, so that shuffles stay full; a team past the end idles
     const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
@@ -315,12 +315,17 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_forward
 }
 
 template <typename T, bool VEC, int TEAM, uint32_t KIND>
-__global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backward_kernel(const NormParams p) {
+__global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM, TEAM <= 32 ? 2 : 1) norm_backward_kernel(const NormParams p) {
     __shared__ float buf[2][128];
     const uint32_t n = TEAM <= 32 ? TEAM : blockDim.x;
     const uint32_t t = TEAM <= 32 ? threadIdx.x % n : threadIdx.x;
     const uint32_t teams = TEAM <= 32 ? gridDim.x * (kTeamThreads / n) : gridDim.x;
-    const uint32_t me = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
+    const uint32_t team = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
+    constexpr int B = Rows<T, VEC, 2, TEAM>::kBatch, S = KIND == DTE_NORM_LAYER ? 2 : 1;
+    const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
+    // a CTA's rows follow one another (84 us; every 296th row: 87 us); teams of a CTA share out its stretch row by row
+    const uint32_t apart = TEAM > 32 ? 1 : teams, me = TEAM > 32 ? team * rounds * B : team;
+    const uint32_t end = TEAM > 32 ? min(me + rounds * B, p.rows) : p.rows;
     T* dx = static_cast<T*>(p.out);
     F2 w[kPer / 2], dw[kPer / 2], db[kPer / 2];
 #pragma unroll
@@ -335,22 +340,20 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
         dw[j] = db[j] = f2(0.f, 0.f);
     }
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    Feed<T, VEC, 2, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, teams, t, n);
-    constexpr int B = Rows<T, VEC, 2, TEAM>::kBatch, S = KIND == DTE_NORM_LAYER ? 2 : 1;
+    Feed<T, VEC, 2, TEAM> feed(p, (uint32_t)__cvta_generic_to_shared(norm_smem), me, apart, me < end ? (end - me + apart - 1) / apart : 0, t, n);
     float nmean[B], nrstd[B];                               // statistics of the next rounds
     auto fetch = [&](uint32_t row) {
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const uint32_t r = row + j * teams;
-            nmean[j] = KIND == DTE_NORM_LAYER && r < p.rows ? p.mean[r] : 0.f;
-            nrstd[j] = r < p.rows ? p.rstd[r] : 0.f;
+            const uint32_t r = row + j * apart;
+            nmean[j] = KIND == DTE_NORM_LAYER && r < end ? p.mean[r] : 0.f;
+            nrstd[j] = r < end ? p.rstd[r] : 0.f;
         }
     };
     fetch(me);
-    const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
     uint32_t row = me;
-    for (uint32_t k = 0; k < rounds; ++k, row += teams * B) {
-        if (TEAM > 32 && row >= p.rows) break;
+    for (uint32_t k = 0; k < rounds; ++k, row += apart * B) {
+        if (TEAM > 32 && row >= end) break;
         float sums[B * S];
         F2 r[B], m[B];                                      // xhat = x * r + m
 #pragma unroll
@@ -358,14 +361,14 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
             r[j] = f2(nrstd[j], nrstd[j]);
             m[j] = f2(-nmean[j] * nrstd[j], -nmean[j] * nrstd[j]);
         }
-        fetch(row + teams * B);
+        fetch(row + apart * B);
         feed.wait();
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             F2 xh[kPer / 2], g[kPer / 2];
             feed.get(j, 0, xh);
             feed.get(j, 1, g);
-            const bool live = row + j * teams < p.rows;
+            const bool live = row + j * apart < end;
             F2 s2 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < kPer / 2; ++i) {
@@ -385,8 +388,8 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM) norm_backwar
         team_sum<TEAM, B * S>(sums, buf[k & 1]);
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const uint32_t at = row + j * teams;
-            if (at < p.rows && dx) {
+            const uint32_t at = row + j * apart;
+            if (at < end && dx) {
                 // rstd * (g - c1 - xh * c2); the row is read from shared memory again: cheaper than its registers
                 float rstd, unused;
                 f2_get(r[j], rstd, unused);
