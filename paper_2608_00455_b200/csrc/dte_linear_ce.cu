@@ -1002,6 +1002,8 @@ static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, cons
         return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^24 vocabulary rows and 2^20 hidden");
     if (align_up(targets->count, kPadRows) * ((x->cols + kBlock - 1) / kBlock) >= (1ull << 31))
         return op_fail(DTE_ERR_INVALID_ARG, "tokens x hidden is too large for one call");
+    if ((targets->count / kTileM + 1) * (weight->rows / 128 + 1) >= (1ull << 31))
+        return op_fail(DTE_ERR_INVALID_ARG, "tokens x vocabulary is too large for one call");
     return DTE_OK;
 }
 
