@@ -61,12 +61,13 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupPara
 }
 
 template <typename TI, typename TO>
-static void lookup_types(const LookupParams& q, bool vec, cudaStream_t st) {
+static void lookup_types(const LookupParams& q, int vec, cudaStream_t st) {
     LookupParams p = q;
-    const uint32_t span = 32 * kLookupUnroll * (vec ? 8 : 1);
+    const uint32_t span = 32 * kLookupUnroll * vec;
     p.chunks = (p.hidden + span - 1) / span;
     const uint64_t ctas = ((uint64_t)p.n * p.chunks + kLookupThreads / 32 - 1) / (kLookupThreads / 32);
-    if (vec) lookup_kernel<TI, TO, 8><<<(unsigned)ctas, kLookupThreads, 0, st>>>(p);
+    if (vec == 8) lookup_kernel<TI, TO, 8><<<(unsigned)ctas, kLookupThreads, 0, st>>>(p);
+    else if (vec == 2) lookup_kernel<TI, TO, 2><<<(unsigned)ctas, kLookupThreads, 0, st>>>(p);
     else lookup_kernel<TI, TO, 1><<<(unsigned)ctas, kLookupThreads, 0, st>>>(p);
 }
 
@@ -256,7 +257,11 @@ struct SumParams {
 
 template <int V>
 __device__ __forceinline__ void load_partial(const float* p, float* f) {       // written by other SMs: from L2
-    if constexpr (V == 8) {
+    if constexpr (V == 2) {
+        const float2 a = __ldcg(reinterpret_cast<const float2*>(p));
+        f[0] = a.x;
+        f[1] = a.y;
+    } else if constexpr (V == 8) {
         const float4 a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
         f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
     } else {
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
     else write_sum<TO, V>(p, p.compact ? first + start : cur, col, active, acc);
 }
 
-static uint64_t sum_chunks(uint64_t hidden, bool vec) { return (hidden + (vec ? 255 : 31)) / (vec ? 256 : 32); }
+static uint64_t sum_chunks(uint64_t hidden, int vec) { return (hidden + 32 * vec - 1) / (32 * vec); }
 
 struct SumLayout {
     uint64_t first, key, pos, counters, partial, total;
@@ -384,11 +389,11 @@ static uint32_t sum_block(uint64_t n, uint64_t chunks) {
 }
 
 static SumLayout sum_layout(uint64_t n, uint64_t rows, uint64_t hidden) {
-    const uint64_t most = sum_chunks(hidden, false);       // element by element
+    const uint64_t most = sum_chunks(hidden, 1);       // element by element
     const uint64_t blocks = (n + kMinSumBlock - 1) / kMinSumBlock;
     // smaller blocks are used only while twice their size gives fewer than kGroupCtas * 32 warps (sum_block)
     const uint64_t by_most = (n + kMaxSumBlock - 1) / kMaxSumBlock;
-    const uint64_t few = 2 * kGroupCtas * 32 / sum_chunks(hidden, true) + 2;
+    const uint64_t few = 2 * kGroupCtas * 32 / sum_chunks(hidden, 8) + 2;
     const uint64_t used = by_most > (blocks < few ? blocks : few) ? by_most : (blocks < few ? blocks : few);
     SumLayout l;
     l.first = 0;
@@ -405,18 +410,20 @@ uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t rows, uint64_t hidden) 
 const uint32_t* sorted_sum_first(const void* workspace) { return static_cast<const uint32_t*>(workspace); }
 
 bool sorted_sum_fits(uint64_t n, uint64_t rows, uint64_t hidden, uint32_t out_dtype) {
-    const uint64_t sums = (n / kMinSumBlock + 1) * sum_chunks(hidden, false);
+    const uint64_t sums = (n / kMinSumBlock + 1) * sum_chunks(hidden, 1);
     const uint64_t fills = rows * (hidden * elem_size(out_dtype) / kFillBytes + 1);
     return sums < (1ull << 31) && fills < (1ull << 31) && sums + fills < (1ull << 31);
 }
 
-template <typename TS, typename TO, int V, bool WEIGHTED = false>
-static dte_status launch_sums(const SumParams& p, unsigned ctas, cudaStream_t st) {
-    DTE_CUDA(launch_after(sum_kernel<TS, TO, V, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
+template <typename TS, typename TO, bool WEIGHTED = false>
+static dte_status launch_sums(const SumParams& p, int vec, unsigned ctas, cudaStream_t st) {
+    if (vec == 8) DTE_CUDA(launch_after(sum_kernel<TS, TO, 8, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
+    else if (vec == 2) DTE_CUDA(launch_after(sum_kernel<TS, TO, 2, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
+    else DTE_CUDA(launch_after(sum_kernel<TS, TO, 1, WEIGHTED>, dim3(ctas), kSumThreads, 0, st, p));
     return DTE_OK;
 }
 
-dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool after, int device, cudaStream_t st) {
+dte_status launch_sorted_sum(const SortedSum& q, int vec, void* workspace, bool after, int device, cudaStream_t st) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const SumLayout l = sum_layout(q.n, q.rows, q.hidden);
     const uint64_t chunks = sum_chunks(q.hidden, vec);
@@ -486,18 +493,11 @@ dte_status launch_sorted_sum(const SortedSum& q, bool vec, void* workspace, bool
     if (q.n == 0) return DTE_OK;
     const unsigned ctas = (unsigned)((blocks * chunks + kSumThreads / 32 - 1) / (kSumThreads / 32));
     const bool sb = q.src_dtype == DTE_BF16, ob = q.out_dtype == DTE_BF16;
-    if (p.weight)                                             // the head's gradient
-        return vec ? launch_sums<__nv_bfloat16, float, 8, true>(p, ctas, st) : launch_sums<__nv_bfloat16, float, 1, true>(p, ctas, st);
-    if (vec) {
-        if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 8>(p, ctas, st);
-        if (sb) return launch_sums<__nv_bfloat16, float, 8>(p, ctas, st);
-        if (ob) return launch_sums<float, __nv_bfloat16, 8>(p, ctas, st);
-        return launch_sums<float, float, 8>(p, ctas, st);
-    }
-    if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16, 1>(p, ctas, st);
-    if (sb) return launch_sums<__nv_bfloat16, float, 1>(p, ctas, st);
-    if (ob) return launch_sums<float, __nv_bfloat16, 1>(p, ctas, st);
-    return launch_sums<float, float, 1>(p, ctas, st);
+    if (p.weight) return launch_sums<__nv_bfloat16, float, true>(p, vec, ctas, st);       // the head's gradient
+    if (sb && ob) return launch_sums<__nv_bfloat16, __nv_bfloat16>(p, vec, ctas, st);
+    if (sb) return launch_sums<__nv_bfloat16, float>(p, vec, ctas, st);
+    if (ob) return launch_sums<float, __nv_bfloat16>(p, vec, ctas, st);
+    return launch_sums<float, float>(p, vec, ctas, st);
 }
 
 dte_status device_sms(int device, int* sms) {
@@ -530,7 +530,7 @@ extern "C" dte_status dte_embedding_forward(const dte_matrix* table, const dte_i
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (ids->count == 0) return DTE_OK;
     OpDeviceGuard g(device);
-    const bool vec = vec8_ok(table) && vec8_ok(out);
+    const int vec = vec_of(table, out);
     LookupParams p = {};
     p.table = table->data;
     p.ids = ids->data;
@@ -545,7 +545,7 @@ extern "C" dte_status dte_embedding_forward(const dte_matrix* table, const dte_i
     p.vocab = (int64_t)vocab;
     p.scale = (float)scale;
     p.flags = flags;
-    const uint64_t span = 32 * kLookupUnroll * (vec ? 8 : 1);
+    const uint64_t span = 32 * kLookupUnroll * vec;
     if (ids->count * ((table->cols + span - 1) / span) >= (1ull << 32))
         return op_fail(DTE_ERR_INVALID_ARG, "ids.count x hidden is too large for one call");
     const bool ib = table->dtype == DTE_BF16, ob = out->dtype == DTE_BF16;
@@ -580,7 +580,7 @@ extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_i
         return op_fail(DTE_ERR_INVALID_ARG, "dout must be ids.count x dtable.cols");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if ((s = check_workspace(workspace, workspace_bytes, sorted_sum_workspace_bytes(ids->count, kMaxTableRows, dout->cols))) != DTE_OK) return s;
-    const bool vec = vec8_ok(dout) && vec8_ok(dtable);
+    const int vec = vec_of(dout, dtable);
     if (dtable->rows > kMaxTableRows) return op_fail(DTE_ERR_INVALID_ARG, "at most 2097151 rows of a table");
     if (!sorted_sum_fits(ids->count, dtable->rows, dout->cols, dtable->dtype))
         return op_fail(DTE_ERR_INVALID_ARG, "ids.count x hidden or dtable is too large for one call");

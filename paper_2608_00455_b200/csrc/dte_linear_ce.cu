@@ -1205,7 +1205,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         q.out_dtype = DTE_F32;
         q.out_ld = H;
         q.compact = true;
-        if ((s = launch_sorted_sum(q, vec8_ok(x), ws + l.sums, true, device, st)) != DTE_OK) return s;
+        if ((s = launch_sorted_sum(q, vec8_ok(x) ? 8 : vec2_ok(x) ? 2 : 1, ws + l.sums, true, device, st)) != DTE_OK) return s;
     }
     CeParams p = {};
     p.tokens = count;

@@ -74,6 +74,15 @@ inline bool vec8_ok(const dte_matrix* m) {
     return !((uintptr_t)m->data & 15u) && (m->cols % 8 == 0) && (m->rows <= 1 || m->ld % unit == 0);
 }
 
+// Pairs of elements: data, every row start and the number of columns a multiple of two.
+inline bool vec2_ok(const dte_matrix* m) {
+    return !((uintptr_t)m->data & (2 * elem_size(m->dtype) - 1)) && m->cols % 2 == 0 && (m->rows <= 1 || m->ld % 2 == 0);
+}
+
+inline int vec_of(const dte_matrix* a, const dte_matrix* b) {
+    return vec8_ok(a) && vec8_ok(b) ? 8 : vec2_ok(a) && vec2_ok(b) ? 2 : 1;
+}
+
 dte_status device_sms(int device, int* sms);   // multiprocessor count, cached per device
 
 // Raises a kernel's dynamic shared memory limit, once per device.
@@ -114,7 +123,8 @@ uint64_t sorted_sum_workspace_bytes(uint64_t n, uint64_t rows, uint64_t hidden);
 const uint32_t* sorted_sum_first(const void* workspace);     // rows + 1 positions, valid behind launch_sorted_sum
 bool sorted_sum_fits(uint64_t n, uint64_t rows, uint64_t hidden, uint32_t out_dtype);
 // after: an earlier kernel of the same call is in front (see launch_after)
-dte_status launch_sorted_sum(const SortedSum& p, bool vec, void* workspace, bool after, int device, cudaStream_t st);
+// vec: elements per access that the matrices allow, 8, 2 or 1
+dte_status launch_sorted_sum(const SortedSum& p, int vec, void* workspace, bool after, int device, cudaStream_t st);
 
 #ifdef __CUDACC__
 // ---- dependent launches ------------------------------------------------------------------------------
@@ -210,11 +220,31 @@ struct Raw8<float> {
     }
 };
 
-// V consecutive elements: V == 8 through Raw8, V == 1 one element of any alignment.
+// V consecutive elements: V == 8 through Raw8, V == 2 a pair on a boundary of its size, V == 1 one element of any alignment.
 template <typename T, int V>
 struct Vec;
 template <typename T>
 struct Vec<T, 8> : Raw8<T> {};
+template <>
+struct Vec<__nv_bfloat16, 2> {
+    uint32_t a;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint32_t*>(p); }
+    __device__ __forceinline__ void load_cs(const __nv_bfloat16* p) { a = __ldcs(reinterpret_cast<const uint32_t*>(p)); }
+    __device__ __forceinline__ void zero() { a = 0; }
+    __device__ __forceinline__ void get(float* f) const { f[0] = bf16_lo(a); f[1] = bf16_hi(a); }
+    __device__ __forceinline__ void set(const float* f) { a = pack_bf16(f[0], f[1]); }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint32_t*>(p) = a; }
+};
+template <>
+struct Vec<float, 2> {
+    float2 a;
+    __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float2*>(p); }
+    __device__ __forceinline__ void load_cs(const float* p) { a = __ldcs(reinterpret_cast<const float2*>(p)); }
+    __device__ __forceinline__ void zero() { a = make_float2(0.f, 0.f); }
+    __device__ __forceinline__ void get(float* f) const { f[0] = a.x; f[1] = a.y; }
+    __device__ __forceinline__ void set(const float* f) { a = make_float2(f[0], f[1]); }
+    __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float2*>(p) = a; }
+};
 template <typename T>
 struct Vec<T, 1> {
     T a;
