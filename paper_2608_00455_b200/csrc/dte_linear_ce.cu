@@ -56,7 +56,8 @@ struct CeParams {
     uint32_t m, n, k;            // extents; the one that counts tokens is replaced by *tokens
     const uint32_t* tokens;      // tokens that count
     uint32_t tile_n, splits;
-    uint32_t x_blocks, prob_blocks;   // blocks of 64 columns in a row of the blocked matrices
+    uint32_t prob_blocks;        // blocks of 64 columns in a row of the blocked f p
+    bool w_chunks;               // kDx: W is mapped as chunks of 64 columns (hidden a multiple of 64)
     uint32_t w_row;              // first row of W of this piece
     uint64_t* flags;
     // kLse, kProb
@@ -364,19 +365,21 @@ __global__ void __launch_bounds__(kCeThreads, 1)
                 const uint32_t bar = CTAS == 2 ? cluster_map(full(stage), 0) : full(stage);
                 if (leader) mbar_expect_tx(full(stage), CTAS * (kStageBytesA + part_n * kTileK * 2));
                 const int k0 = (int)(kb * kTileK);
-                // A: two blocks of a blocked matrix.  Along the rows (K is its columns): 64 rows each; along the columns: 64
-                // columns each.
-                const uint32_t mb = m0 / kBlock, blocks = KIND == kLse || KIND == kProb ? p.x_blocks : p.prob_blocks;
-#pragma unroll
-                for (uint32_t i = 0; i < 2; ++i)
-                    tma_load_2d<CTAS>(a + i * (kStageBytesA / 2), &map_a, 0,
-                                      (int)((kAmn ? kb * blocks + mb + i : (mb + i) * blocks + kb) * kBlock), bar);
+                // One load per operand and stage: with two per operand the loads, not the tensor cores, set the pace of the
+                // products along columns (kDw: 74 % of the tensor cores' cycles).  A: blocks of a blocked matrix, two
+                // rows of blocks along K, or two neighbours in one row of blocks.
+                const int mb = (int)(m0 / kBlock);
+                if (kAmn) tma_load_3d<CTAS>(a, &map_a, 0, (int)m0, (int)kb, bar);
+                else tma_load_3d<CTAS>(a, &map_a, 0, k0, mb, bar);
                 if (KIND == kDw) {
-                    for (uint32_t j = 0; j < part_n; j += kBlock)
-                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, 0, (int)((kb * p.x_blocks + (n0 + j) / kBlock) * kBlock), bar);
+                    tma_load_3d<CTAS>(b, &map_b, 0, (int)n0, (int)kb, bar);
                 } else if (KIND == kDx) {
-                    for (uint32_t j = 0; j < part_n; j += 64)
-                        tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, (int)(n0 + j), k0 + (int)p.w_row, bar);
+                    if (p.w_chunks) {
+                        tma_load_3d<CTAS>(b, &map_b, 0, k0 + (int)p.w_row, (int)(n0 / kBlock), bar);
+                    } else {
+                        for (uint32_t j = 0; j < part_n; j += 64)
+                            tma_load_2d<CTAS>(b + j * kTileK * 2, &map_b, (int)(n0 + j), k0 + (int)p.w_row, bar);
+                    }
                 } else {
                     tma_load_2d<CTAS>(b, &map_b, k0, (int)(n0 + p.w_row), bar);
                 }
@@ -944,9 +947,28 @@ static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint
     return DTE_OK;
 }
 
-// a blocked matrix of rows x blocks blocks of 64 columns
-static dte_status encode_blocked(CUtensorMap* map, const void* base, uint64_t rows, uint64_t blocks) {
-    return encode(map, base, rows * blocks, kBlock, kBlock, kBlock);
+static dte_status encode_3d(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+                            const cuuint32_t (&box)[3]) {
+    EncodeTiled f;
+    dte_status s = encoder(&f);
+    if (s != DTE_OK) return s;
+    const cuuint32_t unit[3] = {1, 1, 1};
+    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, unit,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return op_fail(DTE_ERR_CUDA, "cuTensorMapEncodeTiled refused a matrix");
+    return DTE_OK;
+}
+
+// A blocked matrix of rows x blocks blocks of 64 columns, as (column in the block, block and row in it, row of blocks); boxes of
+// `along` rows within a row of blocks and `down` rows of blocks.
+static dte_status encode_blocked(CUtensorMap* map, const void* base, uint64_t rows, uint64_t blocks, uint32_t along, uint32_t down) {
+    return encode_3d(map, base, {kBlock, blocks * kBlock, rows / kBlock}, {kBlock * 2, blocks * kBlock * kBlock * 2}, {kBlock, along, down});
+}
+
+// rows x cols, cols a multiple of 64, as (column in the chunk, row, chunk of 64 columns); boxes of 64 rows of `chunks` chunks
+static dte_status encode_chunks(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t chunks) {
+    return encode_3d(map, base, {kBlock, rows, cols / kBlock}, {ld * 2, kBlock * 2}, {kBlock, kTileK, chunks});
 }
 
 template <int KIND, int CTAS>
@@ -1109,9 +1131,8 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     p.stats = reinterpret_cast<float2*>(ws + l.stats);
     p.stats_ld = sh.padded;
     p.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
-    p.x_blocks = (uint32_t)((H + kBlock - 1) / kBlock);
     CUtensorMap ma, mb;
-    if ((s = encode_blocked(&ma, ws + l.rows, sh.padded, p.x_blocks)) != DTE_OK) return s;
+    if ((s = encode_blocked(&ma, ws + l.rows, sh.padded, (H + kBlock - 1) / kBlock, kBlock, kTileM / kBlock)) != DTE_OK) return s;
     if ((s = encode(&mb, weight->data, V, H, weight->ld, tn / sh.ctas)) != DTE_OK) return s;
     if ((s = launch_ce<kLse>(sh.ctas, ma, mb, p, n, device, st)) != DTE_OK) return s;
     CombineParams c = {};
@@ -1217,7 +1238,6 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     p.prob = reinterpret_cast<__nv_bfloat16*>(ws + l.prob);
     p.prob_blocks = (uint32_t)(sh.piece / kBlock);
-    p.x_blocks = (uint32_t)((H + kBlock - 1) / kBlock);
     p.dx_sum = reinterpret_cast<float*>(ws + l.dx_sum);
     p.dx_split = sh.padded * H;
     if (dweight) {
@@ -1229,12 +1249,18 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.accumulate = accumulate != 0;
     p.first = sorted_sum_first(ws + l.sums);
     p.target_sum = target_sum;
-    CUtensorMap rows, prob, w_k, w_n;
-    const uint32_t bn = kMaxTileN;
-    if ((s = encode_blocked(&rows, ws + l.rows, sh.padded, p.x_blocks)) != DTE_OK) return s;
-    if ((s = encode_blocked(&prob, ws + l.prob, sh.padded, p.prob_blocks)) != DTE_OK) return s;
-    if ((s = encode(&w_k, weight->data, V, H, weight->ld, bn / sh.ctas)) != DTE_OK) return s;
-    if ((s = encode(&w_n, weight->data, V, H, weight->ld, kTileK)) != DTE_OK) return s;
+    CUtensorMap rows_k, rows_n, prob_k, prob_m, w_k, w_n;
+    const uint32_t bn = kMaxTileN, part = bn / sh.ctas, down = kTileM / kBlock;
+    const uint64_t x_blocks = (H + kBlock - 1) / kBlock;
+    p.w_chunks = H % kBlock == 0;
+    if ((s = encode_blocked(&rows_k, ws + l.rows, sh.padded, x_blocks, kBlock, down)) != DTE_OK) return s;
+    if ((s = encode_blocked(&rows_n, ws + l.rows, sh.padded, x_blocks, part, 1)) != DTE_OK) return s;
+    if ((s = encode_blocked(&prob_k, ws + l.prob, sh.padded, p.prob_blocks, kBlock, down)) != DTE_OK) return s;
+    if ((s = encode_blocked(&prob_m, ws + l.prob, sh.padded, p.prob_blocks, kTileM, 1)) != DTE_OK) return s;
+    if ((s = encode(&w_k, weight->data, V, H, weight->ld, part)) != DTE_OK) return s;
+    if ((s = p.w_chunks ? encode_chunks(&w_n, weight->data, V, H, weight->ld, part / kBlock)
+                        : encode(&w_n, weight->data, V, H, weight->ld, kTileK)) != DTE_OK)
+        return s;
     for (uint64_t piece = 0; piece < sh.pieces; ++piece) {
         const uint64_t v0 = piece * sh.piece, vc = V - v0 < sh.piece ? V - v0 : sh.piece;
         p.w_row = (uint32_t)v0;
@@ -1242,19 +1268,19 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         p.splits = 1;
         p.n = (uint32_t)vc;
         p.k = (uint32_t)H;
-        if ((s = launch_ce<kProb>(sh.ctas, rows, w_k, p, n, device, st)) != DTE_OK) return s;
+        if ((s = launch_ce<kProb>(sh.ctas, rows_k, w_k, p, n, device, st)) != DTE_OK) return s;
         if (dx) {
             p.n = (uint32_t)H;
             p.k = (uint32_t)vc;
             p.splits = sh.splits;
             p.add = piece > 0;
-            if ((s = launch_ce<kDx>(sh.ctas, prob, w_n, p, n, device, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDx>(sh.ctas, prob_k, w_n, p, n, device, st)) != DTE_OK) return s;
         }
         if (dweight) {
             p.m = (uint32_t)vc;
             p.n = (uint32_t)H;
             p.splits = 1;
-            if ((s = launch_ce<kDw>(sh.ctas, prob, rows, p, vc, device, st)) != DTE_OK) return s;
+            if ((s = launch_ce<kDw>(sh.ctas, prob_m, rows_n, p, vc, device, st)) != DTE_OK) return s;
         }
     }
     if (dx) {
