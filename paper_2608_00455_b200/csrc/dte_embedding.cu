@@ -25,7 +25,8 @@ struct LookupParams {
 constexpr int kLookupThreads = 128;
 constexpr int kLookupUnroll = 4;       // accesses in flight per lane
 
-// One warp takes one token's stretch of 32 * V * kLookupUnroll columns.
+// One warp takes one token's stretch of 32 * V * kLookupUnroll columns: small CTAs in the order of the output, which
+// the memory takes fastest.  16384 x 4096 bf16: 35 us, 7.6 TB/s of rows in and out (repeated rows come from L2).
 template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupParams p) {
     const uint64_t w = (uint64_t)blockIdx.x * (kLookupThreads / 32) + threadIdx.x / 32;
@@ -380,8 +381,8 @@ struct SumLayout {
     uint64_t first, key, pos, counters, partial, total;
 };
 
-// Entries of a block: the most, unless that leaves the GPU short of warps (6007 x 2048 fp32 of which a quarter is in the shard:
-// 16 entries 62 us, 4 entries 58 us; 16384 x 4096: 16 entries 394 us, 8 entries 405 us).
+// Entries of a block: the most, unless that leaves the GPU short of warps.  921 entries x 2048 (the head's gradient): blocks
+// of 16 18.5 us, of 4 10.8 us; 16384 x 4096: blocks of 16 393 us with the zeros, of 8 405 us.
 static uint32_t sum_block(uint64_t n, uint64_t chunks) {
     uint32_t block = kMaxSumBlock;
     while (block > kMinSumBlock && n / block * chunks < kGroupCtas * 32) block /= 2;
