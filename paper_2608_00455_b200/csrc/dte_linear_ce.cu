@@ -942,7 +942,7 @@ static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint
     dte_status s = encoder(&f);
     if (s != DTE_OK) return s;
     const cuuint64_t dims[2] = {cols, rows};
-    const cuuint64_t strides[1] = {ld * 2};
+    const cuuint64_t strides[1] = {(rows > 1 ? ld : align_up(cols, 8)) * 2};     // one row: its stride means nothing
     const cuuint32_t box[2] = {kTileK, box_rows};
     const cuuint32_t unit[2] = {1, 1};
     const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, unit,
@@ -973,7 +973,7 @@ static dte_status encode_blocked(CUtensorMap* map, const void* base, uint64_t ro
 
 // rows x cols, cols a multiple of 64, as (column in the chunk, row, chunk of 64 columns); boxes of 64 rows of `chunks` chunks
 static dte_status encode_chunks(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t chunks) {
-    return encode_3d(map, base, {kBlock, rows, cols / kBlock}, {ld * 2, kBlock * 2}, {kBlock, kTileK, chunks});
+    return encode_3d(map, base, {kBlock, rows, cols / kBlock}, {(rows > 1 ? ld : cols) * 2, kBlock * 2}, {kBlock, kTileK, chunks});
 }
 
 template <int KIND, int CTAS>

@@ -108,7 +108,7 @@ def _vector(t: Optional[torch.Tensor], name: str, device: int, count: int, dtype
     """Address of a contiguous vector of `count` values, or None."""
     if t is None:
         return None
-    if t.__class__ is torch.Tensor and t.dtype in dtypes and t.numel() == count and t.get_device() == device and t.is_contiguous():
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.numel() == count and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
     _same_device(t, name, device)
     if t.dtype not in dtypes:

@@ -596,6 +596,73 @@ def test_head_same_bits_every_time():
             assert torch.equal(a, b)
 
 
+# ---- offsets beyond 32 bits ------------------------------------------------------------------------------------
+
+def test_lookup_and_its_gradient_in_a_table_of_more_than_2_to_the_32_bytes_and_elements():
+    rows, hidden, n = 140000, 32768, 64                       # 4.6e9 elements of bf16
+    table = torch.zeros(rows, hidden, dtype=BF16, device=DEV)
+    ids = torch.arange(n, device=DEV) + rows - n
+    ids[0] = 3
+    table[ids] = normal(90, (n, hidden), 1.0, BF16)
+    out = torch.empty(n, hidden, dtype=BF16, device=DEV)
+    dte.dte_embedding_forward(table, ids, out)
+    assert torch.equal(out, table[ids])
+    dout = normal(91, (n, hidden), 1.0, BF16)
+    table.fill_(1.0)
+    dte.dte_embedding_backward(dout, ids, table, workspace(dte.dte_embedding_backward_workspace_bytes(n, hidden)))
+    assert torch.equal(table[ids], dout)
+    assert int(torch.count_nonzero(table[4:rows - n])) == 0 and int(torch.count_nonzero(table[:3])) == 0
+
+
+def test_norm_of_more_than_2_to_the_32_elements():
+    rows, cols = 1100000, 4096
+    x = torch.empty(rows, cols, dtype=BF16, device=DEV)
+    tail = normal(92, (300, cols), 1.0, BF16, 0.5)
+    x.fill_(0.25)
+    x[-300:] = tail
+    out, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    dte.dte_norm_forward(x, None, None, out, mean, rstd, 1e-5)
+    small, m2, r2 = torch.empty_like(tail), torch.empty(300, device=DEV), torch.empty(300, device=DEV)
+    dte.dte_norm_forward(tail, None, None, small, m2, r2, 1e-5)
+    assert torch.equal(out[-300:], small) and torch.equal(rstd[-300:], r2) and bool((out[:-300] == 0).all())
+    dw, dw2 = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    dx2 = torch.empty_like(tail)
+    ws = workspace(dte.dte_norm_backward_workspace_bytes(rows, cols))
+    out[:-300] = 0                                            # as dout: nothing but the last rows counts
+    dx = torch.empty_like(x)
+    dte.dte_norm_backward(out, x, None, mean, rstd, dx, dw, None, ws)
+    dte.dte_norm_backward(small, tail, None, m2, r2, dx2, dw2, None, ws)
+    assert torch.equal(dx[-300:], dx2) and bool((dx[:-300] == 0).all())
+    assert_within(dw, dw2.to(F64), 2 * 340 * E * (small.to(F64).abs() * (tail.to(F64).abs() + 1) * 2).sum(0), "dweight")
+
+
+def test_head_with_more_than_2_to_the_31_weights():
+    tokens, vocab, hidden = 40, 560000, 4096                  # 2.3e9 elements
+    w = torch.zeros(vocab, hidden, dtype=BF16, device=DEV)
+    x = normal(93, (tokens, hidden), 1.0, BF16)
+    hot = torch.arange(tokens, device=DEV) + vocab - tokens
+    w[hot] = normal(94, (tokens, hidden), 0.03, BF16)
+    lse, tl, loss = run_forward(x, w, hot)
+    z = x.to(F64) @ w[hot].to(F64).T
+    want = torch.logsumexp(torch.cat([z, torch.full((tokens, 1), math.log(vocab - tokens), dtype=F64, device=DEV)], 1), 1)
+    dz = (hidden / 16 + 16) * 2.0 ** -23 * (x.to(F64).abs() @ w[hot].to(F64).abs().T)
+    assert_within(lse, want, dz.amax(1) + 2.0 ** -20 + 64 * E * want.abs(), "lse")
+    dloss = normal(95, (tokens,))
+    dx, dw = run_backward(x, w, hot, lse, dloss)
+    p = torch.exp(z - lse.to(F64)[:, None]) * dloss.to(F64)[:, None]
+    g = p - torch.diag(dloss.to(F64))
+    wdx, wdw = g @ w[hot].to(F64), g.T @ x.to(F64)
+    rel = 2.0 ** -8 + 2 * dz + 2.0 ** -18
+    mx = (p.abs() * rel) @ w[hot].to(F64).abs() + (tokens + 100) * 2.0 ** -23 * (g.abs() @ w[hot].to(F64).abs())
+    mw = (p.abs() * rel).T @ x.to(F64).abs() + (tokens + 100) * 2.0 ** -23 * (g.abs().T @ x.to(F64).abs())
+    assert_within(dx, wdx, mx + U[BF16] * wdx.abs() * 1.01, "dx")
+    assert_within(dw[hot], wdw, mw + U[BF16] * wdw.abs() * 1.01, "dweight")
+    # a row of zeros elsewhere: the sum over tokens of dloss / (sum of exponentials) x
+    far = (dloss.to(F64) * torch.exp(-lse.to(F64))) @ x.to(F64)
+    size = (dloss.to(F64).abs() * torch.exp(-lse.to(F64))) @ x.to(F64).abs()
+    assert_within(dw[12345], far, size * 2.0 ** -7 + U[BF16] * far.abs() * 1.01, "dweight of a row far below 2^31")
+
+
 # ---- streams, graphs and refusals ------------------------------------------------------------------------------
 
 def test_operators_run_on_a_side_stream_and_inside_a_graph():
