@@ -35,6 +35,10 @@ constexpr uint32_t kEpilogueWarps = 8;           // two for each quarter of tens
 constexpr uint32_t kCeThreads = 64 + 32 * kEpilogueWarps;   // TMA warp, MMA warp, epilogue
 constexpr uint32_t kStageBytesA = kTileM * kTileK * 2;
 constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one is filled while the other is drained
+// Up to this many tokens half of a tile's rows are free, and so f p is kept as two bf16 numbers, the rounded value and the
+// rest, as if every token were there twice: the gradients of a few tokens, whose roundings do not average out, come out
+// 2^-16 exact for nothing.
+constexpr uint32_t kSplitTokens = 64;
 constexpr uint64_t kPadRows = 256;               // token rows are padded to this, with zero rows
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -72,6 +76,7 @@ struct CeParams {
     float2* stats;               // kLse: (maximum, sum) per tile of columns and token
     uint64_t stats_ld;
     float* target_logit;         // kLse: the target's logit as the tensor cores added it up
+    bool split;                  // kProb: the upper kSplitTokens rows hold what rounding to bf16 took from the lower ones
     const float* f;              // kProb: logit_scale * dloss per token
     const float* neg_lse2;       //        -lse * log2(e)
     __nv_bfloat16* prob;         //        blocked, prob_blocks blocks wide
@@ -186,6 +191,10 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
                     if (j >= (int)left) v[j] = 0.f;
+            }
+            if (p.split && row >= kSplitTokens) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
             }
 #pragma unroll
             for (int j = 0; j < 32; j += 16) {
@@ -474,7 +483,8 @@ struct RowsParams {
     uint32_t targets_dtype, n;
     int64_t vocab_start, vocab;
     uint32_t vocab_rows;
-    uint32_t* count;         // tokens that count
+    uint32_t* count;         // [0] tokens that count, [1] rows of the backward products
+    bool split;              // [1] is twice kSplitTokens, if any token counts
     int32_t* source;         // [i] = token of compact row i
     int32_t* target;         // [i] = its target as a row of this shard, or -1
     int32_t* place;          // [token] = compact row or -1 (NULL: not wanted)
@@ -541,7 +551,7 @@ __global__ void __launch_bounds__(kRowsThreads) ce_rows_kernel(const RowsParams 
         base += all;
         __syncthreads();
     }
-    if (threadIdx.x == 0) *p.count = base;
+    if (threadIdx.x == 0) p.count[0] = p.count[1] = base;
     if (bad && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
 }
 
@@ -582,7 +592,8 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
     __shared__ int32_t s_mine[2];          // token and target of this CTA's row
     wait_for_earlier();
     let_next_start();
-    const uint32_t i = blockIdx.x;
+    const bool split = p.rows_of.split;               // only with few tokens
+    const uint32_t i = blockIdx.x, mine_at = split && i < 2 * kSplitTokens ? i % kSplitTokens : i;
     uint32_t count, src;
     int32_t target;
     if (p.few) {
@@ -625,7 +636,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
             const bool counts = id[j] >= 0;
             const uint64_t row = (uint64_t)id[j] - (uint64_t)q.vocab_start;
             const int32_t to = counts && row < q.vocab_rows ? (int32_t)row : -1;
-            if (counts && at == i) {
+            if (counts && at == mine_at) {
                 s_mine[0] = (int32_t)t;
                 s_mine[1] = to;
             }
@@ -643,7 +654,10 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
             at += counts;
         }
         if (writer) {
-            if (threadIdx.x == 0) *q.count = count;
+            if (threadIdx.x == 0) {
+                q.count[0] = count;
+                q.count[1] = split && count ? 2 * kSplitTokens : count;
+            }
             if (bad && q.flags) atomicOr((unsigned long long*)q.flags, (unsigned long long)DTE_DEV_BOUNDS);
         }
         __syncthreads();
@@ -656,7 +670,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
     }
     const uint32_t padded = (uint32_t)((count + kPadRows - 1) / kPadRows * kPadRows);
     if (i >= padded) return;
-    const bool live = i < count;
+    const bool live = mine_at < count;
     if (!p.exact_logit) target = -1;
     const __nv_bfloat16* in = p.x + (uint64_t)src * p.x_ld;
     float dot = 0.f;
@@ -785,6 +799,7 @@ struct DxParams {
     const float* sums;
     uint64_t split_elems;
     uint32_t splits, hidden;
+    bool split;              // kProb's: two rows per token
     const __nv_bfloat16* weight;
     uint64_t weight_ld;
     __nv_bfloat16* dx;
@@ -808,6 +823,12 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const DxParams p) {
                 r.get(v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] += v[j];
+                if (p.split) {
+                    r.load(p.sums + s * p.split_elems + (uint64_t)(i + kSplitTokens) * p.hidden + c);
+                    r.get(v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) o[j] += v[j];
+                }
             }
             if (target >= 0) {
                 Raw8<__nv_bfloat16> r;
@@ -887,7 +908,7 @@ static uint32_t lse_tile_n(uint64_t tokens, uint64_t vocab) {
 
 static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded, uint64_t& at) {
     CeLayout l = {};
-    l.count = take(at, 4);
+    l.count = take(at, 8);
     l.source = take(at, padded * 4);
     l.target = take(at, padded * 4);
     l.place = take(at, padded * 4);
@@ -1051,6 +1072,7 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     r.count = reinterpret_cast<uint32_t*>(ws + l.count);
     r.source = reinterpret_cast<int32_t*>(ws + l.source);
     r.target = reinterpret_cast<int32_t*>(ws + l.target);
+    r.split = dloss && targets->count <= kSplitTokens;
     r.place = dloss ? reinterpret_cast<int32_t*>(ws + l.place) : nullptr;
     r.lse = lse;
     r.target_logit = target_logit;
@@ -1234,7 +1256,8 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         if ((s = launch_sorted_sum(q, vec8_ok(x) ? 8 : vec2_ok(x) ? 2 : 1, ws + l.sums, true, device, st)) != DTE_OK) return s;
     }
     CeParams p = {};
-    p.tokens = count;
+    p.tokens = count + 1;
+    p.split = n <= kSplitTokens;
     p.flags = flags;
     p.scale = (float)logit_scale;
     p.k2 = (float)(logit_scale * 1.4426950408889634);
@@ -1296,6 +1319,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         d.sums = p.dx_sum;
         d.split_elems = p.dx_split;
         d.splits = sh.splits;
+        d.split = p.split;
         d.hidden = (uint32_t)H;
         d.weight = static_cast<const __nv_bfloat16*>(weight->data);
         d.weight_ld = weight->ld;

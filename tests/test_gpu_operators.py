@@ -347,13 +347,13 @@ class Head:
         for v in (lse, tl, loss):
             assert bool((v[~self.keep] == 0).all())
 
-    def gradients(self, dloss, lse):
-        """(dx, bound, dw, bound) for fp32 lse as passed."""
+    def gradients(self, dloss, lse, kept=2.0 ** -8):
+        """(dx, bound, dw, bound) for fp32 lse as passed; kept: how closely f p is kept (bf16: 8 significant bits)."""
         f = torch.where(self.keep, dloss.to(F64), 0.0) * self.scale
         p = torch.exp(self.z - lse.to(F64)[:, None]) * self.keep[:, None]
         g = f[:, None] * p
-        # p as bf16 (8 significant bits: 2^-8) from exponents that are off by dz and by fp32 roundings of their size
-        rel = 2.0 ** -8 + 1.1 * (self.dz + 8 * E * (self.z.abs() + lse.to(F64).abs()[:, None]) + 2.0 ** -20)
+        # p as it is kept, from exponents that are off by dz and by fp32 roundings of their size
+        rel = kept + 1.1 * (self.dz + 8 * E * (self.z.abs() + lse.to(F64).abs()[:, None]) + 2.0 ** -20)
         dg = g.abs() * rel
         hot = torch.zeros_like(g)
         hot[torch.arange(len(f), device=DEV), self.col] = f * self.here
@@ -440,6 +440,23 @@ def test_head_many_rounds_of_tiles(tokens, vocab, hidden):
     dx, dw = run_backward(x, w, t, lse, dloss)
     assert_within(dx, wx, bx + U[BF16] * wx.abs() * 1.01, "dx")
     assert_within(dw, ww, bw + U[BF16] * ww.abs() * 1.01, "dweight")
+
+
+@pytest.mark.parametrize("tokens,vocab,hidden,ignored", [(1, 700, 64, 0.0), (5, 3000, 200, 0.0), (64, 1000, 264, 0.0), (64, 5000, 128, 0.5),
+                                                         (33, 9000, 1032, 0.2)])
+def test_head_gradients_of_few_tokens_are_closer_than_bf16(tokens, vocab, hidden, ignored):
+    # f p as two bf16 numbers: 2^-17 of it is lost at most; an fp32 weight gradient shows it
+    x, w, t = head_case(tokens, vocab, hidden, 100, ignored)
+    for start, total in ((0, vocab), (vocab, 2 * vocab)):            # with the targets in the shard, and with none of them
+        ref = Head(x, w, t, start=start)
+        lse, dloss = ref.lse.to(F32), normal(101, (tokens,))
+        wx, bx, ww, bw = ref.gradients(dloss, lse, kept=2.0 ** -16)
+        for small in (False, True):
+            dw = torch.full((vocab, hidden), float("nan"), device=DEV)
+            dx, dw = run_backward(x, w, t, lse, dloss, dw=dw, start=start, total=total, small=small)
+            assert_within(dw, ww, bw + 4 * E * ww.abs(), "dweight")
+            assert_within(dx, wx, bx + U[BF16] * wx.abs() * 1.01, "dx")
+            assert bool((dx[~ref.keep] == 0).all())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
