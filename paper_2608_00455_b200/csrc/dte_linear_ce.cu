@@ -1,19 +1,22 @@
 // Softmax cross entropy of a linear head over a large vocabulary, without storing the logits, and its
 // gradient.  z = s x W^T;  lse = log sum_v exp z_v;  with p = exp(z - lse), f = s * dloss:
-//   dx = f (p W - W[target]),   dW = (f p)^T x - (rows of f x, added up by target).
+//   dx = (f p') W + c W[target],   dW = (f p')^T x + (rows of c x, added up by target),
+// where p' is p with 0 in the target's column and c = f (p_target - 1) = f expm1(z_target - lse).
 //
 // Bound by the tensor cores (2 tokens V hidden operations forward, 6 backward: the logits are made
 // again rather than kept) for more than a few hundred tokens, by reading W for a few.  One persistent
 // tcgen05 kernel serves all four products; what differs is how its operands lie in memory and what its
 // epilogue does with a finished tile of accumulators:
 //   kLse   logits tile -> per row the maximum and the sum of exponentials of its columns (registers only)
-//   kProb  logits tile -> f p as bf16, for one piece of the vocabulary
-//   kDx    piece of f p times W: adds to fp32 sums over pieces
-//   kDw    (f p)^T x: complete for the piece's vocabulary rows, less the target term, rounded and written
+//   kProb  logits tile -> f p' as bf16, for one piece of the vocabulary
+//   kDx    piece of f p' times W: adds to fp32 sums over pieces
+//   kDw    (f p')^T x: complete for the piece's vocabulary rows, the target term added, rounded and written
 // Tokens without a target are dropped before the first product: the rows that count are copied together,
-// so prompts cost nothing and what their rows hold (NaN included) reaches no sum.  The target term
-// stays out of the bf16 operand f p: it is the largest entry of its row by far, and its rounding would
-// be most of the gradient's error; both gradients take it in fp32 instead.
+// so prompts cost nothing and what their rows hold (NaN included) reaches no sum.  The target's column stays out
+// of the bf16 operand and has its whole coefficient c in fp32.  For p_target near 0, c is the largest entry of
+// its row by far and its rounding would be most of the gradient's error; for p_target near 1, c is what is left of two
+// nearly equal numbers, so neither of them may be rounded first.  z_target is an fp32 sum for the same
+// reason; an error of c beyond fp32's relative one comes from the lse that is passed in: 2^-24 |lse| f at most.
 //
 // Measured: logits 8192 x 151936 x 4096 7.6 to 7.9 ms = 1.28 to 1.34 PFLOP/s in a loop of seconds at the 1000 W limit (a
 // bf16 library product of that shape, which stores its logits: 7.4 ms); the backward pass 24.1 ms = 1.27 PFLOP/s over its
@@ -35,7 +38,7 @@ constexpr uint32_t kEpilogueWarps = 8;           // two for each quarter of tens
 constexpr uint32_t kCeThreads = 64 + 32 * kEpilogueWarps;   // TMA warp, MMA warp, epilogue
 constexpr uint32_t kStageBytesA = kTileM * kTileK * 2;
 constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one is filled while the other is drained
-// Up to this many tokens half of a tile's rows are free, and so f p is kept as two bf16 numbers, the rounded value and the
+// Up to this many tokens half of a tile's rows are free, and so f p' is kept as two bf16 numbers, the rounded value and the
 // rest, as if every token were there twice: the gradients of a few tokens, whose roundings do not average out, come out
 // 2^-16 exact for nothing.
 constexpr uint32_t kSplitTokens = 64;
@@ -77,7 +80,7 @@ struct CeParams {
     uint64_t stats_ld;
     float* target_logit;         // kLse: the target's logit as the tensor cores added it up
     bool split;                  // kProb: the upper kSplitTokens rows hold what rounding to bf16 took from the lower ones
-    const float* f;              // kProb: logit_scale * dloss per token
+    const float* f;              // kProb: logit_scale * dloss per token (the target's column gets 0, see `target`)
     const float* neg_lse2;       //        -lse * log2(e)
     __nv_bfloat16* prob;         //        blocked, prob_blocks blocks wide
     // kDx
@@ -181,12 +184,19 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
         }
     } else if (KIND == kProb) {
         const float f = p.f[row], nl = p.neg_lse2[row];     // zero for padding rows
+        // the target's column, counted from the tile's first one; of no tile's columns where it is another piece's
+        const int32_t tcol = row < tokens ? p.target[p.split ? row % kSplitTokens : row] - (int32_t)(p.w_row + n0) : -1;
         for (uint32_t c = c0; c < c1; c += 32) {
             float v[32];
             load_tile(tmem + c, v);
             const uint32_t left = p.n > n0 + c ? p.n - (n0 + c) : 0;
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = f * exp2_fast(fmaf(v[j], p.k2, nl));
+            const uint32_t at = (uint32_t)(tcol - (int32_t)c);
+            if (__any_sync(0xFFFFFFFFu, at < 32)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = at == (uint32_t)j ? 0.f : v[j];
+            }
             if (left < 32) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
@@ -263,7 +273,7 @@ __device__ __forceinline__ void ce_epilogue(const CeParams& p, uint32_t tmem, ui
             const uint32_t left = (p.n - (n0 + c)) / 8;      // groups of 8 columns
             float o[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = (empty ? 0.f : v[j]) - __uint_as_float(w[j / 8][j % 8]);
+            for (int j = 0; j < 32; ++j) o[j] = (empty ? 0.f : v[j]) + __uint_as_float(w[j / 8][j % 8]);
             if (p.dweight_bf16) {
                 __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.dweight) + off;
                 if (p.accumulate) add_old(d, left, o);
@@ -566,13 +576,15 @@ struct GatherRowsParams {
     bool vec;
     __nv_bfloat16* rows;     // blocked: padded tokens x blocks of 64
     uint32_t blocks;
-    // forward: the target's logit, added up in fp32 here and, later, by the tensor cores (compact order)
+    // the target's logit is added up in fp32 here
     int32_t* target;
     const __nv_bfloat16* weight;
     uint64_t weight_ld;
-    float* exact_logit;
-    float* target_logit;     // cleared
+    // forward (compact order)
+    float* exact_logit;      // the target's logit
+    float* target_logit;     // the same as the tensor cores add it up later; cleared
     // backward
+    float* coef;             // [token] = f (p_target - 1), of tokens whose target is in this shard
     const float* dloss;
     const float* lse;
     float scale;
@@ -671,7 +683,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
     const uint32_t padded = (uint32_t)((count + kPadRows - 1) / kPadRows * kPadRows);
     if (i >= padded) return;
     const bool live = mine_at < count;
-    if (!p.exact_logit) target = -1;
+    if (mine_at != i) target = -1;       // the second row of a token that is there twice
     const __nv_bfloat16* in = p.x + (uint64_t)src * p.x_ld;
     float dot = 0.f;
     for (uint32_t c = threadIdx.x * 8; c < p.blocks * kBlock; c += kGatherThreads * 8) {
@@ -701,19 +713,26 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
             for (int j = 0; j < 8; ++j) dot = fmaf(f[j], g[j], dot);
         }
     }
-    if (p.exact_logit) {
+    if (target >= 0) {                   // the same for the whole CTA
         dot = warp_sum(dot);
         if ((threadIdx.x & 31) == 0) s_part[threadIdx.x / 32] = dot;
         __syncthreads();
-        if (threadIdx.x == 0) {
+    }
+    if (threadIdx.x) return;
+    float logit = 0.f;
+    if (target >= 0) {
 #pragma unroll
-            for (int w = 1; w < kGatherThreads / 32; ++w) dot += s_part[w];
-            p.exact_logit[i] = target >= 0 ? dot * p.scale : 0.f;
-            p.target_logit[i] = 0.f;
-        }
-    } else if (threadIdx.x == 0) {
-        p.f[i] = live ? p.scale * p.dloss[src] : 0.f;
-        p.neg_lse2[i] = live ? -p.lse[src] * kLog2e : 0.f;
+        for (int w = 1; w < kGatherThreads / 32; ++w) dot += s_part[w];
+        logit = dot * p.scale;
+    }
+    if (p.exact_logit) {
+        p.exact_logit[i] = logit;
+        p.target_logit[i] = 0.f;
+    } else {
+        const float f = live ? p.scale * p.dloss[src] : 0.f, lse = live ? p.lse[src] : 0.f;
+        p.f[i] = f;
+        p.neg_lse2[i] = -lse * kLog2e;
+        if (target >= 0) p.coef[src] = f * expm1f(logit - lse);
     }
 }
 
@@ -795,7 +814,7 @@ __global__ void __launch_bounds__(kCombineThreads) ce_combine_kernel(const Combi
 struct DxParams {
     const int32_t* place;
     const int32_t* target;
-    const float* f;
+    const float* coef;       // [token], see GatherRowsParams
     const float* sums;
     uint64_t split_elems;
     uint32_t splits, hidden;
@@ -806,13 +825,13 @@ struct DxParams {
     uint64_t dx_ld;
 };
 
-// dx of every token: its splits' sums less the target's row; zero for ignored tokens.
+// dx of every token: its splits' sums and the target's row; zero for ignored tokens.
 __global__ void __launch_bounds__(256) ce_dx_kernel(const DxParams p) {
     wait_for_earlier();
     const int32_t i = p.place[blockIdx.x];
     __nv_bfloat16* out = p.dx + (uint64_t)blockIdx.x * p.dx_ld;
     const int32_t target = i >= 0 ? p.target[i] : -1;
-    const float f = i >= 0 ? p.f[i] : 0.f;
+    const float coef = target >= 0 ? p.coef[blockIdx.x] : 0.f;
     for (uint32_t c = threadIdx.x * 8; c < p.hidden; c += 256 * 8) {
         float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (i >= 0) {
@@ -836,7 +855,7 @@ __global__ void __launch_bounds__(256) ce_dx_kernel(const DxParams p) {
                 r.load(p.weight + (uint64_t)target * p.weight_ld + c);
                 r.get(w);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = fmaf(-f, w[j], o[j]);
+                for (int j = 0; j < 8; ++j) o[j] = fmaf(coef, w[j], o[j]);
             }
         }
         Raw8<__nv_bfloat16> r;
@@ -880,7 +899,7 @@ static CeShape ce_shape(uint64_t tokens, uint64_t vocab, uint64_t hidden, uint64
 
 // Offsets of everything in a workspace.
 struct CeLayout {
-    uint64_t count, source, target, place, rows, scalar0, scalar1, stats, prob, dx_sum, target_sum, sums, total;
+    uint64_t count, source, target, place, rows, scalar0, scalar1, stats, coef, prob, dx_sum, target_sum, sums, total;
 };
 
 static uint64_t take(uint64_t& at, uint64_t bytes) {
@@ -932,6 +951,7 @@ static CeLayout forward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden)
 static CeLayout backward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden, const CeShape& s) {
     uint64_t at = 0;
     CeLayout l = common_layout(tokens, hidden, s.padded, at);
+    l.coef = take(at, s.padded * 4);
     l.prob = take(at, s.padded * s.piece * 2);
     l.dx_sum = take(at, s.splits * s.padded * hidden * 4);
     l.target_sum = take(at, s.padded * hidden * 4);
@@ -1090,14 +1110,15 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
     g.rows = reinterpret_cast<__nv_bfloat16*>(ws + l.rows);
     g.blocks = (uint32_t)((x->cols + kBlock - 1) / kBlock);
     g.scale = scale;
+    g.weight = static_cast<const __nv_bfloat16*>(weight->data);
+    g.weight_ld = weight->ld;
     if (dloss) {
         g.dloss = dloss;
         g.lse = lse_in;
+        g.coef = reinterpret_cast<float*>(ws + l.coef);
         g.f = reinterpret_cast<float*>(ws + l.scalar0);
         g.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     } else {
-        g.weight = static_cast<const __nv_bfloat16*>(weight->data);
-        g.weight_ld = weight->ld;
         g.target_logit = reinterpret_cast<float*>(ws + l.scalar0);
         g.exact_logit = reinterpret_cast<float*>(ws + l.scalar1);
     }
@@ -1232,7 +1253,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
                           flags, st)) != DTE_OK)
         return s;
     const uint32_t* count = reinterpret_cast<uint32_t*>(ws + l.count);
-    const float* f = reinterpret_cast<float*>(ws + l.scalar0);
+    const float* coef = reinterpret_cast<float*>(ws + l.coef);
     const int32_t* target = reinterpret_cast<int32_t*>(ws + l.target);
     float* target_sum = reinterpret_cast<float*>(ws + l.target_sum);
     if (dweight) {
@@ -1246,9 +1267,9 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         q.src = x->data;
         q.src_dtype = DTE_BF16;
         q.src_ld = x->ld;
-        q.weight = dloss;
+        q.weight = coef;
         q.hidden = (uint32_t)H;
-        q.scale = (float)logit_scale;
+        q.scale = 1.f;                    // coef has it already
         q.out = target_sum;
         q.out_dtype = DTE_F32;
         q.out_ld = H;
@@ -1262,7 +1283,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.scale = (float)logit_scale;
     p.k2 = (float)(logit_scale * 1.4426950408889634);
     p.target = target;
-    p.f = f;
+    p.f = reinterpret_cast<float*>(ws + l.scalar0);
     p.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);
     p.prob = reinterpret_cast<__nv_bfloat16*>(ws + l.prob);
     p.prob_blocks = (uint32_t)(sh.piece / kBlock);
@@ -1315,7 +1336,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
         DxParams d = {};
         d.place = reinterpret_cast<int32_t*>(ws + l.place);
         d.target = target;
-        d.f = f;
+        d.coef = coef;
         d.sums = p.dx_sum;
         d.split_elems = p.dx_split;
         d.splits = sh.splits;

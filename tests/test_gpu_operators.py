@@ -613,6 +613,100 @@ def test_head_same_bits_every_time():
             assert torch.equal(a, b)
 
 
+# ---- gradients of tokens whose loss is near zero --------------------------------------------------------------------
+
+def confident_case(tokens, vocab, hidden, seed, ignored=0.0, total=None, start=0, scale=1.0):
+    """Tokens with losses from about 1 down to 1e-6: x is a multiple of the target's row of w.  All values lie on grids so
+    coarse (w: 2^-4, x: 2^-3) that every logit and every partial sum of one is exact in fp32 whatever the order."""
+    w = (normal(seed, (vocab, hidden), 2.2 / math.sqrt(hidden)) * 16).round() / 16
+    w = torch.where(w == 0, 1 / 16, w)                 # no empty row
+    t = randint(seed + 1, 0, total or vocab, tokens)
+    if ignored:
+        t[torch.rand(tokens, generator=gen(seed + 2), device=DEV) < ignored] = -100
+    col = (t - start).clamp(0, vocab - 1)
+    # z_t = scale * gain * |w_t|^2 between log(vocab) and log(vocab) + 14
+    want = math.log(vocab) + 14 * torch.arange(tokens, device=DEV) / max(1, tokens - 1)
+    gain = want / scale / (w[col] ** 2).sum(1)
+    x = (gain[:, None] * w[col] * 8).round() / 8
+    assert torch.equal(x.to(BF16).float(), x) and torch.equal(w.to(BF16).float(), w)
+    assert float((x.abs() @ w.abs().T).max()) < 2 ** (24 - 7)
+    return x.to(BF16), w.to(BF16), t
+
+
+def centred_gradients(ref, dloss, lse, kept=2.0 ** -8, dzt=0.0):
+    """(dx, bound, dw, bound) for fp32 lse as passed.  The target's coefficient f (p - 1) is granted fp32 roundings of its
+    own size, of the subtraction z - lse, and dzt, the error of its logit; the other columns f p as it is kept."""
+    f = torch.where(ref.keep, dloss.to(F64), 0.0) * ref.scale
+    lse = lse.to(F64)[:, None]
+    g = f[:, None] * torch.exp(ref.z - lse) * ref.keep[:, None]
+    dg = g.abs() * (kept + 1.1 * (ref.dz + 8 * E * (ref.z.abs() + lse.abs()) + 2.0 ** -20))
+    row = ref.here.nonzero()[:, 0]
+    d = (ref.z - lse)[row, ref.col[row]]
+    # f: two roundings, expm1f: 2 E, the product and the sum it goes into: 8 E; z - lse rounds to E |z - lse|
+    g[row, ref.col[row]] = f[row] * torch.expm1(d)
+    dg[row, ref.col[row]] = f[row].abs() * (8 * E * torch.expm1(d).abs() + torch.exp(d) * (2 * E * d.abs() + dzt))
+    n, v = g.shape
+    bx = dg @ ref.w.abs() + (v / 16 + 64) * 2.0 ** -23 * (g.abs() @ ref.w.abs())
+    bw = dg.T @ ref.x.abs() + (n / 16 + 64) * 2.0 ** -23 * (g.abs().T @ ref.x.abs())
+    return g @ ref.w, bx, g.T @ ref.x, bw
+
+
+@pytest.mark.parametrize("tokens,vocab,hidden,ignored", [(7, 700, 64, 0.0), (64, 2049, 512, 0.2), (65, 2049, 512, 0.0), (128, 300, 72, 0.0),
+                                                         (300, 2049, 512, 0.0), (921, 5000, 264, 0.3)])
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+def test_head_gradients_of_confident_tokens(tokens, vocab, hidden, ignored, scale):
+    for start, total in ((0, vocab), (vocab // 3, 2 * vocab)):       # the whole vocabulary; a shard without some of the targets
+        x, w, t = confident_case(tokens, vocab, hidden, 110, ignored, total, start, scale)
+        ref = Head(x, w, t, scale, start)
+        lse = ref.lse.to(F32)
+        for dloss in (torch.full((tokens,), 1.0 / 921, device=DEV), normal(113, (tokens,))):
+            kept = 2.0 ** -16 if tokens <= 64 else 2.0 ** -8
+            wx, bx, ww, bw = centred_gradients(ref, dloss, lse, kept)
+            for small in (False, True):
+                dw = torch.full((vocab, hidden), float("nan"), device=DEV)
+                dx, dw = run_backward(x, w, t, lse, dloss, scale=scale, start=start, total=total, dw=dw, small=small)
+                assert_within(dw, ww, bw + 4 * E * ww.abs(), "dweight")
+                assert_within(dx, wx, bx + U[BF16] * wx.abs() * 1.01, "dx")
+        # what is granted says something: a few per cent at most of the gradient of any token that has a target here
+        if tokens > 64:
+            part = (bx.norm(dim=1) / wx.norm(dim=1))[ref.here]
+            assert float(part.max()) < 0.1
+
+
+@pytest.mark.parametrize("tokens", [40, 300])
+def test_head_gradients_of_confident_tokens_off_the_grid(tokens):
+    vocab, hidden = 3000, 1288
+    x, w, t = confident_case(tokens, vocab, hidden, 120, scale=0.75)
+    x = (x.float() * (1 + normal(123, x.shape, 0.01))).to(BF16)
+    ref = Head(x, w, t, 0.75)
+    lse, _, loss = run_forward(x, w, t, scale=0.75)
+    dloss = normal(124, (tokens,))
+    # the logit's sum in fp32: hidden / 256 terms of 8 columns per thread, 16 further additions, one product
+    dzt = ((hidden / 256 + 24) * E * 0.75 * (ref.x.abs() @ ref.w.abs().T))[torch.arange(tokens, device=DEV), ref.col]
+    wx, bx, ww, bw = centred_gradients(ref, dloss, lse, dzt=dzt)
+    dx, dw = run_backward(x, w, t, lse, dloss, scale=0.75, dw=torch.full((vocab, hidden), float("nan"), device=DEV))
+    assert_within(dx, wx, bx + U[BF16] * wx.abs() * 1.01, "dx")
+    assert_within(dw, ww, bw + 4 * E * ww.abs(), "dweight")
+
+
+def test_head_training_on_what_is_known_leaves_weights_alone():
+    # the gradient of a mean loss over tokens that are all but certain, against that of the same tokens with their targets
+    # exchanged: a spurious 2^-9 of f in the target's column would be 1e-3 of it
+    tokens, vocab, hidden = 256, 1024, 256
+    x, w, t = confident_case(tokens, vocab, hidden, 130)
+    x = torch.cat([x[-64:]] * 4)
+    t = t[-64:].repeat(4)
+    lse, _, loss = run_forward(x, w, t)
+    assert float(loss.max()) < 1e-3
+    dloss = torch.full((tokens,), 1.0 / 921, device=DEV)
+    known, _ = run_backward(x, w, t, lse, dloss)
+    other, _ = run_backward(x, w, (t + 1) % vocab, lse, dloss)
+    # |dx| = f |sum p (w_v - w_t)| <= f (1 - p) * 2 max |w|, and p = exp(-loss)
+    limit = dloss * (loss + 32 * E * lse.abs()) * 2 * w.float().norm(dim=1).max()
+    assert bool((known.float().norm(dim=1) <= limit * 1.02).all())
+    assert bool((other.float().norm(dim=1) > 1e3 * known.float().norm(dim=1)).all())
+
+
 # ---- offsets beyond 32 bits ------------------------------------------------------------------------------------
 
 def test_lookup_and_its_gradient_in_a_table_of_more_than_2_to_the_32_bytes_and_elements():
