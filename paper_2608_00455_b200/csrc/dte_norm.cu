@@ -358,11 +358,11 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM, TEAM <= 32 ?
     for (uint32_t k = 0; k < rounds; ++k, row += apart * B) {
         if (TEAM > 32 && row >= end) break;
         float sums[B * S];
-        F2 r[B], m[B];                                      // xhat = x * r + m
+        F2 r[B], m[B];                                      // xhat = (x + m) * r: centred first, so that an offset of the row costs no digits
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             r[j] = f2(nrstd[j], nrstd[j]);
-            m[j] = f2(-nmean[j] * nrstd[j], -nmean[j] * nrstd[j]);
+            m[j] = f2(-nmean[j], -nmean[j]);
         }
         fetch(row + apart * B);
         feed.wait();
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM, TEAM <= 32 ?
 #pragma unroll
             for (int i = 0; i < kPer / 2; ++i) {
                 // columns past the end hold zero in g and w, so they add nothing: xh is finite there
-                xh[i] = KIND == DTE_NORM_LAYER ? f2_fma(xh[i], r[j], m[j]) : f2_mul(xh[i], r[j]);
+                xh[i] = f2_mul(KIND == DTE_NORM_LAYER ? f2_add(xh[i], m[j]) : xh[i], r[j]);
                 if (live) {
                     dw[i] = f2_fma(g[i], xh[i], dw[i]);
                     if (KIND == DTE_NORM_LAYER || p.want_bias) db[i] = f2_add(db[i], g[i]);
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM, TEAM <= 32 ?
                 feed.get(j, 1, g);
 #pragma unroll
                 for (int i = 0; i < kPer / 2; ++i) {
-                    xh[i] = KIND == DTE_NORM_LAYER ? f2_fma(xh[i], r[j], m[j]) : f2_mul(xh[i], r[j]);
+                    xh[i] = f2_mul(KIND == DTE_NORM_LAYER ? f2_add(xh[i], m[j]) : xh[i], r[j]);
                     g[i] = f2_mul(g[i], w[i]);
                     g[i] = f2_fma(xh[i], a, KIND == DTE_NORM_LAYER ? f2_fma(g[i], r[j], b) : f2_mul(g[i], r[j]));
                 }

@@ -242,6 +242,38 @@ def test_norm_forward_and_backward(rows, cols, dtype, rms):
             assert_within(db, wdb, chain * E * mdb, "dbias")
 
 
+@pytest.mark.parametrize("rows,cols", [(3, 7), (17, 65), (300, 128), (33, 200), (5, 257), (700, 2048), (40, 4096), (6, 4100), (5, 8192), (4, 8200), (3, 20000)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_layer_norm_gradient_of_rows_with_an_offset(rows, cols, dtype):
+    # rows whose mean is far larger than their deviation, and rows without any: xhat is as exact as x - mean is
+    eps = torch.tensor(1e-5, dtype=F32).item()
+    k = 48 + cols / 256
+    for extra, offset in ((0, 0), (3, 1)):
+        x = normal(140, (rows, cols))
+        x[0] += 1000.0
+        x[1] = -5.0
+        x[2] = x[2] * 1e-2 + 300.0
+        x[rows // 2] += -1e4
+        x = strided(x.to(dtype), cols + extra, offset)
+        w = normal(141, (cols,), 0.3, F32, 1.0)
+        _, m, r = norm_reference(x, w.to(F64), 0.0, eps, False)
+        mean, rstd = m[:, 0].to(F32), r[:, 0].to(F32)
+        dout = strided(normal(142, (rows, cols), 1.0, dtype), cols + extra, offset)
+        dx = strided(torch.zeros(rows, cols, dtype=dtype, device=DEV), cols + extra, offset)
+        dw, db = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+        dte.dte_norm_backward(dout, x, w, mean, rstd, dx, dw, db, workspace(dte.dte_norm_backward_workspace_bytes(rows, cols)))
+        # the formula at the statistics that were passed; x - mean is rounded once, so all is relative to its size
+        m, r = mean.to(F64)[:, None], rstd.to(F64)[:, None]
+        xh, dy = (x.to(F64) - m) * r, dout.to(F64)
+        g = dy * w.to(F64)
+        wdx = r * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
+        mag = r * (g.abs() + g.abs().mean(1, keepdim=True) + xh.abs() * (g * xh).abs().mean(1, keepdim=True))
+        assert_within(dx, wdx, U[dtype] * wdx.abs() * 1.01 + k * E * mag, "dx")
+        chain = 40 + rows / 64
+        assert_within(dw, (dy * xh).sum(0), chain * E * (dy * xh).abs().sum(0), "dweight")
+        assert_within(db, dy.sum(0), chain * E * dy.abs().sum(0), "dbias")
+
+
 def test_norm_optional_parts():
     x, dy = normal(30, (50, 384), 1.0, BF16), normal(31, (50, 384), 1.0, BF16)
     out, plain = torch.empty_like(x), torch.empty_like(x)
