@@ -506,6 +506,9 @@ dte_status device_sms(int device, int* sms) {
     if (device < 0 || device >= kMaxDevices) return op_fail(DTE_ERR_INVALID_ARG, "device ordinal out of range");
     int v = known[device].load(std::memory_order_relaxed);
     if (!v) {
+        int count = 0;
+        DTE_CUDA(cudaGetDeviceCount(&count));
+        if (device >= count) return op_fail(DTE_ERR_INVALID_ARG, "there is no such CUDA device");
         DTE_CUDA(cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device));
         known[device].store(v, std::memory_order_relaxed);
     }
@@ -530,7 +533,8 @@ extern "C" dte_status dte_embedding_forward(const dte_matrix* table, const dte_i
         return op_fail(DTE_ERR_INVALID_ARG, "out must be ids.count x table.cols");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (ids->count == 0) return DTE_OK;
-    OpDeviceGuard g(device);
+    OpDeviceGuard g;
+    if ((s = g.enter(device)) != DTE_OK) return s;
     const int vec = vec_of(table, out);
     LookupParams p = {};
     p.table = table->data;
@@ -586,9 +590,8 @@ extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_i
     if (!sorted_sum_fits(ids->count, dtable->rows, dout->cols, dtable->dtype))
         return op_fail(DTE_ERR_INVALID_ARG, "ids.count x hidden or dtable is too large for one call");
     if (dtable->rows == 0) return DTE_OK;
-    OpDeviceGuard g(device);
-    int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    OpDeviceGuard g;
+    if ((s = g.enter(device)) != DTE_OK) return s;
     SortedSum q = {};
     q.ids = ids->data;
     q.ids_dtype = ids->dtype;

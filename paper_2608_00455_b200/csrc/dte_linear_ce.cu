@@ -1156,9 +1156,8 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     const CeLayout l = forward_layout(n, V, H);
     if ((s = check_workspace(workspace, workspace_bytes, l.total)) != DTE_OK) return s;
     if (n == 0) return DTE_OK;
-    OpDeviceGuard g(device);
-    int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;             // also checks the ordinal
+    OpDeviceGuard g;
+    if ((s = g.enter(device)) != DTE_OK) return s;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const CeShape sh = ce_shape(n, V, H, kProbBytes);
@@ -1240,9 +1239,8 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     if ((s = check_workspace(workspace, workspace_bytes, l.total)) != DTE_OK) return s;
     if (!dx && !dweight) return DTE_OK;
     if (n == 0 && (!dweight || accumulate)) return DTE_OK;
-    OpDeviceGuard g(device);
-    int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;             // also checks the ordinal
+    OpDeviceGuard g;
+    if ((s = g.enter(device)) != DTE_OK) return s;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (n == 0) {

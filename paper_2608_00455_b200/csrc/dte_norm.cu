@@ -662,9 +662,9 @@ extern "C" dte_status dte_norm_forward(const dte_matrix* x, const void* weight, 
         return op_fail(DTE_ERR_INVALID_ARG, "out must have x's shape and type");
     if (((uintptr_t)mean | (uintptr_t)rstd) & 3u) return op_fail(DTE_ERR_INVALID_ARG, "mean / rstd must be 4-byte aligned");
     if (x->rows == 0) return DTE_OK;
-    OpDeviceGuard g(device);
+    OpDeviceGuard g;
     int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    if ((s = g.enter(device, &sms)) != DTE_OK) return s;
     NormParams p = {};
     p.x = x->data;
     p.out = out->data;
@@ -715,9 +715,9 @@ extern "C" dte_status dte_norm_backward(const dte_matrix* dout, const dte_matrix
     if (want && (s = check_workspace(workspace, workspace_bytes, dte_norm_backward_workspace_bytes(x->rows, x->cols))) != DTE_OK)
         return s;
     if (!dx && !want) return DTE_OK;
-    OpDeviceGuard g(device);
+    OpDeviceGuard g;
     int sms = 0;
-    if ((s = device_sms(device, &sms)) != DTE_OK) return s;
+    if ((s = g.enter(device, &sms)) != DTE_OK) return s;
     if (sms > kMostSms) sms = kMostSms;
     NormParams p = {};
     p.x = x->data;

@@ -22,11 +22,27 @@ inline dte_status op_fail(dte_status s, const char* msg) {
     return s;
 }
 
+dte_status device_sms(int device, int* sms);   // checks the ordinal; multiprocessor count, cached per device
+
+// Makes `device` current for a call.  The ordinal is checked first: nothing runs on another device instead, and a refused
+// one leaves no CUDA error behind for a later call to find.
 struct OpDeviceGuard {
     int prev = -1;
-    explicit OpDeviceGuard(int dev) {
-        cudaGetDevice(&prev);
-        if (prev != dev) cudaSetDevice(dev); else prev = -1;
+    dte_status enter(int dev, int* sms = nullptr) {
+        int known = 0;
+        const dte_status s = device_sms(dev, sms ? sms : &known);
+        if (s != DTE_OK) return s;
+        DTE_CUDA(cudaGetDevice(&prev));
+        if (prev == dev) {
+            prev = -1;
+            return DTE_OK;
+        }
+        const cudaError_t e = cudaSetDevice(dev);
+        if (e != cudaSuccess) {
+            prev = -1;
+            return cuda_fail(e, "cudaSetDevice");
+        }
+        return DTE_OK;
     }
     ~OpDeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
@@ -82,8 +98,6 @@ inline bool vec2_ok(const dte_matrix* m) {
 inline int vec_of(const dte_matrix* a, const dte_matrix* b) {
     return vec8_ok(a) && vec8_ok(b) ? 8 : vec2_ok(a) && vec2_ok(b) ? 2 : 1;
 }
-
-dte_status device_sms(int device, int* sms);   // multiprocessor count, cached per device
 
 // Raises a kernel's dynamic shared memory limit, once per device.
 template <typename Kernel>

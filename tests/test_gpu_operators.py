@@ -11,6 +11,7 @@ import pytest
 import torch
 
 import paper_2608_00455_b200 as dte
+from paper_2608_00455_b200 import operators as ops
 
 pytestmark = pytest.mark.gpu
 
@@ -903,3 +904,31 @@ def test_refusals():
     small = dte.dte_linear_ce_backward_workspace_min_bytes(4, 10, 16)
     assert refused("too small", lambda: b(x, w, ids, lse, lse, None, torch.zeros_like(w), ws[:small - 256])) == 3
     torch.cuda.synchronize()
+
+
+def test_a_device_that_does_not_exist_is_refused_and_leaves_nothing_behind():
+    L, none = dte.lib(), 63
+    assert torch.cuda.device_count() <= none
+    stream = torch.cuda.current_stream().cuda_stream
+    n, v, h = 4, 10, 16
+    t, x, w = randint(160, 0, v, n), normal(161, (n, h), 1.0, BF16), normal(162, (v, h), 1.0, BF16)
+    out, dw, s = torch.full_like(x, 7.0), torch.full_like(w, 7.0), torch.full((n,), 7.0, device=DEV)
+    ws = workspace(1 << 26)
+    mat = lambda a: ops._pack_matrix(a.data_ptr(), *a.shape, a.shape[1], ops.DTE_BF16, 0)                       # noqa: E731
+    i, size = ops._pack_ids(t.data_ptr(), n, ops.DTE_I64, 0), ws.numel()
+    m, o, g, p, q = mat(x), mat(out), mat(dw), s.data_ptr(), ws.data_ptr()
+    calls = (lambda d: L.dte_embedding_forward(mat(w), i, 0, v, 1.0, o, None, d, stream),
+             lambda d: L.dte_embedding_backward(m, i, 0, v, 1.0, 0, g, q, size, None, d, stream),
+             lambda d: L.dte_norm_forward(m, None, None, 0, 1, 1e-6, o, None, p, d, stream),
+             lambda d: L.dte_norm_backward(m, m, None, 0, 1, None, p, 0, o, None, None, None, 0, d, stream),
+             lambda d: L.dte_linear_ce_forward(m, mat(w), i, 0, v, 1.0, p, None, None, q, size, None, d, stream),
+             lambda d: L.dte_linear_ce_backward(m, mat(w), i, 0, v, 1.0, p, p, 0, o, g, q, size, None, d, stream))
+    for k, call in enumerate(calls):
+        for a in (out, dw, s):
+            a.fill_(7.0)
+        torch.cuda.synchronize()
+        assert call(none) == 1 and b"device" in L.dte_last_error(), k
+        torch.cuda.synchronize()
+        assert all(bool((a == 7.0).all()) for a in (out, dw, s)), k
+        assert call(0) == 0, (k, L.dte_last_error())
+        torch.cuda.synchronize()

@@ -117,3 +117,15 @@ def test_rows_of_higher_dimensional_tensors():
     assert ops._rows(torch.zeros(2, 5, 16)[..., :8], "t") == (10, 16)
     with pytest.raises(dte.DteError, match="flattened"):
         ops._rows(t[:, :2], "t")
+
+
+@pytest.mark.parametrize("device", [-1, 64, 2 ** 31 - 1])
+def test_every_entry_point_refuses_a_device_ordinal_out_of_range(device):
+    L, m, one, w, p, size = dte.lib(), matrix(4, 16), ids(4), matrix(10, 16), 4096, 1 << 40
+    for call in (lambda: L.dte_embedding_forward(w, one, 0, 10, 1.0, m, None, device, None),
+                 lambda: L.dte_embedding_backward(m, one, 0, 10, 1.0, 0, w, p, size, None, device, None),
+                 lambda: L.dte_norm_forward(m, None, None, 0, 0, 1e-6, m, None, None, device, None),
+                 lambda: L.dte_norm_backward(m, m, None, 0, 1, None, p, 0, m, None, None, None, 0, device, None),
+                 lambda: L.dte_linear_ce_forward(m, w, one, 0, 10, 1.0, p, None, None, p, size, None, device, None),
+                 lambda: L.dte_linear_ce_backward(m, w, one, 0, 10, 1.0, p, p, 0, m, w, p, size, None, device, None)):
+        refused(call(), "device")
