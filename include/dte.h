@@ -425,6 +425,8 @@ DTE_API dte_status dte_extract_delta_host(const dte_layout* layout, const float*
  *     otherwise; 16-byte aligned data with rows a multiple of 16 bytes apart takes the vector path.
  *   - Element types: DTE_F32 and DTE_BF16 for numbers, DTE_I32 and DTE_I64 for token ids.  Sums,
  *     softmax statistics and norm statistics are fp32 whatever the types; results are rounded once.
+ *     Scales and eps are used as fp32: a value that is not finite there (for logit_scale: times log2(e), as
+ *     the exponentials take it) is refused.
  *   - Every operator enqueues kernels (and memsets) only: no allocation, no synchronisation, no state
  *     kept between calls, so a call can be captured into a CUDA graph.  Scratch is the caller's
  *     `workspace` (device memory, 256-byte aligned); its contents do not matter before a call and mean

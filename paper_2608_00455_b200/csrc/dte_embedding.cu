@@ -528,7 +528,7 @@ extern "C" dte_status dte_embedding_forward(const dte_matrix* table, const dte_i
     if ((s = check_matrix(out, "out is null", true)) != DTE_OK) return s;
     if ((s = check_ids(ids)) != DTE_OK) return s;
     if ((s = check_range(row_start, table->rows, vocab)) != DTE_OK) return s;
-    if (!std::isfinite(scale)) return op_fail(DTE_ERR_INVALID_ARG, "scale is not finite");
+    if (!std::isfinite((float)scale)) return op_fail(DTE_ERR_INVALID_ARG, "scale is not finite in fp32");
     if (table->cols != out->cols || out->rows != ids->count)
         return op_fail(DTE_ERR_INVALID_ARG, "out must be ids.count x table.cols");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
@@ -580,7 +580,7 @@ extern "C" dte_status dte_embedding_backward(const dte_matrix* dout, const dte_i
     if ((s = check_matrix(dtable, "dtable is null", true)) != DTE_OK) return s;
     if ((s = check_ids(ids)) != DTE_OK) return s;
     if ((s = check_range(row_start, dtable->rows, vocab)) != DTE_OK) return s;
-    if (!std::isfinite(scale)) return op_fail(DTE_ERR_INVALID_ARG, "scale is not finite");
+    if (!std::isfinite((float)scale)) return op_fail(DTE_ERR_INVALID_ARG, "scale is not finite in fp32");
     if (dtable->cols != dout->cols || dout->rows != ids->count)
         return op_fail(DTE_ERR_INVALID_ARG, "dout must be ids.count x dtable.cols");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");

@@ -43,7 +43,8 @@ constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one i
 // 2^-16 exact for nothing.
 constexpr uint32_t kSplitTokens = 64;
 constexpr uint64_t kPadRows = 256;               // token rows are padded to this, with zero rows
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLog2eD = 1.44269504088896340736;
+constexpr float kLog2e = (float)kLog2eD;
 constexpr float kLn2 = 0.69314718055994530942f;
 // Work is split for this many SMs whatever the device has, so that results do not depend on it.
 constexpr uint32_t kSplitSms = 148;
@@ -1064,7 +1065,8 @@ static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, cons
     if (((uintptr_t)weight->data & 15u) || weight->ld % 8 || (weight->rows > 1 && weight->ld < weight->cols))
         return op_fail(DTE_ERR_INVALID_ARG, "weight must be 16-byte aligned with ld >= cols, a multiple of 8");
     if ((s = check_range(vocab_start, weight->rows, vocab)) != DTE_OK) return s;
-    if (!(logit_scale > 0) || !std::isfinite(logit_scale)) return op_fail(DTE_ERR_INVALID_ARG, "logit_scale must be finite and > 0");
+    if (!(logit_scale > 0) || !std::isfinite((float)(logit_scale * kLog2eD)))
+        return op_fail(DTE_ERR_INVALID_ARG, "logit_scale must be > 0 and, times log2(e), finite in fp32");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (targets->count > (1u << 24) || weight->rows > (1u << 24) || x->cols > (1u << 20))
         return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens, 2^24 vocabulary rows and 2^20 hidden");
@@ -1173,7 +1175,7 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     p.splits = 1;
     p.flags = flags;
     p.scale = (float)logit_scale;
-    p.k2 = (float)(logit_scale * 1.4426950408889634);
+    p.k2 = (float)(logit_scale * kLog2eD);
     p.target = reinterpret_cast<int32_t*>(ws + l.target);
     p.stats = reinterpret_cast<float2*>(ws + l.stats);
     p.stats_ld = sh.padded;
@@ -1279,7 +1281,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     p.split = n <= kSplitTokens;
     p.flags = flags;
     p.scale = (float)logit_scale;
-    p.k2 = (float)(logit_scale * 1.4426950408889634);
+    p.k2 = (float)(logit_scale * kLog2eD);
     p.target = target;
     p.f = reinterpret_cast<float*>(ws + l.scalar0);
     p.neg_lse2 = reinterpret_cast<float*>(ws + l.scalar1);

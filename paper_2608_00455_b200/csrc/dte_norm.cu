@@ -657,7 +657,7 @@ extern "C" dte_status dte_norm_forward(const dte_matrix* x, const void* weight, 
     if ((s = check_matrix(out, "out is null", true)) != DTE_OK) return s;
     if ((s = check_params(weight, bias, param_dtype)) != DTE_OK) return s;
     if (kind != DTE_NORM_LAYER && kind != DTE_NORM_RMS) return op_fail(DTE_ERR_INVALID_ARG, "unknown norm kind");
-    if (!(eps >= 0) || !std::isfinite(eps)) return op_fail(DTE_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if (!(eps >= 0) || !std::isfinite((float)eps)) return op_fail(DTE_ERR_INVALID_ARG, "eps must be finite in fp32 and >= 0");
     if (x->rows != out->rows || x->cols != out->cols || x->dtype != out->dtype)
         return op_fail(DTE_ERR_INVALID_ARG, "out must have x's shape and type");
     if (((uintptr_t)mean | (uintptr_t)rstd) & 3u) return op_fail(DTE_ERR_INVALID_ARG, "mean / rstd must be 4-byte aligned");

@@ -129,3 +129,17 @@ def test_every_entry_point_refuses_a_device_ordinal_out_of_range(device):
                  lambda: L.dte_linear_ce_forward(m, w, one, 0, 10, 1.0, p, None, None, p, size, None, device, None),
                  lambda: L.dte_linear_ce_backward(m, w, one, 0, 10, 1.0, p, p, 0, m, w, p, size, None, device, None)):
         refused(call(), "device")
+
+
+def test_scales_that_fp32_does_not_hold_are_refused():
+    # the kernels multiply in fp32: a finite double beyond it would be an infinity there, and 0 * infinity no number
+    L, m, one, w, p, size, big = dte.lib(), matrix(4, 16), ids(4), matrix(10, 16), 4096, 1 << 40, 3.5e38
+    refused(L.dte_embedding_forward(w, one, 0, 10, big, m, None, -1, None), "scale")
+    refused(L.dte_embedding_forward(w, one, 0, 10, -big, m, None, -1, None), "scale")
+    refused(L.dte_embedding_backward(m, one, 0, 10, big, 0, w, p, size, None, -1, None), "scale")
+    refused(L.dte_norm_forward(m, None, None, 0, 0, big, m, None, None, -1, None), "eps")
+    for scale in (big, 2.4e38):                     # the second one is beyond fp32 in base-2 exponents
+        refused(L.dte_linear_ce_forward(m, w, one, 0, 10, scale, p, None, None, p, size, None, -1, None), "logit_scale")
+        refused(L.dte_linear_ce_backward(m, w, one, 0, 10, scale, p, p, 0, m, w, p, size, None, -1, None), "logit_scale")
+    for scale in (3.4e38, -3.4e38):                 # held: only the device is refused
+        refused(L.dte_embedding_forward(w, one, 0, 10, scale, m, None, -1, None), "device")
