@@ -534,6 +534,11 @@ DTE_API dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matrix*
                                           const dte_matrix* dweight, void* workspace, uint64_t workspace_bytes,
                                           uint64_t* flags, int device, void* cuda_stream);
 
+/* How often a wait inside the head's kernels (for their own copies and products) is tried before the kernel gives up, ends what
+ * it has in flight, sets DTE_DEV_TIMEOUT and returns: for the calls of this process from now on.  0: the default, 2^20 tries
+ * of up to 4 us.  1: every wait that is not over at once, which is how the time-out is tested. */
+DTE_API void dte_linear_ce_set_wait_limit(uint32_t tries);
+
 /* Static strings. */
 DTE_API const char* dte_status_string(dte_status s);
 /* Message of the calling thread's most recent failed call ("" if none). */

@@ -33,6 +33,7 @@ SYMBOLS = [
     "dte_norm_forward", "dte_norm_backward", "dte_norm_backward_workspace_bytes",
     "dte_linear_ce_forward", "dte_linear_ce_forward_workspace_bytes", "dte_linear_ce_backward",
     "dte_linear_ce_backward_workspace_bytes", "dte_linear_ce_backward_workspace_min_bytes",
+    "dte_linear_ce_set_wait_limit",
 ]
 
 
@@ -147,6 +148,8 @@ def lib() -> C.CDLL:
                              ("dte_linear_ce_backward_workspace_min_bytes", 3)):
             getattr(L, name).argtypes = [u64] * n_args
             getattr(L, name).restype = u64
+        L.dte_linear_ce_set_wait_limit.argtypes = [u32]
+        L.dte_linear_ce_set_wait_limit.restype = None
         L.dte_status_string.argtypes = [C.c_int]
         L.dte_status_string.restype = C.c_char_p
         L.dte_last_error.argtypes = []

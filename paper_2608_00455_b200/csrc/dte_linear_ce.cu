@@ -72,6 +72,7 @@ struct CeParams {
     uint32_t prob_blocks;        // blocks of 64 columns in a row of the blocked f p
     bool w_chunks;               // kDx: W is mapped as chunks of 64 columns (hidden a multiple of 64)
     uint32_t w_row;              // first row of W of this piece
+    uint32_t wait_limit;         // tries of a wait inside the kernel
     uint64_t* flags;
     // kLse, kProb
     float k2;                    // logit_scale * log2(e): accumulators -> base-2 exponents
@@ -325,7 +326,8 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     constexpr bool kAmn = KIND == kDw, kBmn = KIND == kDx || KIND == kDw;
     extern __shared__ uint8_t ce_smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S::kStages + 5];
-    __shared__ uint32_t s_tmem, s_gave_up;
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken;      // loads asked for; loads that the products have waited for
+    __shared__ uint32_t s_peer[2];                                 // the other CTA's s_gave_up and s_issued
     __shared__ uint32_t s_ok[2][2][4];
     __shared__ float2 s_stat[KIND == kLse ? 2 : 1][kTileM];
 
@@ -374,6 +376,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     const uint32_t blocks_k = (k + kTileK - 1) / kTileK;
     const uint32_t first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
     const uint32_t part_n = p.tile_n / CTAS;             // columns of B in this CTA
+    const uint32_t load_bytes = kStageBytesA + part_n * kTileK * 2;      // of this CTA per stage
 
     if (warp == 0 && lane == 0) {
         // ---- loads ----
@@ -385,10 +388,10 @@ __global__ void __launch_bounds__(kCeThreads, 1)
             const uint32_t m0 = (tm * CTAS + rank) * kTileM, n0 = tn * p.tile_n + rank * part_n;
             const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
             for (uint32_t kb = kb0; kb < kb1; ++kb) {
-                if (!(ok = mbar_wait(empty(stage), phase ^ 1, gave_up))) break;
+                if (!(ok = mbar_wait(empty(stage), phase ^ 1, p.wait_limit, gave_up))) break;
                 const uint32_t a = stage0 + stage * S::kBytes, b = a + kStageBytesA;
                 const uint32_t bar = CTAS == 2 ? cluster_map(full(stage), 0) : full(stage);
-                if (leader) mbar_expect_tx(full(stage), CTAS * (kStageBytesA + part_n * kTileK * 2));
+                if (leader) mbar_expect_tx(full(stage), CTAS * load_bytes);
                 const int k0 = (int)(kb * kTileK);
                 // One load per operand and stage: with two per operand the loads, not the tensor cores, set the pace of the
                 // products along columns (kDw: 74 % of the tensor cores' cycles).  A: blocks of a blocked matrix, two
@@ -412,28 +415,22 @@ __global__ void __launch_bounds__(kCeThreads, 1)
                 if (++stage == S::kStages) { stage = 0; phase ^= 1; }
             }
         }
-        if (!ok && leader) {
-            // a wait ran out: let the copies in flight land (again with a limit) before shared memory goes away
-            for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
-                const uint32_t s = (stage + S::kStages - 1 - i) % S::kStages;
-                const uint32_t ph = s < stage ? phase : phase ^ 1;
-                for (uint32_t tries = 0; tries < kSpinLimit && !mbar_try_wait(full(s), ph); ++tries) {}
-            }
-        }
+        s_issued = issued;
     } else if (warp == 1 && lane == 0 && leader) {
         // ---- matrix products ----
         const uint32_t desc = mma_desc(kTileM * CTAS, p.tile_n, kAmn, kBmn);
         const uint32_t chunk = kTileK * 128;              // MN-major: 64 columns x 64 k
-        uint32_t stage = 0, phase = 0, use = 0;
+        uint32_t stage = 0, phase = 0, use = 0, taken = 0;
         bool ok = true;
         for (uint32_t t = first; t < total && ok; t += step, ++use) {
             const uint32_t split = t / (tiles_m * tiles_n);
             const uint32_t kb0 = (uint32_t)((uint64_t)split * blocks_k / p.splits), kb1 = (uint32_t)((uint64_t)(split + 1) * blocks_k / p.splits);
             const uint32_t buf = use & 1, acc = tmem + buf * kMaxTileN;
-            if (!(ok = mbar_wait(drained(buf), ((use >> 1) & 1) ^ 1, gave_up))) break;
+            if (!(ok = mbar_wait(drained(buf), ((use >> 1) & 1) ^ 1, p.wait_limit, gave_up))) break;
             tc_fence_after();
             for (uint32_t kb = kb0; kb < kb1; ++kb) {
-                if (!(ok = mbar_wait(full(stage), phase, gave_up))) break;
+                if (!(ok = mbar_wait(full(stage), phase, p.wait_limit, gave_up))) break;
+                ++taken;
                 tc_fence_after();
                 const uint32_t a = stage0 + stage * S::kBytes, b = a + kStageBytesA;
                 uint64_t da = operand_desc(a, kAmn ? chunk : 16), db = operand_desc(b, kBmn ? chunk : 16);
@@ -448,10 +445,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
             }
             if (ok) mma_commit<CTAS>(done(buf));
         }
-        if (!ok) {
-            mma_commit<CTAS>(last_bar);
-            for (uint32_t tries = 0; tries < kSpinLimit && !mbar_try_wait(last_bar, 0); ++tries) {}
-        }
+        s_taken = taken;
     } else if (warp >= 2) {
         // ---- epilogue: warp w may read the quarter w % 4 of tensor memory's lanes ----
         const uint32_t quarter = warp & 3, half = (warp - 2) / 4;
@@ -461,7 +455,7 @@ __global__ void __launch_bounds__(kCeThreads, 1)
             uint32_t split, tm, tn;
             tile_at(t, tiles_m, tiles_n, group, &split, &tm, &tn);
             const uint32_t buf = use & 1;
-            bool ok = mbar_wait(done(buf), (use >> 1) & 1, gave_up);
+            bool ok = mbar_wait(done(buf), (use >> 1) & 1, p.wait_limit, gave_up);
             ok = !__any_sync(0xFFFFFFFFu, !ok);
             if (KIND == kLse) {
                 // the two warps of a quarter go on or stop together: they meet again inside the epilogue
@@ -482,10 +476,37 @@ __global__ void __launch_bounds__(kCeThreads, 1)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (CTAS == 2) cluster_sync_all();     // the peer may still signal barriers here, or read this CTA's operands
+    bool failed = *gave_up;
+    if (CTAS == 2) {
+        if (threadIdx.x == 0) {
+            cluster_store(cluster_map(smem_addr(s_peer), rank ^ 1), *gave_up);
+            cluster_store(cluster_map(smem_addr(s_peer + 1), rank ^ 1), s_issued);
+        }
+        cluster_sync_all();     // the peer may still signal barriers here, or read this CTA's operands
+        failed |= *(volatile uint32_t*)s_peer;
+    }
+    if (failed) {
+        // A wait ran out, whichever it was (all threads of the CTA or pair agree).  All roles have stopped; what they left in
+        // flight ends here, again with a limit: the products of the thread that issued them, and every load that no product
+        // has waited for, before shared and tensor memory go away.
+        if (warp == 1 && lane == 0) {
+            if (leader) mma_commit<CTAS>(last_bar);
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(last_bar, 0); ++i) {}
+        }
+        if (threadIdx.x == 0 && leader) {
+            const uint32_t peer = CTAS == 2 ? *(volatile uint32_t*)(s_peer + 1) : 0, most = max(s_issued, peer);
+            uint32_t left = kWaitTries;
+            for (uint32_t i = s_taken; i < most; ++i) {
+                if (i >= s_issued) mbar_expect_tx(full(i % S::kStages), load_bytes);      // a load of the peer's alone
+                while (left && !mbar_try_wait(full(i % S::kStages), (i / S::kStages) & 1)) --left;
+            }
+        }
+        __syncwarp();
+        if (CTAS == 2) cluster_sync_all(); else __syncthreads();
+    }
     tc_fence_after();
     if (warp == 1) tmem_free<CTAS>(tmem, kTmemColumns);
-    if (threadIdx.x == 0 && *gave_up && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
+    if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
 }
 
 // ---- before and after the products --------------------------------------------------------------------------
@@ -1051,6 +1072,8 @@ static dte_status launch_ce(int ctas, const CUtensorMap& a, const CUtensorMap& b
     return ctas == 2 ? launch_ce_as<KIND, 2>(a, b, p, tiles, device, st) : launch_ce_as<KIND, 1>(a, b, p, tiles, device, st);
 }
 
+static std::atomic<uint32_t> g_wait_limit{kWaitTries};
+
 static dte_status check_head(const dte_matrix* x, const dte_matrix* weight, const dte_ids* targets, uint64_t vocab_start,
                              uint64_t vocab, double logit_scale, const uint64_t* flags) {
     dte_status s;
@@ -1140,6 +1163,10 @@ static dte_status prepare_rows(const CeLayout& l, uint8_t* ws, const dte_matrix*
 
 using namespace dte;
 
+extern "C" void dte_linear_ce_set_wait_limit(uint32_t tries) {
+    g_wait_limit.store(tries ? tries : kWaitTries, std::memory_order_relaxed);
+}
+
 extern "C" uint64_t dte_linear_ce_forward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden) {
     if (!ce_sizes_ok(tokens, vocab_rows, hidden)) return UINT64_MAX;     // refused by the call
     return forward_layout(tokens, vocab_rows, hidden).total;
@@ -1173,6 +1200,7 @@ extern "C" dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matri
     p.tokens = reinterpret_cast<uint32_t*>(ws + l.count);
     p.tile_n = tn;
     p.splits = 1;
+    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     p.flags = flags;
     p.scale = (float)logit_scale;
     p.k2 = (float)(logit_scale * kLog2eD);
@@ -1279,6 +1307,7 @@ extern "C" dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matr
     CeParams p = {};
     p.tokens = count + 1;
     p.split = n <= kSplitTokens;
+    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     p.flags = flags;
     p.scale = (float)logit_scale;
     p.k2 = (float)(logit_scale * kLog2eD);

@@ -23,6 +23,9 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t v) {          // addr: from cluster_map
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -49,12 +52,24 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// Every wait gives up: after kSpinLimit tries (seconds; a tile takes microseconds), or soon after another
-// wait of this CTA has.  `gave_up` is a word of shared memory.
-constexpr uint32_t kSpinLimit = 1u << 24;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
-    if (mbar_try_wait(bar, parity)) return true;
-    for (uint32_t i = 1; i < kSpinLimit; ++i) {
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {    // does not suspend the thread
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Every wait gives up: after `limit` tries, or soon after another wait of this CTA has.  `gave_up` is a word of shared
+// memory.  A try suspends the thread for up to 7800 cycles (measured; 4 us), so 2^20 of them are four seconds where a tile
+// takes microseconds.  The first try does not suspend: with a limit of 1 every wait that is not over yet gives up.
+constexpr uint32_t kWaitTries = 1u << 20;
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit, volatile uint32_t* gave_up) {
+    if (mbar_test_wait(bar, parity)) return true;
+    for (uint32_t i = 1; i < limit; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((i & 255u) == 0 && *gave_up) return false;
     }

@@ -740,6 +740,33 @@ def test_head_training_on_what_is_known_leaves_weights_alone():
     assert bool((other.float().norm(dim=1) > 1e3 * known.float().norm(dim=1)).all())
 
 
+@pytest.mark.parametrize("tokens,vocab,hidden", [(4, 300, 64), (300, 700, 64), (40, 60000, 64), (300, 60000, 64), (300, 3000, 1032)])
+def test_head_waits_that_run_out_are_reported_and_the_next_call_is_right(tokens, vocab, hidden):
+    # one CTA and pairs, one tile and several per CTA, more steps along K than stages: loads are in flight when the waits give up
+    x, w, t = head_case(tokens, vocab, hidden, 170)
+    dloss = normal(173, (tokens,))
+    lse, tl, loss = run_forward(x, w, t)
+    want = (lse, tl, loss, *run_backward(x, w, t, lse, dloss))
+    flags = torch.zeros(1, dtype=torch.int64, device=DEV)
+    ws = workspace(max(dte.dte_linear_ce_forward_workspace_bytes(tokens, vocab, hidden),
+                       dte.dte_linear_ce_backward_workspace_bytes(tokens, vocab, hidden)))
+    spare, dx, dw = torch.empty_like(lse), torch.empty_like(x), torch.empty_like(w)
+    dte.lib().dte_linear_ce_set_wait_limit(1)
+    try:
+        dte.dte_linear_ce_forward(x, w, t, spare, None, None, ws, flags=flags)
+        assert flags.item() == dte.DTE_DEV_TIMEOUT
+        flags.zero_()
+        dte.dte_linear_ce_backward(x, w, t, lse, dloss, dx, dw, ws, flags=flags)
+        assert flags.item() == dte.DTE_DEV_TIMEOUT
+    finally:
+        dte.lib().dte_linear_ce_set_wait_limit(0)
+    flags.zero_()
+    got = run_forward(x, w, t, flags=flags)
+    for a, b in zip(want, (*got, *run_backward(x, w, t, lse, dloss))):
+        assert torch.equal(a, b)
+    assert flags.item() == 0
+
+
 # ---- offsets beyond 32 bits ------------------------------------------------------------------------------------
 
 def test_lookup_and_its_gradient_in_a_table_of_more_than_2_to_the_32_bytes_and_elements():
