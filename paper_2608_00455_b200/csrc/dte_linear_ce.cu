@@ -947,7 +947,7 @@ static uint32_t lse_tile_n(uint64_t tokens, uint64_t vocab) {
     return best;
 }
 
-static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded, uint64_t& at) {
+static CeLayout common_layout(uint64_t hidden, uint64_t padded, uint64_t& at) {
     CeLayout l = {};
     l.count = take(at, 8);
     l.source = take(at, padded * 4);
@@ -956,14 +956,13 @@ static CeLayout common_layout(uint64_t tokens, uint64_t hidden, uint64_t padded,
     l.rows = take(at, padded * align_up(hidden, kBlock) * 2);
     l.scalar0 = take(at, padded * 4);
     l.scalar1 = take(at, padded * 4);
-    (void)tokens;
     return l;
 }
 
 static CeLayout forward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden) {
     const CeShape s = ce_shape(tokens, vocab, hidden, kProbBytes);
     uint64_t at = 0;
-    CeLayout l = common_layout(tokens, hidden, s.padded, at);
+    CeLayout l = common_layout(hidden, s.padded, at);
     const uint64_t tn = lse_tile_n(tokens, vocab);
     l.stats = take(at, (vocab + tn - 1) / tn * s.padded * sizeof(float2));
     l.total = at;
@@ -972,7 +971,7 @@ static CeLayout forward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden)
 
 static CeLayout backward_layout(uint64_t tokens, uint64_t vocab, uint64_t hidden, const CeShape& s) {
     uint64_t at = 0;
-    CeLayout l = common_layout(tokens, hidden, s.padded, at);
+    CeLayout l = common_layout(hidden, s.padded, at);
     l.coef = take(at, s.padded * 4);
     l.prob = take(at, s.padded * s.piece * 2);
     l.dx_sum = take(at, s.splits * s.padded * hidden * 4);

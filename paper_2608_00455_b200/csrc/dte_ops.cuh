@@ -203,7 +203,6 @@ struct Raw8<__nv_bfloat16> {
         a = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     }
     __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = a; }
-    __device__ __forceinline__ void store_cs(__nv_bfloat16* p) const { __stcs(reinterpret_cast<uint4*>(p), a); }
 };
 template <>
 struct Raw8<float> {
@@ -227,10 +226,6 @@ struct Raw8<float> {
     __device__ __forceinline__ void store(float* p) const {
         reinterpret_cast<float4*>(p)[0] = a;
         reinterpret_cast<float4*>(p)[1] = b;
-    }
-    __device__ __forceinline__ void store_cs(float* p) const {
-        __stcs(reinterpret_cast<float4*>(p), a);
-        __stcs(reinterpret_cast<float4*>(p) + 1, b);
     }
 };
 
@@ -268,7 +263,6 @@ struct Vec<T, 1> {
     __device__ __forceinline__ void get(float* f) const { f[0] = to_f<T>(a); }
     __device__ __forceinline__ void set(const float* f) { a = from_f<T>(f[0]); }
     __device__ __forceinline__ void store(T* p) const { *p = a; }
-    __device__ __forceinline__ void store_cs(T* p) const { *p = a; }
 };
 
 __device__ __forceinline__ int64_t load_id(const void* ids, uint32_t dtype, uint64_t i) {
