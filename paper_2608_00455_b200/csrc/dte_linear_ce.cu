@@ -527,58 +527,78 @@ struct RowsParams {
 constexpr int kRowsThreads = 1024;
 constexpr int kRowsPer = 8;      // consecutive tokens of a thread
 
+// One round of a CTA of THREADS threads, each with the kRowsPer tokens from i0 + threadIdx.x * kRowsPer: their targets (-1 past the
+// end), how many tokens of the round that count lie in front of this thread's, and (returned) how many there are.
+// s_warp may be written again behind the next barrier.
+template <int THREADS>
+__device__ __forceinline__ uint32_t count_tokens(const RowsParams& p, uint64_t i0, int64_t (&id)[kRowsPer], uint32_t& before, bool& bad,
+                                                 uint32_t (&s_warp)[THREADS / 32]) {
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < kRowsPer; ++j) {
+        const uint64_t i = i0 + threadIdx.x * kRowsPer + j;
+        id[j] = i < p.n ? load_id(p.targets, p.targets_dtype, i) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kRowsPer; ++j) {
+        mine += id[j] >= 0;
+        bad |= id[j] >= p.vocab;
+    }
+    uint32_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+        if (lane >= (uint32_t)o) inc += v;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    before = inc - mine;
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        before += w < (int)warp ? s_warp[w] : 0;
+        all += s_warp[w];
+    }
+    return all;
+}
+
+// A target as a row of this shard, or -1.
+__device__ __forceinline__ int32_t shard_row(const RowsParams& p, int64_t id) {
+    const uint64_t row = (uint64_t)id - (uint64_t)p.vocab_start;
+    return id >= 0 && row < p.vocab_rows ? (int32_t)row : -1;
+}
+
+// Leaves what the kernels behind need of token i, the at-th that counts if it does.
+__device__ __forceinline__ void leave_token(const RowsParams& p, uint64_t i, int64_t id, uint32_t at) {
+    if (p.place) p.place[i] = id >= 0 ? (int32_t)at : -1;
+    if (id >= 0) {
+        p.source[at] = (int32_t)i;
+        p.target[at] = shard_row(p, id);
+    } else {
+        if (p.lse) p.lse[i] = 0.f;
+        if (p.target_logit) p.target_logit[i] = 0.f;
+        if (p.loss) p.loss[i] = 0.f;
+    }
+}
+
 // Numbers the tokens that count, in order.  One CTA: the list is short next to everything else.
 __global__ void __launch_bounds__(kRowsThreads) ce_rows_kernel(const RowsParams p) {
-    __shared__ uint32_t s_warp[32];
+    __shared__ uint32_t s_warp[kRowsThreads / 32];
     let_next_start();
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     uint32_t base = 0;
     bool bad = false;
     for (uint64_t i0 = 0; i0 < p.n; i0 += kRowsThreads * kRowsPer) {
         int64_t id[kRowsPer];
-        uint32_t mine = 0;
-#pragma unroll
-        for (int j = 0; j < kRowsPer; ++j) {
-            const uint64_t i = i0 + threadIdx.x * kRowsPer + j;
-            id[j] = i < p.n ? load_id(p.targets, p.targets_dtype, i) : -1;
-        }
-#pragma unroll
-        for (int j = 0; j < kRowsPer; ++j) {
-            mine += id[j] >= 0;
-            bad |= id[j] >= p.vocab;
-        }
-        uint32_t inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-            if (lane >= (uint32_t)o) inc += v;
-        }
-        if (lane == 31) s_warp[warp] = inc;
-        __syncthreads();
-        const uint32_t total = s_warp[lane];
-        uint32_t before = lane < warp ? total : 0, all = total;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
-            all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
-        }
-        uint32_t at = base + before + inc - mine;
+        uint32_t at;
+        const uint32_t all = count_tokens<kRowsThreads>(p, i0, id, at, bad, s_warp);
+        at += base;
 #pragma unroll
         for (int j = 0; j < kRowsPer; ++j) {
             const uint64_t i = i0 + threadIdx.x * kRowsPer + j;
             if (i >= p.n) break;
-            const bool counts = id[j] >= 0;
-            if (p.place) p.place[i] = counts ? (int32_t)at : -1;
-            if (counts) {
-                const uint64_t row = (uint64_t)id[j] - (uint64_t)p.vocab_start;
-                p.source[at] = (int32_t)i;
-                p.target[at] = row < p.vocab_rows ? (int32_t)row : -1;
-                ++at;
-            } else {
-                if (p.lse) p.lse[i] = 0.f;
-                if (p.target_logit) p.target_logit[i] = 0.f;
-                if (p.loss) p.loss[i] = 0.f;
-            }
+            leave_token(p, i, id[j], at);
+            at += id[j] >= 0;
         }
         base += all;
         __syncthreads();
@@ -632,60 +652,22 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const GatherR
     int32_t target;
     if (p.few) {
         const RowsParams& q = p.rows_of;
-        const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
         int64_t id[kRowsPer];
-        uint32_t mine = 0;
+        uint32_t at;
         bool bad = false;
-#pragma unroll
-        for (int j = 0; j < kRowsPer; ++j) {
-            const uint32_t t = threadIdx.x * kRowsPer + j;
-            id[j] = t < q.n ? load_id(q.targets, q.targets_dtype, t) : -1;
-        }
-#pragma unroll
-        for (int j = 0; j < kRowsPer; ++j) {
-            mine += id[j] >= 0;
-            bad |= id[j] >= q.vocab;
-        }
-        uint32_t inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-            if (lane >= (uint32_t)o) inc += v;
-        }
-        if (lane == 31) s_warp[warp] = inc;
         if (threadIdx.x < 2) s_mine[threadIdx.x] = threadIdx.x ? -1 : 0;
-        __syncthreads();
-        uint32_t at = inc - mine;
-        count = 0;
-#pragma unroll
-        for (int w = 0; w < kGatherThreads / 32; ++w) {
-            at += w < (int)warp ? s_warp[w] : 0;
-            count += s_warp[w];
-        }
+        count = count_tokens<kGatherThreads>(q, 0, id, at, bad, s_warp);
         const bool writer = i == 0;        // one CTA leaves the numbering for the kernels behind
 #pragma unroll
         for (int j = 0; j < kRowsPer; ++j) {
             const uint32_t t = threadIdx.x * kRowsPer + j;
             if (t >= q.n) break;
-            const bool counts = id[j] >= 0;
-            const uint64_t row = (uint64_t)id[j] - (uint64_t)q.vocab_start;
-            const int32_t to = counts && row < q.vocab_rows ? (int32_t)row : -1;
-            if (counts && at == mine_at) {
+            if (id[j] >= 0 && at == mine_at) {
                 s_mine[0] = (int32_t)t;
-                s_mine[1] = to;
+                s_mine[1] = shard_row(q, id[j]);
             }
-            if (writer) {
-                if (q.place) q.place[t] = counts ? (int32_t)at : -1;
-                if (counts) {
-                    q.source[at] = (int32_t)t;
-                    q.target[at] = to;
-                } else {
-                    if (q.lse) q.lse[t] = 0.f;
-                    if (q.target_logit) q.target_logit[t] = 0.f;
-                    if (q.loss) q.loss[t] = 0.f;
-                }
-            }
-            at += counts;
+            if (writer) leave_token(q, t, id[j], at);
+            at += id[j] >= 0;
         }
         if (writer) {
             if (threadIdx.x == 0) {
