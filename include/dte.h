@@ -520,10 +520,10 @@ DTE_API dte_status dte_linear_ce_forward(const dte_matrix* x, const dte_matrix* 
  *   dweight[v] = logit_scale * (sum_n dloss[n] p[n][v] x[n] - sum over target[n] == v of dloss[n] x[n])
  * dx or dweight may be NULL.  dweight: BF16 or FP32; accumulate != 0 adds to it.  The logits are recomputed
  * in pieces of the vocabulary; a piece's dloss * p is kept in the workspace as BF16, the operand type of
- * the two products that consume it (up to 64 tokens as two BF16 numbers), but for the target's column: its
- * coefficient logit_scale * dloss * (p - 1) is formed in fp32 as expm1(z - lse), so that the gradient of a token
- * whose loss is near zero is as good as the lse passed for it.  dx and dweight rows need 16-byte
- * alignment (data and ld).  A workspace of dte_linear_ce_backward_workspace_bytes holds pieces of the
+ * the two products that consume it (up to 64 tokens, ignored ones included, as two BF16 numbers), but for
+ * the target's column: its coefficient logit_scale * dloss * (p - 1) is formed in fp32 as expm1(z - lse), so that
+ * the gradient of a token whose loss is near zero is as good as the lse passed for it.  dx and dweight rows
+ * need 16-byte alignment (data and ld).  A workspace of dte_linear_ce_backward_workspace_bytes holds pieces of the
  * size that measured best; any workspace from dte_linear_ce_backward_workspace_min_bytes up is accepted
  * and gives smaller pieces. */
 DTE_API uint64_t dte_linear_ce_backward_workspace_bytes(uint64_t tokens, uint64_t vocab_rows, uint64_t hidden);

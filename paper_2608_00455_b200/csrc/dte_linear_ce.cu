@@ -19,9 +19,12 @@
 // reason; an error of c beyond fp32's relative one comes from the lse that is passed in: 2^-24 |lse| f at most.
 //
 // Measured: logits 8192 x 151936 x 4096 7.6 to 7.9 ms = 1.28 to 1.34 PFLOP/s in a loop of seconds at the 1000 W limit (a
-// bf16 library product of that shape, which stores its logits: 7.4 ms); the backward pass 24.1 ms = 1.27 PFLOP/s over its
-// three products; with zero operands, which the power limit does not slow, kProb has its tensor cores active 93 % of
-// the time.  8 tokens: W at 6.3 TB/s.
+// bf16 library product of that shape, which stores its logits: 7.4 ms); the backward pass 24.1 to 24.5 ms = 1.25 to 1.27
+// PFLOP/s over its three products; with zero operands, which the power limit does not slow, kProb has its tensor cores
+// active 93 % of the time.  8 tokens: kLse reads W at 6.4 TB/s.  64 tokens x 151936 x 4096, gradients: kProb 221, kDx 183, kDw 467
+// us, where W and dW are 190 us of memory each: up to 128 tokens there is one piece, so kDx finds nothing of W in L2, and
+// kDw's tiles have one or two steps along K, so its epilogue sets the pace.
+// The tensor cores truncate: log-sum-exps are good to 5e-7 (8 tokens) and 9e-7 (8192), relative, sums in fp32 to 2e-7 and 6e-7.
 #include <atomic>
 
 #include "dte_mma.cuh"
@@ -38,9 +41,10 @@ constexpr uint32_t kEpilogueWarps = 8;           // two for each quarter of tens
 constexpr uint32_t kCeThreads = 64 + 32 * kEpilogueWarps;   // TMA warp, MMA warp, epilogue
 constexpr uint32_t kStageBytesA = kTileM * kTileK * 2;
 constexpr uint32_t kTmemColumns = 512;           // two accumulator tiles: one is filled while the other is drained
-// Up to this many tokens half of a tile's rows are free, and so f p' is kept as two bf16 numbers, the rounded value and the
-// rest, as if every token were there twice: the gradients of a few tokens, whose roundings do not average out, come out
-// 2^-16 exact for nothing.
+// Up to this many tokens (ignored ones included: the host does not know how many those are) half of a tile's rows are free, and
+// so f p' is kept as two bf16 numbers, the rounded value and the rest, as if every token were there twice: of a few tokens,
+// whose roundings do not average out, f p' is stored to 2^-16 for nothing.  p itself is as good as the tensor cores'
+// logits: 4e-6 of a logit at 4096 products.
 constexpr uint32_t kSplitTokens = 64;
 constexpr uint64_t kPadRows = 256;               // token rows are padded to this, with zero rows
 constexpr double kLog2eD = 1.44269504088896340736;
@@ -49,7 +53,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // Work is split for this many SMs whatever the device has, so that results do not depend on it.
 constexpr uint32_t kSplitSms = 148;
 
-// The two matrices that this file makes itself, the rows that count and f p, are stored in blocks of 64 x 64, row-major
+// The two matrices that this file makes itself, the rows that count and f p', are stored in blocks of 64 x 64, row-major
 // inside (8 KB, 128 bytes a row: the swizzled operand tile as TMA writes it).  Every load of them is then 8 KB
 // in one stretch, whether the tile is wanted along its rows or its columns, and one tensor map serves both.
 constexpr uint32_t kBlock = 64;
@@ -69,7 +73,7 @@ struct CeParams {
     uint32_t m, n, k;            // extents; the one that counts tokens is replaced by *tokens
     const uint32_t* tokens;      // tokens that count
     uint32_t tile_n, splits;
-    uint32_t prob_blocks;        // blocks of 64 columns in a row of the blocked f p
+    uint32_t prob_blocks;        // blocks of 64 columns in a row of the blocked f p'
     bool w_chunks;               // kDx: W is mapped as chunks of 64 columns (hidden a multiple of 64)
     uint32_t w_row;              // first row of W of this piece
     uint32_t wait_limit;         // tries of a wait inside the kernel
@@ -877,7 +881,7 @@ struct CeShape {
     uint32_t splits;       // of kDx's long axis
 };
 
-constexpr uint64_t kProbBytes = 256ull << 20;    // f p of one piece
+constexpr uint64_t kProbBytes = 256ull << 20;    // f p' of one piece
 constexpr uint64_t kMinPiece = 2048;
 
 static CeShape ce_shape(uint64_t tokens, uint64_t vocab, uint64_t hidden, uint64_t prob_bytes) {

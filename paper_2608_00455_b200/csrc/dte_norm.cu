@@ -1,21 +1,27 @@
 // Layer norm and RMS norm, forward and backward.
 //
-// Both directions are bound by the bytes of the row matrices: a row is read once into registers,
-// its statistics are reduced there (the variance from the centred values, not as E[x^2] - E[x]^2) and
+// Both directions are bound by the bytes of the row matrices: a row is read from memory once,
+// its statistics are reduced in registers (the variance from the centred values, not as E[x^2] - E[x]^2) and
 // the result is written.  CTAs are persistent over rows: the weights, and in the backward pass the
 // running sums of the weight's gradient, belong to columns and so stay in the same thread's
 // registers for all its rows.  The rows to come are on their way into shared memory meanwhile: every thread copies
 // its own columns of the next rows (asynchronous 16-byte copies) and reads back what it copied, so the
 // ring needs no barrier.  (One row ahead in registers keeps 32 KB per SM in flight: 4.1 TB/s.)  The forward pass reaches
-// 5.9 TB/s (8191 x 4096 fp32, 45 us; a plain copy of the same size 43 us), the backward pass 4.8 TB/s
-// (16384 x 4096 bf16, 84 us): 16 warps per SM, all that the sums' registers leave room for, do not quite hide
-// a row's reduction.
+// 5.9 TB/s (8191 x 4096 fp32, 45 us; a plain copy of the same size 43 us), the backward pass 4.6 TB/s
+// (16384 x 4096 bf16, 88 us, of which centring each row before it is scaled takes 2.4): 16 warps per SM, all that the sums'
+// registers leave room for, do not quite hide a row's reduction.
 //
 // A row is held by a team: 8, 16 or 32 lanes of a warp for up to 512 columns (a head's norm: several
 // rows per warp, reductions by shuffles alone), else one CTA of ceil(columns / 16) threads, sixteen columns
 // per thread, up to 16384 columns.  Sixteen, because what a warp spends on a row beside its columns (reduction,
 // addresses, statistics) was half of its instructions at eight.  Longer rows take the kernels that pass over the
 // row from memory again.
+//
+// The shape was chosen at 4096 and 128 columns.  Elsewhere (2^26 bf16 elements, forward / backward in TB/s): 2048 5.2 / 4.9,
+// 4096 5.1 / 4.8, 6144 4.3 / 4.6, 8192 4.7 / 4.5; just above 4096 an SM holds one CTA of 288 threads instead of 512 threads: 4104
+// 3.0 / 3.6, 5120 3.7 / 4.3.  From 8193 columns a CTA has more than 512 threads, so 64 registers each, and a row spills to
+// local memory: 16384 2.6 / 3.1.  Columns or strides that allow no 16-byte accesses go element by element, one row ahead:
+// 2001 and 2002 2.3 / 2.3.  20000 (several passes) 0.9 / 0.9.
 #include "dte_ops.cuh"
 
 namespace dte {
@@ -25,7 +31,7 @@ constexpr int kTeamThreads = 256;        // CTA size when teams are parts of a w
 constexpr uint32_t kMaxRegCols = 1024 * kPer;
 constexpr int kLongThreads = 512;
 // Shared memory of a thread's rows in flight and threads per SM, measured together (us, layer norm 8191 x 4096 fp32 / its
-// gradient 16384 x 4096 bf16): these 45 / 84; half the ring 53 / 99; 1024 threads 46 forward.  More rows in flight
+// gradient 16384 x 4096 bf16, then without centring): these 45 / 84; half the ring 53 / 99; 1024 threads 46 forward.  More rows in flight
 // than 64 KB per SM make the forward pass slower, not faster.
 constexpr int kRingForward = 128, kRingBackward = 256;
 constexpr unsigned kSmThreadsForward = 512, kSmThreadsBackward = 512;
@@ -139,7 +145,8 @@ struct RowPart<T, false> {
 // their way or at work, in shared memory.
 template <typename T, bool VEC, int INPUTS, int TEAM>
 struct Rows {
-    static constexpr int kMost = INPUTS == 1 ? kRingForward : TEAM > 512 ? 128 : kRingBackward;   // an SM has 227 KB
+    // an SM has 227 KB: of fp32 rows of more than 8192 columns the backward ring holds just the one at work
+    static constexpr int kMost = INPUTS == 1 ? kRingForward : TEAM > 512 ? 128 : kRingBackward;
     static constexpr int kRowBytes = kPer * sizeof(T) * INPUTS;      // of a thread
     static constexpr int kBatch = VEC && sizeof(T) * INPUTS <= 4 && kMost >= 2 * kRowBytes ? 2 : 1;
     static constexpr int kRing = VEC ? kMost / kRowBytes : kBatch;
@@ -326,7 +333,7 @@ __global__ void __launch_bounds__(TEAM <= 32 ? kTeamThreads : TEAM, TEAM <= 32 ?
     const uint32_t team = TEAM <= 32 ? blockIdx.x * (kTeamThreads / n) + threadIdx.x / n : blockIdx.x;
     constexpr int B = Rows<T, VEC, 2, TEAM>::kBatch, S = KIND == DTE_NORM_LAYER ? 2 : 1;
     const uint32_t rounds = (p.rows + teams * B - 1) / (teams * B);
-    // a CTA's rows follow one another (84 us; every 296th row: 87 us); teams of a CTA share out its stretch row by row
+    // a CTA's rows follow one another (every 296th row: 3 us more of 84, without centring); teams of a CTA share out its stretch row by row
     const uint32_t apart = TEAM > 32 ? 1 : teams, me = TEAM > 32 ? team * rounds * B : team;
     const uint32_t end = TEAM > 32 ? min(me + rounds * B, p.rows) : p.rows;
     T* dx = static_cast<T*>(p.out);
