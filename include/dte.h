@@ -539,6 +539,101 @@ DTE_API dte_status dte_linear_ce_backward(const dte_matrix* x, const dte_matrix*
  * of up to 4 us.  1: every wait that is not over at once, which is how the time-out is tested. */
 DTE_API void dte_linear_ce_set_wait_limit(uint32_t tries);
 
+/* ---- Operators inside and behind the model's layers ------------------------------------------------
+ * What a training step runs between the lookup and the head, and in front of AdamW: rotary positions, causal
+ * attention over packed prompts, the global gradient norm with clipping.  The conventions of the section
+ * above hold.  A matrix of heads is tokens x (heads * head_dim), head after head in a row, so that queries,
+ * keys and values may be columns of one projection's output. */
+
+/* Rotary positions: pair i of a head's first `rot` columns (even; the others are copied) is turned by
+ * position * frequencies[i]:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * DTE_ROPE_HALF pairs columns i and i + rot / 2, DTE_ROPE_INTERLEAVED columns 2 i and 2 i + 1. */
+#define DTE_ROPE_HALF 0u
+#define DTE_ROPE_INTERLEAVED 1u
+
+/* Frequencies of rot / 2 pairs, 64 bits, into HOST memory, and the amplitude that goes with them.  With
+ * f_i = base^(-2 i / rot):
+ *   DTE_ROPE_PLAIN   f_i
+ *   DTE_ROPE_LINEAR  f_i / factor                                   (positions squeezed into the trained range)
+ *   DTE_ROPE_BASE    the same with base * factor^(rot / (rot - 2))  (slow pairs stretched, the fastest kept; rot > 2)
+ *   DTE_ROPE_RAMP    f_i where a pair turns more than fast_turns times over original_positions, f_i / factor where
+ *                    fewer than slow_turns, in between a ramp over the pair's index (its ends rounded outwards to
+ *                    whole indices, inside [0, rot - 1]); amplitude 0.1 ln(factor) + 1 (as YaRN defines them)
+ * The amplitude of the others is 1.  base > 1, factor >= 1, rot even, 2 <= rot <= 1024.  Host only. */
+#define DTE_ROPE_PLAIN 0u
+#define DTE_ROPE_LINEAR 1u
+#define DTE_ROPE_BASE 2u
+#define DTE_ROPE_RAMP 3u
+DTE_API dte_status dte_rope_frequencies(uint32_t rot, double base, uint32_t scaling, double factor, double original_positions,
+                                        double fast_turns, double slow_turns, double* frequencies, double* amplitude);
+
+/* q and k (NULL: none) are turned by the same positions, one per row, into q_out and k_out, each of its input's shape and
+ * type: the input itself (same data and ld; columns that are not turned are then not touched) or a matrix that
+ * overlaps no input.  A row with a negative position (padding) is copied.  frequencies: DEVICE, rot / 2 values in radians per
+ * position.  Angles are 64-bit products, good to 2^-52 of the number of turns, and are reduced to an eighth of a
+ * turn before they are rounded to fp32.  inverse != 0 turns backwards: the gradient.  head_dim <= 1024,
+ * rot <= head_dim, at most 4095 heads. */
+DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t head_dim, const dte_ids* positions,
+                            const double* frequencies, uint32_t rot, uint32_t layout, double amplitude, int inverse,
+                            const dte_matrix* q_out, const dte_matrix* k_out, int device, void* cuda_stream);
+
+/* Causal attention over packed sequences.  Rows starts[s] .. starts[s + 1] - 1 are sequence s; a query sees the keys of
+ * its sequence up to its own row:
+ *   z = scale * q . k^T over those keys,  lse = log sum exp z,  out = sum exp(z - lse) v
+ * Query head h reads key head h / (query heads / key heads).  All matrices BF16; head_dim a multiple of 8 up to 128;
+ * data 16-byte aligned, ld >= cols and a multiple of 8 (rows go through the tensor memory accelerator).  lse: fp32,
+ * heads x tokens.  Rows that belong to no sequence (in front of starts[0], behind the last one) are left as they
+ * were in every output, and what they hold in the inputs, NaN included, reaches no result; nor does what one sequence
+ * holds reach another.  Inside a sequence a NaN or infinity in k reaches only queries that see it; in v (and backwards
+ * in q and dout) it may also reach rows of the same block of 128 on the other side of the diagonal, through 0 * infinity.
+ *
+ * dte_attention_plan reads the n_sequences + 1 starts (DEVICE, not decreasing, inside [0, tokens]; empty sequences are
+ * allowed) once per packed batch and leaves in `plan` (DEVICE, 256-byte aligned) the order of work that the calls on
+ * batches with these starts take, in every layer, forwards and backwards.  Starts that decrease or leave the range set
+ * DTE_DEV_BOUNDS and give a plan without work; a call whose token count differs from its plan's sets DTE_DEV_BOUNDS and
+ * writes nothing.  plan_bytes of the calls: the size of the plan's buffer.  At most 2^24 tokens and 2^20 sequences. */
+DTE_API uint64_t dte_attention_plan_bytes(uint64_t tokens, uint64_t n_sequences);
+DTE_API dte_status dte_attention_plan(const dte_ids* starts, uint64_t tokens, void* plan, uint64_t plan_bytes, uint64_t* flags,
+                                      int device, void* cuda_stream);
+DTE_API dte_status dte_attention_forward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
+                                         const void* plan, uint64_t plan_bytes, double scale, const dte_matrix* out, float* lse,
+                                         uint64_t* flags, int device, void* cuda_stream);
+
+/* Gradients of dte_attention_forward from its outputs and dout, with p = exp(z - lse) and delta = sum over columns of dout * out:
+ *   dv = p^T dout,  dz = p (dout v^T - delta),  dq = scale * dz k,  dk = scale * dz^T q
+ * dk and dv are sums over the query heads of a key head.  Deterministic; the scores are made again in both passes over them. */
+DTE_API uint64_t dte_attention_backward_workspace_bytes(uint64_t tokens, uint64_t heads);
+DTE_API dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
+                                          const dte_matrix* out, const float* lse, const dte_matrix* dout, const void* plan,
+                                          uint64_t plan_bytes, double scale, const dte_matrix* dq, const dte_matrix* dk,
+                                          const dte_matrix* dv, void* workspace, uint64_t workspace_bytes, uint64_t* flags,
+                                          int device, void* cuda_stream);
+
+/* Global gradient norm and clipping over many tensors.  The array is HOST memory, read before the call returns; each entry is a
+ * contiguous DEVICE tensor of any size (0 included) and any alignment of its type.  At most 2^20 tensors and 2^44
+ * elements in a call. */
+typedef struct dte_tensor {
+    void* data;
+    uint64_t numel;
+    uint32_t dtype; /* DTE_F32 or DTE_BF16 */
+    uint32_t reserved;
+} dte_tensor;
+
+/* *sum_squares (DEVICE, fp64) = sum of the squares of all elements, added to what it holds if accumulate != 0.  Ranks that
+ * hold parts of the gradients add their sums before clipping.  Squares that fp32 would overflow or lose are
+ * formed in fp64; sums of 32 to 64 squares in fp32, everything beyond in fp64, in an order that does not depend on the device. */
+DTE_API uint64_t dte_grad_sum_squares_workspace_bytes(uint64_t n_tensors);
+DTE_API dte_status dte_grad_sum_squares(const dte_tensor* tensors, uint64_t n_tensors, int accumulate, double* sum_squares,
+                                        void* workspace, uint64_t workspace_bytes, int device, void* cuda_stream);
+
+/* norm = sqrt(*sum_squares), to *norm (DEVICE, fp32, may be NULL); every element times max_norm / norm where norm > max_norm, unchanged
+ * otherwise and where the norm is not finite (a step to be skipped: the caller sees it in *norm).  outs: HOST array, n_tensors
+ * entries with the tensors' sizes and types of their own, or NULL for in place; an entry may be its tensor itself
+ * (same data and dtype), else it overlaps no tensor.  In place with nothing to clip, nothing is read or written.  max_norm > 0. */
+DTE_API dte_status dte_grad_clip(const dte_tensor* tensors, uint64_t n_tensors, const double* sum_squares, double max_norm,
+                                 const dte_tensor* outs, float* norm, int device, void* cuda_stream);
+
 /* Static strings. */
 DTE_API const char* dte_status_string(dte_status s);
 /* Message of the calling thread's most recent failed call ("" if none). */

@@ -34,6 +34,9 @@ SYMBOLS = [
     "dte_linear_ce_forward", "dte_linear_ce_forward_workspace_bytes", "dte_linear_ce_backward",
     "dte_linear_ce_backward_workspace_bytes", "dte_linear_ce_backward_workspace_min_bytes",
     "dte_linear_ce_set_wait_limit",
+    "dte_rope_frequencies", "dte_rope", "dte_attention_plan_bytes", "dte_attention_plan", "dte_attention_forward",
+    "dte_attention_backward_workspace_bytes", "dte_attention_backward",
+    "dte_grad_sum_squares_workspace_bytes", "dte_grad_sum_squares", "dte_grad_clip",
 ]
 
 
@@ -140,12 +143,21 @@ def lib() -> C.CDLL:
         L.dte_norm_backward.argtypes = [vp, vp, vp, u32, u32, vp, vp, i, vp, vp, vp, vp, u64, i, vp]
         L.dte_linear_ce_forward.argtypes = [vp, vp, vp, u64, u64, dbl, vp, vp, vp, vp, u64, vp, i, vp]
         L.dte_linear_ce_backward.argtypes = [vp, vp, vp, u64, u64, dbl, vp, vp, i, vp, vp, vp, u64, vp, i, vp]
+        L.dte_rope_frequencies.argtypes = [u32, dbl, u32, dbl, dbl, dbl, dbl, vp, vp]
+        L.dte_rope.argtypes = [vp, vp, u32, vp, vp, u32, u32, dbl, i, vp, vp, i, vp]
+        L.dte_attention_plan.argtypes = [vp, u64, vp, u64, vp, i, vp]
+        L.dte_attention_forward.argtypes = [vp, vp, vp, u32, vp, u64, dbl, vp, vp, vp, i, vp]
+        L.dte_attention_backward.argtypes = [vp, vp, vp, u32, vp, vp, vp, vp, u64, dbl, vp, vp, vp, vp, u64, vp, i, vp]
+        L.dte_grad_sum_squares.argtypes = [vp, u64, i, vp, vp, u64, i, vp]
+        L.dte_grad_clip.argtypes = [vp, u64, vp, dbl, vp, vp, i, vp]
         for name in ("dte_embedding_forward", "dte_embedding_backward", "dte_norm_forward", "dte_norm_backward",
-                     "dte_linear_ce_forward", "dte_linear_ce_backward"):
+                     "dte_linear_ce_forward", "dte_linear_ce_backward", "dte_rope_frequencies", "dte_rope", "dte_attention_plan",
+                     "dte_attention_forward", "dte_attention_backward", "dte_grad_sum_squares", "dte_grad_clip"):
             getattr(L, name).restype = i
         for name, n_args in (("dte_embedding_backward_workspace_bytes", 2), ("dte_norm_backward_workspace_bytes", 2),
                              ("dte_linear_ce_forward_workspace_bytes", 3), ("dte_linear_ce_backward_workspace_bytes", 3),
-                             ("dte_linear_ce_backward_workspace_min_bytes", 3)):
+                             ("dte_linear_ce_backward_workspace_min_bytes", 3), ("dte_attention_plan_bytes", 2),
+                             ("dte_attention_backward_workspace_bytes", 2), ("dte_grad_sum_squares_workspace_bytes", 1)):
             getattr(L, name).argtypes = [u64] * n_args
             getattr(L, name).restype = u64
         L.dte_linear_ce_set_wait_limit.argtypes = [u32]

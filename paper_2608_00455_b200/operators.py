@@ -1,5 +1,6 @@
-"""Embedding lookup, layer / RMS norm and the linear head's cross entropy, with their gradients: argument
-marshalling for the operators of the C ABI (include/dte.h says what each computes).
+"""Embedding lookup, layer / RMS norm, rotary positions, causal attention over packed sequences and the linear head's
+cross entropy, with their gradients, and the global gradient norm with clipping: argument marshalling for the
+operators of the C ABI (include/dte.h says what each computes).
 
 Tensors are CUDA tensors the caller owns; every call enqueues on `stream` (default: the current stream of the
 tensors' device) and returns.  A tensor that belongs to another stream is the caller's to order and to
@@ -12,8 +13,9 @@ rows a fixed stride apart.  Workspaces are uint8 tensors of at least the bytes t
 """
 from __future__ import annotations
 
+import ctypes
 import struct
-from typing import Optional
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -21,16 +23,19 @@ from .binding import DTE_OK, DteError, _check, lib
 
 DTE_F32, DTE_BF16, DTE_I32, DTE_I64 = 0, 1, 2, 3
 DTE_NORM_LAYER, DTE_NORM_RMS = 0, 1
+DTE_ROPE_HALF, DTE_ROPE_INTERLEAVED = 0, 1
+DTE_ROPE_PLAIN, DTE_ROPE_LINEAR, DTE_ROPE_BASE, DTE_ROPE_RAMP = 0, 1, 2, 3
 _INVALID_ARG = 1
 
 _NUMBERS = {torch.float32: DTE_F32, torch.bfloat16: DTE_BF16}
 _IDS = {torch.int32: DTE_I32, torch.int64: DTE_I64}
 
 
-# dte_matrix and dte_ids of the C ABI as packed bytes (natural alignment, no padding): cheaper to make per call than
+# dte_matrix, dte_ids and dte_tensor of the C ABI as packed bytes (natural alignment, no padding): cheaper to make per call than
 # a ctypes structure
 _pack_matrix = struct.Struct("=QQQQII").pack
 _pack_ids = struct.Struct("=QQII").pack
+_pack_tensor = _pack_ids
 assert struct.calcsize("=QQQQII") == 40 and struct.calcsize("=QQII") == 24
 
 
@@ -276,3 +281,152 @@ def dte_linear_ce_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch
                                        _vector(lse, "lse", device, n), _vector(dloss, "dloss", device, n),
                                        bool(accumulate), d, g, ws,
                                        size, _flags(flags, device), device, _stream(stream, device)))
+
+
+def _heads(t: torch.Tensor, name: str, device: int):
+    """(packed dte_matrix, tokens, heads, head_dim) of a tensor (tokens, heads, head_dim) whose heads lie side by side."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _same_device(t, name, device)
+    dtype = _NUMBERS.get(t.dtype)
+    if dtype is None:
+        _refuse(f"{name} must be float32 or bfloat16")
+    if t.dim() != 3:
+        _refuse(f"{name} must be tokens x heads x head_dim")
+    tokens, heads, dim = t.shape
+    ld, step, unit = t.stride()
+    if (unit != 1 and dim != 1) or (step != dim and heads != 1):
+        _refuse(f"{name}: the heads of a token must lie side by side")
+    return _pack_matrix(t.data_ptr(), tokens, heads * dim, heads * dim if tokens == 1 else ld, dtype, 0), tokens, heads, dim
+
+
+def dte_rope_frequencies(rot: int, base: float, scaling: int = DTE_ROPE_PLAIN, factor: float = 1.0, original_positions: float = 0.0,
+                         fast_turns: float = 32.0, slow_turns: float = 1.0) -> Tuple[torch.Tensor, float]:
+    """(radians per position of each of the rot / 2 pairs: a float64 tensor on the CPU, amplitude)."""
+    if not 0 <= rot < 2 ** 32 or not 0 <= scaling < 2 ** 32:
+        _refuse("rot and scaling must not be negative")
+    f, amplitude = (ctypes.c_double * max(1, min(rot, 1024) // 2))(), ctypes.c_double()
+    _done(lib().dte_rope_frequencies(rot, base, scaling, factor, original_positions, fast_turns, slow_turns, f, ctypes.byref(amplitude)))
+    return torch.tensor(list(f), dtype=torch.float64), amplitude.value
+
+
+def dte_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor,
+             q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, interleaved: bool = False,
+             amplitude: float = 1.0, inverse: bool = False, stream=None) -> None:
+    """Turns the first 2 * len(frequencies) columns of every head of q and k (tokens, heads, head_dim) by positions * frequencies,
+    in place where no output is given; inverse: the gradient."""
+    device = _device(q, "q")
+    m, _, _, dim = _heads(q, "q", device)
+    o = m if q_out is None else _heads(q_out, "q_out", device)[0]
+    mk = ok = None
+    if k is not None:
+        mk, _, _, dim_k = _heads(k, "k", device)
+        if dim_k != dim:
+            _refuse("q and k must have one head_dim")
+        ok = mk if k_out is None else _heads(k_out, "k_out", device)[0]
+    elif k_out is not None:
+        _refuse("k_out without k")
+    p, _ = _ids(positions, "positions", device)
+    if not isinstance(frequencies, torch.Tensor) or frequencies.dim() != 1:
+        _refuse("frequencies must be a vector")
+    pairs = frequencies.numel()
+    f = _vector(frequencies, "frequencies", device, pairs, (torch.float64,))
+    _done(lib().dte_rope(m, mk, dim, p, f, 2 * pairs, DTE_ROPE_INTERLEAVED if interleaved else DTE_ROPE_HALF, amplitude, bool(inverse),
+                         o, ok, device, _stream(stream, device)))
+
+
+def dte_attention_plan_bytes(tokens: int, n_sequences: int) -> int:
+    return lib().dte_attention_plan_bytes(tokens, n_sequences)
+
+
+def dte_attention_plan(starts: torch.Tensor, tokens: int, plan: torch.Tensor, flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Leaves in plan the order of work on sequences starts[s] .. starts[s + 1] - 1 of a batch of `tokens` rows."""
+    device = _device(starts, "starts")
+    if tokens < 0:
+        _refuse("tokens must not be negative")
+    i, _ = _ids(starts, "starts", device)
+    ws, size = _workspace(plan, device)
+    _done(lib().dte_attention_plan(i, tokens, ws, size, _flags(flags, device), device, _stream(stream, device)))
+
+
+def _per_head(t: Optional[torch.Tensor], name: str, device: int, heads: int, tokens: int):
+    if t is not None and tuple(t.shape) != (heads, tokens):
+        _refuse(f"{name} must be heads x tokens")
+    return _vector(t, name, device, heads * tokens)
+
+
+def dte_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: torch.Tensor, out: torch.Tensor,
+                          lse: Optional[torch.Tensor], scale: Optional[float] = None, flags: Optional[torch.Tensor] = None,
+                          stream=None) -> None:
+    """Causal attention of q (tokens, heads, head_dim) over k and v (tokens, key heads, head_dim) of its sequence; lse (heads,
+    tokens) is what the backward pass reads.  scale: 1 / sqrt(head_dim) unless given."""
+    device = _device(q, "q")
+    m, tokens, heads, dim = _heads(q, "q", device)
+    mk, mv, mo = (_heads(t, name, device) for t, name in ((k, "k"), (v, "v"), (out, "out")))
+    if not dim == mk[3] == mv[3] == mo[3]:
+        _refuse("q, k, v and out must have one head_dim")
+    ws, size = _workspace(plan, device)
+    _done(lib().dte_attention_forward(m, mk[0], mv[0], dim, ws, size, dim ** -0.5 if scale is None else scale, mo[0],
+                                      _per_head(lse, "lse", device, heads, tokens), _flags(flags, device), device,
+                                      _stream(stream, device)))
+
+
+def dte_attention_backward_workspace_bytes(tokens: int, heads: int) -> int:
+    return lib().dte_attention_backward_workspace_bytes(tokens, heads)
+
+
+def dte_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                           plan: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, workspace: torch.Tensor,
+                           scale: Optional[float] = None, flags: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of dte_attention_forward from its outputs and dout."""
+    device = _device(q, "q")
+    m, tokens, heads, dim = _heads(q, "q", device)
+    others = [_heads(t, name, device) for t, name in ((k, "k"), (v, "v"), (out, "out"), (dout, "dout"), (dq, "dq"), (dk, "dk"), (dv, "dv"))]
+    if any(o[3] != dim for o in others):
+        _refuse("all matrices must have one head_dim")
+    mk, mv, mo, md, gq, gk, gv = (o[0] for o in others)
+    ws, size = _workspace(plan, device)
+    scratch, scratch_size = _workspace(workspace, device)
+    _done(lib().dte_attention_backward(m, mk, mv, dim, mo, _per_head(lse, "lse", device, heads, tokens), md, ws, size,
+                                       dim ** -0.5 if scale is None else scale, gq, gk, gv, scratch, scratch_size,
+                                       _flags(flags, device), device, _stream(stream, device)))
+
+
+def _tensors(tensors: Sequence[torch.Tensor], name: str, device: int) -> bytes:
+    """Packed dte_tensor array."""
+    out = []
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.get_device() != device:
+            _same_device(t, name, device)
+        dtype = _NUMBERS.get(t.dtype)
+        if dtype is None:
+            _refuse(f"{name} must be float32 or bfloat16")
+        if not t.is_contiguous():
+            _refuse(f"{name} must be contiguous")
+        out.append(_pack_tensor(t.data_ptr(), t.numel(), dtype, 0))
+    return b"".join(out)
+
+
+def dte_grad_sum_squares_workspace_bytes(n_tensors: int) -> int:
+    return lib().dte_grad_sum_squares_workspace_bytes(n_tensors)
+
+
+def dte_grad_sum_squares(tensors: Sequence[torch.Tensor], sum_squares: torch.Tensor, workspace: torch.Tensor, accumulate: bool = False,
+                         stream=None) -> None:
+    """sum_squares (one float64) = sum of the squares of all elements of all tensors (accumulate: added to it)."""
+    device = _device(sum_squares, "sum_squares")
+    ws, size = _workspace(workspace, device)
+    _done(lib().dte_grad_sum_squares(_tensors(tensors, "tensors", device), len(tensors), bool(accumulate),
+                                     _vector(sum_squares, "sum_squares", device, 1, (torch.float64,)), ws, size, device,
+                                     _stream(stream, device)))
+
+
+def dte_grad_clip(tensors: Sequence[torch.Tensor], sum_squares: torch.Tensor, max_norm: float, norm: Optional[torch.Tensor] = None,
+                  outs: Optional[Sequence[torch.Tensor]] = None, stream=None) -> None:
+    """Every element times max_norm / norm where norm = sqrt(sum_squares) is finite and larger; into outs, or in place."""
+    device = _device(sum_squares, "sum_squares")
+    if outs is not None and len(outs) != len(tensors):
+        _refuse("outs must have one tensor per tensor")
+    _done(lib().dte_grad_clip(_tensors(tensors, "tensors", device), len(tensors),
+                              _vector(sum_squares, "sum_squares", device, 1, (torch.float64,)), max_norm,
+                              None if outs is None else _tensors(outs, "outs", device), _vector(norm, "norm", device, 1), device,
+                              _stream(stream, device)))
