@@ -610,6 +610,9 @@ DTE_API dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix*
                                           const dte_matrix* dv, void* workspace, uint64_t workspace_bytes, uint64_t* flags,
                                           int device, void* cuda_stream);
 
+/* As dte_linear_ce_set_wait_limit, for the kernels of attention. */
+DTE_API void dte_attention_set_wait_limit(uint32_t tries);
+
 /* Global gradient norm and clipping over many tensors.  The array is HOST memory, read before the call returns; each entry is a
  * contiguous DEVICE tensor of any size (0 included) and any alignment of its type.  At most 2^20 tensors and 2^44
  * elements in a call. */

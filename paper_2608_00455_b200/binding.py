@@ -35,7 +35,7 @@ SYMBOLS = [
     "dte_linear_ce_backward_workspace_bytes", "dte_linear_ce_backward_workspace_min_bytes",
     "dte_linear_ce_set_wait_limit",
     "dte_rope_frequencies", "dte_rope", "dte_attention_plan_bytes", "dte_attention_plan", "dte_attention_forward",
-    "dte_attention_backward_workspace_bytes", "dte_attention_backward",
+    "dte_attention_backward_workspace_bytes", "dte_attention_backward", "dte_attention_set_wait_limit",
     "dte_grad_sum_squares_workspace_bytes", "dte_grad_sum_squares", "dte_grad_clip",
 ]
 
@@ -162,6 +162,8 @@ def lib() -> C.CDLL:
             getattr(L, name).restype = u64
         L.dte_linear_ce_set_wait_limit.argtypes = [u32]
         L.dte_linear_ce_set_wait_limit.restype = None
+        L.dte_attention_set_wait_limit.argtypes = [u32]
+        L.dte_attention_set_wait_limit.restype = None
         L.dte_status_string.argtypes = [C.c_int]
         L.dte_status_string.restype = C.c_char_p
         L.dte_last_error.argtypes = []

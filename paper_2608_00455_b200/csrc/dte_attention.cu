@@ -1,4 +1,7 @@
 // Causal attention over packed sequences with grouped heads, and its gradient.
+#include <atomic>
+
+#include "dte_mma.cuh"
 #include "dte_ops.cuh"
 
 namespace dte {
@@ -10,6 +13,7 @@ constexpr uint32_t kPlanLevels = 4096;
 constexpr uint64_t kPlanMagic = 0x6474652d61747431ull;
 constexpr uint64_t kMaxAttTokens = 1ull << 24, kMaxSequences = 1ull << 20;
 constexpr uint64_t kPlanHeader = 256;
+constexpr double kLog2eD = 1.44269504088896340736;
 
 // One tile of one sequence.
 struct PlanItem {
@@ -112,7 +116,10 @@ struct AttParams {
     const uint8_t* plan;
     uint64_t plan_bytes, tokens;
     uint32_t head_dim, group;
-    float scale;
+    uint32_t units;            // of work per tile: pairs of query heads, or query heads
+    bool pair_heads;
+    uint32_t wait_limit;       // tries of a wait inside the kernel
+    float scale, k2;           // k2: scale * log2(e)
     const __nv_bfloat16 *q, *k, *v, *o, *d_o;
     uint64_t q_ld, k_ld, v_ld, o_ld, do_ld;
     __nv_bfloat16 *out, *dq, *dk, *dv;
@@ -122,13 +129,14 @@ struct AttParams {
     uint64_t* flags;
 };
 
-// Tiles of a plan that was made for this many tokens and lies in its buffer; another one's are none, and flagged.
-__device__ __forceinline__ uint32_t plan_tiles(const AttParams& p) {
+// Whether a plan was made for this many tokens and lies in its buffer; another one is flagged.
+__device__ __forceinline__ bool plan_ok(const AttParams& p) {
     const PlanHead* h = reinterpret_cast<const PlanHead*>(p.plan);
-    if (h->magic == kPlanMagic && h->tokens == p.tokens && h->pairs_at + (uint64_t)h->pairs * sizeof(PlanItem) <= p.plan_bytes) return h->tiles;
+    if (h->magic == kPlanMagic && h->tokens == p.tokens && h->pairs_at + (uint64_t)h->pairs * sizeof(PlanItem) <= p.plan_bytes) return true;
     if (threadIdx.x + blockIdx.x + blockIdx.y == 0 && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
-    return 0;
+    return false;
 }
+__device__ __forceinline__ uint32_t plan_tiles(const AttParams& p) { return plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles : 0; }
 
 struct Row {
     float f[4];
@@ -149,29 +157,346 @@ struct Row {
     __device__ void zero() { for (int j = 0; j < 4; ++j) f[j] = 0; }
 };
 
-__global__ void __launch_bounds__(256) att_forward_kernel(const AttParams p) {
-    if (blockIdx.x >= plan_tiles(p)) return;
-    const PlanItem it = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)[blockIdx.x];
-    const uint32_t lane = threadIdx.x & 31, d = p.head_dim, h = blockIdx.y, kh = h / p.group;
-    for (uint32_t r = it.tile * kAttTile + threadIdx.x / 32; r < min(it.len, (it.tile + 1) * kAttTile); r += 8) {
-        const uint64_t row = it.start + r;
-        Row q, k, o;
-        q.load(p.q + row * p.q_ld + h * d, lane, d);
-        o.zero();
-        float top = -INFINITY, sum = 0;
-        for (uint32_t j = 0; j <= r; ++j) {
-            k.load(p.k + (uint64_t)(it.start + j) * p.k_ld + kh * d, lane, d);
-            const float z = q.dot(k) * p.scale, now = fmaxf(top, z), from = now == -INFINITY ? 0.f : now;
-            const float w = expf(z - from), keep = expf(top - from);
-            k.load(p.v + (uint64_t)(it.start + j) * p.v_ld + kh * d, lane, d);
-            o.mul(keep);
-            o.add(w, k);
-            sum = sum * keep + w;
-            top = now;
-        }
-        o.store(p.out + row * p.out_ld + h * d, lane, d, 1.f / sum);
-        if (p.lse && lane == 0) p.lse[h * p.tokens + row] = top + logf(sum);
+// ---- forward ------------------------------------------------------------------------------------------------
+// One CTA per SM takes pairs of tiles of 128 queries that share keys and values: two query heads of one key head, or, where the
+// group of query heads is odd, two neighbouring tiles of one head.  Each half of the pair ("slot") has its own
+// accumulators in tensor memory and its own four softmax warps, so that the tensor cores work for one slot while the other
+// one's exponentials are made.  Per tile of 128 keys and slot:
+//   MMA warp       S = Q K^T into tensor memory                               -> s_full
+//   softmax warps  row maximum, P = exp2(S - m) as bf16 over S, sums in fp32  -> p_full
+//   MMA warp       O += P V, P straight from tensor memory
+// A thread holds a whole row of S (tensor memory's lane), so no reduction crosses threads.
+// A warpgroup of which one warp loads and one issues products, then one per slot.  Registers: 168 each at launch, 384 * 168 = 64512
+// in all; the first warpgroup gives up what the others, with whole rows of S in registers, take: 128 * (72 + 2 * 208) = 62464.
+constexpr uint32_t kFwdThreads = 3 * 128;
+constexpr int kFewRegs = 72, kManyRegs = 208;
+constexpr uint32_t kTileBytes = kAttTile * 256;   // 128 rows of up to 128 bf16: chunks of 64 columns, 16 KB each
+constexpr uint32_t kChunkBytes = kAttTile * 128;
+constexpr uint32_t kFwdRing = 5;                  // tiles of K and V in flight, in turn
+constexpr uint32_t kFwdSmem = (2 + kFwdRing) * kTileBytes + 1024;
+// O is brought to a new maximum only when that has grown by more than 2^8: until then P is up to 2^8 instead of 1, which costs
+// bf16 and fp32 nothing.
+constexpr float kRescaleAbove = 8.f;
+
+struct FwdWork {
+    uint32_t start, len;
+    uint32_t n[2], row0[2], head[2];     // per slot: tiles of keys (0: the slot is empty), first row, query head
+    uint32_t kv_head, n_max;
+};
+
+__device__ __forceinline__ FwdWork fwd_work(const AttParams& p, const PlanItem* list, uint32_t w) {
+    const uint32_t rank = w / p.units, unit = w - rank * p.units;
+    const PlanItem it = list[rank];
+    FwdWork f;
+    f.start = it.start;
+    f.len = it.len;
+    if (p.pair_heads) {
+        f.head[0] = 2 * unit;
+        f.head[1] = 2 * unit + 1;
+        f.row0[0] = f.row0[1] = it.tile * kAttTile;
+        f.n[0] = f.n[1] = it.tile + 1;
+    } else {
+        f.head[0] = f.head[1] = unit;
+        f.row0[0] = 2 * it.tile * kAttTile;
+        f.row0[1] = f.row0[0] + kAttTile;
+        f.n[0] = 2 * it.tile + 1;
+        f.n[1] = f.row0[1] < it.len ? 2 * it.tile + 2 : 0;
     }
+    f.kv_head = f.head[0] / p.group;
+    f.n_max = max(f.n[0], f.n[1]);
+    return f;
+}
+
+// Both chunks of a tile of 128 rows of a head.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t chunks, uint32_t head, uint32_t row, uint32_t bar) {
+    for (uint32_t c = 0; c < chunks; ++c) tma_load_3d<1>(dst + c * kChunkBytes, map, (int)(c * 64), (int)head, (int)row, bar);
+}
+
+// Rows from `from` on of a tile in shared memory become zeros, by one warp: rows of another sequence, or of none, would otherwise
+// meet zeros of P, and 0 * NaN is NaN.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from) {
+    const uint32_t per = (kAttTile - from) * 8;
+    for (uint32_t i = threadIdx.x & 31; i < per * chunks; i += 32) {
+        const uint32_t c = i / per, r = i - c * per;
+        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + from * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+// D (+)= A B^T over head_dim: both operands rows of a head, along their columns.
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t steps, uint32_t desc) {
+    for (uint32_t i = 0; i < steps; ++i) {
+        const uint32_t at = (i / 4) * kChunkBytes + (i % 4) * 32;
+        mma_bf16<1>(d, operand_desc(a + at, 16), operand_desc(b + at, 16), desc, i != 0);
+    }
+}
+
+// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head.
+__device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
+#pragma unroll
+    for (uint32_t i = 0; i < kAttTile / 16; ++i) mma_bf16_tmem(d, a + i * 8, operand_desc(b + i * 2048, kChunkBytes), desc, add || i != 0);
+}
+
+__global__ void __launch_bounds__(kFwdThreads, 1)
+    att_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttParams p) {
+    extern __shared__ uint8_t att_smem_raw[];
+    __shared__ __align__(8) uint64_t s_bar[2 * kFwdRing + 10 + 1];
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_q_issued[2], s_q_taken[2];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)att_smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t q0 = smem_addr(smem), ring0 = q0 + 2 * kTileBytes, bar0 = smem_addr(s_bar);
+    auto full = [&](uint32_t i) { return bar0 + 8 * i; };
+    auto empty = [&](uint32_t i) { return bar0 + 8 * (kFwdRing + i); };
+    auto bar = [&](uint32_t kind, uint32_t s) { return bar0 + 8 * (2 * kFwdRing + 2 * kind + s); };
+    enum { kQFull, kQEmpty, kSFull, kPFull, kOFull };
+    const uint32_t last_bar = bar0 + 8 * (2 * kFwdRing + 10);
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&map_q);
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+        for (uint32_t i = 0; i < 2 * kFwdRing; ++i) mbar_init(bar0 + 8 * i, 1);
+        for (uint32_t s = 0; s < 2; ++s) {
+            mbar_init(bar(kQFull, s), 1);
+            mbar_init(bar(kQEmpty, s), 1);
+            mbar_init(bar(kSFull, s), 1);
+            mbar_init(bar(kPFull, s), 4);
+            mbar_init(bar(kOFull, s), 1);
+        }
+        mbar_init(last_bar, 1);
+        s_gave_up = s_issued = s_taken = s_q_issued[0] = s_q_issued[1] = s_q_taken[0] = s_q_taken[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<1>(smem_addr(&s_tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;         // S of the slots at columns 0 and 128, O at 256 and 384
+    volatile uint32_t* gave_up = &s_gave_up;
+    const PlanHead* head = reinterpret_cast<const PlanHead*>(p.plan);
+    const uint32_t items = plan_ok(p) ? (p.pair_heads ? head->tiles : head->pairs) : 0, total = items * p.units;
+    const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + (p.pair_heads ? kPlanHeader : items ? head->pairs_at : 0));
+    const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
+
+    if (warp < 4) {
+    regs_down<kFewRegs>();
+    if (warp == 0 && lane == 0) {
+        // ---- loads ----
+        uint32_t issued = 0, q_issued[2] = {0, 0};
+        bool ok = true;
+        auto load = [&](const CUtensorMap* map, uint32_t head_at, uint32_t row) {
+            const uint32_t i = issued % kFwdRing;
+            if (!(ok = ok && mbar_wait(empty(i), (issued / kFwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
+            mbar_expect_tx(full(i), tile_bytes);
+            load_rows(ring0 + i * kTileBytes, map, chunks, head_at, row, full(i));
+            ++issued;
+        };
+        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
+            const FwdWork f = fwd_work(p, list, w);
+            for (uint32_t s = 0; s < 2 && ok; ++s) {
+                if (!f.n[s]) continue;
+                if (!(ok = mbar_wait(bar(kQEmpty, s), (q_issued[s] & 1) ^ 1, p.wait_limit, gave_up))) break;
+                mbar_expect_tx(bar(kQFull, s), tile_bytes);
+                load_rows(q0 + s * kTileBytes, &map_q, chunks, f.head[s], f.start + f.row0[s], bar(kQFull, s));
+                ++q_issued[s];
+                if (s == 0) load(&map_k, f.kv_head, f.start);
+            }
+            for (uint32_t t = 0; t < f.n_max && ok; ++t) {
+                load(&map_v, f.kv_head, f.start + t * kAttTile);
+                if (t + 1 < f.n_max) load(&map_k, f.kv_head, f.start + (t + 1) * kAttTile);
+            }
+        }
+        s_issued = issued;
+        s_q_issued[0] = q_issued[0];
+        s_q_issued[1] = q_issued[1];
+    } else if (warp == 1) {
+        // ---- matrix products: the whole warp waits, one lane issues ----
+        const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false);
+        const uint32_t desc_o = mma_desc(kAttTile, (p.head_dim + 15) / 16 * 16, false, true), steps = (p.head_dim + 15) / 16;
+        uint32_t taken = 0, q_taken[2] = {0, 0}, p_taken[2] = {0, 0};
+        bool ok = true;
+        auto wait = [&](uint32_t b, uint32_t parity) {
+            ok = ok && mbar_wait(b, parity, p.wait_limit, gave_up);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            tc_fence_after();
+            return ok;
+        };
+        auto take = [&]() {                       // the next tile of the ring; where it lies
+            const uint32_t i = taken % kFwdRing;
+            if (wait(full(i), taken / kFwdRing & 1)) ++taken;
+            return i;
+        };
+        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
+            const FwdWork f = fwd_work(p, list, w);
+            auto scores = [&](uint32_t s, uint32_t t, uint32_t k) {
+                if (t == 0) {
+                    if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
+                    ++q_taken[s];
+                }
+                if (lane == 0) {
+                    mma_rows(tmem + s * 128, q0 + s * kTileBytes, ring0 + k * kTileBytes, steps, desc_s);
+                    mma_commit<1>(bar(kSFull, s));
+                    if (t + 1 == f.n[s]) mma_commit<1>(bar(kQEmpty, s));
+                }
+            };
+            const uint32_t k0 = take();
+            for (uint32_t s = 0; s < 2 && ok; ++s)
+                if (f.n[s]) scores(s, 0, k0);
+            if (lane == 0 && ok) mma_commit<1>(empty(k0));
+            for (uint32_t t = 0; t < f.n_max && ok; ++t) {
+                const uint32_t v = take();
+                if (!ok) break;
+                if ((t + 1) * kAttTile > f.len) clear_rows(smem + (2 + v) * kTileBytes, chunks, f.len - t * kAttTile);
+                uint32_t k = 0;
+                for (uint32_t s = 0; s < 2 && ok; ++s) {
+                    if (t >= f.n[s]) continue;
+                    if (!wait(bar(kPFull, s), p_taken[s] & 1)) break;
+                    ++p_taken[s];
+                    if (lane == 0) {
+                        mma_tile(tmem + 256 + s * 128, tmem + s * 128, ring0 + v * kTileBytes, desc_o, t != 0);
+                        if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
+                    }
+                    if (t + 1 < f.n[s]) {
+                        if (s == 0 || t + 1 >= f.n[0]) k = take();
+                        if (ok) scores(s, t + 1, k);
+                    }
+                }
+                if (lane == 0 && ok) {
+                    mma_commit<1>(empty(v));
+                    if (t + 1 < f.n_max) mma_commit<1>(empty(k));
+                }
+            }
+        }
+        if (lane == 0) {
+            s_taken = taken;
+            s_q_taken[0] = q_taken[0];
+            s_q_taken[1] = q_taken[1];
+        }
+    }
+    } else {
+        regs_up<kManyRegs>();
+        // ---- softmax: warp w may read the quarter w % 4 of tensor memory's lanes ----
+        const uint32_t s = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t lanes = quarter * 32 << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
+        const float k2 = p.k2;
+        uint32_t s_taken_ = 0, o_taken = 0;
+        bool ok = true;
+        auto wait = [&](uint32_t b, uint32_t parity) {
+            ok = mbar_wait(b, parity, p.wait_limit, gave_up);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            tc_fence_after();
+            return ok;
+        };
+        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
+            const FwdWork f = fwd_work(p, list, w);
+            if (!f.n[s]) continue;
+            const uint32_t row = f.row0[s] + r;             // in its sequence
+            float top = -INFINITY, sum = 0.f;               // top: what O and sum are relative to
+            for (uint32_t t = 0; t < f.n[s]; ++t) {
+                if (!wait(bar(kSFull, s), s_taken_++ & 1)) break;
+                float z[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    tmem_load32(s_at + c * 32, v);
+                    tmem_load_wait(v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[c * 32 + j] = __uint_as_float(v[j]);
+                }
+                if (t + 1 == f.n[s]) {                      // the tile on the diagonal
+#pragma unroll
+                    for (int j = 0; j < 128; ++j) z[j] = (uint32_t)j > r ? -INFINITY : z[j];
+                }
+                float peak = top;
+#pragma unroll
+                for (int j = 0; j < 128; ++j) peak = fmaxf(peak, z[j]);
+                if (t == 0) {
+                    top = peak;
+                } else if (__any_sync(0xFFFFFFFFu, (peak - top) * k2 > kRescaleAbove)) {
+                    const float by = peak == -INFINITY ? 1.f : exp2_fast((top - peak) * k2);
+                    top = peak;
+                    sum *= by;
+                    for (uint32_t c = 0; c < p.head_dim; c += 32) {
+                        uint32_t v[32];
+                        tmem_load32(o_at + c, v);
+                        tmem_load_wait(v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
+                        tmem_store32(o_at + c, v);
+                    }
+                }
+                const float from = top == -INFINITY ? 0.f : -top * k2;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float a = exp2_fast(fmaf(z[c * 64 + 2 * j], k2, from)), b = exp2_fast(fmaf(z[c * 64 + 2 * j + 1], k2, from));
+                        part[j & 1] += a;
+                        part[2 + (j & 1)] += b;
+                        v[j] = pack_bf16(a, b);
+                    }
+                    tmem_store32(s_at + c * 32, v);
+                }
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kPFull, s));
+            }
+            if (!ok || !wait(bar(kOFull, s), o_taken++ & 1)) break;
+            const bool valid = row < f.len;
+            const uint64_t at = (uint64_t)f.start + row;
+            if (valid && p.lse) p.lse[f.head[s] * p.tokens + at] = fmaf(top, p.scale, logf(sum));
+            const float by = 1.f / sum;
+            __nv_bfloat16* out = p.out + at * p.out_ld + f.head[s] * p.head_dim;
+            for (uint32_t c = 0; c < p.head_dim; c += 32) {
+                uint32_t v[32];
+                tmem_load32(o_at + c, v);
+                tmem_load_wait(v);
+                if (!valid) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c + 8 * j >= p.head_dim) break;
+                    float o[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(v[8 * j + i]) * by;
+                    Raw8<__nv_bfloat16> x;
+                    x.set(o);
+                    x.store(out + c + 8 * j);
+                }
+            }
+            tc_fence_before();
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    const bool failed = *gave_up;
+    if (failed) {
+        // A wait ran out: all roles have stopped.  What they left in flight ends here, again with a limit: the products, and every
+        // load that no product has waited for.
+        if (warp == 1 && lane == 0) {
+            mma_commit<1>(last_bar);
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(last_bar, 0); ++i) {}
+        }
+        if (threadIdx.x == 0) {
+            uint32_t left = kWaitTries;
+            for (uint32_t i = s_taken; i < s_issued; ++i)
+                while (left && !mbar_try_wait(full(i % kFwdRing), i / kFwdRing & 1)) --left;
+            for (uint32_t s = 0; s < 2; ++s)
+                for (uint32_t i = s_q_taken[s]; i < s_q_issued[s]; ++i)
+                    while (left && !mbar_try_wait(bar(kQFull, s), i & 1)) --left;
+        }
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 1) tmem_free<1>(tmem, 512);
+    if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
 }
 
 __global__ void __launch_bounds__(256) att_dq_kernel(const AttParams p) {
@@ -227,6 +552,12 @@ __global__ void __launch_bounds__(256) att_dkv_kernel(const AttParams p) {
 static uint64_t plan_tiles_most(uint64_t tokens, uint64_t n, uint64_t rows) { return tokens / rows + n; }
 static uint64_t plan_pairs_at(uint64_t tokens, uint64_t n) { return kPlanHeader + plan_tiles_most(tokens, n, kAttTile) * sizeof(PlanItem); }
 
+// Tiles that a plan of this size can list; one at least, to look at the plan.
+static uint64_t tiles_most(uint64_t plan_bytes, uint64_t tokens) {
+    const uint64_t room = plan_bytes < kPlanHeader ? 0 : (plan_bytes - kPlanHeader) / sizeof(PlanItem), most = room < tokens ? room : tokens;
+    return most ? most : 1;
+}
+
 static dte_status check_heads(const dte_matrix* m, const char* null_msg, uint32_t head_dim, uint64_t rows, bool output) {
     dte_status s;
     if ((s = check_matrix(m, null_msg, output)) != DTE_OK) return s;
@@ -249,12 +580,23 @@ static dte_status check_attention(const dte_matrix* q, const dte_matrix* k, cons
     if (k->cols != v->cols || q->cols % k->cols) return op_fail(DTE_ERR_INVALID_ARG, "query heads must be a multiple of k's heads, v must have k's");
     if (q->rows > kMaxAttTokens) return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens");
     if (q->cols / head_dim > 65535) return op_fail(DTE_ERR_INVALID_ARG, "at most 65535 heads");
-    if (!(scale > 0) || !std::isfinite((float)(scale * 1.44269504088896340736)))
+    if (tiles_most(plan_bytes, q->rows) * (q->cols / head_dim) >= (1ull << 31))
+        return op_fail(DTE_ERR_INVALID_ARG, "the plan's tiles x heads are too many for one call");
+    if (!(scale > 0) || !std::isfinite((float)(scale * kLog2eD)))
         return op_fail(DTE_ERR_INVALID_ARG, "scale must be > 0 and, times log2(e), finite in fp32");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (!plan || ((uintptr_t)plan & (kWorkspaceAlign - 1)) || plan_bytes < kPlanHeader)
         return op_fail(DTE_ERR_INVALID_ARG, "plan is null, not 256-byte aligned or too small");
     return DTE_OK;
+}
+
+static std::atomic<uint32_t> g_att_wait_limit{kWaitTries};
+
+// A matrix of heads as (column, head, token), read in boxes of 64 columns of one head and kAttTile tokens; columns past the
+// head are zeros.
+static dte_status encode_heads(CUtensorMap* map, const dte_matrix* m, uint32_t head_dim) {
+    const uint64_t ld = m->rows > 1 ? m->ld : m->cols;
+    return encode_3d(map, m->data, {head_dim, m->cols / head_dim, m->rows}, {head_dim * 2ull, ld * 2}, {64, 1, kAttTile});
 }
 
 static AttParams att_params(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim, const void* plan, uint64_t plan_bytes,
@@ -266,6 +608,8 @@ static AttParams att_params(const dte_matrix* q, const dte_matrix* k, const dte_
     p.head_dim = head_dim;
     p.group = (uint32_t)(q->cols / k->cols);
     p.scale = (float)scale;
+    p.k2 = (float)(scale * kLog2eD);
+    p.wait_limit = g_att_wait_limit.load(std::memory_order_relaxed);
     p.q = static_cast<const __nv_bfloat16*>(q->data);
     p.k = static_cast<const __nv_bfloat16*>(k->data);
     p.v = static_cast<const __nv_bfloat16*>(v->data);
@@ -276,15 +620,13 @@ static AttParams att_params(const dte_matrix* q, const dte_matrix* k, const dte_
     return p;
 }
 
-// Tiles that a plan of this size can list; one at least, to look at the plan.
-static unsigned tiles_most(uint64_t plan_bytes, uint64_t tokens) {
-    const uint64_t room = (plan_bytes - kPlanHeader) / sizeof(PlanItem), most = room < tokens ? room : tokens;
-    return (unsigned)(most ? most : 1);
-}
-
 }  // namespace dte
 
 using namespace dte;
+
+extern "C" void dte_attention_set_wait_limit(uint32_t tries) {
+    g_att_wait_limit.store(tries ? tries : kWaitTries, std::memory_order_relaxed);
+}
 
 extern "C" uint64_t dte_attention_plan_bytes(uint64_t tokens, uint64_t n_sequences) {
     if (tokens > kMaxAttTokens || n_sequences > kMaxSequences) return UINT64_MAX;       // refused by the call
@@ -322,15 +664,25 @@ extern "C" dte_status dte_attention_forward(const dte_matrix* q, const dte_matri
     if ((s = check_heads(out, "out is null", head_dim, q->rows, true)) != DTE_OK) return s;
     if (out->cols != q->cols) return op_fail(DTE_ERR_INVALID_ARG, "out must have q's columns");
     if ((uintptr_t)lse & 3u) return op_fail(DTE_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-    const unsigned tiles = tiles_most(plan_bytes, q->rows);
+    const uint64_t tiles = tiles_most(plan_bytes, q->rows);
     if (q->rows == 0) return DTE_OK;
     OpDeviceGuard g;
-    if ((s = g.enter(device)) != DTE_OK) return s;
+    int sms = 0;
+    if ((s = g.enter(device, &sms)) != DTE_OK) return s;
     AttParams p = att_params(q, k, v, head_dim, plan, plan_bytes, scale, flags);
     p.out = static_cast<__nv_bfloat16*>(out->data);
     p.out_ld = out->ld;
     p.lse = lse;
-    att_forward_kernel<<<dim3(tiles, (unsigned)(q->cols / head_dim)), 256, 0, (cudaStream_t)cuda_stream>>>(p);
+    p.pair_heads = p.group % 2 == 0;
+    p.units = (uint32_t)(q->cols / head_dim / (p.pair_heads ? 2 : 1));
+    CUtensorMap mq, mk, mv;
+    if ((s = encode_heads(&mq, q, head_dim)) != DTE_OK) return s;
+    if ((s = encode_heads(&mk, k, head_dim)) != DTE_OK) return s;
+    if ((s = encode_heads(&mv, v, head_dim)) != DTE_OK) return s;
+    static std::atomic<uint64_t> ready{0};
+    if ((s = allow_smem(att_forward_kernel, kFwdSmem, device, ready)) != DTE_OK) return s;
+    const uint64_t work = (uint64_t)tiles * p.units;
+    att_forward_kernel<<<(unsigned)(work < (uint64_t)sms ? work : sms), kFwdThreads, kFwdSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, p);
     DTE_CUDA(cudaGetLastError());
     return DTE_OK;
 }
@@ -357,7 +709,7 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     if (q->rows && (!lse || ((uintptr_t)lse & 3u))) return op_fail(DTE_ERR_INVALID_ARG, "lse is null or not 4-byte aligned");
     const uint64_t heads = q->cols / head_dim;
     if ((s = check_workspace(workspace, workspace_bytes, dte_attention_backward_workspace_bytes(q->rows, heads))) != DTE_OK) return s;
-    const unsigned tiles = tiles_most(plan_bytes, q->rows);
+    const uint64_t tiles = tiles_most(plan_bytes, q->rows);
     if (q->rows == 0) return DTE_OK;
     OpDeviceGuard g;
     if ((s = g.enter(device)) != DTE_OK) return s;
@@ -375,9 +727,9 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     p.lse_in = lse;
     p.delta = static_cast<float*>(workspace);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    att_dq_kernel<<<dim3(tiles, (unsigned)heads), 256, 0, st>>>(p);
+    att_dq_kernel<<<dim3((unsigned)tiles, (unsigned)heads), 256, 0, st>>>(p);
     DTE_CUDA(cudaGetLastError());
-    att_dkv_kernel<<<dim3(tiles, (unsigned)(k->cols / head_dim)), 256, 0, st>>>(p);
+    att_dkv_kernel<<<dim3((unsigned)tiles, (unsigned)(k->cols / head_dim)), 256, 0, st>>>(p);
     DTE_CUDA(cudaGetLastError());
     return DTE_OK;
 }

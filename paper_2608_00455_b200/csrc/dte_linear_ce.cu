@@ -1000,7 +1000,7 @@ static dte_status encode(CUtensorMap* map, const void* base, uint64_t rows, uint
     return DTE_OK;
 }
 
-static dte_status encode_3d(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+dte_status encode_3d(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
                             const cuuint32_t (&box)[3]) {
     EncodeTiled f;
     dte_status s = encoder(&f);

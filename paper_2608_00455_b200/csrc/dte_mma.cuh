@@ -6,7 +6,13 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include "dte.h"
+
 namespace dte {
+
+// Tensor map of a bf16 matrix of three dimensions, 128-byte swizzle; strides in bytes.
+dte_status encode_3d(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+                     const cuuint32_t (&box)[3]);
 
 #ifdef __CUDACC__
 
@@ -36,6 +42,9 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
 }
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // bar: shared::cluster address, possibly of another CTA of the cluster
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
@@ -153,6 +162,20 @@ __device__ __forceinline__ void tmem_load_wait(uint32_t (&r)[32]) {
         : "memory");
 }
 
+// The other way: v[j] becomes column j of this thread's lane; complete after tmem_store_wait.
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // ---- tensor cores ---------------------------------------------------------------------------------------
 // Shared-memory operand descriptor, 128-byte swizzle (descriptor version 1 in bits 46-48, layout 2 in bits
 // 61-63).  K-major tile: rows of 64 bf16 along K, groups of 8 rows 1024 bytes apart (stride offset).
@@ -177,6 +200,12 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
                      "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
                      : "memory");
 }
+// A in tensor memory: 128 lanes are its rows, a column holds two consecutive bf16 along K.
+__device__ __forceinline__ void mma_bf16_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+                 "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+                 : "memory");
+}
 // Arrives on `bar` (in every CTA of the pair) once all MMAs issued so far by this thread have finished.
 template <int CTAS>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -199,6 +228,11 @@ __device__ __forceinline__ void load32(const void* p, uint32_t (&v)[8]) {
                  : "l"(p)
                  : "memory");
 }
+// Registers of a warpgroup (all its threads call this): given up to, or taken from, what the CTA was launched with.
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
