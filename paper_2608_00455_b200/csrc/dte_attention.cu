@@ -1,33 +1,12 @@
 // Causal attention over packed sequences with grouped heads, and its gradient.
 #include <atomic>
 
-#include "dte_mma.cuh"
-#include "dte_ops.cuh"
+#include "dte_attention.cuh"
 
 namespace dte {
 
-constexpr uint32_t kAttTile = 128;               // rows of a tile of queries or keys
-constexpr uint32_t kMaxAttDim = 128;
 constexpr uint32_t kPlanThreads = 1024;
 constexpr uint32_t kPlanLevels = 4096;
-constexpr uint64_t kPlanMagic = 0x6474652d61747431ull;
-constexpr uint64_t kMaxAttTokens = 1ull << 24, kMaxSequences = 1ull << 20;
-constexpr uint64_t kPlanHeader = 256;
-constexpr double kLog2eD = 1.44269504088896340736;
-
-// One tile of one sequence.
-struct PlanItem {
-    uint32_t start, len;       // the sequence's rows
-    uint32_t tile;             // tile of the sequence
-    uint32_t pad;
-};
-
-struct PlanHead {
-    uint64_t magic, tokens;
-    uint32_t tiles, pairs;     // tiles of kAttTile rows, tiles of twice as many
-    uint64_t pairs_at;         // where in the plan the second list starts; the first follows the header
-};
-static_assert(sizeof(PlanItem) == 16 && sizeof(PlanHead) <= kPlanHeader, "");
 
 struct PlanParams {
     const void* starts;
@@ -112,51 +91,6 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     }
 }
 
-struct AttParams {
-    const uint8_t* plan;
-    uint64_t plan_bytes, tokens;
-    uint32_t head_dim, group;
-    uint32_t units;            // of work per tile: pairs of query heads, or query heads
-    bool pair_heads;
-    uint32_t wait_limit;       // tries of a wait inside the kernel
-    float scale, k2;           // k2: scale * log2(e)
-    const __nv_bfloat16 *q, *k, *v, *o, *d_o;
-    uint64_t q_ld, k_ld, v_ld, o_ld, do_ld;
-    __nv_bfloat16 *out, *dq, *dk, *dv;
-    uint64_t out_ld, dq_ld, dk_ld, dv_ld;
-    float *lse, *delta;
-    const float* lse_in;
-    uint64_t* flags;
-};
-
-// Whether a plan was made for this many tokens and lies in its buffer; another one is flagged.
-__device__ __forceinline__ bool plan_ok(const AttParams& p) {
-    const PlanHead* h = reinterpret_cast<const PlanHead*>(p.plan);
-    if (h->magic == kPlanMagic && h->tokens == p.tokens && h->pairs_at + (uint64_t)h->pairs * sizeof(PlanItem) <= p.plan_bytes) return true;
-    if (threadIdx.x + blockIdx.x + blockIdx.y == 0 && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
-    return false;
-}
-__device__ __forceinline__ uint32_t plan_tiles(const AttParams& p) { return plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles : 0; }
-
-struct Row {
-    float f[4];
-    __device__ void load(const __nv_bfloat16* p, uint32_t lane, uint32_t d) {
-        for (int j = 0; j < 4; ++j) f[j] = lane * 4 + j < d ? to_f(p[lane * 4 + j]) : 0.f;
-    }
-    __device__ void store(__nv_bfloat16* p, uint32_t lane, uint32_t d, float s) const {
-        for (int j = 0; j < 4; ++j)
-            if (lane * 4 + j < d) p[lane * 4 + j] = from_f<__nv_bfloat16>(f[j] * s);
-    }
-    __device__ float dot(const Row& o) const {
-        float s = 0;
-        for (int j = 0; j < 4; ++j) s = fmaf(f[j], o.f[j], s);
-        return warp_sum(s);
-    }
-    __device__ void add(float a, const Row& o) { for (int j = 0; j < 4; ++j) f[j] = fmaf(a, o.f[j], f[j]); }
-    __device__ void mul(float a) { for (int j = 0; j < 4; ++j) f[j] *= a; }
-    __device__ void zero() { for (int j = 0; j < 4; ++j) f[j] = 0; }
-};
-
 // ---- forward ------------------------------------------------------------------------------------------------
 // One CTA per SM takes pairs of tiles of 128 queries that share keys and values: two query heads of one key head, or, where the
 // group of query heads is odd, two neighbouring tiles of one head.  Each half of the pair ("slot") has its own
@@ -170,10 +104,8 @@ struct Row {
 // in all; the first warpgroup gives up what the others, with whole rows of S in registers, take: 128 * (72 + 2 * 208) = 62464.
 constexpr uint32_t kFwdThreads = 3 * 128;
 constexpr int kFewRegs = 72, kManyRegs = 208;
-constexpr uint32_t kTileBytes = kAttTile * 256;   // 128 rows of up to 128 bf16: chunks of 64 columns, 16 KB each
-constexpr uint32_t kChunkBytes = kAttTile * 128;
 constexpr uint32_t kFwdRing = 5;                  // tiles of K and V in flight, in turn
-constexpr uint32_t kFwdSmem = (2 + kFwdRing) * kTileBytes + 1024;
+constexpr uint32_t kFwdSmem = (2 + kFwdRing) * kTileBytes;
 // O is brought to a new maximum only when that has grown by more than 2^8: until then P is up to 2^8 instead of 1, which costs
 // bf16 and fp32 nothing.
 constexpr float kRescaleAbove = 8.f;
@@ -207,44 +139,12 @@ __device__ __forceinline__ FwdWork fwd_work(const AttParams& p, const PlanItem* 
     return f;
 }
 
-// Both chunks of a tile of 128 rows of a head.
-__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t chunks, uint32_t head, uint32_t row, uint32_t bar) {
-    for (uint32_t c = 0; c < chunks; ++c) tma_load_3d<1>(dst + c * kChunkBytes, map, (int)(c * 64), (int)head, (int)row, bar);
-}
-
-// Rows from `from` on of a tile in shared memory become zeros, by one warp: rows of another sequence, or of none, would otherwise
-// meet zeros of P, and 0 * NaN is NaN.
-__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from) {
-    const uint32_t per = (kAttTile - from) * 8;
-    for (uint32_t i = threadIdx.x & 31; i < per * chunks; i += 32) {
-        const uint32_t c = i / per, r = i - c * per;
-        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + from * 128 + r * 16) = make_uint4(0, 0, 0, 0);
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-}
-
-// D (+)= A B^T over head_dim: both operands rows of a head, along their columns.
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t steps, uint32_t desc) {
-    for (uint32_t i = 0; i < steps; ++i) {
-        const uint32_t at = (i / 4) * kChunkBytes + (i % 4) * 32;
-        mma_bf16<1>(d, operand_desc(a + at, 16), operand_desc(b + at, 16), desc, i != 0);
-    }
-}
-
-// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head.
-__device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
-#pragma unroll
-    for (uint32_t i = 0; i < kAttTile / 16; ++i) mma_bf16_tmem(d, a + i * 8, operand_desc(b + i * 2048, kChunkBytes), desc, add || i != 0);
-}
-
 __global__ void __launch_bounds__(kFwdThreads, 1)
     att_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttParams p) {
-    extern __shared__ uint8_t att_smem_raw[];
+    extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
     __shared__ __align__(8) uint64_t s_bar[2 * kFwdRing + 10 + 1];
     __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_q_issued[2], s_q_taken[2];
-    uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)att_smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t q0 = smem_addr(smem), ring0 = q0 + 2 * kTileBytes, bar0 = smem_addr(s_bar);
     auto full = [&](uint32_t i) { return bar0 + 8 * i; };
     auto empty = [&](uint32_t i) { return bar0 + 8 * (kFwdRing + i); };
@@ -294,8 +194,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             load_rows(ring0 + i * kTileBytes, map, chunks, head_at, row, full(i));
             ++issued;
         };
-        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
-            const FwdWork f = fwd_work(p, list, w);
+        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+            if (work_at(i) >= total) continue;
+            const FwdWork f = fwd_work(p, list, work_at(i));
             for (uint32_t s = 0; s < 2 && ok; ++s) {
                 if (!f.n[s]) continue;
                 if (!(ok = mbar_wait(bar(kQEmpty, s), (q_issued[s] & 1) ^ 1, p.wait_limit, gave_up))) break;
@@ -329,8 +230,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             if (wait(full(i), taken / kFwdRing & 1)) ++taken;
             return i;
         };
-        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
-            const FwdWork f = fwd_work(p, list, w);
+        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+            if (work_at(i) >= total) continue;
+            const FwdWork f = fwd_work(p, list, work_at(i));
             auto scores = [&](uint32_t s, uint32_t t, uint32_t k) {
                 if (t == 0) {
                     if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
@@ -356,7 +258,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     if (!wait(bar(kPFull, s), p_taken[s] & 1)) break;
                     ++p_taken[s];
                     if (lane == 0) {
-                        mma_tile(tmem + 256 + s * 128, tmem + s * 128, ring0 + v * kTileBytes, desc_o, t != 0);
+                        mma_tile<32>(tmem + 256 + s * 128, tmem + s * 128, ring0 + v * kTileBytes, desc_o, t != 0);
                         if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
                     }
                     if (t + 1 < f.n[s]) {
@@ -390,8 +292,9 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             tc_fence_after();
             return ok;
         };
-        for (uint32_t w = blockIdx.x; w < total && ok; w += gridDim.x) {
-            const FwdWork f = fwd_work(p, list, w);
+        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+            if (work_at(i) >= total) continue;
+            const FwdWork f = fwd_work(p, list, work_at(i));
             if (!f.n[s]) continue;
             const uint32_t row = f.row0[s] + r;             // in its sequence
             float top = -INFINITY, sum = 0.f;               // top: what O and sum are relative to
@@ -486,66 +389,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         }
         if (threadIdx.x == 0) {
             uint32_t left = kWaitTries;
-            for (uint32_t i = s_taken; i < s_issued; ++i)
-                while (left && !mbar_try_wait(full(i % kFwdRing), i / kFwdRing & 1)) --left;
-            for (uint32_t s = 0; s < 2; ++s)
-                for (uint32_t i = s_q_taken[s]; i < s_q_issued[s]; ++i)
-                    while (left && !mbar_try_wait(bar(kQFull, s), i & 1)) --left;
+            drain_loads(full(0), kFwdRing, s_taken, s_issued, left);
+            for (uint32_t s = 0; s < 2; ++s) drain_loads(bar(kQFull, s), 1, s_q_taken[s], s_q_issued[s], left);
         }
         __syncthreads();
     }
     tc_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 512);
     if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
-}
-
-__global__ void __launch_bounds__(256) att_dq_kernel(const AttParams p) {
-    if (blockIdx.x >= plan_tiles(p)) return;
-    const PlanItem it = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)[blockIdx.x];
-    const uint32_t lane = threadIdx.x & 31, d = p.head_dim, h = blockIdx.y, kh = h / p.group;
-    for (uint32_t r = it.tile * kAttTile + threadIdx.x / 32; r < min(it.len, (it.tile + 1) * kAttTile); r += 8) {
-        const uint64_t row = it.start + r;
-        Row q, k, o, g;
-        q.load(p.q + row * p.q_ld + h * d, lane, d);
-        g.load(p.d_o + row * p.do_ld + h * d, lane, d);
-        o.load(p.o + row * p.o_ld + h * d, lane, d);
-        const float delta = g.dot(o), lse = p.lse_in[h * p.tokens + row];
-        if (lane == 0) p.delta[h * p.tokens + row] = delta;
-        o.zero();
-        for (uint32_t j = 0; j <= r && r; ++j) {           // a query that sees one key: its weight is constant
-            Row v;
-            k.load(p.k + (uint64_t)(it.start + j) * p.k_ld + kh * d, lane, d);
-            v.load(p.v + (uint64_t)(it.start + j) * p.v_ld + kh * d, lane, d);
-            o.add(expf(q.dot(k) * p.scale - lse) * (g.dot(v) - delta), k);
-        }
-        if (p.dq) o.store(p.dq + row * p.dq_ld + h * d, lane, d, p.scale);
-    }
-}
-
-__global__ void __launch_bounds__(256) att_dkv_kernel(const AttParams p) {
-    if (blockIdx.x >= plan_tiles(p)) return;
-    const PlanItem it = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)[blockIdx.x];
-    const uint32_t lane = threadIdx.x & 31, d = p.head_dim, kh = blockIdx.y;
-    for (uint32_t j = it.tile * kAttTile + threadIdx.x / 32; j < min(it.len, (it.tile + 1) * kAttTile); j += 8) {
-        const uint64_t row = it.start + j;
-        Row k, v, dk, dv;
-        k.load(p.k + row * p.k_ld + kh * d, lane, d);
-        v.load(p.v + row * p.v_ld + kh * d, lane, d);
-        dk.zero();
-        dv.zero();
-        for (uint32_t h = kh * p.group; h < (kh + 1) * p.group; ++h)
-            for (uint32_t r = j; r < it.len; ++r) {
-                Row q, g;
-                const uint64_t at = it.start + r;
-                q.load(p.q + at * p.q_ld + h * d, lane, d);
-                g.load(p.d_o + at * p.do_ld + h * d, lane, d);
-                const float w = expf(q.dot(k) * p.scale - p.lse_in[h * p.tokens + at]);
-                dv.add(w, g);
-                if (r) dk.add(w * (g.dot(v) - p.delta[h * p.tokens + at]), q);
-            }
-        dk.store(p.dk + row * p.dk_ld + kh * d, lane, d, p.scale);
-        dv.store(p.dv + row * p.dv_ld + kh * d, lane, d, 1.f);
-    }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------
@@ -594,7 +445,7 @@ static std::atomic<uint32_t> g_att_wait_limit{kWaitTries};
 
 // A matrix of heads as (column, head, token), read in boxes of 64 columns of one head and kAttTile tokens; columns past the
 // head are zeros.
-static dte_status encode_heads(CUtensorMap* map, const dte_matrix* m, uint32_t head_dim) {
+dte_status encode_heads(CUtensorMap* map, const dte_matrix* m, uint32_t head_dim) {
     const uint64_t ld = m->rows > 1 ? m->ld : m->cols;
     return encode_3d(map, m->data, {head_dim, m->cols / head_dim, m->rows}, {head_dim * 2ull, ld * 2}, {64, 1, kAttTile});
 }
@@ -712,7 +563,8 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     const uint64_t tiles = tiles_most(plan_bytes, q->rows);
     if (q->rows == 0) return DTE_OK;
     OpDeviceGuard g;
-    if ((s = g.enter(device)) != DTE_OK) return s;
+    int sms = 0;
+    if ((s = g.enter(device, &sms)) != DTE_OK) return s;
     AttParams p = att_params(q, k, v, head_dim, plan, plan_bytes, scale, flags);
     p.o = static_cast<const __nv_bfloat16*>(out->data);
     p.d_o = static_cast<const __nv_bfloat16*>(dout->data);
@@ -726,10 +578,5 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     p.dv_ld = dv->ld;
     p.lse_in = lse;
     p.delta = static_cast<float*>(workspace);
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    att_dq_kernel<<<dim3((unsigned)tiles, (unsigned)heads), 256, 0, st>>>(p);
-    DTE_CUDA(cudaGetLastError());
-    att_dkv_kernel<<<dim3((unsigned)tiles, (unsigned)(k->cols / head_dim)), 256, 0, st>>>(p);
-    DTE_CUDA(cudaGetLastError());
-    return DTE_OK;
+    return launch_attention_backward(p, q, k, v, dout, tiles, device, sms, (cudaStream_t)cuda_stream);
 }

@@ -1,0 +1,111 @@
+// What the kernels of causal attention over packed sequences share: the plan, tiles of a head's rows and the products of two
+// of them.
+#pragma once
+
+#include "dte_mma.cuh"
+#include "dte_ops.cuh"
+
+namespace dte {
+
+constexpr uint32_t kAttTile = 128;               // rows of a tile of queries or keys
+constexpr uint32_t kMaxAttDim = 128;
+constexpr uint64_t kPlanMagic = 0x6474652d61747431ull;
+constexpr uint64_t kMaxAttTokens = 1ull << 24, kMaxSequences = 1ull << 20;
+constexpr uint64_t kPlanHeader = 256;
+constexpr double kLog2eD = 1.44269504088896340736;
+
+// One tile of one sequence.
+struct PlanItem {
+    uint32_t start, len;       // the sequence's rows
+    uint32_t tile;             // tile of the sequence
+    uint32_t pad;
+};
+
+struct PlanHead {
+    uint64_t magic, tokens;
+    uint32_t tiles, pairs;     // tiles of kAttTile rows, tiles of twice as many
+    uint64_t pairs_at;         // where in the plan the second list starts; the first follows the header
+};
+static_assert(sizeof(PlanItem) == 16 && sizeof(PlanHead) <= kPlanHeader, "");
+
+constexpr uint32_t kChunkBytes = kAttTile * 128; // a tile's 64 columns: one swizzled operand of 16 KB
+constexpr uint32_t kTileBytes = 2 * kChunkBytes; // up to 128 columns
+
+struct AttParams {
+    const uint8_t* plan;
+    uint64_t plan_bytes, tokens;
+    uint32_t head_dim, group;
+    uint32_t units;            // of work per tile: pairs of query heads, or query heads
+    bool pair_heads;
+    uint32_t wait_limit;       // tries of a wait inside the kernel
+    float scale, k2;           // k2: scale * log2(e)
+    const __nv_bfloat16 *q, *k, *v, *o, *d_o;
+    uint64_t q_ld, k_ld, v_ld, o_ld, do_ld;
+    __nv_bfloat16 *out, *dq, *dk, *dv;
+    uint64_t out_ld, dq_ld, dk_ld, dv_ld;
+    float *lse, *delta;
+    const float* lse_in;
+    uint64_t* flags;
+};
+
+// The two passes over the scores of the backward pass.
+dte_status launch_attention_backward(const AttParams& p, const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, const dte_matrix* dout,
+                                     uint64_t tiles, int device, int sms, cudaStream_t st);
+dte_status encode_heads(CUtensorMap* map, const dte_matrix* m, uint32_t head_dim);
+
+#ifdef __CUDACC__
+// Whether a plan was made for this many tokens and lies in its buffer; another one is flagged.
+__device__ __forceinline__ bool plan_ok(const AttParams& p) {
+    const PlanHead* h = reinterpret_cast<const PlanHead*>(p.plan);
+    if (h->magic == kPlanMagic && h->tokens == p.tokens && h->pairs_at + (uint64_t)h->pairs * sizeof(PlanItem) <= p.plan_bytes) return true;
+    if (threadIdx.x + blockIdx.x + blockIdx.y == 0 && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
+    return false;
+}
+
+// Both chunks of a tile of 128 rows of a head.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t chunks, uint32_t head, uint32_t row, uint32_t bar) {
+    for (uint32_t c = 0; c < chunks; ++c) tma_load_3d<1>(dst + c * kChunkBytes, map, (int)(c * 64), (int)head, (int)row, bar);
+}
+
+// Rows from `from` on of a tile in shared memory become zeros, by one warp: rows of another sequence, or of none, would otherwise
+// meet zeros of the other operand, and 0 * NaN is NaN.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from) {
+    const uint32_t per = (kAttTile - from) * 8;
+    for (uint32_t i = threadIdx.x & 31; i < per * chunks; i += 32) {
+        const uint32_t c = i / per, r = i - c * per;
+        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + from * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+// D (+)= A B^T over head_dim: both operands rows of a head, along their columns.
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t steps, uint32_t desc) {
+    for (uint32_t i = 0; i < steps; ++i) {
+        const uint32_t at = (i / 4) * kChunkBytes + (i % 4) * 32;
+        mma_bf16<1>(d, operand_desc(a + at, 16), operand_desc(b + at, 16), desc, i != 0);
+    }
+}
+
+// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head.  HALF: columns of tensor memory from A's first 64 bf16 to the
+// other 64.
+template <uint32_t HALF>
+__device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
+#pragma unroll
+    for (uint32_t i = 0; i < kAttTile / 16; ++i)
+        mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, operand_desc(b + i * 2048, kChunkBytes), desc, add || i != 0);
+}
+
+// Which piece of work this CTA takes in round i of its loop: the list is in falling order of work, and every other
+// round runs backwards, so that the shares come out even.
+__device__ __forceinline__ uint32_t work_at(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+
+// Waits for the loads that no product has waited for, after a wait that ran out: load i signals the barrier at
+// bars + 8 * (i % n) for the (i / n)-th time.
+__device__ __forceinline__ void drain_loads(uint32_t bars, uint32_t n, uint32_t taken, uint32_t issued, uint32_t& left) {
+    for (uint32_t i = taken; i < issued; ++i)
+        while (left && !mbar_try_wait(bars + 8 * (i % n), i / n & 1)) --left;
+}
+#endif  // __CUDACC__
+
+}  // namespace dte

@@ -1,0 +1,571 @@
+// Gradient of causal attention over packed sequences, in two passes over the scores that share nothing but delta, so that
+// every sum has one owner and its order is fixed (one pass would have to add dq up across CTAs):
+//   att_dq_kernel   a tile of 128 queries of one head against its keys:  delta, dq
+//   att_dkv_kernel  a tile of 128 keys of one key head against the queries of its group that see them:  dk, dv
+// With p = exp(z - lse), dz = p (dout v^T - delta): dq = scale dz k, dk = scale dz^T q, dv = p^T dout.  The first pass has three
+// products per pair of tiles, the second four, where one pass would have five.
+//
+// Both: one CTA per SM, a warp that loads, a warp that issues products, eight warps that turn scores into operands, each thread
+// half a row.  The second pass works on the transposed scores (rows are keys), so that p and dz are, as they come out of the
+// registers, the left operands of dv and dk in tensor memory.  p and dz are rounded to bf16, the operands' type; sums are fp32.
+#include <atomic>
+
+#include "dte_attention.cuh"
+
+namespace dte {
+
+constexpr uint32_t kBwdThreads = 3 * 128;         // registers as in the forward kernel
+constexpr uint32_t kBwdWarps = 8;                 // that work on scores
+constexpr int kFewRegs = 72, kManyRegs = 208;     // 128 * (72 + 2 * 208) = 62464 of the 384 * 168 = 64512 at launch
+constexpr uint32_t kBwdRing = 5;
+constexpr uint32_t kBwdSmem = (2 + kBwdRing) * kTileBytes;
+constexpr uint32_t kHalf = kAttTile / 2;          // columns of a tile that a thread works on
+// In tensor memory a tile of scores takes 128 columns.  The bf16 operand made of it lies over it, each half over the
+// columns that the same threads have read.
+
+// Columns c .. c + 31 of this thread's row, times by, as bf16.
+__device__ __forceinline__ void store_columns(__nv_bfloat16* out, uint32_t tmem, uint32_t c, uint32_t head_dim, float by, bool valid) {
+    uint32_t v[32];
+    tmem_load32(tmem + c, v);
+    tmem_load_wait(v);
+    if (!valid) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (c + 8 * j >= head_dim) break;
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(v[8 * j + i]) * by;
+        Raw8<__nv_bfloat16> x;
+        x.set(o);
+        x.store(out + c + 8 * j);
+    }
+}
+
+__device__ __forceinline__ void load_half(uint32_t tmem, float (&z)[kHalf]) {
+    uint32_t a[32], b[32];
+    tmem_load32(tmem, a);
+    tmem_load32(tmem + 32, b);
+    tmem_load_wait(a);
+    tmem_load_wait(b);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        z[j] = __uint_as_float(a[j]);
+        z[32 + j] = __uint_as_float(b[j]);
+    }
+}
+
+__device__ __forceinline__ void store_half(uint32_t tmem, const float (&z)[kHalf]) {
+    uint32_t v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = pack_bf16(z[2 * j], z[2 * j + 1]);
+    tmem_store32(tmem, v);
+    tmem_store_wait();
+    tc_fence_before();
+    __syncwarp();
+}
+
+// ---- dq -------------------------------------------------------------------------------------------------------
+// Tensor memory: S at columns 0 and 128 in turn (dz over it), dP at 256, dq at 384.
+__global__ void __launch_bounds__(kBwdThreads, 1)
+    att_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
+    enum { kRingFull, kRingEmpty = kBwdRing, kQFull = 2 * kBwdRing, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull, kDelta, kLast, kBars };
+    __shared__ __align__(8) uint64_t s_bar[kBars];
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_q_issued, s_q_taken;
+    __shared__ float s_delta[2][2][kAttTile];
+    const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, ring0 = q0 + 2 * kTileBytes;
+    auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&map_q);
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+        tma_prefetch_map(&map_do);
+        for (uint32_t i = 0; i < kBars; ++i)
+            mbar_init(bar(i), i == kDsFull || i == kDsFull + 1 || i == kDpRead || i == kDelta ? kBwdWarps : 1);
+        s_gave_up = s_issued = s_taken = s_q_issued = s_q_taken = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<1>(smem_addr(&s_tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
+    volatile uint32_t* gave_up = &s_gave_up;
+    const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
+    const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
+    const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
+
+    if (warp < 4) {
+        regs_down<kFewRegs>();
+        if (warp == 0 && lane == 0) {
+            // ---- loads ----
+            uint32_t issued = 0, q_issued = 0;
+            bool ok = true;
+            auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
+                const uint32_t i = issued % kBwdRing;
+                if (!(ok = ok && mbar_wait(bar(kRingEmpty + i), (issued / kBwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
+                mbar_expect_tx(bar(kRingFull + i), tile_bytes);
+                load_rows(ring0 + i * kTileBytes, map, chunks, head, row, bar(kRingFull + i));
+                ++issued;
+            };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                const uint32_t w = work_at(i);
+                if (w >= total) continue;
+                const PlanItem it = list[w / p.units];
+                const uint32_t h = w % p.units, kh = h / p.group, row = it.start + it.tile * kAttTile;
+                if (!(ok = mbar_wait(bar(kQEmpty), (q_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
+                mbar_expect_tx(bar(kQFull), 2 * tile_bytes);
+                load_rows(q0, &map_q, chunks, h, row, bar(kQFull));
+                load_rows(do0, &map_do, chunks, h, row, bar(kQFull));
+                ++q_issued;
+                for (uint32_t t = 0; t <= it.tile && ok; ++t) {
+                    load(&map_k, kh, it.start + t * kAttTile);
+                    load(&map_v, kh, it.start + t * kAttTile);
+                }
+            }
+            s_issued = issued;
+            s_q_issued = q_issued;
+        } else if (warp == 1) {
+            // ---- matrix products: the whole warp waits, one lane issues ----
+            const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
+            const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
+            uint32_t taken = 0, q_taken = 0, g = 0, dp_issued = 0;
+            bool ok = true;
+            auto wait = [&](uint32_t b, uint32_t parity) {
+                ok = ok && mbar_wait(bar(b), parity, p.wait_limit, gave_up);
+                ok = !__any_sync(0xFFFFFFFFu, !ok);
+                tc_fence_after();
+                return ok;
+            };
+            auto take = [&]() {
+                const uint32_t i = taken % kBwdRing;
+                if (wait(kRingFull + i, taken / kBwdRing & 1)) ++taken;
+                return i;
+            };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                const uint32_t w = work_at(i);
+                if (w >= total) continue;
+                const PlanItem it = list[w / p.units];
+                const uint32_t n = it.tile + 1;
+                if (!wait(kQFull, q_taken & 1)) break;
+                ++q_taken;
+                // S and dP of tile t of the keys, into S's buffer `at`
+                auto scores = [&](uint32_t t, uint32_t at) {
+                    const uint32_t k = take();
+                    if (!ok) return k;
+                    if ((t + 1) * kAttTile > it.len) clear_rows(smem + (2 + k) * kTileBytes, chunks, it.len - t * kAttTile);
+                    if (lane == 0) {
+                        mma_rows(tmem + at * 128, q0, ring0 + k * kTileBytes, steps, desc_s);
+                        mma_commit<1>(bar(kSFull + at));
+                    }
+                    if (dp_issued && !wait(kDpRead, (dp_issued - 1) & 1)) return k;
+                    const uint32_t v = take();
+                    if (!ok) return k;
+                    ++dp_issued;
+                    if (lane == 0) {
+                        mma_rows(tmem + 256, do0, ring0 + v * kTileBytes, steps, desc_s);
+                        mma_commit<1>(bar(kDpFull));
+                        mma_commit<1>(bar(kRingEmpty + v));
+                        if (t + 1 == n) mma_commit<1>(bar(kQEmpty));
+                    }
+                    return k;
+                };
+                uint32_t k = scores(0, g & 1);
+                for (uint32_t t = 0; t < n && ok; ++t, ++g) {
+                    const uint32_t next = t + 1 < n ? scores(t + 1, (g + 1) & 1) : 0;
+                    if (!ok || !wait(kDsFull + (g & 1), g >> 1 & 1)) break;
+                    if (lane == 0) {
+                        mma_tile<kHalf>(tmem + 384, tmem + (g & 1) * 128, ring0 + k * kTileBytes, desc_d, t != 0);
+                        mma_commit<1>(bar(kRingEmpty + k));
+                        if (t + 1 == n) mma_commit<1>(bar(kDqFull));
+                    }
+                    k = next;
+                }
+            }
+            if (lane == 0) {
+                s_taken = taken;
+                s_q_taken = q_taken;
+            }
+        }
+    } else {
+        regs_up<kManyRegs>();
+        // ---- scores: warp w may read the quarter w % 4 of tensor memory's lanes ----
+        const uint32_t half = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t mine = tmem + (quarter * 32 << 16);
+        uint32_t g = 0, done = 0;
+        bool ok = true;
+        auto wait = [&](uint32_t b, uint32_t parity) {
+            ok = mbar_wait(bar(b), parity, p.wait_limit, gave_up);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            tc_fence_after();
+            return ok;
+        };
+        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+            const uint32_t w = work_at(i);
+            if (w >= total) continue;
+            const PlanItem it = list[w / p.units];
+            const uint32_t h = w % p.units, n = it.tile + 1, row = it.tile * kAttTile + r;
+            const bool valid = row < it.len;
+            const uint64_t at = (uint64_t)it.start + row;
+            // delta: each of a row's two threads takes every other group of eight columns
+            float part = 0.f;
+            if (valid) {
+                const __nv_bfloat16 *o = p.o + at * p.o_ld + h * p.head_dim, *d = p.d_o + at * p.do_ld + h * p.head_dim;
+                for (uint32_t c = half * 8; c < p.head_dim; c += 16) {
+                    Raw8<__nv_bfloat16> x, y;
+                    float a[8], b[8];
+                    x.load(o + c);
+                    y.load(d + c);
+                    x.get(a);
+                    y.get(b);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) part = fmaf(a[j], b[j], part);
+                }
+            }
+            const float lse2 = valid ? p.lse_in[h * p.tokens + at] * -(float)kLog2eD : 0.f;
+            s_delta[done & 1][half][r] = part;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kDelta));
+            if (!wait(kDelta, done & 1)) break;
+            const float delta = s_delta[done & 1][0][r] + s_delta[done & 1][1][r];
+            if (valid && half == 0) p.delta[h * p.tokens + at] = delta;
+            for (uint32_t t = 0; t < n; ++t, ++g) {
+                const uint32_t s_at = mine + (g & 1) * 128 + half * kHalf;
+                if (!wait(kSFull + (g & 1), g >> 1 & 1)) break;
+                float z[kHalf];
+                load_half(s_at, z);
+#pragma unroll
+                for (int j = 0; j < (int)kHalf; ++j) z[j] = exp2_fast(fmaf(z[j], p.k2, lse2));
+                if (!wait(kDpFull, g & 1)) break;
+                float d[kHalf];
+                load_half(mine + 256 + half * kHalf, d);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kDpRead));
+#pragma unroll
+                for (int j = 0; j < (int)kHalf; ++j) z[j] *= d[j] - delta;
+                if (t + 1 == n) {             // on the diagonal; a query that sees one key has a constant weight
+#pragma unroll
+                    for (int j = 0; j < (int)kHalf; ++j) z[j] = half * kHalf + j > r || row == 0 ? 0.f : z[j];
+                }
+                store_half(s_at, z);
+                if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
+            }
+            if (!ok || !wait(kDqFull, done & 1)) break;
+            ++done;
+            __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
+            for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid);
+            tc_fence_before();
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    const bool failed = *gave_up;
+    if (failed) {      // as in the forward kernel
+        if (warp == 1 && lane == 0) {
+            mma_commit<1>(bar(kLast));
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
+        }
+        if (threadIdx.x == 0) {
+            uint32_t left = kWaitTries;
+            drain_loads(bar(kRingFull), kBwdRing, s_taken, s_issued, left);
+            drain_loads(bar(kQFull), 1, s_q_taken, s_q_issued, left);
+        }
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 1) tmem_free<1>(tmem, 512);
+    if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
+}
+
+// ---- dk, dv -----------------------------------------------------------------------------------------------------
+// A key tile's work: for each query head of the group, the query tiles from its own to the sequence's last.
+struct DkvWork {
+    uint32_t start, len, kv_head, tile, tiles, n;     // tiles: of queries per head; n: in all
+};
+
+__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, const PlanItem* list, uint32_t w) {
+    // the list falls in the number of tiles in front: taken from the other end, in the number of tiles behind
+    const PlanItem it = list[w / p.units];
+    DkvWork f;
+    f.start = it.start;
+    f.len = it.len;
+    f.kv_head = w % p.units;
+    f.tiles = it.tile + 1;
+    f.tile = (it.len + kAttTile - 1) / kAttTile - f.tiles;
+    f.n = f.tiles * p.group;
+    return f;
+}
+
+// Tensor memory: transposed S at column 0 (p over it), transposed dP at 128 (dz over it), dv at 256, dk at 384.  While dz is made
+// of one pair of tiles, the tensor cores add its dv up and make the next pair's S; while p is made of that, dk and the next dP.
+__global__ void __launch_bounds__(kBwdThreads, 1)
+    att_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
+    enum { kRingFull, kRingEmpty = kBwdRing, kKvFull = 2 * kBwdRing, kKvEmpty, kSFull, kPFull, kDpFull, kDsFull, kAccFull, kStatFull, kStatEmpty = kStatFull + 2,
+           kLast = kStatEmpty + 2, kBars };
+    __shared__ __align__(8) uint64_t s_bar[kBars];
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_kv_issued, s_kv_taken;
+    __shared__ __align__(16) float s_stat[2][2][kAttTile];       // -lse log2(e) and -delta of a tile of queries
+    const uint32_t k0 = smem_addr(smem), v0 = k0 + kTileBytes, ring0 = k0 + 2 * kTileBytes;
+    auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        tma_prefetch_map(&map_q);
+        tma_prefetch_map(&map_k);
+        tma_prefetch_map(&map_v);
+        tma_prefetch_map(&map_do);
+        for (uint32_t i = 0; i < kBars; ++i)
+            mbar_init(bar(i), i == kPFull || i == kDsFull || i == kStatEmpty || i == kStatEmpty + 1 ? kBwdWarps : i == kStatFull || i == kStatFull + 1 ? 2 : 1);
+        s_gave_up = s_issued = s_taken = s_kv_issued = s_kv_taken = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<1>(smem_addr(&s_tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
+    volatile uint32_t* gave_up = &s_gave_up;
+    const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
+    const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
+    const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
+
+    if (warp < 4) {
+        regs_down<kFewRegs>();
+        if (warp == 0 && lane == 0) {
+            // ---- loads ----
+            uint32_t issued = 0, kv_issued = 0;
+            bool ok = true;
+            auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
+                const uint32_t i = issued % kBwdRing;
+                if (!(ok = ok && mbar_wait(bar(kRingEmpty + i), (issued / kBwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
+                mbar_expect_tx(bar(kRingFull + i), tile_bytes);
+                load_rows(ring0 + i * kTileBytes, map, chunks, head, row, bar(kRingFull + i));
+                ++issued;
+            };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                if (work_at(i) >= total) continue;
+                const DkvWork f = dkv_work(p, list, work_at(i));
+                if (!(ok = mbar_wait(bar(kKvEmpty), (kv_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
+                mbar_expect_tx(bar(kKvFull), 2 * tile_bytes);
+                load_rows(k0, &map_k, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
+                load_rows(v0, &map_v, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
+                ++kv_issued;
+                for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
+                    for (uint32_t t = f.tile; t < f.tile + f.tiles && ok; ++t) {
+                        load(&map_q, h, f.start + t * kAttTile);
+                        load(&map_do, h, f.start + t * kAttTile);
+                    }
+            }
+            s_issued = issued;
+            s_kv_issued = kv_issued;
+        } else if (warp == 1) {
+            // ---- matrix products: the whole warp waits, one lane issues ----
+            const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
+            const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
+            uint32_t taken = 0, kv_taken = 0, g = 0;
+            bool ok = true;
+            auto wait = [&](uint32_t b, uint32_t parity) {
+                ok = ok && mbar_wait(bar(b), parity, p.wait_limit, gave_up);
+                ok = !__any_sync(0xFFFFFFFFu, !ok);
+                tc_fence_after();
+                return ok;
+            };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                if (work_at(i) >= total) continue;
+                const DkvWork f = dkv_work(p, list, work_at(i));
+                if (!wait(kKvFull, kv_taken & 1)) break;
+                ++kv_taken;
+                // the next tile of the ring; rows past the sequence are cleared.  t: its tile of queries
+                auto take = [&](uint32_t t) {
+                    const uint32_t i = taken % kBwdRing;
+                    if (!wait(kRingFull + i, taken / kBwdRing & 1)) return i;
+                    ++taken;
+                    if ((t + 1) * kAttTile > f.len) clear_rows(smem + (2 + i) * kTileBytes, chunks, f.len - t * kAttTile);
+                    return i;
+                };
+                uint32_t ahead = f.tile;               // tile of queries of the next S and dP
+                auto scores = [&](uint32_t d, uint32_t a, uint32_t full, bool last) {
+                    const uint32_t at = take(ahead);
+                    if (lane == 0 && ok) {
+                        mma_rows(tmem + d, a, ring0 + at * kTileBytes, steps, desc_s);
+                        mma_commit<1>(bar(full));
+                        if (last) mma_commit<1>(bar(kKvEmpty));
+                    }
+                    return at;
+                };
+                uint32_t q = scores(0, k0, kSFull, false);
+                uint32_t d_o = scores(128, v0, kDpFull, f.n == 1);
+                for (uint32_t j = 0; j < f.n && ok; ++j, ++g) {
+                    const bool more = j + 1 < f.n;
+                    if (++ahead == f.tile + f.tiles) ahead = f.tile;
+                    if (!wait(kPFull, g & 1)) break;
+                    if (lane == 0) {
+                        mma_tile<kHalf>(tmem + 256, tmem, ring0 + d_o * kTileBytes, desc_d, j != 0);
+                        mma_commit<1>(bar(kRingEmpty + d_o));
+                    }
+                    const uint32_t next = more ? scores(0, k0, kSFull, false) : 0;
+                    if (!wait(kDsFull, g & 1)) break;
+                    if (lane == 0) {
+                        mma_tile<kHalf>(tmem + 384, tmem + 128, ring0 + q * kTileBytes, desc_d, j != 0);
+                        mma_commit<1>(bar(kRingEmpty + q));
+                        if (!more) mma_commit<1>(bar(kAccFull));
+                    }
+                    if (more) d_o = scores(128, v0, kDpFull, j + 2 == f.n);
+                    q = next;
+                }
+            }
+            if (lane == 0) {
+                s_taken = taken;
+                s_kv_taken = kv_taken;
+            }
+        } else if (warp >= 2) {
+            // ---- lse (warp 2) and delta (warp 3) of the tiles of queries ----
+            const float* from = warp == 2 ? p.lse_in : p.delta;
+            const float by = warp == 2 ? -(float)kLog2eD : -1.f;
+            uint32_t g = 0;
+            bool ok = true;
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                if (work_at(i) >= total) continue;
+                const DkvWork f = dkv_work(p, list, work_at(i));
+                for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
+                    for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
+                        ok = mbar_wait(bar(kStatEmpty + (g & 1)), (g >> 1 & 1) ^ 1, p.wait_limit, gave_up);
+                        ok = !__any_sync(0xFFFFFFFFu, !ok);
+                        if (!ok) break;
+                        const uint32_t row = t * kAttTile + lane * 4;
+                        const float* x = from + h * p.tokens + f.start + row;
+                        float4 v;
+                        v.x = row < f.len ? x[0] * by : 0.f;
+                        v.y = row + 1 < f.len ? x[1] * by : 0.f;
+                        v.z = row + 2 < f.len ? x[2] * by : 0.f;
+                        v.w = row + 3 < f.len ? x[3] * by : 0.f;
+                        *reinterpret_cast<float4*>(&s_stat[g & 1][warp - 2][lane * 4]) = v;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(kStatFull + (g & 1)));
+                    }
+            }
+        }
+    } else {
+        regs_up<kManyRegs>();
+        // ---- scores: warp w may read the quarter w % 4 of tensor memory's lanes ----
+        const uint32_t half = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t mine = tmem + (quarter * 32 << 16), s_at = mine + half * kHalf, d_at = s_at + 128;
+        uint32_t g = 0, done = 0;
+        bool ok = true;
+        auto wait = [&](uint32_t b, uint32_t parity) {
+            ok = mbar_wait(bar(b), parity, p.wait_limit, gave_up);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            tc_fence_after();
+            return ok;
+        };
+        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+            if (work_at(i) >= total) continue;
+            const DkvWork f = dkv_work(p, list, work_at(i));
+            uint32_t t = f.tile;
+            for (uint32_t j = 0; j < f.n; ++j, ++g) {
+                const uint32_t first = t * kAttTile + half * kHalf;       // query of this thread's first column
+                const bool edge = t == f.tile || (t + 1) * kAttTile > f.len;
+                const float4* lse = reinterpret_cast<const float4*>(&s_stat[g & 1][0][half * kHalf]);
+                const float4* delta = reinterpret_cast<const float4*>(&s_stat[g & 1][1][half * kHalf]);
+                if (!wait(kStatFull + (g & 1), g >> 1 & 1) || !wait(kSFull, g & 1)) break;
+                float z[kHalf];
+                load_half(s_at, z);
+#pragma unroll
+                for (int c = 0; c < (int)kHalf / 4; ++c) {
+                    const float4 l = lse[c];
+                    z[4 * c] = exp2_fast(fmaf(z[4 * c], p.k2, l.x));
+                    z[4 * c + 1] = exp2_fast(fmaf(z[4 * c + 1], p.k2, l.y));
+                    z[4 * c + 2] = exp2_fast(fmaf(z[4 * c + 2], p.k2, l.z));
+                    z[4 * c + 3] = exp2_fast(fmaf(z[4 * c + 3], p.k2, l.w));
+                }
+                if (edge) {                   // on the diagonal, or past the sequence
+                    const uint32_t key = f.tile * kAttTile + r;
+#pragma unroll
+                    for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len ? 0.f : z[c];
+                }
+                store_half(s_at, z);
+                if (lane == 0) mbar_arrive(bar(kPFull));
+                if (!wait(kDpFull, g & 1)) break;
+                float d[kHalf];
+                load_half(d_at, d);
+#pragma unroll
+                for (int c = 0; c < (int)kHalf / 4; ++c) {
+                    const float4 l = delta[c];
+                    z[4 * c] *= d[4 * c] + l.x;
+                    z[4 * c + 1] *= d[4 * c + 1] + l.y;
+                    z[4 * c + 2] *= d[4 * c + 2] + l.z;
+                    z[4 * c + 3] *= d[4 * c + 3] + l.w;
+                }
+                if (edge) {                   // 0 * what lies past the sequence; a query that sees one key has a constant weight
+                    const uint32_t key = f.tile * kAttTile + r;
+#pragma unroll
+                    for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len || first + c == 0 ? 0.f : z[c];
+                }
+                store_half(d_at, z);
+                if (lane == 0) {
+                    mbar_arrive(bar(kDsFull));
+                    mbar_arrive(bar(kStatEmpty + (g & 1)));
+                }
+                if (++t == f.tile + f.tiles) t = f.tile;
+            }
+            if (!ok || !wait(kAccFull, done++ & 1)) break;
+            const uint32_t row = f.tile * kAttTile + r;
+            const uint64_t at = (uint64_t)f.start + row;
+            for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
+                store_columns(p.dv + at * p.dv_ld + f.kv_head * p.head_dim, mine + 256, c, p.head_dim, 1.f, row < f.len);
+                store_columns(p.dk + at * p.dk_ld + f.kv_head * p.head_dim, mine + 384, c, p.head_dim, p.scale, row < f.len);
+            }
+            tc_fence_before();
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    const bool failed = *gave_up;
+    if (failed) {      // as in the forward kernel
+        if (warp == 1 && lane == 0) {
+            mma_commit<1>(bar(kLast));
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
+        }
+        if (threadIdx.x == 0) {
+            uint32_t left = kWaitTries;
+            drain_loads(bar(kRingFull), kBwdRing, s_taken, s_issued, left);
+            drain_loads(bar(kKvFull), 1, s_kv_taken, s_kv_issued, left);
+        }
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 1) tmem_free<1>(tmem, 512);
+    if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
+}
+
+dte_status launch_attention_backward(const AttParams& params, const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, const dte_matrix* dout,
+                                     uint64_t tiles, int device, int sms, cudaStream_t st) {
+    dte_status s;
+    CUtensorMap mq, mk, mv, md;
+    if ((s = encode_heads(&mq, q, params.head_dim)) != DTE_OK) return s;
+    if ((s = encode_heads(&mk, k, params.head_dim)) != DTE_OK) return s;
+    if ((s = encode_heads(&mv, v, params.head_dim)) != DTE_OK) return s;
+    if ((s = encode_heads(&md, dout, params.head_dim)) != DTE_OK) return s;
+    static std::atomic<uint64_t> ready_dq{0}, ready_dkv{0};
+    if ((s = allow_smem(att_dq_kernel, kBwdSmem, device, ready_dq)) != DTE_OK) return s;
+    if ((s = allow_smem(att_dkv_kernel, kBwdSmem, device, ready_dkv)) != DTE_OK) return s;
+    AttParams p = params;
+    auto grid = [&] { return (unsigned)(tiles * p.units < (uint64_t)sms ? tiles * p.units : sms); };
+    p.units = (uint32_t)(q->cols / p.head_dim);
+    att_dq_kernel<<<grid(), kBwdThreads, kBwdSmem, st>>>(mq, mk, mv, md, p);
+    DTE_CUDA(cudaGetLastError());
+    p.units = (uint32_t)(k->cols / p.head_dim);
+    att_dkv_kernel<<<grid(), kBwdThreads, kBwdSmem, st>>>(mq, mk, mv, md, p);
+    DTE_CUDA(cudaGetLastError());
+    return DTE_OK;
+}
+
+}  // namespace dte
