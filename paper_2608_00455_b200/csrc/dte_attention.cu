@@ -300,27 +300,29 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             float top = -INFINITY, sum = 0.f;               // top: what O and sum are relative to
             for (uint32_t t = 0; t < f.n[s]; ++t) {
                 if (!wait(bar(kSFull, s), s_taken_++ & 1)) break;
-                float z[128];
+                uint32_t v[4][32];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_load32(s_at + c * 32, v);
-                    tmem_load_wait(v);
+                for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, v[c]);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) z[c * 32 + j] = __uint_as_float(v[j]);
-                }
+                for (int c = 0; c < 4; ++c) tmem_load_wait(v[c]);
                 if (t + 1 == f.n[s]) {                      // the tile on the diagonal
 #pragma unroll
-                    for (int j = 0; j < 128; ++j) z[j] = (uint32_t)j > r ? -INFINITY : z[j];
+                    for (int j = 0; j < 128; ++j) v[j / 32][j % 32] = (uint32_t)j > r ? __float_as_uint(-INFINITY) : v[j / 32][j % 32];
                 }
-                float peak = top;
+                // four chains, so that latencies overlap; a NaN spreads to the whole row through the maximum
+                float high[4] = {top, top, top, top};
 #pragma unroll
-                for (int j = 0; j < 128; ++j) peak = fmaxf(peak, z[j]);
+                for (int j = 0; j < 32; j += 2)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) high[c] = max3_nan(high[c], __uint_as_float(v[c][j]), __uint_as_float(v[c][j + 1]));
+                const float peak = max3_nan(max3_nan(high[0], high[1], high[2]), high[3], high[3]);
+                // each row decides for itself, so that no row's rounding depends on its neighbours; a NaN counts as growth
+                const bool grown = t != 0 && !((peak - top) * k2 <= kRescaleAbove);
                 if (t == 0) {
                     top = peak;
-                } else if (__any_sync(0xFFFFFFFFu, (peak - top) * k2 > kRescaleAbove)) {
-                    const float by = peak == -INFINITY ? 1.f : exp2_fast((top - peak) * k2);
-                    top = peak;
+                } else if (__any_sync(0xFFFFFFFFu, grown)) {
+                    const float by = !grown || peak == -INFINITY ? 1.f : exp2_fast((top - peak) * k2);
+                    top = grown ? peak : top;
                     sum *= by;
                     for (uint32_t c = 0; c < p.head_dim; c += 32) {
                         uint32_t v[32];
@@ -332,20 +334,26 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     }
                 }
                 const float from = top == -INFINITY ? 0.f : -top * k2;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                const F2 by2 = f2(k2, k2), from2 = f2(from, from);
+                F2 part[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
+                    uint32_t w[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        const float a = exp2_fast(fmaf(z[c * 64 + 2 * j], k2, from)), b = exp2_fast(fmaf(z[c * 64 + 2 * j + 1], k2, from));
-                        part[j & 1] += a;
-                        part[2 + (j & 1)] += b;
-                        v[j] = pack_bf16(a, b);
+                        const uint32_t* x = &v[2 * c + j / 16][j % 16 * 2];
+                        float lo, hi;
+                        f2_get(f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), by2, from2), lo, hi);
+                        lo = exp2_fast(lo);
+                        hi = exp2_fast(hi);
+                        part[j % 4] = f2_add(part[j % 4], f2(lo, hi));
+                        w[j] = pack_bf16(lo, hi);
                     }
-                    tmem_store32(s_at + c * 32, v);
+                    tmem_store32(s_at + c * 32, w);
                 }
-                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                float even, odd;
+                f2_get(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), even, odd);
+                sum += even + odd;
                 tmem_store_wait();
                 tc_fence_before();
                 __syncwarp();
