@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;         // S of the slots at columns 0 and 128, O at 256 and 384
+    const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);         // S of the slots at columns 0 and 128, O at 256 and 384
     volatile uint32_t* gave_up = &s_gave_up;
     const PlanHead* head = reinterpret_cast<const PlanHead*>(p.plan);
     const uint32_t items = plan_ok(p) ? (p.pair_heads ? head->tiles : head->pairs) : 0, total = items * p.units;
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         auto take = [&]() {                       // the next tile of the ring; where it lies
             const uint32_t i = taken % kFwdRing;
             if (wait(full(i), taken / kFwdRing & 1)) ++taken;
-            return i;
+            return uniform(i);
         };
         for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
             if (work_at(i) >= total) continue;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
                     ++q_taken[s];
                 }
-                if (lane == 0) {
+                if (elect_lane()) {
                     mma_rows(tmem + s * 128, q0 + s * kTileBytes, ring0 + k * kTileBytes, steps, desc_s);
                     mma_commit<1>(bar(kSFull, s));
                     if (t + 1 == f.n[s]) mma_commit<1>(bar(kQEmpty, s));
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             const uint32_t k0 = take();
             for (uint32_t s = 0; s < 2 && ok; ++s)
                 if (f.n[s]) scores(s, 0, k0);
-            if (lane == 0 && ok) mma_commit<1>(empty(k0));
+            if (ok && elect_lane()) mma_commit<1>(empty(k0));
             for (uint32_t t = 0; t < f.n_max && ok; ++t) {
                 const uint32_t v = take();
                 if (!ok) break;
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     if (t >= f.n[s]) continue;
                     if (!wait(bar(kPFull, s), p_taken[s] & 1)) break;
                     ++p_taken[s];
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_tile<32>(tmem + 256 + s * 128, tmem + s * 128, ring0 + v * kTileBytes, desc_o, t != 0);
                         if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
                     }
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                         if (ok) scores(s, t + 1, k);
                     }
                 }
-                if (lane == 0 && ok) {
+                if (ok && elect_lane()) {
                     mma_commit<1>(empty(v));
                     if (t + 1 < f.n_max) mma_commit<1>(empty(k));
                 }
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     if (failed) {
         // A wait ran out: all roles have stopped.  What they left in flight ends here, again with a limit: the products, and every
         // load that no product has waited for.
-        if (warp == 1 && lane == 0) {
+        if (warp == 1 && elect_lane()) {      // the lane that issued them
             mma_commit<1>(last_bar);
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(last_bar, 0); ++i) {}
         }

@@ -79,21 +79,28 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint3
     __syncwarp();
 }
 
+// Products are issued by one lane that the warp elects: the compiler then knows the branch, and with `uniform` the operands'
+// addresses, to be the same for the whole warp, and keeps descriptors in uniform registers.  (An issue by `lane == 0`, descriptors made
+// anew for each: 147 cycles per instruction that takes the tensor cores 64.)
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
 // D (+)= A B^T over head_dim: both operands rows of a head, along their columns.
 __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t steps, uint32_t desc) {
-    for (uint32_t i = 0; i < steps; ++i) {
-        const uint32_t at = (i / 4) * kChunkBytes + (i % 4) * 32;
-        mma_bf16<1>(d, operand_desc(a + at, 16), operand_desc(b + at, 16), desc, i != 0);
+    const uint64_t da = operand_desc(a, 16), db = operand_desc(b, 16);
+#pragma unroll
+    for (uint32_t i = 0; i < kMaxAttDim / 16; ++i) {
+        const uint32_t at = ((i / 4) * kChunkBytes + (i % 4) * 32) >> 4;
+        if (i < steps) mma_bf16<1>(d, da + at, db + at, desc, i != 0);
     }
 }
 
-// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head.  HALF: columns of tensor memory from A's first 64 bf16 to the
-// other 64.
-template <uint32_t HALF>
+// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head; steps FROM to TO of 16 along K.  HALF: columns of tensor memory
+// from A's first 64 bf16 to the other 64.
+template <uint32_t HALF, uint32_t FROM = 0, uint32_t TO = kAttTile / 16>
 __device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
+    const uint64_t db = operand_desc(b, kChunkBytes);
 #pragma unroll
-    for (uint32_t i = 0; i < kAttTile / 16; ++i)
-        mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, operand_desc(b + i * 2048, kChunkBytes), desc, add || i != 0);
+    for (uint32_t i = FROM; i < TO; ++i) mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, db + (i * 2048 >> 4), desc, add || i != 0);
 }
 
 // Which piece of work this CTA takes in round i of its loop: the list is in falling order of work, and every other

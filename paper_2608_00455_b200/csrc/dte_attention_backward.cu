@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
+    const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);
     volatile uint32_t* gave_up = &s_gave_up;
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             auto take = [&]() {
                 const uint32_t i = taken % kBwdRing;
                 if (wait(kRingFull + i, taken / kBwdRing & 1)) ++taken;
-                return i;
+                return uniform(i);
             };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 const uint32_t w = work_at(i);
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     const uint32_t k = take();
                     if (!ok) return k;
                     if ((t + 1) * kAttTile > it.len) clear_rows(smem + (2 + k) * kTileBytes, chunks, it.len - t * kAttTile);
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_rows(tmem + at * 128, q0, ring0 + k * kTileBytes, steps, desc_s);
                         mma_commit<1>(bar(kSFull + at));
                     }
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     const uint32_t v = take();
                     if (!ok) return k;
                     ++dp_issued;
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_rows(tmem + 256, do0, ring0 + v * kTileBytes, steps, desc_s);
                         mma_commit<1>(bar(kDpFull));
                         mma_commit<1>(bar(kRingEmpty + v));
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 for (uint32_t t = 0; t < n && ok; ++t, ++g) {
                     const uint32_t next = t + 1 < n ? scores(t + 1, (g + 1) & 1) : 0;
                     if (!ok || !wait(kDsFull + (g & 1), g >> 1 & 1)) break;
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_tile<kHalf>(tmem + 384, tmem + (g & 1) * 128, ring0 + k * kTileBytes, desc_d, t != 0);
                         mma_commit<1>(bar(kRingEmpty + k));
                         if (t + 1 == n) mma_commit<1>(bar(kDqFull));
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     __syncthreads();
     const bool failed = *gave_up;
     if (failed) {      // as in the forward kernel
-        if (warp == 1 && lane == 0) {
+        if (warp == 1 && elect_lane()) {      // the lane that issued them
             mma_commit<1>(bar(kLast));
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
         }
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *(volatile uint32_t*)&s_tmem;
+    const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);
     volatile uint32_t* gave_up = &s_gave_up;
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
@@ -385,15 +385,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 // the next tile of the ring; rows past the sequence are cleared.  t: its tile of queries
                 auto take = [&](uint32_t t) {
                     const uint32_t i = taken % kBwdRing;
-                    if (!wait(kRingFull + i, taken / kBwdRing & 1)) return i;
+                    if (!wait(kRingFull + i, taken / kBwdRing & 1)) return uniform(i);
                     ++taken;
                     if ((t + 1) * kAttTile > f.len) clear_rows(smem + (2 + i) * kTileBytes, chunks, f.len - t * kAttTile);
-                    return i;
+                    return uniform(i);
                 };
                 uint32_t ahead = f.tile;               // tile of queries of the next S and dP
                 auto scores = [&](uint32_t d, uint32_t a, uint32_t full, bool last) {
                     const uint32_t at = take(ahead);
-                    if (lane == 0 && ok) {
+                    if (ok && elect_lane()) {
                         mma_rows(tmem + d, a, ring0 + at * kTileBytes, steps, desc_s);
                         mma_commit<1>(bar(full));
                         if (last) mma_commit<1>(bar(kKvEmpty));
@@ -406,13 +406,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     const bool more = j + 1 < f.n;
                     if (++ahead == f.tile + f.tiles) ahead = f.tile;
                     if (!wait(kPFull, g & 1)) break;
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_tile<kHalf>(tmem + 256, tmem, ring0 + d_o * kTileBytes, desc_d, j != 0);
                         mma_commit<1>(bar(kRingEmpty + d_o));
                     }
                     const uint32_t next = more ? scores(0, k0, kSFull, false) : 0;
                     if (!wait(kDsFull, g & 1)) break;
-                    if (lane == 0) {
+                    if (elect_lane()) {
                         mma_tile<kHalf>(tmem + 384, tmem + 128, ring0 + q * kTileBytes, desc_d, j != 0);
                         mma_commit<1>(bar(kRingEmpty + q));
                         if (!more) mma_commit<1>(bar(kAccFull));
@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     __syncthreads();
     const bool failed = *gave_up;
     if (failed) {      // as in the forward kernel
-        if (warp == 1 && lane == 0) {
+        if (warp == 1 && elect_lane()) {      // the lane that issued them
             mma_commit<1>(bar(kLast));
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
         }

@@ -174,9 +174,24 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- tensor cores ---------------------------------------------------------------------------------------
+// True in one lane of a whole warp.
+__device__ __forceinline__ bool elect_lane() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
 // Shared-memory operand descriptor, 128-byte swizzle (descriptor version 1 in bits 46-48, layout 2 in bits
 // 61-63).  K-major tile: rows of 64 bf16 along K, groups of 8 rows 1024 bytes apart (stride offset).
 // MN-major tile: rows of 64 bf16 along M or N, one per k; groups of 8 k 1024 bytes apart (stride offset), the next
