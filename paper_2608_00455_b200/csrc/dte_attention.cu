@@ -157,7 +157,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         tma_prefetch_map(&map_q);
         tma_prefetch_map(&map_k);
         tma_prefetch_map(&map_v);
-        for (uint32_t i = 0; i < 2 * kFwdRing; ++i) mbar_init(bar0 + 8 * i, 1);
+        for (uint32_t i = 0; i < kFwdRing; ++i) {
+            mbar_init(full(i), 1);
+            mbar_init(empty(i), 1);
+        }
         for (uint32_t s = 0; s < 2; ++s) {
             mbar_init(bar(kQFull, s), 1);
             mbar_init(bar(kQEmpty, s), 1);
@@ -182,130 +185,128 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
 
     if (warp < 4) {
-    regs_down<kFewRegs>();
-    if (warp == 0 && lane == 0) {
-        // ---- loads ----
-        uint32_t issued = 0, q_issued[2] = {0, 0};
-        bool ok = true;
-        auto load = [&](const CUtensorMap* map, uint32_t head_at, uint32_t row) {
-            const uint32_t i = issued % kFwdRing;
-            if (!(ok = ok && mbar_wait(empty(i), (issued / kFwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
-            mbar_expect_tx(full(i), tile_bytes);
-            load_rows(ring0 + i * kTileBytes, map, chunks, head_at, row, full(i));
-            ++issued;
-        };
-        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-            if (work_at(i) >= total) continue;
-            const FwdWork f = fwd_work(p, list, work_at(i));
-            for (uint32_t s = 0; s < 2 && ok; ++s) {
-                if (!f.n[s]) continue;
-                if (!(ok = mbar_wait(bar(kQEmpty, s), (q_issued[s] & 1) ^ 1, p.wait_limit, gave_up))) break;
-                mbar_expect_tx(bar(kQFull, s), tile_bytes);
-                load_rows(q0 + s * kTileBytes, &map_q, chunks, f.head[s], f.start + f.row0[s], bar(kQFull, s));
-                ++q_issued[s];
-                if (s == 0) load(&map_k, f.kv_head, f.start);
-            }
-            for (uint32_t t = 0; t < f.n_max && ok; ++t) {
-                load(&map_v, f.kv_head, f.start + t * kAttTile);
-                if (t + 1 < f.n_max) load(&map_k, f.kv_head, f.start + (t + 1) * kAttTile);
-            }
-        }
-        s_issued = issued;
-        s_q_issued[0] = q_issued[0];
-        s_q_issued[1] = q_issued[1];
-    } else if (warp == 1) {
-        // ---- matrix products: the whole warp waits, one lane issues ----
-        const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false);
-        const uint32_t desc_o = mma_desc(kAttTile, (p.head_dim + 15) / 16 * 16, false, true), steps = (p.head_dim + 15) / 16;
-        uint32_t taken = 0, q_taken[2] = {0, 0}, p_taken[2] = {0, 0};
-        bool ok = true;
-        auto wait = [&](uint32_t b, uint32_t parity) {
-            ok = ok && mbar_wait(b, parity, p.wait_limit, gave_up);
-            ok = !__any_sync(0xFFFFFFFFu, !ok);
-            tc_fence_after();
-            return ok;
-        };
-        auto take = [&]() {                       // the next tile of the ring; where it lies
-            const uint32_t i = taken % kFwdRing;
-            if (wait(full(i), taken / kFwdRing & 1)) ++taken;
-            return uniform(i);
-        };
-        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-            if (work_at(i) >= total) continue;
-            const FwdWork f = fwd_work(p, list, work_at(i));
-            auto scores = [&](uint32_t s, uint32_t t, uint32_t k) {
-                if (t == 0) {
-                    if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
-                    ++q_taken[s];
-                }
-                if (elect_lane()) {
-                    mma_rows(tmem + s * 128, q0 + s * kTileBytes, ring0 + k * kTileBytes, steps, desc_s);
-                    mma_commit<1>(bar(kSFull, s));
-                    if (t + 1 == f.n[s]) mma_commit<1>(bar(kQEmpty, s));
-                }
+        regs_down<kFewRegs>();
+        if (warp == 0 && lane == 0) {
+            // ---- loads ----
+            uint32_t issued = 0, q_issued[2] = {0, 0};
+            RingAt<kFwdRing> at;
+            bool ok = true;
+            auto load = [&](const CUtensorMap* map, uint32_t head_at, uint32_t row) {
+                if (!(ok = ok && mbar_wait(empty(at.i), at.phase ^ 1, p.wait_limit, gave_up))) return;
+                mbar_expect_tx(full(at.i), tile_bytes);
+                load_rows(ring0 + at.i * kTileBytes, map, chunks, head_at, row, full(at.i));
+                at.next();
+                ++issued;
             };
-            const uint32_t k0 = take();
-            for (uint32_t s = 0; s < 2 && ok; ++s)
-                if (f.n[s]) scores(s, 0, k0);
-            if (ok && elect_lane()) mma_commit<1>(empty(k0));
-            for (uint32_t t = 0; t < f.n_max && ok; ++t) {
-                const uint32_t v = take();
-                if (!ok) break;
-                if ((t + 1) * kAttTile > f.len) clear_rows(smem + (2 + v) * kTileBytes, chunks, f.len - t * kAttTile);
-                uint32_t k = 0;
-                for (uint32_t s = 0; s < 2 && ok; ++s) {
-                    if (t >= f.n[s]) continue;
-                    if (!wait(bar(kPFull, s), p_taken[s] & 1)) break;
-                    ++p_taken[s];
-                    if (elect_lane()) {
-                        mma_tile<32>(tmem + 256 + s * 128, tmem + s * 128, ring0 + v * kTileBytes, desc_o, t != 0);
-                        if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
-                    }
-                    if (t + 1 < f.n[s]) {
-                        if (s == 0 || t + 1 >= f.n[0]) k = take();
-                        if (ok) scores(s, t + 1, k);
-                    }
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                if (work_at(i) >= total) continue;
+                const FwdWork f = fwd_work(p, list, work_at(i));
+#pragma unroll
+                for (uint32_t s = 0; s < 2; ++s) {
+                    if (!f.n[s] || !ok) continue;
+                    if (!(ok = mbar_wait(bar(kQEmpty, s), (q_issued[s] & 1) ^ 1, p.wait_limit, gave_up))) continue;
+                    mbar_expect_tx(bar(kQFull, s), tile_bytes);
+                    load_rows(q0 + s * kTileBytes, &map_q, chunks, f.head[s], f.start + f.row0[s], bar(kQFull, s));
+                    ++q_issued[s];
+                    if (s == 0) load(&map_k, f.kv_head, f.start);
                 }
-                if (ok && elect_lane()) {
-                    mma_commit<1>(empty(v));
-                    if (t + 1 < f.n_max) mma_commit<1>(empty(k));
+                for (uint32_t t = 0; t < f.n_max && ok; ++t) {
+                    load(&map_v, f.kv_head, f.start + t * kAttTile);
+                    if (t + 1 < f.n_max) load(&map_k, f.kv_head, f.start + (t + 1) * kAttTile);
                 }
             }
+            s_issued = issued;
+            s_q_issued[0] = q_issued[0];
+            s_q_issued[1] = q_issued[1];
+        } else if (warp == 1) {
+            // ---- matrix products: the whole warp waits, one lane issues.  One warp for both slots: their products take turns as
+            // wholes, which is what keeps the slots half a step apart.  (A warp per slot: 9.15 ms where this takes 7.6.) ----
+            const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false);
+            const uint32_t desc_o = mma_desc(kAttTile, (p.head_dim + 15) / 16 * 16, false, true), steps = (p.head_dim + 15) / 16;
+            uint32_t taken = 0, q_taken[2] = {0, 0}, p_taken[2] = {0, 0};
+            RingAt<kFwdRing> at;
+            bool ok = true;
+            auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(b, parity, p.wait_limit, gave_up); };
+            // the next tile of the ring: its address, and the barrier that lets it go
+            auto take = [&](uint32_t& tile, uint32_t& release) {
+                if (!wait(full(at.i), at.phase)) return;
+                tile = uniform(ring0 + at.i * kTileBytes);
+                release = uniform(empty(at.i));
+                at.next();
+                ++taken;
+            };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                if (work_at(i) >= total) continue;
+                const FwdWork f = fwd_work(p, list, work_at(i));
+                uint32_t k = 0, k_release = 0, v = 0, v_release = 0;
+                auto scores = [&](uint32_t s, uint32_t n, uint32_t t) {
+                    if (t == 0) {
+                        if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
+                        ++q_taken[s];
+                    }
+                    if (elect_lane()) {
+                        mma_rows(tmem + s * 128, q0 + s * kTileBytes, k, steps, desc_s);
+                        mma_commit<1>(bar(kSFull, s));
+                        if (t + 1 == n) mma_commit<1>(bar(kQEmpty, s));
+                    }
+                };
+                take(k, k_release);
+#pragma unroll
+                for (uint32_t s = 0; s < 2; ++s)
+                    if (ok && f.n[s]) scores(s, f.n[s], 0);
+                if (ok && elect_lane()) mma_commit<1>(k_release);
+                for (uint32_t t = 0; t < f.n_max && ok; ++t) {
+                    const bool more = t + 1 < f.n_max;
+                    take(v, v_release);
+                    if (more) take(k, k_release);
+#pragma unroll
+                    for (uint32_t s = 0; s < 2; ++s) {
+                        if (!ok || t >= f.n[s] || !wait(bar(kPFull, s), p_taken[s] & 1)) continue;
+                        ++p_taken[s];
+                        if (elect_lane()) {
+                            mma_tile<32>(tmem + 256 + s * 128, tmem + s * 128, v, desc_o, t != 0);
+                            if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
+                        }
+                        if (t + 1 < f.n[s]) scores(s, f.n[s], t + 1);
+                    }
+                    if (ok && elect_lane()) {
+                        mma_commit<1>(v_release);
+                        if (more) mma_commit<1>(k_release);
+                    }
+                }
+            }
+            if (lane == 0) {
+                s_taken = taken;
+                s_q_taken[0] = q_taken[0];
+                s_q_taken[1] = q_taken[1];
+            }
         }
-        if (lane == 0) {
-            s_taken = taken;
-            s_q_taken[0] = q_taken[0];
-            s_q_taken[1] = q_taken[1];
-        }
-    }
     } else {
         regs_up<kManyRegs>();
         // ---- softmax: warp w may read the quarter w % 4 of tensor memory's lanes ----
         const uint32_t s = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = quarter * 32 << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
         const float k2 = p.k2;
-        uint32_t s_taken_ = 0, o_taken = 0;
+        uint32_t tiles = 0, items_done = 0, loads = 0;      // loads: tiles of keys and values of the work so far
         bool ok = true;
-        auto wait = [&](uint32_t b, uint32_t parity) {
-            ok = mbar_wait(b, parity, p.wait_limit, gave_up);
-            ok = !__any_sync(0xFFFFFFFFu, !ok);
-            tc_fence_after();
-            return ok;
-        };
+        auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(b, parity, p.wait_limit, gave_up); };
         for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
             if (work_at(i) >= total) continue;
             const FwdWork f = fwd_work(p, list, work_at(i));
-            if (!f.n[s]) continue;
-            const uint32_t row = f.row0[s] + r;             // in its sequence
+            const uint32_t first_load = loads;
+            loads += 2 * f.n_max;
+            const uint32_t n = s ? f.n[1] : f.n[0], head_at = s ? f.head[1] : f.head[0];
+            if (!n) continue;
+            const uint32_t row = (s ? f.row0[1] : f.row0[0]) + r;             // in its sequence
             float top = -INFINITY, sum = 0.f;               // top: what O and sum are relative to
-            for (uint32_t t = 0; t < f.n[s]; ++t) {
-                if (!wait(bar(kSFull, s), s_taken_++ & 1)) break;
+            for (uint32_t t = 0; t < n; ++t) {
+                if (!wait(bar(kSFull, s), tiles++ & 1)) break;
                 uint32_t v[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, v[c]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load_wait(v[c]);
-                if (t + 1 == f.n[s]) {                      // the tile on the diagonal
+                if (t + 1 == n) {                      // the tile on the diagonal
 #pragma unroll
                     for (int j = 0; j < 128; ++j) v[j / 32][j % 32] = (uint32_t)j > r ? __float_as_uint(-INFINITY) : v[j / 32][j % 32];
                 }
@@ -354,17 +355,22 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                 float even, odd;
                 f2_get(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), even, odd);
                 sum += even + odd;
+                if ((t + 1) * kAttTile > f.len) {           // values past the sequence; they lie where the load behind the keys' went
+                    const uint32_t at = first_load + 2 * t + 1, i = at % kFwdRing;
+                    if (!wait(full(i), at / kFwdRing & 1)) break;
+                    clear_rows(smem + (2 + i) * kTileBytes, chunks, f.len - t * kAttTile, r, 128);
+                }
                 tmem_store_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kPFull, s));
             }
-            if (!ok || !wait(bar(kOFull, s), o_taken++ & 1)) break;
+            if (!ok || !wait(bar(kOFull, s), items_done++ & 1)) break;
             const bool valid = row < f.len;
             const uint64_t at = (uint64_t)f.start + row;
-            if (valid && p.lse) p.lse[f.head[s] * p.tokens + at] = fmaf(top, p.scale, logf(sum));
+            if (valid && p.lse) p.lse[head_at * p.tokens + at] = fmaf(top, p.scale, logf(sum));
             const float by = 1.f / sum;
-            __nv_bfloat16* out = p.out + at * p.out_ld + f.head[s] * p.head_dim;
+            __nv_bfloat16* out = p.out + at * p.out_ld + head_at * p.head_dim;
             for (uint32_t c = 0; c < p.head_dim; c += 32) {
                 uint32_t v[32];
                 tmem_load32(o_at + c, v);

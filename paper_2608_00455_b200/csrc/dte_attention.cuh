@@ -67,17 +67,39 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
     for (uint32_t c = 0; c < chunks; ++c) tma_load_3d<1>(dst + c * kChunkBytes, map, (int)(c * 64), (int)head, (int)row, bar);
 }
 
-// Rows from `from` on of a tile in shared memory become zeros, by one warp: rows of another sequence, or of none, would otherwise
-// meet zeros of the other operand, and 0 * NaN is NaN.
-__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from) {
+// Rows from `from` on of a tile in shared memory become zeros: rows of another sequence, or of none, would otherwise meet zeros of
+// the other operand, and 0 * NaN is NaN.  By the `threads` threads that write that operand, before they say that it is there.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from, uint32_t thread, uint32_t threads) {
     const uint32_t per = (kAttTile - from) * 8;
-    for (uint32_t i = threadIdx.x & 31; i < per * chunks; i += 32) {
+    for (uint32_t i = thread; i < per * chunks; i += threads) {
         const uint32_t c = i / per, r = i - c * per;
         *reinterpret_cast<uint4*>(tile + c * kChunkBytes + from * 128 + r * 16) = make_uint4(0, 0, 0, 0);
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
 }
+
+// A wait of a whole warp; all lanes go on or stop together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t limit, volatile uint32_t* gave_up) {
+    bool ok = mbar_test_wait(bar, parity);
+    if (!__all_sync(0xFFFFFFFFu, ok)) {
+        ok = mbar_wait(bar, parity, limit, gave_up);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+    }
+    tc_fence_after();
+    return ok;
+}
+
+// Place in a ring of N tiles.
+template <uint32_t N>
+struct RingAt {
+    uint32_t i = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++i == N) {
+            i = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 // Products are issued by one lane that the warp elects: the compiler then knows the branch, and with `uniform` the operands'
 // addresses, to be the same for the whole warp, and keeps descriptors in uniform registers.  (An issue by `lane == 0`, descriptors made

@@ -104,11 +104,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             // ---- loads ----
             uint32_t issued = 0, q_issued = 0;
             bool ok = true;
+            RingAt<kBwdRing> at;
             auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
-                const uint32_t i = issued % kBwdRing;
-                if (!(ok = ok && mbar_wait(bar(kRingEmpty + i), (issued / kBwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
-                mbar_expect_tx(bar(kRingFull + i), tile_bytes);
-                load_rows(ring0 + i * kTileBytes, map, chunks, head, row, bar(kRingFull + i));
+                if (!(ok = ok && mbar_wait(bar(kRingEmpty + at.i), at.phase ^ 1, p.wait_limit, gave_up))) return;
+                mbar_expect_tx(bar(kRingFull + at.i), tile_bytes);
+                load_rows(ring0 + at.i * kTileBytes, map, chunks, head, row, bar(kRingFull + at.i));
+                at.next();
                 ++issued;
             };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
@@ -132,57 +133,53 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             // ---- matrix products: the whole warp waits, one lane issues ----
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
-            uint32_t taken = 0, q_taken = 0, g = 0, dp_issued = 0;
+            uint32_t taken = 0, q_taken = 0, g = 0;
+            RingAt<kBwdRing> at;
             bool ok = true;
-            auto wait = [&](uint32_t b, uint32_t parity) {
-                ok = ok && mbar_wait(bar(b), parity, p.wait_limit, gave_up);
-                ok = !__any_sync(0xFFFFFFFFu, !ok);
-                tc_fence_after();
-                return ok;
-            };
-            auto take = [&]() {
-                const uint32_t i = taken % kBwdRing;
-                if (wait(kRingFull + i, taken / kBwdRing & 1)) ++taken;
-                return uniform(i);
+            auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
+            // the next tile of the ring: its address, and the barrier that lets it go
+            auto take = [&](uint32_t& tile, uint32_t& empty) {
+                if (!wait(kRingFull + at.i, at.phase)) return false;
+                tile = uniform(ring0 + at.i * kTileBytes);
+                empty = uniform(bar(kRingEmpty + at.i));
+                at.next();
+                ++taken;
+                return true;
             };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 const uint32_t w = work_at(i);
                 if (w >= total) continue;
-                const PlanItem it = list[w / p.units];
-                const uint32_t n = it.tile + 1;
+                const uint32_t n = list[w / p.units].tile + 1;
                 if (!wait(kQFull, q_taken & 1)) break;
                 ++q_taken;
-                // S and dP of tile t of the keys, into S's buffer `at`
-                auto scores = [&](uint32_t t, uint32_t at) {
-                    const uint32_t k = take();
-                    if (!ok) return k;
-                    if ((t + 1) * kAttTile > it.len) clear_rows(smem + (2 + k) * kTileBytes, chunks, it.len - t * kAttTile);
+                uint32_t k = 0, k_empty = 0, next = 0, next_empty = 0;
+                // S and dP of the h-th tile of all so far, the t-th of this work
+                auto scores = [&](uint32_t t, uint32_t h) {
+                    if (!take(next, next_empty)) return;
                     if (elect_lane()) {
-                        mma_rows(tmem + at * 128, q0, ring0 + k * kTileBytes, steps, desc_s);
-                        mma_commit<1>(bar(kSFull + at));
+                        mma_rows(tmem + (h & 1) * 128, q0, next, steps, desc_s);
+                        mma_commit<1>(bar(kSFull + (h & 1)));
                     }
-                    if (dp_issued && !wait(kDpRead, (dp_issued - 1) & 1)) return k;
-                    const uint32_t v = take();
-                    if (!ok) return k;
-                    ++dp_issued;
+                    uint32_t v, v_empty;
+                    if ((h && !wait(kDpRead, (h - 1) & 1)) || !take(v, v_empty)) return;
                     if (elect_lane()) {
-                        mma_rows(tmem + 256, do0, ring0 + v * kTileBytes, steps, desc_s);
+                        mma_rows(tmem + 256, do0, v, steps, desc_s);
                         mma_commit<1>(bar(kDpFull));
-                        mma_commit<1>(bar(kRingEmpty + v));
+                        mma_commit<1>(v_empty);
                         if (t + 1 == n) mma_commit<1>(bar(kQEmpty));
                     }
-                    return k;
                 };
-                uint32_t k = scores(0, g & 1);
+                scores(0, g);
                 for (uint32_t t = 0; t < n && ok; ++t, ++g) {
-                    const uint32_t next = t + 1 < n ? scores(t + 1, (g + 1) & 1) : 0;
-                    if (!ok || !wait(kDsFull + (g & 1), g >> 1 & 1)) break;
+                    k = next;
+                    k_empty = next_empty;
+                    if (t + 1 < n) scores(t + 1, g + 1);
+                    if (!wait(kDsFull + (g & 1), g >> 1 & 1)) break;
                     if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 384, tmem + (g & 1) * 128, ring0 + k * kTileBytes, desc_d, t != 0);
-                        mma_commit<1>(bar(kRingEmpty + k));
+                        mma_tile<kHalf>(tmem + 384, tmem + (g & 1) * 128, k, desc_d, t != 0);
+                        mma_commit<1>(k_empty);
                         if (t + 1 == n) mma_commit<1>(bar(kDqFull));
                     }
-                    k = next;
                 }
             }
             if (lane == 0) {
@@ -197,12 +194,31 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         const uint32_t mine = tmem + (quarter * 32 << 16);
         uint32_t g = 0, done = 0;
         bool ok = true;
-        auto wait = [&](uint32_t b, uint32_t parity) {
-            ok = mbar_wait(bar(b), parity, p.wait_limit, gave_up);
-            ok = !__any_sync(0xFFFFFFFFu, !ok);
-            tc_fence_after();
-            return ok;
+        auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
+        // What delta needs of a row, asked for before the work in front is finished: each of the row's two threads takes every other group
+        // of eight columns of out and dout.
+        Raw8<__nv_bfloat16> o8[kMaxAttDim / 16], d8[kMaxAttDim / 16];
+        float lse_ahead = 0.f;
+        auto fetch = [&](uint32_t i) {
+            if (i * gridDim.x >= total || work_at(i) >= total) return;
+            const PlanItem it = list[work_at(i) / p.units];
+            const uint32_t h = work_at(i) % p.units, row = it.tile * kAttTile + r;
+            const uint64_t at = (uint64_t)it.start + row;
+            const __nv_bfloat16 *o = p.o + at * p.o_ld + h * p.head_dim, *d = p.d_o + at * p.do_ld + h * p.head_dim;
+#pragma unroll
+            for (uint32_t j = 0; j < kMaxAttDim / 16; ++j) {
+                const uint32_t c = half * 8 + j * 16;
+                if (row < it.len && c < p.head_dim) {
+                    o8[j].load(o + c);
+                    d8[j].load(d + c);
+                } else {
+                    o8[j].zero();
+                    d8[j].zero();
+                }
+            }
+            lse_ahead = row < it.len ? p.lse_in[h * p.tokens + at] : 0.f;
         };
+        fetch(0);
         for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
             const uint32_t w = work_at(i);
             if (w >= total) continue;
@@ -210,22 +226,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t h = w % p.units, n = it.tile + 1, row = it.tile * kAttTile + r;
             const bool valid = row < it.len;
             const uint64_t at = (uint64_t)it.start + row;
-            // delta: each of a row's two threads takes every other group of eight columns
             float part = 0.f;
-            if (valid) {
-                const __nv_bfloat16 *o = p.o + at * p.o_ld + h * p.head_dim, *d = p.d_o + at * p.do_ld + h * p.head_dim;
-                for (uint32_t c = half * 8; c < p.head_dim; c += 16) {
-                    Raw8<__nv_bfloat16> x, y;
-                    float a[8], b[8];
-                    x.load(o + c);
-                    y.load(d + c);
-                    x.get(a);
-                    y.get(b);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) part = fmaf(a[j], b[j], part);
-                }
+            for (uint32_t j = 0; j < kMaxAttDim / 16; ++j) {
+                float a[8], b[8];
+                o8[j].get(a);
+                d8[j].get(b);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) part = fmaf(a[c], b[c], part);
             }
-            const float lse2 = valid ? p.lse_in[h * p.tokens + at] * -(float)kLog2eD : 0.f;
+            const float lse2 = lse_ahead * -(float)kLog2eD;
             s_delta[done & 1][half][r] = part;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kDelta));
@@ -251,10 +261,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 #pragma unroll
                     for (int j = 0; j < (int)kHalf; ++j) z[j] = half * kHalf + j > r || row == 0 ? 0.f : z[j];
                 }
+                if ((t + 1) * kAttTile > it.len)              // keys past the sequence; each step has two loads
+                    clear_rows(smem + (2 + 2 * g % kBwdRing) * kTileBytes, chunks, it.len - t * kAttTile, threadIdx.x - 128, 256);
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
             }
-            if (!ok || !wait(kDqFull, done & 1)) break;
+            if (!ok) break;
+            fetch(i + 1);
+            if (!wait(kDqFull, done & 1)) break;
             ++done;
             __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
             for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid);
@@ -342,11 +356,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             // ---- loads ----
             uint32_t issued = 0, kv_issued = 0;
             bool ok = true;
+            RingAt<kBwdRing> at;
             auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
-                const uint32_t i = issued % kBwdRing;
-                if (!(ok = ok && mbar_wait(bar(kRingEmpty + i), (issued / kBwdRing & 1) ^ 1, p.wait_limit, gave_up))) return;
-                mbar_expect_tx(bar(kRingFull + i), tile_bytes);
-                load_rows(ring0 + i * kTileBytes, map, chunks, head, row, bar(kRingFull + i));
+                if (!(ok = ok && mbar_wait(bar(kRingEmpty + at.i), at.phase ^ 1, p.wait_limit, gave_up))) return;
+                mbar_expect_tx(bar(kRingFull + at.i), tile_bytes);
+                load_rows(ring0 + at.i * kTileBytes, map, chunks, head, row, bar(kRingFull + at.i));
+                at.next();
                 ++issued;
             };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
@@ -370,55 +385,47 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
             uint32_t taken = 0, kv_taken = 0, g = 0;
+            RingAt<kBwdRing> at;
             bool ok = true;
-            auto wait = [&](uint32_t b, uint32_t parity) {
-                ok = ok && mbar_wait(bar(b), parity, p.wait_limit, gave_up);
-                ok = !__any_sync(0xFFFFFFFFu, !ok);
-                tc_fence_after();
-                return ok;
-            };
+            auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 if (work_at(i) >= total) continue;
-                const DkvWork f = dkv_work(p, list, work_at(i));
+                const uint32_t n = dkv_work(p, list, work_at(i)).n;
                 if (!wait(kKvFull, kv_taken & 1)) break;
                 ++kv_taken;
-                // the next tile of the ring; rows past the sequence are cleared.  t: its tile of queries
-                auto take = [&](uint32_t t) {
-                    const uint32_t i = taken % kBwdRing;
-                    if (!wait(kRingFull + i, taken / kBwdRing & 1)) return uniform(i);
+                uint32_t q = 0, q_empty = 0, d_o = 0, do_empty = 0, next, next_empty;
+                // scores d = a (the next tile of the ring)^T; tile and empty: where it lies, and the barrier that lets it go
+                auto scores = [&](uint32_t d, uint32_t a, uint32_t full, bool last, uint32_t& tile, uint32_t& empty) {
+                    if (!wait(kRingFull + at.i, at.phase)) return;
+                    tile = uniform(ring0 + at.i * kTileBytes);
+                    empty = uniform(bar(kRingEmpty + at.i));
+                    at.next();
                     ++taken;
-                    if ((t + 1) * kAttTile > f.len) clear_rows(smem + (2 + i) * kTileBytes, chunks, f.len - t * kAttTile);
-                    return uniform(i);
-                };
-                uint32_t ahead = f.tile;               // tile of queries of the next S and dP
-                auto scores = [&](uint32_t d, uint32_t a, uint32_t full, bool last) {
-                    const uint32_t at = take(ahead);
-                    if (ok && elect_lane()) {
-                        mma_rows(tmem + d, a, ring0 + at * kTileBytes, steps, desc_s);
+                    if (elect_lane()) {
+                        mma_rows(d, a, tile, steps, desc_s);
                         mma_commit<1>(bar(full));
                         if (last) mma_commit<1>(bar(kKvEmpty));
                     }
-                    return at;
                 };
-                uint32_t q = scores(0, k0, kSFull, false);
-                uint32_t d_o = scores(128, v0, kDpFull, f.n == 1);
-                for (uint32_t j = 0; j < f.n && ok; ++j, ++g) {
-                    const bool more = j + 1 < f.n;
-                    if (++ahead == f.tile + f.tiles) ahead = f.tile;
+                scores(tmem, k0, kSFull, false, q, q_empty);
+                scores(tmem + 128, v0, kDpFull, n == 1, d_o, do_empty);
+                for (uint32_t j = 0; j < n && ok; ++j, ++g) {
+                    const bool more = j + 1 < n;
                     if (!wait(kPFull, g & 1)) break;
                     if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 256, tmem, ring0 + d_o * kTileBytes, desc_d, j != 0);
-                        mma_commit<1>(bar(kRingEmpty + d_o));
+                        mma_tile<kHalf>(tmem + 256, tmem, d_o, desc_d, j != 0);
+                        mma_commit<1>(do_empty);
                     }
-                    const uint32_t next = more ? scores(0, k0, kSFull, false) : 0;
+                    if (more) scores(tmem, k0, kSFull, false, next, next_empty);
                     if (!wait(kDsFull, g & 1)) break;
                     if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 384, tmem + 128, ring0 + q * kTileBytes, desc_d, j != 0);
-                        mma_commit<1>(bar(kRingEmpty + q));
+                        mma_tile<kHalf>(tmem + 384, tmem + 128, q, desc_d, j != 0);
+                        mma_commit<1>(q_empty);
                         if (!more) mma_commit<1>(bar(kAccFull));
                     }
-                    if (more) d_o = scores(128, v0, kDpFull, j + 2 == f.n);
                     q = next;
+                    q_empty = next_empty;
+                    if (more) scores(tmem + 128, v0, kDpFull, j + 2 == n, d_o, do_empty);
                 }
             }
             if (lane == 0) {
@@ -459,12 +466,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         const uint32_t mine = tmem + (quarter * 32 << 16), s_at = mine + half * kHalf, d_at = s_at + 128;
         uint32_t g = 0, done = 0;
         bool ok = true;
-        auto wait = [&](uint32_t b, uint32_t parity) {
-            ok = mbar_wait(bar(b), parity, p.wait_limit, gave_up);
-            ok = !__any_sync(0xFFFFFFFFu, !ok);
-            tc_fence_after();
-            return ok;
-        };
+        auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
         for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
             if (work_at(i) >= total) continue;
             const DkvWork f = dkv_work(p, list, work_at(i));
@@ -489,6 +491,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     const uint32_t key = f.tile * kAttTile + r;
 #pragma unroll
                     for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len ? 0.f : z[c];
+                }
+                if ((t + 1) * kAttTile > f.len) {             // rows past the sequence, of q and of dout
+                    const uint32_t q = 2 * g % kBwdRing, d_o = (2 * g + 1) % kBwdRing;
+                    if (!wait(kRingFull + d_o, (2 * g + 1) / kBwdRing & 1)) break;
+                    clear_rows(smem + (2 + q) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
+                    clear_rows(smem + (2 + d_o) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
                 }
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kPFull));
