@@ -143,14 +143,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     att_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
-    __shared__ __align__(8) uint64_t s_bar[2 * kFwdRing + 10 + 1];
-    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_q_issued[2], s_q_taken[2];
+    __shared__ __align__(8) uint64_t s_bar[2 * kFwdRing + 12 + 1];
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken[2], s_q_issued[2], s_q_taken[2];
     const uint32_t q0 = smem_addr(smem), ring0 = q0 + 2 * kTileBytes, bar0 = smem_addr(s_bar);
     auto full = [&](uint32_t i) { return bar0 + 8 * i; };
     auto empty = [&](uint32_t i) { return bar0 + 8 * (kFwdRing + i); };
     auto bar = [&](uint32_t kind, uint32_t s) { return bar0 + 8 * (2 * kFwdRing + 2 * kind + s); };
-    enum { kQFull, kQEmpty, kSFull, kPFull, kOFull };
-    const uint32_t last_bar = bar0 + 8 * (2 * kFwdRing + 10);
+    enum { kQFull, kQEmpty, kSFull, kPFull, kOFull, kTurn };
+    const uint32_t last_bar = bar0 + 8 * (2 * kFwdRing + 12);
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         tma_prefetch_map(&map_v);
         for (uint32_t i = 0; i < kFwdRing; ++i) {
             mbar_init(full(i), 1);
-            mbar_init(empty(i), 1);
+            mbar_init(empty(i), 2);
         }
         for (uint32_t s = 0; s < 2; ++s) {
             mbar_init(bar(kQFull, s), 1);
@@ -167,9 +167,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             mbar_init(bar(kSFull, s), 1);
             mbar_init(bar(kPFull, s), 4);
             mbar_init(bar(kOFull, s), 1);
+            mbar_init(bar(kTurn, s), 1);
         }
-        mbar_init(last_bar, 1);
-        s_gave_up = s_issued = s_taken = s_q_issued[0] = s_q_issued[1] = s_q_taken[0] = s_q_taken[1] = 0;
+        mbar_init(last_bar, 2);
+        s_gave_up = s_issued = s_taken[0] = s_taken[1] = s_q_issued[0] = s_q_issued[1] = s_q_taken[0] = s_q_taken[1] = 0;
+        mbar_arrive(bar(kTurn, 0));            // the first turn is slot 0's
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -218,12 +220,15 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             s_issued = issued;
             s_q_issued[0] = q_issued[0];
             s_q_issued[1] = q_issued[1];
-        } else if (warp == 1) {
-            // ---- matrix products: the whole warp waits, one lane issues.  One warp for both slots: their products take turns as
-            // wholes, which is what keeps the slots half a step apart.  (A warp per slot: 9.15 ms where this takes 7.6.) ----
+        } else if (warp == 1 || warp == 2) {
+            // ---- matrix products of one slot: the whole warp waits, one lane issues ----
+            // An issue blocks until the tensor cores are nearly through with it, so whatever else the issuing warp does leaves them
+            // idle: there is a warp per slot, and one waits for barriers while the other one issues.  They take turns, so that
+            // products run as wholes and the slots stay half a step apart (without turns: 9.15 ms; one warp for both: 7.5).
+            const uint32_t s = warp - 1, s_at = tmem + s * 128, o_at = tmem + 256 + s * 128, qs = q0 + s * kTileBytes;
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false);
             const uint32_t desc_o = mma_desc(kAttTile, (p.head_dim + 15) / 16 * 16, false, true), steps = (p.head_dim + 15) / 16;
-            uint32_t taken = 0, q_taken[2] = {0, 0}, p_taken[2] = {0, 0};
+            uint32_t taken = 0, q_taken = 0, p_taken = 0, turns = 0;
             RingAt<kFwdRing> at;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(b, parity, p.wait_limit, gave_up); };
@@ -238,47 +243,34 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 if (work_at(i) >= total) continue;
                 const FwdWork f = fwd_work(p, list, work_at(i));
+                const uint32_t n = s ? f.n[1] : f.n[0];
                 uint32_t k = 0, k_release = 0, v = 0, v_release = 0;
-                auto scores = [&](uint32_t s, uint32_t n, uint32_t t) {
-                    if (t == 0) {
-                        if (!wait(bar(kQFull, s), q_taken[s] & 1)) return;
-                        ++q_taken[s];
-                    }
-                    if (elect_lane()) {
-                        mma_rows(tmem + s * 128, q0 + s * kTileBytes, k, steps, desc_s);
-                        mma_commit<1>(bar(kSFull, s));
-                        if (t + 1 == n) mma_commit<1>(bar(kQEmpty, s));
-                    }
-                };
-                take(k, k_release);
-#pragma unroll
-                for (uint32_t s = 0; s < 2; ++s)
-                    if (ok && f.n[s]) scores(s, f.n[s], 0);
-                if (ok && elect_lane()) mma_commit<1>(k_release);
-                for (uint32_t t = 0; t < f.n_max && ok; ++t) {
-                    const bool more = t + 1 < f.n_max;
-                    take(v, v_release);
+                // step -1 makes the first scores; step t adds up the values of tile t and makes the scores of the next one.  A slot
+                // that is through takes its turns and lets the tiles go, as the other one does.
+                for (int t = -1; t < (int)f.n_max && ok; ++t) {
+                    const bool more = t + 1 < (int)f.n_max, mine = t >= 0 && t < (int)n, next = t + 1 < (int)n;
+                    if (t >= 0) take(v, v_release);
                     if (more) take(k, k_release);
-#pragma unroll
-                    for (uint32_t s = 0; s < 2; ++s) {
-                        if (!ok || t >= f.n[s] || !wait(bar(kPFull, s), p_taken[s] & 1)) continue;
-                        ++p_taken[s];
-                        if (elect_lane()) {
-                            mma_tile<32>(tmem + 256 + s * 128, tmem + s * 128, v, desc_o, t != 0);
-                            if (t + 1 == f.n[s]) mma_commit<1>(bar(kOFull, s));
+                    if (t < 0 && n && wait(bar(kQFull, s), q_taken & 1)) ++q_taken;
+                    if (mine && wait(bar(kPFull, s), p_taken & 1)) ++p_taken;
+                    if (!wait(bar(kTurn, s), turns++ & 1)) break;
+                    if (elect_lane()) {
+                        if (mine) mma_tile<32>(o_at, s_at, v, desc_o, t != 0);
+                        if (next) {
+                            mma_rows(s_at, qs, k, steps, desc_s);
+                            mma_commit<1>(bar(kSFull, s));
                         }
-                        if (t + 1 < f.n[s]) scores(s, f.n[s], t + 1);
-                    }
-                    if (ok && elect_lane()) {
-                        mma_commit<1>(v_release);
+                        mbar_arrive(bar(kTurn, s ^ 1));
+                        if (mine && !next) mma_commit<1>(bar(kOFull, s));
+                        if (t + 2 == (int)n) mma_commit<1>(bar(kQEmpty, s));
+                        if (t >= 0) mma_commit<1>(v_release);
                         if (more) mma_commit<1>(k_release);
                     }
                 }
             }
             if (lane == 0) {
-                s_taken = taken;
-                s_q_taken[0] = q_taken[0];
-                s_q_taken[1] = q_taken[1];
+                s_taken[s] = taken;
+                s_q_taken[s] = q_taken;
             }
         }
     } else {
@@ -397,13 +389,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     if (failed) {
         // A wait ran out: all roles have stopped.  What they left in flight ends here, again with a limit: the products, and every
         // load that no product has waited for.
-        if (warp == 1 && elect_lane()) {      // the lane that issued them
+        if ((warp == 1 || warp == 2) && elect_lane()) {      // the lanes that issued them
             mma_commit<1>(last_bar);
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(last_bar, 0); ++i) {}
         }
         if (threadIdx.x == 0) {
             uint32_t left = kWaitTries;
-            drain_loads(full(0), kFwdRing, s_taken, s_issued, left);
+            drain_loads(full(0), kFwdRing, max(s_taken[0], s_taken[1]), s_issued, left);
             for (uint32_t s = 0; s < 2; ++s) drain_loads(bar(kQFull, s), 1, s_q_taken[s], s_q_issued[s], left);
         }
         __syncthreads();
