@@ -139,6 +139,47 @@ __device__ __forceinline__ FwdWork fwd_work(const AttParams& p, const PlanItem* 
     return f;
 }
 
+// This thread's row of S; on the diagonal, keys behind the row are hidden.
+__device__ __forceinline__ void load_scores(uint32_t (&v)[4][32], uint32_t s_at, bool diagonal, uint32_t row) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, v[c]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) tmem_load_wait(v[c]);
+    if (diagonal) {
+#pragma unroll
+        for (int j = 0; j < 128; ++j) v[j / 32][j % 32] = (uint32_t)j > row ? __float_as_uint(-INFINITY) : v[j / 32][j % 32];
+    }
+}
+
+// The largest of a row and `top`, in four chains so that latencies overlap; a NaN spreads to the whole row through it.
+__device__ __forceinline__ float row_max(const uint32_t (&v)[4][32], float top) {
+    float high[4] = {top, top, top, top};
+#pragma unroll
+    for (int j = 0; j < 32; j += 2)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) high[c] = max3_nan(high[c], __uint_as_float(v[c][j]), __uint_as_float(v[c][j + 1]));
+    return max3_nan(max3_nan(high[0], high[1], high[2]), high[3], high[3]);
+}
+
+// P of a row, as bf16 pairs, and its sum in fp32.
+__device__ __forceinline__ float make_weights(const uint32_t (&v)[4][32], float k2, float from, uint32_t (&w)[64]) {
+    const F2 by2 = f2(k2, k2), from2 = f2(from, from);
+    F2 part[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+        const uint32_t* x = &v[j / 16][j % 16 * 2];
+        const F2 arg = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), by2, from2);
+        float lo, hi;
+        f2_get(arg, lo, hi);
+        const F2 e = f2(exp2_fast(lo), exp2_fast(hi));
+        part[j % 4] = f2_add(part[j % 4], e);
+        w[j] = pack_bf16(e);
+    }
+    float even, odd;
+    f2_get(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), even, odd);
+    return even + odd;
+}
+
 __global__ void __launch_bounds__(kFwdThreads, 1)
     att_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttParams p) {
@@ -252,8 +293,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                     if (t >= 0) take(v, v_release);
                     if (more) take(k, k_release);
                     if (t < 0 && n && wait(bar(kQFull, s), q_taken & 1)) ++q_taken;
-                    if (mine && wait(bar(kPFull, s), p_taken & 1)) ++p_taken;
                     if (!wait(bar(kTurn, s), turns++ & 1)) break;
+                    if (mine && !wait(bar(kPFull, s), p_taken++ & 1)) break;      // last: what is behind it is the tensor cores' time
                     if (elect_lane()) {
                         if (mine) mma_tile<32>(o_at, s_at, v, desc_o, t != 0);
                         if (next) {
@@ -293,60 +334,32 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             float top = -INFINITY, sum = 0.f;               // top: what O and sum are relative to
             for (uint32_t t = 0; t < n; ++t) {
                 if (!wait(bar(kSFull, s), tiles++ & 1)) break;
-                uint32_t v[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, v[c]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load_wait(v[c]);
-                if (t + 1 == n) {                      // the tile on the diagonal
-#pragma unroll
-                    for (int j = 0; j < 128; ++j) v[j / 32][j % 32] = (uint32_t)j > r ? __float_as_uint(-INFINITY) : v[j / 32][j % 32];
-                }
-                // four chains, so that latencies overlap; a NaN spreads to the whole row through the maximum
-                float high[4] = {top, top, top, top};
-#pragma unroll
-                for (int j = 0; j < 32; j += 2)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) high[c] = max3_nan(high[c], __uint_as_float(v[c][j]), __uint_as_float(v[c][j + 1]));
-                const float peak = max3_nan(max3_nan(high[0], high[1], high[2]), high[3], high[3]);
-                // each row decides for itself, so that no row's rounding depends on its neighbours; a NaN counts as growth
-                const bool grown = t != 0 && !((peak - top) * k2 <= kRescaleAbove);
-                if (t == 0) {
-                    top = peak;
-                } else if (__any_sync(0xFFFFFFFFu, grown)) {
-                    const float by = !grown || peak == -INFINITY ? 1.f : exp2_fast((top - peak) * k2);
+                const bool diagonal = t + 1 == n;
+                uint32_t v[4][32], w[64];
+                load_scores(v, s_at, diagonal, r);
+                float peak = row_max(v, top);
+                if (t == 0) top = peak;
+                // P relative to the maximum of the tiles in front, made beside this tile's maximum; only where that has grown by much
+                // (each row decides for itself, so that no row's rounding depends on its neighbours; a NaN counts, once) P is made again
+                float part = make_weights(v, k2, top == -INFINITY ? 0.f : -top * k2, w);
+                const bool grown = (peak - top) * k2 > kRescaleAbove || (peak != peak && top == top);
+                if (__any_sync(0xFFFFFFFFu, grown)) {
+                    const float by = grown ? exp2_fast((top - peak) * k2) : 1.f;
                     top = grown ? peak : top;
                     sum *= by;
                     for (uint32_t c = 0; c < p.head_dim; c += 32) {
-                        uint32_t v[32];
-                        tmem_load32(o_at + c, v);
-                        tmem_load_wait(v);
+                        uint32_t o[32];
+                        tmem_load32(o_at + c, o);
+                        tmem_load_wait(o);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * by);
-                        tmem_store32(o_at + c, v);
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by);
+                        tmem_store32(o_at + c, o);
                     }
+                    load_scores(v, s_at, diagonal, r);
+                    part = make_weights(v, k2, top == -INFINITY ? 0.f : -top * k2, w);
                 }
-                const float from = top == -INFINITY ? 0.f : -top * k2;
-                const F2 by2 = f2(k2, k2), from2 = f2(from, from);
-                F2 part[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t* x = &v[2 * c + j / 16][j % 16 * 2];
-                        float lo, hi;
-                        f2_get(f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), by2, from2), lo, hi);
-                        lo = exp2_fast(lo);
-                        hi = exp2_fast(hi);
-                        part[j % 4] = f2_add(part[j % 4], f2(lo, hi));
-                        w[j] = pack_bf16(lo, hi);
-                    }
-                    tmem_store32(s_at + c * 32, w);
-                }
-                float even, odd;
-                f2_get(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), even, odd);
-                sum += even + odd;
+                sum += part;
+                tmem_store64(s_at, w);
                 if ((t + 1) * kAttTile > f.len) {           // values past the sequence; they lie where the load behind the keys' went
                     const uint32_t at = first_load + 2 * t + 1, i = at % kFwdRing;
                     if (!wait(full(i), at / kFwdRing & 1)) break;

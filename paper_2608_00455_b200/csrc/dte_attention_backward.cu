@@ -17,8 +17,8 @@ namespace dte {
 constexpr uint32_t kBwdThreads = 3 * 128;         // registers as in the forward kernel
 constexpr uint32_t kBwdWarps = 8;                 // that work on scores
 constexpr int kFewRegs = 72, kManyRegs = 208;     // 128 * (72 + 2 * 208) = 62464 of the 384 * 168 = 64512 at launch
-constexpr uint32_t kBwdRing = 5;
-constexpr uint32_t kBwdSmem = (2 + kBwdRing) * kTileBytes;
+constexpr uint32_t kRing3 = 3, kRing2 = 2;         // tiles in flight of the two streams, a ring each: every barrier has one reader in order
+constexpr uint32_t kBwdSmem = (2 + kRing3 + kRing2) * kTileBytes;
 constexpr uint32_t kHalf = kAttTile / 2;          // columns of a tile that a thread works on
 // In tensor memory a tile of scores takes 128 columns.  The bf16 operand made of it lies over it, each half over the
 // columns that the same threads have read.
@@ -70,11 +70,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     att_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
-    enum { kRingFull, kRingEmpty = kBwdRing, kQFull = 2 * kBwdRing, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull, kDelta, kLast, kBars };
+    enum { kKFull, kKEmpty = kRing3, kVFull = 2 * kRing3, kVEmpty = kVFull + kRing2, kQFull = kVEmpty + kRing2, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull, kDelta, kLast, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
-    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_q_issued, s_q_taken;
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of K, V, and Q with dout
     __shared__ float s_delta[2][2][kAttTile];
-    const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, ring0 = q0 + 2 * kTileBytes;
+    const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, kt0 = q0 + 2 * kTileBytes, vt0 = kt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -83,8 +83,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         tma_prefetch_map(&map_v);
         tma_prefetch_map(&map_do);
         for (uint32_t i = 0; i < kBars; ++i)
-            mbar_init(bar(i), i == kDsFull || i == kDsFull + 1 || i == kDpRead || i == kDelta ? kBwdWarps : 1);
-        s_gave_up = s_issued = s_taken = s_q_issued = s_q_taken = 0;
+            mbar_init(bar(i), i == kDsFull || i == kDsFull + 1 || i == kDpRead || i == kDelta ? kBwdWarps : i == kQEmpty || i == kLast ? 2 : 1);
+        s_gave_up = 0;
+        for (uint32_t i = 0; i < 3; ++i) s_issued[i] = s_taken[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -102,16 +103,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         regs_down<kFewRegs>();
         if (warp == 0 && lane == 0) {
             // ---- loads ----
-            uint32_t issued = 0, q_issued = 0;
+            uint32_t tiles = 0, k_issued = 0, q_issued = 0;
+            RingAt<kRing3> ka;
+            RingAt<kRing2> va;
             bool ok = true;
-            RingAt<kBwdRing> at;
-            auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
-                if (!(ok = ok && mbar_wait(bar(kRingEmpty + at.i), at.phase ^ 1, p.wait_limit, gave_up))) return;
-                mbar_expect_tx(bar(kRingFull + at.i), tile_bytes);
-                load_rows(ring0 + at.i * kTileBytes, map, chunks, head, row, bar(kRingFull + at.i));
-                at.next();
-                ++issued;
-            };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 const uint32_t w = work_at(i);
                 if (w >= total) continue;
@@ -122,70 +117,93 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 load_rows(q0, &map_q, chunks, h, row, bar(kQFull));
                 load_rows(do0, &map_do, chunks, h, row, bar(kQFull));
                 ++q_issued;
-                for (uint32_t t = 0; t <= it.tile && ok; ++t) {
-                    load(&map_k, kh, it.start + t * kAttTile);
-                    load(&map_v, kh, it.start + t * kAttTile);
+                for (uint32_t t = 0; t <= it.tile; ++t) {
+                    if (!(ok = mbar_wait(bar(kKEmpty + ka.i), ka.phase ^ 1, p.wait_limit, gave_up))) break;
+                    mbar_expect_tx(bar(kKFull + ka.i), tile_bytes);
+                    load_rows(kt0 + ka.i * kTileBytes, &map_k, chunks, kh, it.start + t * kAttTile, bar(kKFull + ka.i));
+                    ka.next();
+                    ++k_issued;
+                    if (!(ok = mbar_wait(bar(kVEmpty + va.i), va.phase ^ 1, p.wait_limit, gave_up))) break;
+                    mbar_expect_tx(bar(kVFull + va.i), tile_bytes);
+                    load_rows(vt0 + va.i * kTileBytes, &map_v, chunks, kh, it.start + t * kAttTile, bar(kVFull + va.i));
+                    va.next();
+                    ++tiles;
                 }
             }
-            s_issued = issued;
-            s_q_issued = q_issued;
+            s_issued[0] = k_issued;
+            s_issued[1] = tiles;
+            s_issued[2] = q_issued;
         } else if (warp == 1) {
-            // ---- matrix products: the whole warp waits, one lane issues ----
+            // ---- products, S and dq: the whole warp waits, one lane issues.  An issue blocks until the tensor cores are nearly
+            // through with it, so dP has a warp of its own ----
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
-            uint32_t taken = 0, q_taken = 0, g = 0;
-            RingAt<kBwdRing> at;
+            uint32_t q_taken = 0, g = 0, made = 0;       // steps of dq and of S so far
+            RingAt<kRing3> sa, da;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            // the next tile of the ring: its address, and the barrier that lets it go
-            auto take = [&](uint32_t& tile, uint32_t& empty) {
-                if (!wait(kRingFull + at.i, at.phase)) return false;
-                tile = uniform(ring0 + at.i * kTileBytes);
-                empty = uniform(bar(kRingEmpty + at.i));
-                at.next();
-                ++taken;
-                return true;
-            };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 const uint32_t w = work_at(i);
                 if (w >= total) continue;
                 const uint32_t n = list[w / p.units].tile + 1;
                 if (!wait(kQFull, q_taken & 1)) break;
                 ++q_taken;
-                uint32_t k = 0, k_empty = 0, next = 0, next_empty = 0;
-                // S and dP of the h-th tile of all so far, the t-th of this work
-                auto scores = [&](uint32_t t, uint32_t h) {
-                    if (!take(next, next_empty)) return;
+                auto scores = [&](uint32_t t) {
+                    if (!wait(kKFull + sa.i, sa.phase)) return;
+                    const uint32_t k = uniform(kt0 + sa.i * kTileBytes), to = uniform(made & 1);
                     if (elect_lane()) {
-                        mma_rows(tmem + (h & 1) * 128, q0, next, steps, desc_s);
-                        mma_commit<1>(bar(kSFull + (h & 1)));
-                    }
-                    uint32_t v, v_empty;
-                    if ((h && !wait(kDpRead, (h - 1) & 1)) || !take(v, v_empty)) return;
-                    if (elect_lane()) {
-                        mma_rows(tmem + 256, do0, v, steps, desc_s);
-                        mma_commit<1>(bar(kDpFull));
-                        mma_commit<1>(v_empty);
+                        mma_rows(tmem + to * 128, q0, k, steps, desc_s);
+                        mma_commit<1>(bar(kSFull + to));
                         if (t + 1 == n) mma_commit<1>(bar(kQEmpty));
                     }
+                    sa.next();
+                    ++made;
                 };
-                scores(0, g);
+                scores(0);
+                if (n > 1) scores(1);
                 for (uint32_t t = 0; t < n && ok; ++t, ++g) {
-                    k = next;
-                    k_empty = next_empty;
-                    if (t + 1 < n) scores(t + 1, g + 1);
+                    const uint32_t k = uniform(kt0 + da.i * kTileBytes), release = uniform(bar(kKEmpty + da.i)), from = uniform(tmem + (g & 1) * 128);
                     if (!wait(kDsFull + (g & 1), g >> 1 & 1)) break;
                     if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 384, tmem + (g & 1) * 128, k, desc_d, t != 0);
-                        mma_commit<1>(k_empty);
+                        mma_tile<kHalf>(tmem + 384, from, k, desc_d, t != 0);
+                        mma_commit<1>(release);
                         if (t + 1 == n) mma_commit<1>(bar(kDqFull));
                     }
+                    da.next();
+                    if (t + 2 < n) scores(t + 2);
                 }
             }
             if (lane == 0) {
-                s_taken = taken;
-                s_q_taken = q_taken;
+                s_taken[0] = made;
+                s_taken[2] = q_taken;
             }
+        } else if (warp == 2) {
+            // ---- products, dP ----
+            const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
+            uint32_t q_taken = 0, g = 0;
+            RingAt<kRing2> va;
+            bool ok = true;
+            auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
+            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
+                const uint32_t w = work_at(i);
+                if (w >= total) continue;
+                const uint32_t n = list[w / p.units].tile + 1;
+                if (!wait(kQFull, q_taken++ & 1)) break;
+                for (uint32_t t = 0; t < n && ok; ++t) {
+                    if (!wait(kVFull + va.i, va.phase)) break;
+                    const uint32_t v = uniform(vt0 + va.i * kTileBytes), release = uniform(bar(kVEmpty + va.i));
+                    va.next();
+                    ++g;
+                    if (g > 1 && !wait(kDpRead, g & 1)) break;
+                    if (elect_lane()) {
+                        mma_rows(tmem + 256, do0, v, steps, desc_s);
+                        mma_commit<1>(bar(kDpFull));
+                        mma_commit<1>(release);
+                        if (t + 1 == n) mma_commit<1>(bar(kQEmpty));
+                    }
+                }
+            }
+            if (lane == 0) s_taken[1] = g;
         }
     } else {
         regs_up<kManyRegs>();
@@ -261,8 +279,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 #pragma unroll
                     for (int j = 0; j < (int)kHalf; ++j) z[j] = half * kHalf + j > r || row == 0 ? 0.f : z[j];
                 }
-                if ((t + 1) * kAttTile > it.len)              // keys past the sequence; each step has two loads
-                    clear_rows(smem + (2 + 2 * g % kBwdRing) * kTileBytes, chunks, it.len - t * kAttTile, threadIdx.x - 128, 256);
+                if ((t + 1) * kAttTile > it.len)              // keys past the sequence
+                    clear_rows(smem + (2 + g % kRing3) * kTileBytes, chunks, it.len - t * kAttTile, threadIdx.x - 128, 256);
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
             }
@@ -280,14 +298,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     __syncthreads();
     const bool failed = *gave_up;
     if (failed) {      // as in the forward kernel
-        if (warp == 1 && elect_lane()) {      // the lane that issued them
+        if ((warp == 1 || warp == 2) && elect_lane()) {      // the lanes that issued them
             mma_commit<1>(bar(kLast));
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
         }
         if (threadIdx.x == 0) {
             uint32_t left = kWaitTries;
-            drain_loads(bar(kRingFull), kBwdRing, s_taken, s_issued, left);
-            drain_loads(bar(kQFull), 1, s_q_taken, s_q_issued, left);
+            drain_loads(bar(kKFull), kRing3, s_taken[0], s_issued[0], left);
+            drain_loads(bar(kVFull), kRing2, s_taken[1], s_issued[1], left);
+            drain_loads(bar(kQFull), 1, s_taken[2], s_issued[2], left);
         }
         __syncthreads();
     }
@@ -321,12 +340,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     att_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
-    enum { kRingFull, kRingEmpty = kBwdRing, kKvFull = 2 * kBwdRing, kKvEmpty, kSFull, kPFull, kDpFull, kDsFull, kAccFull, kStatFull, kStatEmpty = kStatFull + 2,
-           kLast = kStatEmpty + 2, kBars };
+    enum { kQFull, kQEmpty = kRing3, kDoFull = 2 * kRing3, kDoEmpty = kDoFull + kRing2, kKvFull = kDoEmpty + kRing2, kKvEmpty, kSFull, kPFull, kDpFull, kDsFull,
+           kAccFull, kTurn, kStatFull = kTurn + 2, kStatEmpty = kStatFull + 2, kLast = kStatEmpty + 2, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
-    __shared__ uint32_t s_tmem, s_gave_up, s_issued, s_taken, s_kv_issued, s_kv_taken;
+    __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of Q, dout, and K with V
     __shared__ __align__(16) float s_stat[2][2][kAttTile];       // -lse log2(e) and -delta of a tile of queries
-    const uint32_t k0 = smem_addr(smem), v0 = k0 + kTileBytes, ring0 = k0 + 2 * kTileBytes;
+    const uint32_t k0 = smem_addr(smem), v0 = k0 + kTileBytes, qt0 = k0 + 2 * kTileBytes, dot0 = qt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -334,9 +353,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         tma_prefetch_map(&map_k);
         tma_prefetch_map(&map_v);
         tma_prefetch_map(&map_do);
-        for (uint32_t i = 0; i < kBars; ++i)
-            mbar_init(bar(i), i == kPFull || i == kDsFull || i == kStatEmpty || i == kStatEmpty + 1 ? kBwdWarps : i == kStatFull || i == kStatFull + 1 ? 2 : 1);
-        s_gave_up = s_issued = s_taken = s_kv_issued = s_kv_taken = 0;
+        for (uint32_t i = 0; i < kBars; ++i) {
+            const bool warps = i == kPFull || i == kDsFull || i == kStatEmpty || i == kStatEmpty + 1;
+            const bool both = (i >= kQEmpty && i < kDoFull) || (i >= kDoEmpty && i < kKvFull) || i == kKvEmpty || i == kAccFull || i == kLast;
+            mbar_init(bar(i), warps ? kBwdWarps : both ? 2 : 1);
+        }
+        s_gave_up = 0;
+        for (uint32_t i = 0; i < 3; ++i) s_issued[i] = s_taken[i] = 0;
+        mbar_arrive(bar(kTurn));               // the first turn is warp 1's
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -354,16 +378,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         regs_down<kFewRegs>();
         if (warp == 0 && lane == 0) {
             // ---- loads ----
-            uint32_t issued = 0, kv_issued = 0;
+            uint32_t q_issued = 0, do_issued = 0, kv_issued = 0;
+            RingAt<kRing3> qa;
+            RingAt<kRing2> da;
             bool ok = true;
-            RingAt<kBwdRing> at;
-            auto load = [&](const CUtensorMap* map, uint32_t head, uint32_t row) {
-                if (!(ok = ok && mbar_wait(bar(kRingEmpty + at.i), at.phase ^ 1, p.wait_limit, gave_up))) return;
-                mbar_expect_tx(bar(kRingFull + at.i), tile_bytes);
-                load_rows(ring0 + at.i * kTileBytes, map, chunks, head, row, bar(kRingFull + at.i));
-                at.next();
-                ++issued;
-            };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 if (work_at(i) >= total) continue;
                 const DkvWork f = dkv_work(p, list, work_at(i));
@@ -373,69 +391,80 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 load_rows(v0, &map_v, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
                 ++kv_issued;
                 for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
-                    for (uint32_t t = f.tile; t < f.tile + f.tiles && ok; ++t) {
-                        load(&map_q, h, f.start + t * kAttTile);
-                        load(&map_do, h, f.start + t * kAttTile);
+                    for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t) {
+                        if (!(ok = mbar_wait(bar(kQEmpty + qa.i), qa.phase ^ 1, p.wait_limit, gave_up))) break;
+                        mbar_expect_tx(bar(kQFull + qa.i), tile_bytes);
+                        load_rows(qt0 + qa.i * kTileBytes, &map_q, chunks, h, f.start + t * kAttTile, bar(kQFull + qa.i));
+                        qa.next();
+                        ++q_issued;
+                        if (!(ok = mbar_wait(bar(kDoEmpty + da.i), da.phase ^ 1, p.wait_limit, gave_up))) break;
+                        mbar_expect_tx(bar(kDoFull + da.i), tile_bytes);
+                        load_rows(dot0 + da.i * kTileBytes, &map_do, chunks, h, f.start + t * kAttTile, bar(kDoFull + da.i));
+                        da.next();
+                        ++do_issued;
                     }
             }
-            s_issued = issued;
-            s_kv_issued = kv_issued;
-        } else if (warp == 1) {
-            // ---- matrix products: the whole warp waits, one lane issues ----
+            s_issued[0] = q_issued;
+            s_issued[1] = do_issued;
+            s_issued[2] = kv_issued;
+        } else if (warp == 1 || warp == 2) {
+            // ---- products: the whole warp waits, one lane issues.  Warp 1 has what reads and writes S and p (S of the next step behind dv
+            // of this one), warp 2 what reads and writes dP and dz (dk, the next dP).  An issue blocks until the tensor cores are
+            // nearly through with it: one waits for barriers while the other one issues, and they take turns ----
+            const bool first = warp == 1;
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
-            uint32_t taken = 0, kv_taken = 0, g = 0;
-            RingAt<kBwdRing> at;
+            const uint32_t scores_at = first ? tmem : tmem + 128, sums_at = first ? tmem + 256 : tmem + 384, own = first ? k0 : v0;
+            const uint32_t made_bar = first ? kSFull : kDpFull, ready_bar = first ? kPFull : kDsFull;
+            uint32_t kv_taken = 0, g = 0, turns = 0, taken = 0;
+            RingAt<kRing3> qa;                  // warp 1: the next tile for S; warp 2: the tile for dk
+            RingAt<kRing2> da;                  // warp 1: the tile for dv; warp 2: the next tile for dP
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
                 if (work_at(i) >= total) continue;
-                const uint32_t n = dkv_work(p, list, work_at(i)).n;
+                const int n = (int)dkv_work(p, list, work_at(i)).n;
                 if (!wait(kKvFull, kv_taken & 1)) break;
                 ++kv_taken;
-                uint32_t q = 0, q_empty = 0, d_o = 0, do_empty = 0, next, next_empty;
-                // scores d = a (the next tile of the ring)^T; tile and empty: where it lies, and the barrier that lets it go
-                auto scores = [&](uint32_t d, uint32_t a, uint32_t full, bool last, uint32_t& tile, uint32_t& empty) {
-                    if (!wait(kRingFull + at.i, at.phase)) return;
-                    tile = uniform(ring0 + at.i * kTileBytes);
-                    empty = uniform(bar(kRingEmpty + at.i));
-                    at.next();
-                    ++taken;
-                    if (elect_lane()) {
-                        mma_rows(d, a, tile, steps, desc_s);
-                        mma_commit<1>(bar(full));
-                        if (last) mma_commit<1>(bar(kKvEmpty));
-                    }
-                };
-                scores(tmem, k0, kSFull, false, q, q_empty);
-                scores(tmem + 128, v0, kDpFull, n == 1, d_o, do_empty);
-                for (uint32_t j = 0; j < n && ok; ++j, ++g) {
+                // step -1 makes the first scores; step j adds step j's product up and makes the scores of the next one
+                for (int j = -1; j < n && ok; ++j) {
                     const bool more = j + 1 < n;
-                    if (!wait(kPFull, g & 1)) break;
-                    if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 256, tmem, d_o, desc_d, j != 0);
-                        mma_commit<1>(do_empty);
+                    // made from, and added up with: a tile of q and one of dout, or the other way round
+                    uint32_t from = 0, from_release = 0, with = 0, with_release = 0;
+                    if (more) {
+                        if (!(first ? wait(kQFull + qa.i, qa.phase) : wait(kDoFull + da.i, da.phase))) break;
+                        from = uniform(first ? qt0 + qa.i * kTileBytes : dot0 + da.i * kTileBytes);
+                        from_release = uniform(first ? bar(kQEmpty + qa.i) : bar(kDoEmpty + da.i));
+                        if (first) qa.next(); else da.next();
+                        ++taken;
                     }
-                    if (more) scores(tmem, k0, kSFull, false, next, next_empty);
-                    if (!wait(kDsFull, g & 1)) break;
+                    if (j >= 0) {
+                        with = uniform(first ? dot0 + da.i * kTileBytes : qt0 + qa.i * kTileBytes);
+                        with_release = uniform(first ? bar(kDoEmpty + da.i) : bar(kQEmpty + qa.i));
+                        if (first) da.next(); else qa.next();
+                    }
+                    if (!wait(first ? kTurn : kTurn + 1, turns++ & 1)) break;
+                    if (j >= 0 && !wait(ready_bar, g++ & 1)) break;       // last: what is behind it is the tensor cores' time
                     if (elect_lane()) {
-                        mma_tile<kHalf>(tmem + 384, tmem + 128, q, desc_d, j != 0);
-                        mma_commit<1>(q_empty);
+                        if (j >= 0) mma_tile<kHalf>(sums_at, scores_at, with, desc_d, j != 0);
+                        if (more) {
+                            mma_rows(scores_at, own, from, steps, desc_s);
+                            mma_commit<1>(bar(made_bar));
+                        }
+                        mbar_arrive(bar(first ? kTurn + 1 : kTurn));
+                        if (j >= 0) mma_commit<1>(with_release);
+                        if (more) mma_commit<1>(from_release);
+                        if (j + 2 == n) mma_commit<1>(bar(kKvEmpty));
                         if (!more) mma_commit<1>(bar(kAccFull));
                     }
-                    q = next;
-                    q_empty = next_empty;
-                    if (more) scores(tmem + 128, v0, kDpFull, j + 2 == n, d_o, do_empty);
                 }
             }
             if (lane == 0) {
-                s_taken = taken;
-                s_kv_taken = kv_taken;
+                s_taken[first ? 0 : 1] = taken;
+                if (first) s_taken[2] = kv_taken;
             }
-        } else if (warp >= 2) {
-            // ---- lse (warp 2) and delta (warp 3) of the tiles of queries ----
-            const float* from = warp == 2 ? p.lse_in : p.delta;
-            const float by = warp == 2 ? -(float)kLog2eD : -1.f;
+        } else if (warp == 3) {
+            // ---- lse and delta of the tiles of queries ----
             uint32_t g = 0;
             bool ok = true;
             for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
@@ -443,17 +472,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 const DkvWork f = dkv_work(p, list, work_at(i));
                 for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
                     for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
-                        ok = mbar_wait(bar(kStatEmpty + (g & 1)), (g >> 1 & 1) ^ 1, p.wait_limit, gave_up);
-                        ok = !__any_sync(0xFFFFFFFFu, !ok);
-                        if (!ok) break;
                         const uint32_t row = t * kAttTile + lane * 4;
-                        const float* x = from + h * p.tokens + f.start + row;
-                        float4 v;
-                        v.x = row < f.len ? x[0] * by : 0.f;
-                        v.y = row + 1 < f.len ? x[1] * by : 0.f;
-                        v.z = row + 2 < f.len ? x[2] * by : 0.f;
-                        v.w = row + 3 < f.len ? x[3] * by : 0.f;
-                        *reinterpret_cast<float4*>(&s_stat[g & 1][warp - 2][lane * 4]) = v;
+                        const uint64_t at = h * p.tokens + f.start + row;
+                        float l[4], d[4];
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j) {
+                            l[j] = row + j < f.len ? p.lse_in[at + j] * -(float)kLog2eD : 0.f;
+                            d[j] = row + j < f.len ? -p.delta[at + j] : 0.f;
+                        }
+                        if (!(ok = warp_wait(bar(kStatEmpty + (g & 1)), (g >> 1 & 1) ^ 1, p.wait_limit, gave_up))) break;
+                        *reinterpret_cast<float4*>(&s_stat[g & 1][0][lane * 4]) = make_float4(l[0], l[1], l[2], l[3]);
+                        *reinterpret_cast<float4*>(&s_stat[g & 1][1][lane * 4]) = make_float4(d[0], d[1], d[2], d[3]);
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(kStatFull + (g & 1)));
                     }
@@ -493,10 +522,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len ? 0.f : z[c];
                 }
                 if ((t + 1) * kAttTile > f.len) {             // rows past the sequence, of q and of dout
-                    const uint32_t q = 2 * g % kBwdRing, d_o = (2 * g + 1) % kBwdRing;
-                    if (!wait(kRingFull + d_o, (2 * g + 1) / kBwdRing & 1)) break;
-                    clear_rows(smem + (2 + q) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
-                    clear_rows(smem + (2 + d_o) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
+                    if (!wait(kDoFull + g % kRing2, g / kRing2 & 1)) break;
+                    clear_rows(smem + (2 + g % kRing3) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
+                    clear_rows(smem + (2 + kRing3 + g % kRing2) * kTileBytes, chunks, f.len - t * kAttTile, threadIdx.x - 128, 256);
                 }
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kPFull));
@@ -538,14 +566,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     __syncthreads();
     const bool failed = *gave_up;
     if (failed) {      // as in the forward kernel
-        if (warp == 1 && elect_lane()) {      // the lane that issued them
+        if ((warp == 1 || warp == 2) && elect_lane()) {      // the lanes that issued them
             mma_commit<1>(bar(kLast));
             for (uint32_t i = 0; i < kWaitTries && !mbar_try_wait(bar(kLast), 0); ++i) {}
         }
         if (threadIdx.x == 0) {
             uint32_t left = kWaitTries;
-            drain_loads(bar(kRingFull), kBwdRing, s_taken, s_issued, left);
-            drain_loads(bar(kKvFull), 1, s_kv_taken, s_kv_issued, left);
+            drain_loads(bar(kQFull), kRing3, s_taken[0], s_issued[0], left);
+            drain_loads(bar(kDoFull), kRing2, s_taken[1], s_issued[1], left);
+            drain_loads(bar(kKvFull), 1, s_taken[2], s_issued[2], left);
         }
         __syncthreads();
     }
