@@ -376,22 +376,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             if (valid && p.lse) p.lse[head_at * p.tokens + at] = fmaf(top, p.scale, logf(sum));
             const float by = 1.f / sum;
             __nv_bfloat16* out = p.out + at * p.out_ld + head_at * p.head_dim;
-            for (uint32_t c = 0; c < p.head_dim; c += 32) {
-                uint32_t v[32];
-                tmem_load32(o_at + c, v);
-                tmem_load_wait(v);
-                if (!valid) continue;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c + 8 * j >= p.head_dim) break;
-                    float o[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(v[8 * j + i]) * by;
-                    Raw8<__nv_bfloat16> x;
-                    x.set(o);
-                    x.store(out + c + 8 * j);
-                }
-            }
+            for (uint32_t c = 0; c < p.head_dim; c += 32) store_columns(out, o_at, c, p.head_dim, by, valid, p.sectors);
             tc_fence_before();
         }
     }
@@ -543,6 +528,7 @@ extern "C" dte_status dte_attention_forward(const dte_matrix* q, const dte_matri
     p.out = static_cast<__nv_bfloat16*>(out->data);
     p.out_ld = out->ld;
     p.lse = lse;
+    p.sectors = !(((uintptr_t)out->data | out->ld * 2 | head_dim * 2u) & 31u);
     p.pair_heads = p.group % 2 == 0;
     p.units = (uint32_t)(q->cols / head_dim / (p.pair_heads ? 2 : 1));
     CUtensorMap mq, mk, mv;

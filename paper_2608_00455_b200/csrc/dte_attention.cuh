@@ -46,6 +46,7 @@ struct AttParams {
     float *lse, *delta;
     const float* lse_in;
     uint64_t* flags;
+    bool sectors;              // every 16 columns of the outputs are a whole sector of 32 bytes
 };
 
 // The two passes over the scores of the backward pass.
@@ -123,6 +124,29 @@ __device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uin
     const uint64_t db = operand_desc(b, kChunkBytes);
 #pragma unroll
     for (uint32_t i = FROM; i < TO; ++i) mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, db + (i * 2048 >> 4), desc, add || i != 0);
+}
+
+// Columns c .. c + 31 of this thread's row in tensor memory, times by, as bf16.  Every lane writes to another row: whole sectors where
+// the rows allow it.
+__device__ __forceinline__ void store_columns(__nv_bfloat16* out, uint32_t tmem, uint32_t c, uint32_t head_dim, float by, bool valid, bool sectors) {
+    uint32_t v[32];
+    tmem_load32(tmem + c, v);
+    tmem_load_wait(v);
+    if (!valid) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16(__uint_as_float(v[16 * j + 2 * i]) * by, __uint_as_float(v[16 * j + 2 * i + 1]) * by);
+        const uint32_t at = c + 16 * j;
+        if (sectors && at < head_dim) {
+            store32(out + at, w);
+        } else {
+            uint4* to = reinterpret_cast<uint4*>(out + at);
+            if (at < head_dim) to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (at + 8 < head_dim) to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
 }
 
 // Which piece of work this CTA takes in round i of its loop: the list is in falling order of work, and every other

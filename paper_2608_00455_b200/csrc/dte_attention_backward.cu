@@ -23,24 +23,6 @@ constexpr uint32_t kHalf = kAttTile / 2;          // columns of a tile that a th
 // In tensor memory a tile of scores takes 128 columns.  The bf16 operand made of it lies over it, each half over the
 // columns that the same threads have read.
 
-// Columns c .. c + 31 of this thread's row, times by, as bf16.
-__device__ __forceinline__ void store_columns(__nv_bfloat16* out, uint32_t tmem, uint32_t c, uint32_t head_dim, float by, bool valid) {
-    uint32_t v[32];
-    tmem_load32(tmem + c, v);
-    tmem_load_wait(v);
-    if (!valid) return;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (c + 8 * j >= head_dim) break;
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __uint_as_float(v[8 * j + i]) * by;
-        Raw8<__nv_bfloat16> x;
-        x.set(o);
-        x.store(out + c + 8 * j);
-    }
-}
-
 __device__ __forceinline__ void load_half(uint32_t tmem, float (&z)[kHalf]) {
     uint32_t a[32], b[32];
     tmem_load32(tmem, a);
@@ -73,7 +55,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     enum { kKFull, kKEmpty = kRing3, kVFull = 2 * kRing3, kVEmpty = kVFull + kRing2, kQFull = kVEmpty + kRing2, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull, kDelta, kLast, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of K, V, and Q with dout
-    __shared__ float s_delta[2][2][kAttTile];
+    __shared__ float s_delta[2][kAttTile];
     const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, kt0 = q0 + 2 * kTileBytes, vt0 = kt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -213,28 +195,29 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         uint32_t g = 0, done = 0;
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-        // What delta needs of a row, asked for before the work in front is finished: each of the row's two threads takes every other group
-        // of eight columns of out and dout.
-        Raw8<__nv_bfloat16> o8[kMaxAttDim / 16], d8[kMaxAttDim / 16];
+        // What delta needs, asked for before the work in front is finished: a warp takes 16 rows, two at a time, 16 lanes a row, so that
+        // accesses are whole lines.  (Each thread its own row: 9 us per tile for 64 KB.)
+        constexpr uint32_t kPairs = kAttTile / kBwdWarps / 2;
+        const uint32_t delta_row = (warp - 4) * 2 * kPairs + lane / 16, delta_col = lane % 16 * 8;
+        Raw8<__nv_bfloat16> o8[kPairs], d8[kPairs];
         float lse_ahead = 0.f;
         auto fetch = [&](uint32_t i) {
             if (i * gridDim.x >= total || work_at(i) >= total) return;
             const PlanItem it = list[work_at(i) / p.units];
-            const uint32_t h = work_at(i) % p.units, row = it.tile * kAttTile + r;
-            const uint64_t at = (uint64_t)it.start + row;
-            const __nv_bfloat16 *o = p.o + at * p.o_ld + h * p.head_dim, *d = p.d_o + at * p.do_ld + h * p.head_dim;
+            const uint32_t h = work_at(i) % p.units, tile = it.tile * kAttTile;
 #pragma unroll
-            for (uint32_t j = 0; j < kMaxAttDim / 16; ++j) {
-                const uint32_t c = half * 8 + j * 16;
-                if (row < it.len && c < p.head_dim) {
-                    o8[j].load(o + c);
-                    d8[j].load(d + c);
+            for (uint32_t j = 0; j < kPairs; ++j) {
+                const uint32_t row = tile + delta_row + 2 * j;
+                const uint64_t at = (uint64_t)it.start + row;
+                if (row < it.len && delta_col < p.head_dim) {
+                    o8[j].load(p.o + at * p.o_ld + h * p.head_dim + delta_col);
+                    d8[j].load(p.d_o + at * p.do_ld + h * p.head_dim + delta_col);
                 } else {
                     o8[j].zero();
                     d8[j].zero();
                 }
             }
-            lse_ahead = row < it.len ? p.lse_in[h * p.tokens + at] : 0.f;
+            lse_ahead = tile + r < it.len ? p.lse_in[h * p.tokens + it.start + tile + r] : 0.f;
         };
         fetch(0);
         for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
@@ -244,21 +227,22 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t h = w % p.units, n = it.tile + 1, row = it.tile * kAttTile + r;
             const bool valid = row < it.len;
             const uint64_t at = (uint64_t)it.start + row;
-            float part = 0.f;
 #pragma unroll
-            for (uint32_t j = 0; j < kMaxAttDim / 16; ++j) {
-                float a[8], b[8];
+            for (uint32_t j = 0; j < kPairs; ++j) {
+                float a[8], b[8], part = 0.f;
                 o8[j].get(a);
                 d8[j].get(b);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) part = fmaf(a[c], b[c], part);
+#pragma unroll
+                for (int c = 8; c; c >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, c);
+                if (lane % 16 == 0) s_delta[done & 1][delta_row + 2 * j] = part;
             }
             const float lse2 = lse_ahead * -(float)kLog2eD;
-            s_delta[done & 1][half][r] = part;
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kDelta));
             if (!wait(kDelta, done & 1)) break;
-            const float delta = s_delta[done & 1][0][r] + s_delta[done & 1][1][r];
+            const float delta = s_delta[done & 1][r];
             if (valid && half == 0) p.delta[h * p.tokens + at] = delta;
             for (uint32_t t = 0; t < n; ++t, ++g) {
                 const uint32_t s_at = mine + (g & 1) * 128 + half * kHalf;
@@ -289,7 +273,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             if (!wait(kDqFull, done & 1)) break;
             ++done;
             __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
-            for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid);
+            for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid, p.sectors);
             tc_fence_before();
         }
     }
@@ -555,8 +539,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t row = f.tile * kAttTile + r;
             const uint64_t at = (uint64_t)f.start + row;
             for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
-                store_columns(p.dv + at * p.dv_ld + f.kv_head * p.head_dim, mine + 256, c, p.head_dim, 1.f, row < f.len);
-                store_columns(p.dk + at * p.dk_ld + f.kv_head * p.head_dim, mine + 384, c, p.head_dim, p.scale, row < f.len);
+                store_columns(p.dv + at * p.dv_ld + f.kv_head * p.head_dim, mine + 256, c, p.head_dim, 1.f, row < f.len, p.sectors);
+                store_columns(p.dk + at * p.dk_ld + f.kv_head * p.head_dim, mine + 384, c, p.head_dim, p.scale, row < f.len, p.sectors);
             }
             tc_fence_before();
         }
@@ -595,6 +579,8 @@ dte_status launch_attention_backward(const AttParams& params, const dte_matrix* 
     if ((s = allow_smem(att_dq_kernel, kBwdSmem, device, ready_dq)) != DTE_OK) return s;
     if ((s = allow_smem(att_dkv_kernel, kBwdSmem, device, ready_dkv)) != DTE_OK) return s;
     AttParams p = params;
+    auto sectors = [&](const __nv_bfloat16* x, uint64_t ld) { return !(((uintptr_t)x | ld * 2 | p.head_dim * 2u) & 31u); };
+    p.sectors = sectors(p.dq, p.dq_ld) && sectors(p.dk, p.dk_ld) && sectors(p.dv, p.dv_ld);
     auto grid = [&] { return (unsigned)(tiles * p.units < (uint64_t)sms ? tiles * p.units : sms); };
     p.units = (uint32_t)(q->cols / p.head_dim);
     att_dq_kernel<<<grid(), kBwdThreads, kBwdSmem, st>>>(mq, mk, mv, md, p);
