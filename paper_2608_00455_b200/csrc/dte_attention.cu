@@ -116,9 +116,10 @@ struct FwdWork {
     uint32_t kv_head, n_max;
 };
 
-__device__ __forceinline__ FwdWork fwd_work(const AttParams& p, const PlanItem* list, uint32_t w) {
-    const uint32_t rank = w / p.units, unit = w - rank * p.units;
-    const PlanItem it = list[rank];
+__device__ __forceinline__ FwdWork fwd_work(const AttParams& p, Turns& turns) {
+    PlanItem it;
+    uint32_t unit;
+    turns.take(it, unit);
     FwdWork f;
     f.start = it.start;
     f.len = it.len;
@@ -241,9 +242,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                 at.next();
                 ++issued;
             };
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                if (work_at(i) >= total) continue;
-                const FwdWork f = fwd_work(p, list, work_at(i));
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                const FwdWork f = fwd_work(p, work);
 #pragma unroll
                 for (uint32_t s = 0; s < 2; ++s) {
                     if (!f.n[s] || !ok) continue;
@@ -281,9 +281,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
                 at.next();
                 ++taken;
             };
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                if (work_at(i) >= total) continue;
-                const FwdWork f = fwd_work(p, list, work_at(i));
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                const FwdWork f = fwd_work(p, work);
                 const uint32_t n = s ? f.n[1] : f.n[0];
                 uint32_t k = 0, k_release = 0, v = 0, v_release = 0;
                 // step -1 makes the first scores; step t adds up the values of tile t and makes the scores of the next one.  A slot
@@ -323,9 +322,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         uint32_t tiles = 0, items_done = 0, loads = 0;      // loads: tiles of keys and values of the work so far
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(b, parity, p.wait_limit, gave_up); };
-        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-            if (work_at(i) >= total) continue;
-            const FwdWork f = fwd_work(p, list, work_at(i));
+        for (Turns work(list, total, p.units); work.more() && ok;) {
+            const FwdWork f = fwd_work(p, work);
             const uint32_t first_load = loads;
             loads += 2 * f.n_max;
             const uint32_t n = s ? f.n[1] : f.n[0], head_at = s ? f.head[1] : f.head[0];

@@ -71,11 +71,9 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
 // Rows from `from` on of a tile in shared memory become zeros: rows of another sequence, or of none, would otherwise meet zeros of
 // the other operand, and 0 * NaN is NaN.  By the `threads` threads that write that operand, before they say that it is there.
 __device__ __forceinline__ void clear_rows(uint8_t* tile, uint32_t chunks, uint32_t from, uint32_t thread, uint32_t threads) {
-    const uint32_t per = (kAttTile - from) * 8;
-    for (uint32_t i = thread; i < per * chunks; i += threads) {
-        const uint32_t c = i / per, r = i - c * per;
-        *reinterpret_cast<uint4*>(tile + c * kChunkBytes + from * 128 + r * 16) = make_uint4(0, 0, 0, 0);
-    }
+    for (uint32_t c = 0; c < chunks; ++c)
+        for (uint32_t i = from * 8 + thread; i < kAttTile * 8; i += threads)
+            *reinterpret_cast<uint4*>(tile + c * kChunkBytes + i * 16) = make_uint4(0, 0, 0, 0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
@@ -149,9 +147,27 @@ __device__ __forceinline__ void store_columns(__nv_bfloat16* out, uint32_t tmem,
     }
 }
 
-// Which piece of work this CTA takes in round i of its loop: the list is in falling order of work, and every other
-// round runs backwards, so that the shares come out even.
-__device__ __forceinline__ uint32_t work_at(uint32_t i) { return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+// The pieces of work of this CTA: item w / units of the list and unit w % units of it, for the w of each of its rounds.  The list is in
+// falling order of work, and every other round runs backwards, so that the shares come out even.  The next item is read while the
+// one in front is worked on.
+struct Turns {
+    const PlanItem* list;
+    uint32_t total, units, round, w;
+    PlanItem ahead;            // item of w, if w < total
+    __device__ __forceinline__ Turns(const PlanItem* list_, uint32_t total_, uint32_t units_) : list(list_), total(total_), units(units_), round(0) { look(); }
+    __device__ __forceinline__ void look() {
+        w = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        if (w < total) ahead = list[w / units];
+    }
+    __device__ __forceinline__ bool more() const { return w < total; }      // past the end, no later round has work either
+    __device__ __forceinline__ uint32_t unit() const { return w % units; }
+    __device__ __forceinline__ void take(PlanItem& it, uint32_t& unit_) {
+        it = ahead;
+        unit_ = unit();
+        ++round;
+        look();
+    }
+};
 
 // Waits for the loads that no product has waited for, after a wait that ran out: load i signals the barrier at
 // bars + 8 * (i % n) for the (i / n)-th time.

@@ -89,11 +89,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing3> ka;
             RingAt<kRing2> va;
             bool ok = true;
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                const uint32_t w = work_at(i);
-                if (w >= total) continue;
-                const PlanItem it = list[w / p.units];
-                const uint32_t h = w % p.units, kh = h / p.group, row = it.start + it.tile * kAttTile;
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                PlanItem it;
+                uint32_t h;
+                work.take(it, h);
+                const uint32_t kh = h / p.group, row = it.start + it.tile * kAttTile;
                 if (!(ok = mbar_wait(bar(kQEmpty), (q_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
                 mbar_expect_tx(bar(kQFull), 2 * tile_bytes);
                 load_rows(q0, &map_q, chunks, h, row, bar(kQFull));
@@ -124,10 +124,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing3> sa, da;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                const uint32_t w = work_at(i);
-                if (w >= total) continue;
-                const uint32_t n = list[w / p.units].tile + 1;
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                PlanItem it;
+                uint32_t h;
+                work.take(it, h);
+                const uint32_t n = it.tile + 1;
                 if (!wait(kQFull, q_taken & 1)) break;
                 ++q_taken;
                 auto scores = [&](uint32_t t) {
@@ -166,10 +167,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing2> va;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                const uint32_t w = work_at(i);
-                if (w >= total) continue;
-                const uint32_t n = list[w / p.units].tile + 1;
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                PlanItem it;
+                uint32_t h;
+                work.take(it, h);
+                const uint32_t n = it.tile + 1;
                 if (!wait(kQFull, q_taken++ & 1)) break;
                 for (uint32_t t = 0; t < n && ok; ++t) {
                     if (!wait(kVFull + va.i, va.phase)) break;
@@ -201,30 +203,26 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         const uint32_t delta_row = (warp - 4) * 2 * kPairs + lane / 16, delta_col = lane % 16 * 8;
         Raw8<__nv_bfloat16> o8[kPairs], d8[kPairs];
         float lse_ahead = 0.f;
-        auto fetch = [&](uint32_t i) {
-            if (i * gridDim.x >= total || work_at(i) >= total) return;
-            const PlanItem it = list[work_at(i) / p.units];
-            const uint32_t h = work_at(i) % p.units, tile = it.tile * kAttTile;
+        Turns work(list, total, p.units);
+        // every load from an address inside, whatever the row and column: a branch around it would wait for it
+        auto fetch = [&]() {
+            if (!work.more()) return;
+            const PlanItem it = work.ahead;
+            const uint32_t h = work.unit(), tile = it.tile * kAttTile, col = delta_col < p.head_dim ? delta_col : 0;
 #pragma unroll
             for (uint32_t j = 0; j < kPairs; ++j) {
-                const uint32_t row = tile + delta_row + 2 * j;
-                const uint64_t at = (uint64_t)it.start + row;
-                if (row < it.len && delta_col < p.head_dim) {
-                    o8[j].load(p.o + at * p.o_ld + h * p.head_dim + delta_col);
-                    d8[j].load(p.d_o + at * p.do_ld + h * p.head_dim + delta_col);
-                } else {
-                    o8[j].zero();
-                    d8[j].zero();
-                }
+                const uint64_t at = (uint64_t)it.start + min(tile + delta_row + 2 * j, it.len - 1);
+                o8[j].load(p.o + at * p.o_ld + h * p.head_dim + col);
+                d8[j].load(p.d_o + at * p.do_ld + h * p.head_dim + col);
             }
-            lse_ahead = tile + r < it.len ? p.lse_in[h * p.tokens + it.start + tile + r] : 0.f;
+            lse_ahead = p.lse_in[h * p.tokens + it.start + min(tile + r, it.len - 1)];
         };
-        fetch(0);
-        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-            const uint32_t w = work_at(i);
-            if (w >= total) continue;
-            const PlanItem it = list[w / p.units];
-            const uint32_t h = w % p.units, n = it.tile + 1, row = it.tile * kAttTile + r;
+        fetch();
+        while (work.more() && ok) {
+            PlanItem it;
+            uint32_t h;
+            work.take(it, h);
+            const uint32_t n = it.tile + 1, row = it.tile * kAttTile + r;
             const bool valid = row < it.len;
             const uint64_t at = (uint64_t)it.start + row;
 #pragma unroll
@@ -234,6 +232,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 d8[j].get(b);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) part = fmaf(a[c], b[c], part);
+                part = delta_col < p.head_dim ? part : 0.f;
 #pragma unroll
                 for (int c = 8; c; c >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, c);
                 if (lane % 16 == 0) s_delta[done & 1][delta_row + 2 * j] = part;
@@ -269,7 +268,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
             }
             if (!ok) break;
-            fetch(i + 1);
+            fetch();
             if (!wait(kDqFull, done & 1)) break;
             ++done;
             __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
@@ -305,13 +304,13 @@ struct DkvWork {
     uint32_t start, len, kv_head, tile, tiles, n;     // tiles: of queries per head; n: in all
 };
 
-__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, const PlanItem* list, uint32_t w) {
+__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, Turns& turns) {
     // the list falls in the number of tiles in front: taken from the other end, in the number of tiles behind
-    const PlanItem it = list[w / p.units];
+    PlanItem it;
     DkvWork f;
+    turns.take(it, f.kv_head);
     f.start = it.start;
     f.len = it.len;
-    f.kv_head = w % p.units;
     f.tiles = it.tile + 1;
     f.tile = (it.len + kAttTile - 1) / kAttTile - f.tiles;
     f.n = f.tiles * p.group;
@@ -366,9 +365,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing3> qa;
             RingAt<kRing2> da;
             bool ok = true;
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                if (work_at(i) >= total) continue;
-                const DkvWork f = dkv_work(p, list, work_at(i));
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                const DkvWork f = dkv_work(p, work);
                 if (!(ok = mbar_wait(bar(kKvEmpty), (kv_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
                 mbar_expect_tx(bar(kKvFull), 2 * tile_bytes);
                 load_rows(k0, &map_k, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
@@ -405,9 +403,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing2> da;                  // warp 1: the tile for dv; warp 2: the next tile for dP
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                if (work_at(i) >= total) continue;
-                const int n = (int)dkv_work(p, list, work_at(i)).n;
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                const int n = (int)dkv_work(p, work).n;
                 if (!wait(kKvFull, kv_taken & 1)) break;
                 ++kv_taken;
                 // step -1 makes the first scores; step j adds step j's product up and makes the scores of the next one
@@ -451,9 +448,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             // ---- lse and delta of the tiles of queries ----
             uint32_t g = 0;
             bool ok = true;
-            for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-                if (work_at(i) >= total) continue;
-                const DkvWork f = dkv_work(p, list, work_at(i));
+            for (Turns work(list, total, p.units); work.more() && ok;) {
+                const DkvWork f = dkv_work(p, work);
                 for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
                     for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
                         const uint32_t row = t * kAttTile + lane * 4;
@@ -480,9 +476,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         uint32_t g = 0, done = 0;
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-        for (uint32_t i = 0; i * gridDim.x < total && ok; ++i) {
-            if (work_at(i) >= total) continue;
-            const DkvWork f = dkv_work(p, list, work_at(i));
+        for (Turns work(list, total, p.units); work.more() && ok;) {
+            const DkvWork f = dkv_work(p, work);
             uint32_t t = f.tile;
             for (uint32_t j = 0; j < f.n; ++j, ++g) {
                 const uint32_t first = t * kAttTile + half * kHalf;       // query of this thread's first column
