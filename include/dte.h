@@ -573,7 +573,7 @@ DTE_API dte_status dte_rope_frequencies(uint32_t rot, double base, uint32_t scal
  * overlaps no input.  A row with a negative position (padding) is copied.  frequencies: DEVICE, rot / 2 values in radians per
  * position.  Angles are 64-bit products, good to 2^-52 of the number of turns, and are reduced to an eighth of a
  * turn before they are rounded to fp32.  inverse != 0 turns backwards: the gradient.  head_dim <= 1024,
- * rot <= head_dim, at most 4095 heads. */
+ * rot <= head_dim, at most 4095 heads of q and k together. */
 DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t head_dim, const dte_ids* positions,
                             const double* frequencies, uint32_t rot, uint32_t layout, double amplitude, int inverse,
                             const dte_matrix* q_out, const dte_matrix* k_out, int device, void* cuda_stream);

@@ -6,19 +6,22 @@
 
 namespace dte {
 
-constexpr int kRopeThreads = 256;
+constexpr uint32_t kRopeThreads = 256;
 constexpr uint32_t kMaxHeadDim = 1024;
-constexpr uint32_t kMaxRopeHeads = 4095;     // times the square of a head's pieces (1024 at most): below 2^32, see RopeParams::magic
+constexpr uint32_t kMaxRopeHeads = 4095;     // of queries and keys together; see RopeParams::by_pieces
+// Tokens of a CTA: four, so that every thread has one angle and several vectors of a head of 128 (16384 tokens of 40 heads: 69 us
+// with one), where that leaves each multiprocessor some CTAs; one for few tokens.
+constexpr uint32_t kRopeTokens = 4;
 
 struct RopeSide {
     const void* x;
     void* y;
     uint64_t x_ld, y_ld;
-    uint32_t heads;
 };
 
 struct RopeParams {
-    RopeSide side[2];            // queries, keys (heads = 0: none)
+    RopeSide side[2];            // queries, keys
+    uint32_t q_heads, heads;     // heads: of both
     const void* positions;
     uint32_t positions_dtype;
     uint32_t tokens, head_dim, rot;
@@ -26,7 +29,8 @@ struct RopeParams {
     float amplitude;
     bool inverse;
     uint32_t pieces, turned;     // vectors of work per head, and how many of them are pairs
-    uint32_t magic;              // ceil(2^32 / pieces): the quotient by multiplication is exact below 2^32 / pieces
+    uint32_t per_cta;            // tokens
+    uint32_t by_pieces, by_heads;  // ceil(2^32 / n): the quotient by multiplication is exact below 2^32 / n
 };
 
 // cos and sin of position * frequency.  In turns, so that whole ones drop out exactly: what is left of the product after
@@ -48,81 +52,98 @@ __device__ __forceinline__ void rope_pair(float2 t, float a, float b, float& lo,
     hi = fmaf(b, t.x, a * t.y);
 }
 
-// One CTA per token.  A piece is V pairs (half layout: V columns of each half), V / 2 pairs (interleaved; V = 1: a pair)
-// or V columns that are copied.
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t by) { return d == 1 ? n : __umulhi(n, by); }
+
+// A piece is V pairs (half layout: V columns of each half), V / 2 pairs (interleaved; V = 1: a pair) or V columns that are
+// copied.  kAhead pieces of a thread are loaded before the first one is used.
 template <typename T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
-    __shared__ float2 s_turn[kMaxHeadDim / 2];
-    const uint32_t token = blockIdx.x;
-    const int64_t position = load_id(p.positions, p.positions_dtype, token);
-    const bool padding = position < 0;
-    const uint32_t half = p.rot / 2;
-    if (!padding) {
-        for (uint32_t i = threadIdx.x; i < half; i += kRopeThreads) {
-            const float2 t = rope_turn(position, p.frequencies[i], p.inverse);
-            s_turn[i] = make_float2(t.x * p.amplitude, t.y * p.amplitude);
+    extern __shared__ float2 s_turn[];               // per token: rot / 2 cosines and sines
+    __shared__ bool s_padding[kRopeTokens];
+    constexpr int kAhead = 2;
+    constexpr int W = INTERLEAVED && V == 1 ? 2 : V;     // columns of a piece of interleaved pairs
+    const uint32_t first = blockIdx.x * p.per_cta, tokens = min(p.per_cta, p.tokens - first), half = p.rot / 2;
+    const uint32_t work = tokens * p.heads * p.pieces;
+    struct Piece {
+        const T* x;
+        T* y;
+        uint32_t turn, kind;                         // turn: in s_turn, token in the upper 8 bits; kind 0: pairs, 1: copied, 2: nothing to do
+        Vec<T, V> a, b;
+    };
+    auto load = [&](uint32_t i, Piece& c) {
+        c.kind = 2;
+        if (i >= work) return;
+        const uint32_t row = quotient(i, p.pieces, p.by_pieces), piece = i - row * p.pieces;
+        const uint32_t token = quotient(row, p.heads, p.by_heads), head = row - token * p.heads;
+        const RopeSide& side = p.side[head >= p.q_heads];
+        const bool pairs = piece < p.turned;
+        const uint32_t col = (head - (head >= p.q_heads ? p.q_heads : 0)) * p.head_dim +
+                             (!pairs ? p.rot + (piece - p.turned) * V : INTERLEAVED ? piece * W : piece * V);
+        c.x = static_cast<const T*>(side.x) + (uint64_t)(first + token) * side.x_ld + col;
+        c.y = static_cast<T*>(side.y) + (uint64_t)(first + token) * side.y_ld + col;
+        c.turn = (token * half + (INTERLEAVED ? piece * W / 2 : piece * V)) | token << 24;
+        c.kind = pairs ? 0 : c.x == c.y ? 2 : 1;
+        if (c.kind == 2) return;
+        c.a.load(c.x);
+        if (pairs && !INTERLEAVED) c.b.load(c.x + half);
+        if (pairs && INTERLEAVED && V == 1) c.b.load(c.x + 1);
+    };
+    auto finish = [&](Piece& c) {
+        if (c.kind == 2) return;
+        if (c.kind == 1) {
+            c.a.store(c.y);
+            return;
         }
+        const bool padding = s_padding[c.turn >> 24];
+        const float2* turn = s_turn + (c.turn & 0xFFFFFFu);
+        float a[V], b[V];
+        c.a.get(a);
+        if (INTERLEAVED && V > 1) {
+            if (!padding) {
+#pragma unroll
+                for (int j = 0; j + 1 < V; j += 2) rope_pair(turn[j / 2], a[j], a[j + 1], a[j], a[j + 1]);
+            }
+            c.a.set(a);
+            c.a.store(c.y);
+        } else {
+            c.b.get(b);
+            if (!padding) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) rope_pair(turn[j], a[j], b[j], a[j], b[j]);
+            }
+            c.a.set(a);
+            c.b.set(b);
+            c.a.store(c.y);
+            c.b.store(c.y + (INTERLEAVED ? 1 : half));
+        }
+    };
+    Piece c[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load(threadIdx.x + u * kRopeThreads, c[u]);      // on the way while the angles are made
+    for (uint32_t i = threadIdx.x; i < tokens * half; i += kRopeThreads) {
+        const uint32_t token = i / half, pair = i - token * half;
+        const int64_t position = load_id(p.positions, p.positions_dtype, first + token);
+        if (pair == 0) s_padding[token] = position < 0;
+        const float2 t = rope_turn(position, p.frequencies[pair], p.inverse);
+        s_turn[i] = make_float2(t.x * p.amplitude, t.y * p.amplitude);
     }
     __syncthreads();
-    constexpr int W = INTERLEAVED && V == 1 ? 2 : V;     // columns of a piece of interleaved pairs
-    for (int which = 0; which < 2; ++which) {
-        const RopeSide& side = p.side[which];
-        const T* x = static_cast<const T*>(side.x) + (uint64_t)token * side.x_ld;
-        T* y = static_cast<T*>(side.y) + (uint64_t)token * side.y_ld;
-        const uint32_t work = side.heads * p.pieces;
-        for (uint32_t i = threadIdx.x; i < work; i += kRopeThreads) {
-            const uint32_t head = p.pieces == 1 ? i : __umulhi(i, p.magic), piece = i - head * p.pieces;
-            const uint32_t base = head * p.head_dim;
-            if (piece < p.turned && INTERLEAVED) {
-                const uint32_t c = base + piece * W;
-                if (V == 1) {
-                    const float a = to_f(x[c]), b = to_f(x[c + 1]);
-                    float lo = a, hi = b;
-                    if (!padding) rope_pair(s_turn[piece], a, b, lo, hi);
-                    y[c] = from_f<T>(lo);
-                    y[c + 1] = from_f<T>(hi);
-                } else {
-                    Vec<T, V> r;
-                    float f[V];
-                    r.load(x + c);
-                    r.get(f);
-                    if (!padding) {
+    for (uint32_t i = threadIdx.x; i < work; i += kAhead * kRopeThreads) {
+        if (i != threadIdx.x) {
 #pragma unroll
-                        for (int j = 0; j < V; j += 2) rope_pair(s_turn[(piece * V + j) / 2], f[j], f[j + (V > 1)], f[j], f[j + (V > 1)]);
-                    }
-                    r.set(f);
-                    r.store(y + c);
-                }
-            } else if (piece < p.turned) {
-                const uint32_t c = base + piece * V;
-                Vec<T, V> ra, rb;
-                float a[V], b[V];
-                ra.load(x + c);
-                rb.load(x + c + half);
-                ra.get(a);
-                rb.get(b);
-                if (!padding) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) rope_pair(s_turn[piece * V + j], a[j], b[j], a[j], b[j]);
-                }
-                ra.set(a);
-                rb.set(b);
-                ra.store(y + c);
-                rb.store(y + c + half);
-            } else if (x != y) {
-                const uint32_t c = base + p.rot + (piece - p.turned) * V;
-                Vec<T, V> r;
-                r.load(x + c);
-                r.store(y + c);
-            }
+            for (int u = 0; u < kAhead; ++u) load(i + u * kRopeThreads, c[u]);
         }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) finish(c[u]);
     }
 }
 
 template <typename T, int V>
 static void launch_rope(const RopeParams& p, bool interleaved, cudaStream_t st) {
-    if (interleaved) rope_kernel<T, V, true><<<p.tokens, kRopeThreads, 0, st>>>(p);
-    else rope_kernel<T, V, false><<<p.tokens, kRopeThreads, 0, st>>>(p);
+    const unsigned grid = (p.tokens + p.per_cta - 1) / p.per_cta;
+    const size_t smem = p.per_cta * (p.rot / 2) * sizeof(float2);        // 16 KB at most
+    if (interleaved) rope_kernel<T, V, true><<<grid, kRopeThreads, smem, st>>>(p);
+    else rope_kernel<T, V, false><<<grid, kRopeThreads, smem, st>>>(p);
 }
 
 template <typename T>
@@ -211,8 +232,10 @@ extern "C" dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_
         side.y = out[i]->data;
         side.x_ld = in[i]->ld;
         side.y_ld = out[i]->ld;
-        if (in[i]->cols / head_dim > kMaxRopeHeads) return op_fail(DTE_ERR_INVALID_ARG, "at most 4095 heads");
-        side.heads = (uint32_t)(in[i]->cols / head_dim);
+        const uint64_t heads = in[i]->cols / head_dim;
+        if (p.heads + heads > kMaxRopeHeads) return op_fail(DTE_ERR_INVALID_ARG, "at most 4095 heads");
+        if (i == 0) p.q_heads = (uint32_t)heads;
+        p.heads += (uint32_t)heads;
         const int v = rope_vec(in[i], out[i], head_dim, rot, interleaved);
         vec = v < vec ? v : vec;
     }
@@ -226,10 +249,14 @@ extern "C" dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_
     p.inverse = inverse != 0;
     p.turned = interleaved && vec > 1 ? rot / vec : rot / 2 / (interleaved ? 1 : vec);
     p.pieces = p.turned + (head_dim - rot) / vec;
-    p.magic = (uint32_t)(((1ull << 32) + p.pieces - 1) / p.pieces);
+    p.by_pieces = (uint32_t)(((1ull << 32) + p.pieces - 1) / p.pieces);
+    p.by_heads = (uint32_t)(((1ull << 32) + p.heads - 1) / p.heads);
     if (p.tokens == 0) return DTE_OK;
     OpDeviceGuard g;
-    if ((s = g.enter(device)) != DTE_OK) return s;
+    int sms = 0;
+    if ((s = g.enter(device, &sms)) != DTE_OK) return s;
+    const uint64_t reach = (uint64_t)kRopeTokens * p.heads * p.pieces * (p.pieces > p.heads ? p.pieces : p.heads);
+    p.per_cta = p.tokens >= (uint32_t)sms * 4 * kRopeTokens && reach < (1ull << 32) ? kRopeTokens : 1;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (q->dtype == DTE_BF16) launch_rope_vec<__nv_bfloat16>(p, vec, interleaved, st);
     else launch_rope_vec<float>(p, vec, interleaved, st);

@@ -13,6 +13,7 @@ rows a fixed stride apart.  Workspaces are uint8 tensors of at least the bytes t
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import struct
 from typing import Optional, Sequence, Tuple
@@ -31,11 +32,10 @@ _NUMBERS = {torch.float32: DTE_F32, torch.bfloat16: DTE_BF16}
 _IDS = {torch.int32: DTE_I32, torch.int64: DTE_I64}
 
 
-# dte_matrix, dte_ids and dte_tensor of the C ABI as packed bytes (natural alignment, no padding): cheaper to make per call than
+# dte_matrix and dte_ids of the C ABI as packed bytes (natural alignment, no padding): cheaper to make per call than
 # a ctypes structure
 _pack_matrix = struct.Struct("=QQQQII").pack
 _pack_ids = struct.Struct("=QQII").pack
-_pack_tensor = _pack_ids
 assert struct.calcsize("=QQQQII") == 40 and struct.calcsize("=QQII") == 24
 
 
@@ -393,7 +393,7 @@ def dte_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ou
 
 def _tensors(tensors: Sequence[torch.Tensor], name: str, device: int) -> bytes:
     """Packed dte_tensor array."""
-    out = []
+    flat = []
     for t in tensors:
         if not isinstance(t, torch.Tensor) or t.get_device() != device:
             _same_device(t, name, device)
@@ -402,8 +402,8 @@ def _tensors(tensors: Sequence[torch.Tensor], name: str, device: int) -> bytes:
             _refuse(f"{name} must be float32 or bfloat16")
         if not t.is_contiguous():
             _refuse(f"{name} must be contiguous")
-        out.append(_pack_tensor(t.data_ptr(), t.numel(), dtype, 0))
-    return b"".join(out)
+        flat += (t.data_ptr(), t.numel(), dtype)       # dtype and the reserved word as one number: both little-endian
+    return array.array("Q", flat).tobytes()
 
 
 def dte_grad_sum_squares_workspace_bytes(n_tensors: int) -> int:

@@ -21,7 +21,7 @@ def ids(count, dtype=ops.DTE_I64, data=8192):
 
 
 def tensor(numel, dtype=ops.DTE_F32, data=4096):
-    return ops._pack_tensor(data, numel, dtype, 0)
+    return ops._pack_ids(data, numel, dtype, 0)        # the same fields
 
 
 def refused(status, word):
