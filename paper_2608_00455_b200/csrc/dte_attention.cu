@@ -433,8 +433,8 @@ static dte_status check_attention(const dte_matrix* q, const dte_matrix* k, cons
     if (k->cols != v->cols || q->cols % k->cols) return op_fail(DTE_ERR_INVALID_ARG, "query heads must be a multiple of k's heads, v must have k's");
     if (q->rows > kMaxAttTokens) return op_fail(DTE_ERR_INVALID_ARG, "at most 2^24 tokens");
     if (q->cols / head_dim > 65535) return op_fail(DTE_ERR_INVALID_ARG, "at most 65535 heads");
-    if (tiles_most(plan_bytes, q->rows) * (q->cols / head_dim) >= (1ull << 31))
-        return op_fail(DTE_ERR_INVALID_ARG, "the plan's tiles x heads are too many for one call");
+    if (tiles_most(plan_bytes, q->rows) * (q->cols / head_dim) >= (1ull << 31) || (q->rows / kAttTile + 1) * (q->cols / head_dim) >= (1ull << 31))
+        return op_fail(DTE_ERR_INVALID_ARG, "tiles x heads are too many for one call");
     if (!(scale > 0) || !std::isfinite((float)(scale * kLog2eD)))
         return op_fail(DTE_ERR_INVALID_ARG, "scale must be > 0 and, times log2(e), finite in fp32");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
@@ -543,7 +543,7 @@ extern "C" dte_status dte_attention_forward(const dte_matrix* q, const dte_matri
 
 extern "C" uint64_t dte_attention_backward_workspace_bytes(uint64_t tokens, uint64_t heads) {
     if (tokens > kMaxAttTokens || heads > 65535) return UINT64_MAX;
-    return align_up(tokens * heads * sizeof(float), kWorkspaceAlign);
+    return align_up(tokens * heads * sizeof(float), kWorkspaceAlign) + kWorkspaceAlign;      // delta and the counter
 }
 
 extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
@@ -581,5 +581,6 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     p.dv_ld = dv->ld;
     p.lse_in = lse;
     p.delta = static_cast<float*>(workspace);
+    p.next = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + align_up(q->rows * heads * sizeof(float), kWorkspaceAlign));
     return launch_attention_backward(p, q, k, v, dout, tiles, device, sms, (cudaStream_t)cuda_stream);
 }

@@ -1,12 +1,14 @@
 // Gradient of causal attention over packed sequences, in two passes over the scores that share nothing but delta, so that
 // every sum has one owner and its order is fixed (one pass would have to add dq up across CTAs):
-//   att_dq_kernel   a tile of 128 queries of one head against its keys:  delta, dq
-//   att_dkv_kernel  a tile of 128 keys of one key head against the queries of its group that see them:  dk, dv
-// With p = exp(z - lse), dz = p (dout v^T - delta): dq = scale dz k, dk = scale dz^T q, dv = p^T dout.  The first pass has three
-// products per pair of tiles, the second four, where one pass would have five.
+//   att_delta_kernel  delta = sum over a head's columns of dout * out
+//   att_dkv_kernel    a tile of 128 keys of one key head against the queries of its group that see them:  dk, dv
+//   att_dq_kernel     a tile of 128 queries of one head against its keys:  dq
+// With p = exp(z - lse), dz = p (dout v^T - delta): dq = scale dz k, dk = scale dz^T q, dv = p^T dout.  The first pass has four products
+// per pair of tiles, the second three, where one pass would have five.  The second one starts on the SMs that the first one leaves
+// and draws its tiles from a counter: a batch with few, unequal key tiles leaves most SMs early.
 //
-// Both: one CTA per SM, a warp that loads, a warp that issues products, eight warps that turn scores into operands, each thread
-// half a row.  The second pass works on the transposed scores (rows are keys), so that p and dz are, as they come out of the
+// Both: one CTA per SM, a warp that loads, two that issue products, eight that turn scores into operands, each thread half a
+// row.  The first pass works on the transposed scores (rows are keys), so that p and dz are, as they come out of the
 // registers, the left operands of dv and dk in tensor memory.  p and dz are rounded to bf16, the operands' type; sums are fp32.
 #include <atomic>
 
@@ -46,16 +48,55 @@ __device__ __forceinline__ void store_half(uint32_t tmem, const float (&z)[kHalf
     __syncwarp();
 }
 
+// ---- delta ------------------------------------------------------------------------------------------------------
+constexpr uint32_t kDeltaThreads = 256;
+
+// A warp takes 32 tokens of a head, two at a time, 16 lanes a row.  Also sets the second pass's counter to zero.
+__global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttParams p, uint32_t heads) {
+    let_next_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.next = 0;
+    const uint64_t unit = (uint64_t)blockIdx.x * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * 32;
+    const uint32_t lane = threadIdx.x & 31, h = (uint32_t)(unit % heads), col = lane % 16 * 8;
+    if (first >= p.tokens) return;
+    const bool here = col < p.head_dim;
+    float mine = 0.f;
+#pragma unroll
+    for (uint32_t k = 0; k < 16; k += 8) {
+        Raw8<__nv_bfloat16> o[8], d[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            const uint64_t at = min(first + 2 * (k + j) + lane / 16, p.tokens - 1);
+            o[j].load(p.o + at * p.o_ld + h * p.head_dim + (here ? col : 0));
+            d[j].load(p.d_o + at * p.do_ld + h * p.head_dim + (here ? col : 0));
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            float a[8], b[8], sum = 0.f;
+            o[j].get(a);
+            d[j].get(b);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum = fmaf(a[c], b[c], sum);
+            sum = here ? sum : 0.f;
+#pragma unroll
+            for (int c = 8; c; c >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, c);
+            if (lane % 16 == k + j) mine = sum;
+        }
+    }
+    const uint64_t token = first + 2 * (lane % 16) + lane / 16;
+    if (token < p.tokens) p.delta[h * p.tokens + token] = mine;
+}
+
 // ---- dq -------------------------------------------------------------------------------------------------------
 // Tensor memory: S at columns 0 and 128 in turn (dz over it), dP at 256, dq at 384.
 __global__ void __launch_bounds__(kBwdThreads, 1)
     att_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
-    enum { kKFull, kKEmpty = kRing3, kVFull = 2 * kRing3, kVEmpty = kVFull + kRing2, kQFull = kVEmpty + kRing2, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull, kDelta, kLast, kBars };
+    enum { kKFull, kKEmpty = kRing3, kVFull = 2 * kRing3, kVEmpty = kVFull + kRing2, kQFull = kVEmpty + kRing2, kQEmpty, kSFull, kDsFull = kSFull + 2, kDpFull = kDsFull + 2, kDpRead, kDqFull,
+           kWorkFull, kWorkEmpty = kWorkFull + 2, kLast = kWorkEmpty + 2, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of K, V, and Q with dout
-    __shared__ float s_delta[2][kAttTile];
+    __shared__ uint4 s_work[2];            // start, length, tile and head of the next pieces of work; no tile: the end
     const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, kt0 = q0 + 2 * kTileBytes, vt0 = kt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
@@ -65,7 +106,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         tma_prefetch_map(&map_v);
         tma_prefetch_map(&map_do);
         for (uint32_t i = 0; i < kBars; ++i)
-            mbar_init(bar(i), i == kDsFull || i == kDsFull + 1 || i == kDpRead || i == kDelta ? kBwdWarps : i == kQEmpty || i == kLast ? 2 : 1);
+            mbar_init(bar(i), i == kDsFull || i == kDsFull + 1 || i == kDpRead ? kBwdWarps
+                              : i == kWorkEmpty || i == kWorkEmpty + 1         ? 3 + kBwdWarps
+                              : i == kQEmpty || i == kLast                     ? 2
+                                                                               : 1);
         s_gave_up = 0;
         for (uint32_t i = 0; i < 3; ++i) s_issued[i] = s_taken[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -80,54 +124,69 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
+    // The next piece of work, by a whole warp; false at the end, or where the wait runs out.
+    auto take_work = [&](uint32_t& n, PlanItem& it, uint32_t& h) {
+        if (!warp_wait(bar(kWorkFull + (n & 1)), n >> 1 & 1, p.wait_limit, gave_up)) return false;
+        const uint4 w = s_work[n & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kWorkEmpty + (n & 1)));
+        ++n;
+        it = PlanItem{w.x, w.y, w.z, 0};
+        h = w.w;
+        return w.z != kNone;
+    };
 
     if (warp < 4) {
         regs_down<kFewRegs>();
-        if (warp == 0 && lane == 0) {
-            // ---- loads ----
-            uint32_t tiles = 0, k_issued = 0, q_issued = 0;
+        if (warp == 0) {
+            // ---- loads: one lane ----
+            uint32_t tiles = 0, k_issued = 0, q_issued = 0, works = 0;
             RingAt<kRing3> ka;
             RingAt<kRing2> va;
             bool ok = true;
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                PlanItem it;
-                uint32_t h;
-                work.take(it, h);
-                const uint32_t kh = h / p.group, row = it.start + it.tile * kAttTile;
-                if (!(ok = mbar_wait(bar(kQEmpty), (q_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
-                mbar_expect_tx(bar(kQFull), 2 * tile_bytes);
-                load_rows(q0, &map_q, chunks, h, row, bar(kQFull));
-                load_rows(do0, &map_do, chunks, h, row, bar(kQFull));
-                ++q_issued;
-                for (uint32_t t = 0; t <= it.tile; ++t) {
-                    if (!(ok = mbar_wait(bar(kKEmpty + ka.i), ka.phase ^ 1, p.wait_limit, gave_up))) break;
-                    mbar_expect_tx(bar(kKFull + ka.i), tile_bytes);
-                    load_rows(kt0 + ka.i * kTileBytes, &map_k, chunks, kh, it.start + t * kAttTile, bar(kKFull + ka.i));
-                    ka.next();
-                    ++k_issued;
-                    if (!(ok = mbar_wait(bar(kVEmpty + va.i), va.phase ^ 1, p.wait_limit, gave_up))) break;
-                    mbar_expect_tx(bar(kVFull + va.i), tile_bytes);
-                    load_rows(vt0 + va.i * kTileBytes, &map_v, chunks, kh, it.start + t * kAttTile, bar(kVFull + va.i));
-                    va.next();
-                    ++tiles;
+            PlanItem it;
+            uint32_t h;
+            while (ok && take_work(works, it, h)) {
+                if (lane == 0) {
+                    const uint32_t kh = h / p.group, row = it.start + it.tile * kAttTile;
+                    if ((ok = mbar_wait(bar(kQEmpty), (q_issued & 1) ^ 1, p.wait_limit, gave_up))) {
+                        mbar_expect_tx(bar(kQFull), 2 * tile_bytes);
+                        load_rows(q0, &map_q, chunks, h, row, bar(kQFull));
+                        load_rows(do0, &map_do, chunks, h, row, bar(kQFull));
+                        ++q_issued;
+                    }
+                    for (uint32_t t = 0; t <= it.tile && ok; ++t) {
+                        if (!(ok = mbar_wait(bar(kKEmpty + ka.i), ka.phase ^ 1, p.wait_limit, gave_up))) break;
+                        mbar_expect_tx(bar(kKFull + ka.i), tile_bytes);
+                        load_rows(kt0 + ka.i * kTileBytes, &map_k, chunks, kh, it.start + t * kAttTile, bar(kKFull + ka.i));
+                        ka.next();
+                        ++k_issued;
+                        if (!(ok = mbar_wait(bar(kVEmpty + va.i), va.phase ^ 1, p.wait_limit, gave_up))) break;
+                        mbar_expect_tx(bar(kVFull + va.i), tile_bytes);
+                        load_rows(vt0 + va.i * kTileBytes, &map_v, chunks, kh, it.start + t * kAttTile, bar(kVFull + va.i));
+                        va.next();
+                        ++tiles;
+                    }
                 }
+                ok = __all_sync(0xFFFFFFFFu, ok);
             }
-            s_issued[0] = k_issued;
-            s_issued[1] = tiles;
-            s_issued[2] = q_issued;
+            if (lane == 0) {
+                s_issued[0] = k_issued;
+                s_issued[1] = tiles;
+                s_issued[2] = q_issued;
+            }
         } else if (warp == 1) {
             // ---- products, S and dq: the whole warp waits, one lane issues.  An issue blocks until the tensor cores are nearly
             // through with it, so dP has a warp of its own ----
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             const uint32_t desc_d = mma_desc(kAttTile, steps * 16, false, true);
-            uint32_t q_taken = 0, g = 0, made = 0;       // steps of dq and of S so far
+            uint32_t q_taken = 0, works = 0, g = 0, made = 0;       // g, made: steps of dq and of S so far
             RingAt<kRing3> sa, da;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                PlanItem it;
-                uint32_t h;
-                work.take(it, h);
+            PlanItem it;
+            uint32_t h;
+            while (ok && take_work(works, it, h)) {
                 const uint32_t n = it.tile + 1;
                 if (!wait(kQFull, q_taken & 1)) break;
                 ++q_taken;
@@ -163,14 +222,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         } else if (warp == 2) {
             // ---- products, dP ----
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
-            uint32_t q_taken = 0, g = 0;
+            uint32_t q_taken = 0, works = 0, g = 0;
             RingAt<kRing2> va;
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                PlanItem it;
-                uint32_t h;
-                work.take(it, h);
+            PlanItem it;
+            uint32_t h;
+            while (ok && take_work(works, it, h)) {
                 const uint32_t n = it.tile + 1;
                 if (!wait(kQFull, q_taken++ & 1)) break;
                 for (uint32_t t = 0; t < n && ok; ++t) {
@@ -188,61 +246,38 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 }
             }
             if (lane == 0) s_taken[1] = g;
+        } else if (lane == 0) {
+            // ---- work: tiles of queries in falling order of their keys, from the counter that all CTAs share ----
+            uint32_t w = atomicAdd(p.next, 1u);
+            for (uint32_t n = 0;; ++n) {
+                const bool more = w < total;
+                uint4 v = make_uint4(0, 0, kNone, 0);
+                if (more) {
+                    const PlanItem it = list[w / p.units];
+                    v = make_uint4(it.start, it.len, it.tile, w % p.units);
+                    w = atomicAdd(p.next, 1u);
+                }
+                if (!mbar_wait(bar(kWorkEmpty + (n & 1)), (n >> 1 & 1) ^ 1, p.wait_limit, gave_up)) break;
+                s_work[n & 1] = v;
+                mbar_arrive(bar(kWorkFull + (n & 1)));
+                if (!more) break;
+            }
         }
     } else {
         regs_up<kManyRegs>();
         // ---- scores: warp w may read the quarter w % 4 of tensor memory's lanes ----
         const uint32_t half = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t mine = tmem + (quarter * 32 << 16);
-        uint32_t g = 0, done = 0;
+        uint32_t g = 0, done = 0, works = 0;
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-        // What delta needs, asked for before the work in front is finished: a warp takes 16 rows, two at a time, 16 lanes a row, so that
-        // accesses are whole lines.  (Each thread its own row: 9 us per tile for 64 KB.)
-        constexpr uint32_t kPairs = kAttTile / kBwdWarps / 2;
-        const uint32_t delta_row = (warp - 4) * 2 * kPairs + lane / 16, delta_col = lane % 16 * 8;
-        Raw8<__nv_bfloat16> o8[kPairs], d8[kPairs];
-        float lse_ahead = 0.f;
-        Turns work(list, total, p.units);
-        // every load from an address inside, whatever the row and column: a branch around it would wait for it
-        auto fetch = [&]() {
-            if (!work.more()) return;
-            const PlanItem it = work.ahead;
-            const uint32_t h = work.unit(), tile = it.tile * kAttTile, col = delta_col < p.head_dim ? delta_col : 0;
-#pragma unroll
-            for (uint32_t j = 0; j < kPairs; ++j) {
-                const uint64_t at = (uint64_t)it.start + min(tile + delta_row + 2 * j, it.len - 1);
-                o8[j].load(p.o + at * p.o_ld + h * p.head_dim + col);
-                d8[j].load(p.d_o + at * p.do_ld + h * p.head_dim + col);
-            }
-            lse_ahead = p.lse_in[h * p.tokens + it.start + min(tile + r, it.len - 1)];
-        };
-        fetch();
-        while (work.more() && ok) {
-            PlanItem it;
-            uint32_t h;
-            work.take(it, h);
+        PlanItem it;
+        uint32_t h;
+        while (ok && take_work(works, it, h)) {
             const uint32_t n = it.tile + 1, row = it.tile * kAttTile + r;
             const bool valid = row < it.len;
-            const uint64_t at = (uint64_t)it.start + row;
-#pragma unroll
-            for (uint32_t j = 0; j < kPairs; ++j) {
-                float a[8], b[8], part = 0.f;
-                o8[j].get(a);
-                d8[j].get(b);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) part = fmaf(a[c], b[c], part);
-                part = delta_col < p.head_dim ? part : 0.f;
-#pragma unroll
-                for (int c = 8; c; c >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, c);
-                if (lane % 16 == 0) s_delta[done & 1][delta_row + 2 * j] = part;
-            }
-            const float lse2 = lse_ahead * -(float)kLog2eD;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kDelta));
-            if (!wait(kDelta, done & 1)) break;
-            const float delta = s_delta[done & 1][r];
-            if (valid && half == 0) p.delta[h * p.tokens + at] = delta;
+            const uint64_t at = (uint64_t)it.start + row, stat = h * p.tokens + it.start + min(row, it.len - 1);
+            const float lse2 = p.lse_in[stat] * -(float)kLog2eD, delta = p.delta[stat];
             for (uint32_t t = 0; t < n; ++t, ++g) {
                 const uint32_t s_at = mine + (g & 1) * 128 + half * kHalf;
                 if (!wait(kSFull + (g & 1), g >> 1 & 1)) break;
@@ -267,10 +302,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
             }
-            if (!ok) break;
-            fetch();
-            if (!wait(kDqFull, done & 1)) break;
-            ++done;
+            if (!ok || !wait(kDqFull, done++ & 1)) break;
             __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
             for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid, p.sectors);
             tc_fence_before();
@@ -295,6 +327,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     }
     tc_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 512);
+    wait_for_earlier();        // the first pass may still run; what follows in the stream must find both done
     if (threadIdx.x == 0 && failed && p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_TIMEOUT);
 }
 
@@ -353,6 +386,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     tc_fence_after();
     const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);
     volatile uint32_t* gave_up = &s_gave_up;
+    wait_for_earlier();        // delta is there,
+    let_next_start();          // for the second pass, too
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
@@ -577,12 +612,14 @@ dte_status launch_attention_backward(const AttParams& params, const dte_matrix* 
     auto sectors = [&](const __nv_bfloat16* x, uint64_t ld) { return !(((uintptr_t)x | ld * 2 | p.head_dim * 2u) & 31u); };
     p.sectors = sectors(p.dq, p.dq_ld) && sectors(p.dk, p.dk_ld) && sectors(p.dv, p.dv_ld);
     auto grid = [&] { return (unsigned)(tiles * p.units < (uint64_t)sms ? tiles * p.units : sms); };
-    p.units = (uint32_t)(q->cols / p.head_dim);
-    att_dq_kernel<<<grid(), kBwdThreads, kBwdSmem, st>>>(mq, mk, mv, md, p);
+    const uint32_t heads = (uint32_t)(q->cols / p.head_dim);
+    const uint64_t warps = (p.tokens + 31) / 32 * heads, per_cta = kDeltaThreads / 32;
+    att_delta_kernel<<<(unsigned)((warps + per_cta - 1) / per_cta), kDeltaThreads, 0, st>>>(p, heads);
     DTE_CUDA(cudaGetLastError());
     p.units = (uint32_t)(k->cols / p.head_dim);
-    att_dkv_kernel<<<grid(), kBwdThreads, kBwdSmem, st>>>(mq, mk, mv, md, p);
-    DTE_CUDA(cudaGetLastError());
+    DTE_CUDA(launch_after(att_dkv_kernel, dim3(grid()), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
+    p.units = heads;
+    DTE_CUDA(launch_after(att_dq_kernel, dim3(grid()), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
     return DTE_OK;
 }
 

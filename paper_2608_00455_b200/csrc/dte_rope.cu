@@ -6,12 +6,12 @@
 
 namespace dte {
 
-constexpr uint32_t kRopeThreads = 256;
+constexpr uint32_t kRopeThreads = 128;
 constexpr uint32_t kMaxHeadDim = 1024;
 constexpr uint32_t kMaxRopeHeads = 4095;     // of queries and keys together; see RopeParams::by_pieces
-// Tokens of a CTA: four, so that every thread has one angle and several vectors of a head of 128 (16384 tokens of 40 heads: 69 us
-// with one), where that leaves each multiprocessor some CTAs; one for few tokens.
-constexpr uint32_t kRopeTokens = 4;
+// Tokens of a CTA: two, so that every thread has one angle and several vectors of heads of 128 (16384 tokens of 40 heads: 60 us; 69
+// with one, 63 with four and 256 threads), where that leaves each multiprocessor some CTAs; one for few tokens.
+constexpr uint32_t kRopeTokens = 2;
 
 struct RopeSide {
     const void* x;
