@@ -44,7 +44,7 @@ struct AttParams {
     __nv_bfloat16 *out, *dq, *dk, *dv;
     uint64_t out_ld, dq_ld, dk_ld, dv_ld;
     float *lse, *delta;
-    uint32_t* next;            // backwards: the second pass's next piece of work
+    uint32_t* next;            // backwards: the next piece of work of the two passes
     const float* lse_in;
     uint64_t* flags;
     bool sectors;              // every 16 columns of the outputs are a whole sector of 32 bytes

@@ -4,8 +4,9 @@
 //   att_dkv_kernel    a tile of 128 keys of one key head against the queries of its group that see them:  dk, dv
 //   att_dq_kernel     a tile of 128 queries of one head against its keys:  dq
 // With p = exp(z - lse), dz = p (dout v^T - delta): dq = scale dz k, dk = scale dz^T q, dv = p^T dout.  The first pass has four products
-// per pair of tiles, the second three, where one pass would have five.  The second one starts on the SMs that the first one leaves
-// and draws its tiles from a counter: a batch with few, unequal key tiles leaves most SMs early.
+// per pair of tiles, the second three, where one pass would have five.  Both draw their tiles, the
+// largest first, from a counter, and the second one starts on the SMs that the first one leaves: few, unequal key tiles leave
+// most SMs early.
 //
 // Both: one CTA per SM, a warp that loads, two that issue products, eight that turn scores into operands, each thread half a
 // row.  The first pass works on the transposed scores (rows are keys), so that p and dz are, as they come out of the
@@ -51,10 +52,10 @@ __device__ __forceinline__ void store_half(uint32_t tmem, const float (&z)[kHalf
 // ---- delta ------------------------------------------------------------------------------------------------------
 constexpr uint32_t kDeltaThreads = 256;
 
-// A warp takes 32 tokens of a head, two at a time, 16 lanes a row.  Also sets the second pass's counter to zero.
+// A warp takes 32 tokens of a head, two at a time, 16 lanes a row.  Also sets the counters of the two passes to zero.
 __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttParams p, uint32_t heads) {
     let_next_start();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.next = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.next[0] = p.next[1] = 0;
     const uint64_t unit = (uint64_t)blockIdx.x * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * 32;
     const uint32_t lane = threadIdx.x & 31, h = (uint32_t)(unit % heads), col = lane % 16 * 8;
     if (first >= p.tokens) return;
@@ -248,14 +249,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             if (lane == 0) s_taken[1] = g;
         } else if (lane == 0) {
             // ---- work: tiles of queries in falling order of their keys, from the counter that all CTAs share ----
-            uint32_t w = atomicAdd(p.next, 1u);
+            uint32_t w = atomicAdd(p.next + 1, 1u);
             for (uint32_t n = 0;; ++n) {
                 const bool more = w < total;
                 uint4 v = make_uint4(0, 0, kNone, 0);
                 if (more) {
                     const PlanItem it = list[w / p.units];
                     v = make_uint4(it.start, it.len, it.tile, w % p.units);
-                    w = atomicAdd(p.next, 1u);
+                    w = atomicAdd(p.next + 1, 1u);
                 }
                 if (!mbar_wait(bar(kWorkEmpty + (n & 1)), (n >> 1 & 1) ^ 1, p.wait_limit, gave_up)) break;
                 s_work[n & 1] = v;
@@ -271,12 +272,21 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         uint32_t g = 0, done = 0, works = 0;
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
+        // A finished tile's dq is read from tensor memory only when the next work's first p is made: its last product and the next
+        // one's first scores take their time meanwhile.
+        __nv_bfloat16* out = nullptr;                   // of the tile that waits, NULL: a row past its sequence
+        bool waits = false;
+        auto finish = [&]() {
+            if (!wait(kDqFull, done++ & 1)) return;
+            for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, out != nullptr, p.sectors);
+            tc_fence_before();
+            waits = false;
+        };
         PlanItem it;
         uint32_t h;
         while (ok && take_work(works, it, h)) {
             const uint32_t n = it.tile + 1, row = it.tile * kAttTile + r;
-            const bool valid = row < it.len;
-            const uint64_t at = (uint64_t)it.start + row, stat = h * p.tokens + it.start + min(row, it.len - 1);
+            const uint64_t stat = h * p.tokens + it.start + min(row, it.len - 1);
             const float lse2 = p.lse_in[stat] * -(float)kLog2eD, delta = p.delta[stat];
             for (uint32_t t = 0; t < n; ++t, ++g) {
                 const uint32_t s_at = mine + (g & 1) * 128 + half * kHalf;
@@ -285,6 +295,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 load_half(s_at, z);
 #pragma unroll
                 for (int j = 0; j < (int)kHalf; ++j) z[j] = exp2_fast(fmaf(z[j], p.k2, lse2));
+                if (waits) finish();
                 if (!wait(kDpFull, g & 1)) break;
                 float d[kHalf];
                 load_half(mine + 256 + half * kHalf, d);
@@ -293,20 +304,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 if (lane == 0) mbar_arrive(bar(kDpRead));
 #pragma unroll
                 for (int j = 0; j < (int)kHalf; ++j) z[j] *= d[j] - delta;
-                if (t + 1 == n) {             // on the diagonal; a query that sees one key has a constant weight
+                if (t + 1 == n) {             // on the diagonal: columns up to `last`; a query that sees one key has a constant weight
+                    const int last = row == 0 ? -1 : (int)r - (int)(half * kHalf);
 #pragma unroll
-                    for (int j = 0; j < (int)kHalf; ++j) z[j] = half * kHalf + j > r || row == 0 ? 0.f : z[j];
+                    for (int j = 0; j < (int)kHalf; ++j) z[j] = j > last ? 0.f : z[j];
                 }
                 if ((t + 1) * kAttTile > it.len)              // keys past the sequence
                     clear_rows(smem + (2 + g % kRing3) * kTileBytes, chunks, it.len - t * kAttTile, threadIdx.x - 128, 256);
                 store_half(s_at, z);
                 if (lane == 0) mbar_arrive(bar(kDsFull + (g & 1)));
             }
-            if (!ok || !wait(kDqFull, done++ & 1)) break;
-            __nv_bfloat16* out = p.dq + at * p.dq_ld + h * p.head_dim;
-            for (uint32_t c = half * 32; c < p.head_dim; c += 64) store_columns(out, mine + 384, c, p.head_dim, p.scale, valid, p.sectors);
-            tc_fence_before();
+            out = row < it.len ? p.dq + ((uint64_t)it.start + row) * p.dq_ld + h * p.head_dim : nullptr;
+            waits = true;
         }
+        if (ok && waits) finish();
     }
     __syncwarp();
     tc_fence_before();
@@ -337,11 +348,10 @@ struct DkvWork {
     uint32_t start, len, kv_head, tile, tiles, n;     // tiles: of queries per head; n: in all
 };
 
-__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, Turns& turns) {
-    // the list falls in the number of tiles in front: taken from the other end, in the number of tiles behind
-    PlanItem it;
+// it: an item of the list, which falls in the number of tiles in front: taken from the other end, in the number of tiles behind.
+__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, const PlanItem& it, uint32_t kv_head) {
     DkvWork f;
-    turns.take(it, f.kv_head);
+    f.kv_head = kv_head;
     f.start = it.start;
     f.len = it.len;
     f.tiles = it.tile + 1;
@@ -357,9 +367,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                    const __grid_constant__ CUtensorMap map_do, const __grid_constant__ AttParams p) {
     extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle's period
     enum { kQFull, kQEmpty = kRing3, kDoFull = 2 * kRing3, kDoEmpty = kDoFull + kRing2, kKvFull = kDoEmpty + kRing2, kKvEmpty, kSFull, kPFull, kDpFull, kDsFull,
-           kAccFull, kTurn, kStatFull = kTurn + 2, kStatEmpty = kStatFull + 2, kLast = kStatEmpty + 2, kBars };
+           kAccFull, kTurn, kStatFull = kTurn + 2, kStatEmpty = kStatFull + 2, kWorkFull = kStatEmpty + 2, kWorkEmpty = kWorkFull + 2, kLast = kWorkEmpty + 2, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of Q, dout, and K with V
+    __shared__ uint4 s_work[2];            // as in att_dq_kernel
     __shared__ __align__(16) float s_stat[2][2][kAttTile];       // -lse log2(e) and -delta of a tile of queries
     const uint32_t k0 = smem_addr(smem), v0 = k0 + kTileBytes, qt0 = k0 + 2 * kTileBytes, dot0 = qt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
@@ -372,7 +383,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         for (uint32_t i = 0; i < kBars; ++i) {
             const bool warps = i == kPFull || i == kDsFull || i == kStatEmpty || i == kStatEmpty + 1;
             const bool both = (i >= kQEmpty && i < kDoFull) || (i >= kDoEmpty && i < kKvFull) || i == kKvEmpty || i == kAccFull || i == kLast;
-            mbar_init(bar(i), warps ? kBwdWarps : both ? 2 : 1);
+            const bool all = i == kWorkEmpty || i == kWorkEmpty + 1;
+            mbar_init(bar(i), warps ? kBwdWarps : all ? 3 + kBwdWarps : both ? 2 : 1);
         }
         s_gave_up = 0;
         for (uint32_t i = 0; i < 3; ++i) s_issued[i] = s_taken[i] = 0;
@@ -391,39 +403,53 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
+    // The next piece of work, by a whole warp; false at the end, or where the wait runs out.
+    auto take_work = [&](uint32_t& n, DkvWork& f) {
+        if (!warp_wait(bar(kWorkFull + (n & 1)), n >> 1 & 1, p.wait_limit, gave_up)) return false;
+        const uint4 w = s_work[n & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kWorkEmpty + (n & 1)));
+        ++n;
+        f = dkv_work(p, PlanItem{w.x, w.y, w.z, 0}, w.w);
+        return w.z != kNone;
+    };
 
     if (warp < 4) {
         regs_down<kFewRegs>();
-        if (warp == 0 && lane == 0) {
-            // ---- loads ----
-            uint32_t q_issued = 0, do_issued = 0, kv_issued = 0;
+        if (warp == 0) {
+            // ---- loads: one lane ----
+            uint32_t q_issued = 0, do_issued = 0, kv_issued = 0, works = 0;
             RingAt<kRing3> qa;
             RingAt<kRing2> da;
             bool ok = true;
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                const DkvWork f = dkv_work(p, work);
-                if (!(ok = mbar_wait(bar(kKvEmpty), (kv_issued & 1) ^ 1, p.wait_limit, gave_up))) break;
-                mbar_expect_tx(bar(kKvFull), 2 * tile_bytes);
-                load_rows(k0, &map_k, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
-                load_rows(v0, &map_v, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
-                ++kv_issued;
-                for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
-                    for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t) {
-                        if (!(ok = mbar_wait(bar(kQEmpty + qa.i), qa.phase ^ 1, p.wait_limit, gave_up))) break;
-                        mbar_expect_tx(bar(kQFull + qa.i), tile_bytes);
-                        load_rows(qt0 + qa.i * kTileBytes, &map_q, chunks, h, f.start + t * kAttTile, bar(kQFull + qa.i));
-                        qa.next();
-                        ++q_issued;
-                        if (!(ok = mbar_wait(bar(kDoEmpty + da.i), da.phase ^ 1, p.wait_limit, gave_up))) break;
-                        mbar_expect_tx(bar(kDoFull + da.i), tile_bytes);
-                        load_rows(dot0 + da.i * kTileBytes, &map_do, chunks, h, f.start + t * kAttTile, bar(kDoFull + da.i));
-                        da.next();
-                        ++do_issued;
-                    }
+            DkvWork f;
+            while (ok && take_work(works, f)) {
+                if (lane == 0 && (ok = mbar_wait(bar(kKvEmpty), (kv_issued & 1) ^ 1, p.wait_limit, gave_up))) {
+                    mbar_expect_tx(bar(kKvFull), 2 * tile_bytes);
+                    load_rows(k0, &map_k, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
+                    load_rows(v0, &map_v, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
+                    ++kv_issued;
+                    for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
+                        for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t) {
+                            if (!(ok = mbar_wait(bar(kQEmpty + qa.i), qa.phase ^ 1, p.wait_limit, gave_up))) break;
+                            mbar_expect_tx(bar(kQFull + qa.i), tile_bytes);
+                            load_rows(qt0 + qa.i * kTileBytes, &map_q, chunks, h, f.start + t * kAttTile, bar(kQFull + qa.i));
+                            qa.next();
+                            ++q_issued;
+                            if (!(ok = mbar_wait(bar(kDoEmpty + da.i), da.phase ^ 1, p.wait_limit, gave_up))) break;
+                            mbar_expect_tx(bar(kDoFull + da.i), tile_bytes);
+                            load_rows(dot0 + da.i * kTileBytes, &map_do, chunks, h, f.start + t * kAttTile, bar(kDoFull + da.i));
+                            da.next();
+                            ++do_issued;
+                        }
+                }
+                ok = __all_sync(0xFFFFFFFFu, ok);
             }
-            s_issued[0] = q_issued;
-            s_issued[1] = do_issued;
-            s_issued[2] = kv_issued;
+            if (lane == 0) {
+                s_issued[0] = q_issued;
+                s_issued[1] = do_issued;
+                s_issued[2] = kv_issued;
+            }
         } else if (warp == 1 || warp == 2) {
             // ---- products: the whole warp waits, one lane issues.  Warp 1 has what reads and writes S and p (S of the next step behind dv
             // of this one), warp 2 what reads and writes dP and dz (dk, the next dP).  An issue blocks until the tensor cores are
@@ -438,8 +464,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             RingAt<kRing2> da;                  // warp 1: the tile for dv; warp 2: the next tile for dP
             bool ok = true;
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                const int n = (int)dkv_work(p, work).n;
+            uint32_t works = 0;
+            DkvWork f;
+            while (ok && take_work(works, f)) {
+                const int n = (int)f.n;
                 if (!wait(kKvFull, kv_taken & 1)) break;
                 ++kv_taken;
                 // step -1 makes the first scores; step j adds step j's product up and makes the scores of the next one
@@ -480,11 +508,31 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 if (first) s_taken[2] = kv_taken;
             }
         } else if (warp == 3) {
-            // ---- lse and delta of the tiles of queries ----
-            uint32_t g = 0;
+            // ---- work, from the counter that all CTAs share, and lse and delta of its tiles of queries ----
+            uint32_t g = 0, works = 0;
             bool ok = true;
-            for (Turns work(list, total, p.units); work.more() && ok;) {
-                const DkvWork f = dkv_work(p, work);
+            auto draw = [&]() {
+                const uint32_t w = __shfl_sync(0xFFFFFFFFu, lane == 0 ? atomicAdd(p.next, 1u) : 0u, 0);
+                if (w >= total) return make_uint4(0, 0, kNone, 0);
+                const PlanItem it = list[w / p.units];
+                return make_uint4(it.start, it.len, it.tile, w % p.units);
+            };
+            auto publish = [&](const uint4& w) {
+                if (!(ok = warp_wait(bar(kWorkEmpty + (works & 1)), (works >> 1 & 1) ^ 1, p.wait_limit, gave_up))) return;
+                if (lane == 0) {
+                    s_work[works & 1] = w;
+                    mbar_arrive(bar(kWorkFull + (works & 1)));
+                }
+                ++works;
+            };
+            uint4 now = draw();
+            publish(now);
+            while (ok && now.z != kNone) {
+                const uint4 next = draw();
+                publish(next);
+                if (!ok) break;
+                const DkvWork f = dkv_work(p, PlanItem{now.x, now.y, now.z, 0}, now.w);
+                now = next;
                 for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
                     for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
                         const uint32_t row = t * kAttTile + lane * 4;
@@ -511,12 +559,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         uint32_t g = 0, done = 0;
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
-        for (Turns work(list, total, p.units); work.more() && ok;) {
-            const DkvWork f = dkv_work(p, work);
+        uint32_t works = 0;
+        DkvWork f;
+        while (ok && take_work(works, f)) {
             uint32_t t = f.tile;
             for (uint32_t j = 0; j < f.n; ++j, ++g) {
                 const uint32_t first = t * kAttTile + half * kHalf;       // query of this thread's first column
                 const bool edge = t == f.tile || (t + 1) * kAttTile > f.len;
+                const int low = (int)(f.tile * kAttTile + r) - (int)first, high = (int)f.len - (int)first;      // columns [low, high) are seen
                 const float4* lse = reinterpret_cast<const float4*>(&s_stat[g & 1][0][half * kHalf]);
                 const float4* delta = reinterpret_cast<const float4*>(&s_stat[g & 1][1][half * kHalf]);
                 if (!wait(kStatFull + (g & 1), g >> 1 & 1) || !wait(kSFull, g & 1)) break;
@@ -531,9 +581,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     z[4 * c + 3] = exp2_fast(fmaf(z[4 * c + 3], p.k2, l.w));
                 }
                 if (edge) {                   // on the diagonal, or past the sequence
-                    const uint32_t key = f.tile * kAttTile + r;
 #pragma unroll
-                    for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len ? 0.f : z[c];
+                    for (int c = 0; c < (int)kHalf; ++c) z[c] = c < low || c >= high ? 0.f : z[c];
                 }
                 if ((t + 1) * kAttTile > f.len) {             // rows past the sequence, of q and of dout
                     if (!wait(kDoFull + g % kRing2, g / kRing2 & 1)) break;
@@ -554,9 +603,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     z[4 * c + 3] *= d[4 * c + 3] + l.w;
                 }
                 if (edge) {                   // 0 * what lies past the sequence; a query that sees one key has a constant weight
-                    const uint32_t key = f.tile * kAttTile + r;
+                    const int from = first == 0 && low < 1 ? 1 : low;
 #pragma unroll
-                    for (int c = 0; c < (int)kHalf; ++c) z[c] = first + c < key || first + c >= f.len || first + c == 0 ? 0.f : z[c];
+                    for (int c = 0; c < (int)kHalf; ++c) z[c] = c < from || c >= high ? 0.f : z[c];
                 }
                 store_half(d_at, z);
                 if (lane == 0) {
