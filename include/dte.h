@@ -585,8 +585,8 @@ DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t h
  * data 16-byte aligned, ld >= cols and a multiple of 8 (rows go through the tensor memory accelerator).  lse: fp32,
  * heads x tokens.  Rows that belong to no sequence (in front of starts[0], behind the last one) are left as they
  * were in every output, and what they hold in the inputs, NaN included, reaches no result; nor does what one sequence
- * holds reach another.  Inside a sequence a NaN or infinity in k reaches only queries that see it; in v (and backwards
- * in q and dout) it may also reach rows of the same block of 128 on the other side of the diagonal, through 0 * infinity.
+ * holds reach another.  Inside a sequence, forwards, a NaN or infinity in k reaches only queries that see it; in v, and backwards
+ * in any input, it may also reach rows of the same block of 128 on the other side of the diagonal, through 0 * infinity.
  *
  * dte_attention_plan reads the n_sequences + 1 starts (DEVICE, not decreasing, inside [0, tokens]; empty sequences are
  * allowed) once per packed batch and leaves in `plan` (DEVICE, 256-byte aligned) the order of work that the calls on
@@ -602,7 +602,9 @@ DTE_API dte_status dte_attention_forward(const dte_matrix* q, const dte_matrix* 
 
 /* Gradients of dte_attention_forward from its outputs and dout, with p = exp(z - lse) and delta = sum over columns of dout * out:
  *   dv = p^T dout,  dz = p (dout v^T - delta),  dq = scale * dz k,  dk = scale * dz^T q
- * dk and dv are sums over the query heads of a key head.  Deterministic; the scores are made again in both passes over them. */
+ * dk and dv are sums over the query heads of a key head.  p and dz are rounded to BF16, the operand type of the products they enter, out
+ * is taken as it was rounded, and sums are fp32; a query that sees one key has dz = 0.  The scores are made again, twice: once for dk and
+ * dv, once for dq, so that every sum has one owner and a fixed order.  workspace: delta and two counters. */
 DTE_API uint64_t dte_attention_backward_workspace_bytes(uint64_t tokens, uint64_t heads);
 DTE_API dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
                                           const dte_matrix* out, const float* lse, const dte_matrix* dout, const void* plan,

@@ -194,6 +194,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     enum { kQFull, kQEmpty, kSFull, kPFull, kOFull, kTurn };
     const uint32_t last_bar = bar0 + 8 * (2 * kFwdRing + 12);
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    // asked for before the setup, needed behind it
+    const PlanHead* head = reinterpret_cast<const PlanHead*>(p.plan);
+    const uint32_t items = plan_ok(p) ? (p.pair_heads ? head->tiles : head->pairs) : 0, total = items * p.units;
+    const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + (p.pair_heads ? kPlanHeader : items ? head->pairs_at : 0));
 
     if (threadIdx.x == 0) {
         tma_prefetch_map(&map_q);
@@ -223,9 +227,6 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
     tc_fence_after();
     const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);         // S of the slots at columns 0 and 128, O at 256 and 384
     volatile uint32_t* gave_up = &s_gave_up;
-    const PlanHead* head = reinterpret_cast<const PlanHead*>(p.plan);
-    const uint32_t items = plan_ok(p) ? (p.pair_heads ? head->tiles : head->pairs) : 0, total = items * p.units;
-    const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + (p.pair_heads ? kPlanHeader : items ? head->pairs_at : 0));
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
 
     if (warp < 4) {

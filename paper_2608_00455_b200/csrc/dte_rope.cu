@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
 template <typename T, int V>
 static void launch_rope(const RopeParams& p, bool interleaved, cudaStream_t st) {
     const unsigned grid = (p.tokens + p.per_cta - 1) / p.per_cta;
-    const size_t smem = p.per_cta * (p.rot / 2) * sizeof(float2);        // 16 KB at most
+    const size_t smem = p.per_cta * (p.rot / 2) * sizeof(float2);        // 8 KB at most
     if (interleaved) rope_kernel<T, V, true><<<grid, kRopeThreads, smem, st>>>(p);
     else rope_kernel<T, V, false><<<grid, kRopeThreads, smem, st>>>(p);
 }

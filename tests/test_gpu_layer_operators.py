@@ -607,3 +607,56 @@ def test_clip_captured_and_replayed():
         assert abs(float(norm) - want) <= 8 * E * want
         for t, o in zip(g, outs):
             assert_within(o, t.to(F64) / want, 16 * E * t.to(F64).abs() + 1e-38, "replayed")
+
+
+# ---- waits that run out -------------------------------------------------------------------------------------------
+
+def test_a_wait_that_runs_out_sets_the_flag_and_leaves_the_device_usable():
+    for hq, hk, dim, lengths in ((4, 2, 128, [700, 90]), (3, 3, 64, [400])):
+        b = Batch(lengths, hq, hk, dim)
+        ws = workspace(dte.dte_attention_backward_workspace_bytes(b.tokens, hq))
+        b.forward()
+        dte.lib().dte_attention_set_wait_limit(1)             # every wait that is not over at once gives up
+        try:
+            flags = torch.zeros(2, dtype=torch.int64, device=DEV)
+            dte.dte_attention_forward(b.q, b.k, b.v, b.plan, torch.empty_like(b.out), None, flags=flags[:1])
+            dte.dte_attention_backward(b.q, b.k, b.v, b.out, b.lse, b.dout, b.plan, *(torch.empty_like(g) for g in b.grads), ws, flags=flags[1:])
+            torch.cuda.synchronize()
+        finally:
+            dte.lib().dte_attention_set_wait_limit(0)
+        assert flags.tolist() == [dte.DTE_DEV_TIMEOUT] * 2
+        b.forward()
+        b.check_forward()
+        b.backward()
+        b.check_backward()
+
+
+def test_attention_on_two_streams_with_one_plan():
+    a, b = Batch([500, 300], 4, 2, 128), Batch([500, 300], 4, 2, 128, seed=40)
+    b.plan = a.plan
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [workspace(dte.dte_attention_backward_workspace_bytes(800, 4)) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, s, ws in zip((a, b), streams, spaces):
+            x.forward(s)
+            x.backward(s, ws)
+    torch.cuda.synchronize()
+    for x in (a, b):
+        x.check_forward()
+        x.check_backward()
+
+
+def test_work_behind_the_gradient_in_the_stream_sees_all_of_it():
+    # the passes overlap inside the call; what follows in the stream must find both finished
+    b = Batch([1500, 700, 40], 8, 2, 64)
+    b.forward()
+    b.backward()
+    want = [g.clone() for g in b.grads]
+    for _ in range(20):
+        for g in b.grads:
+            g.zero_()
+        b.backward()
+        got = [g + 0 for g in b.grads]
+        for g, w in zip(got, want):
+            assert same_bits(g, w)
