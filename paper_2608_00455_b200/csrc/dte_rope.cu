@@ -12,6 +12,7 @@ constexpr uint32_t kMaxRopeHeads = 4095;     // of queries and keys together; se
 // Tokens of a CTA: two, so that every thread has one angle and several vectors of heads of 128 (16384 tokens of 40 heads: 60 us; 69
 // with one, 63 with four and 256 threads), where that leaves each multiprocessor some CTAs; one for few tokens.
 constexpr uint32_t kRopeTokens = 2;
+constexpr int kAhead = 2;                    // pieces that a thread loads before it uses the first one
 
 struct RopeSide {
     const void* x;
@@ -30,6 +31,7 @@ struct RopeParams {
     bool inverse;
     uint32_t pieces, turned;     // vectors of work per head, and how many of them are pairs
     uint32_t per_cta;            // tokens
+    bool few;                    // tokens: fewer than multiprocessors
     uint32_t by_pieces, by_heads;  // ceil(2^32 / n): the quotient by multiplication is exact below 2^32 / n
 };
 
@@ -55,12 +57,11 @@ __device__ __forceinline__ void rope_pair(float2 t, float a, float b, float& lo,
 __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t by) { return d == 1 ? n : __umulhi(n, by); }
 
 // A piece is V pairs (half layout: V columns of each half), V / 2 pairs (interleaved; V = 1: a pair) or V columns that are
-// copied.  kAhead pieces of a thread are loaded before the first one is used.
+// copied.
 template <typename T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
     extern __shared__ float2 s_turn[];               // per token: rot / 2 cosines and sines
     __shared__ bool s_padding[kRopeTokens];
-    constexpr int kAhead = 2;
     constexpr int W = INTERLEAVED && V == 1 ? 2 : V;     // columns of a piece of interleaved pairs
     const uint32_t first = blockIdx.x * p.per_cta, tokens = min(p.per_cta, p.tokens - first), half = p.rot / 2;
     const uint32_t work = tokens * p.heads * p.pieces;
@@ -117,9 +118,11 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
             c.b.store(c.y + (INTERLEAVED ? 1 : half));
         }
     };
+    // few tokens: their heads are shared by the CTAs of a column of the grid
+    const uint32_t start = blockIdx.y * kAhead * kRopeThreads + threadIdx.x;
     Piece c[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load(threadIdx.x + u * kRopeThreads, c[u]);      // on the way while the angles are made
+    for (int u = 0; u < kAhead; ++u) load(start + u * kRopeThreads, c[u]);      // on the way while the angles are made
     for (uint32_t i = threadIdx.x; i < tokens * half; i += kRopeThreads) {
         const uint32_t token = i / half, pair = i - token * half;
         const int64_t position = load_id(p.positions, p.positions_dtype, first + token);
@@ -128,8 +131,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
         s_turn[i] = make_float2(t.x * p.amplitude, t.y * p.amplitude);
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < work; i += kAhead * kRopeThreads) {
-        if (i != threadIdx.x) {
+    for (uint32_t i = start; i < work; i += gridDim.y * kAhead * kRopeThreads) {
+        if (i != start) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) load(i + u * kRopeThreads, c[u]);
         }
@@ -140,7 +143,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
 
 template <typename T, int V>
 static void launch_rope(const RopeParams& p, bool interleaved, cudaStream_t st) {
-    const unsigned grid = (p.tokens + p.per_cta - 1) / p.per_cta;
+    const uint32_t work = p.per_cta * p.heads * p.pieces, round = kAhead * kRopeThreads;
+    const dim3 grid((p.tokens + p.per_cta - 1) / p.per_cta, p.few ? (work + round - 1) / round : 1);
     const size_t smem = p.per_cta * (p.rot / 2) * sizeof(float2);        // 8 KB at most
     if (interleaved) rope_kernel<T, V, true><<<grid, kRopeThreads, smem, st>>>(p);
     else rope_kernel<T, V, false><<<grid, kRopeThreads, smem, st>>>(p);
@@ -257,6 +261,7 @@ extern "C" dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_
     if ((s = g.enter(device, &sms)) != DTE_OK) return s;
     const uint64_t reach = (uint64_t)kRopeTokens * p.heads * p.pieces * (p.pieces > p.heads ? p.pieces : p.heads);
     p.per_cta = p.tokens >= (uint32_t)sms * 4 * kRopeTokens && reach < (1ull << 32) ? kRopeTokens : 1;
+    p.few = p.tokens < (uint32_t)sms;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (q->dtype == DTE_BF16) launch_rope_vec<__nv_bfloat16>(p, vec, interleaved, st);
     else launch_rope_vec<float>(p, vec, interleaved, st);
