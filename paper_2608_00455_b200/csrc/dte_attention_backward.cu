@@ -49,42 +49,50 @@ __device__ __forceinline__ void store_half(uint32_t tmem, const float (&z)[kHalf
     __syncwarp();
 }
 
+// Zeros for the columns outside [low, high), which may lie anywhere.
+__device__ __forceinline__ void keep_columns(float (&z)[kHalf], int low, int high) {
+    auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; };
+    const uint32_t kept[2] = {below(high) & ~below(low), below(high - 32) & ~below(low - 32)};
+#pragma unroll
+    for (int c = 0; c < (int)kHalf; ++c) z[c] = kept[c / 32] & (1u << (c % 32)) ? z[c] : 0.f;
+}
+
 // ---- delta ------------------------------------------------------------------------------------------------------
 constexpr uint32_t kDeltaThreads = 256;
 
-// A warp takes 32 tokens of a head, two at a time, 16 lanes a row.  Also sets the counters of the two passes to zero.
+// A warp takes eight times LANES' share of 32 rows of a head: LANES lanes a row, 8 columns each.  Also sets the counters of the two
+// passes to zero.
+template <uint32_t LANES>
 __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttParams p, uint32_t heads) {
+    constexpr uint32_t kRows = 32 / LANES, kTokens = 8 * kRows;
     let_next_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) p.next[0] = p.next[1] = 0;
-    const uint64_t unit = (uint64_t)blockIdx.x * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * 32;
-    const uint32_t lane = threadIdx.x & 31, h = (uint32_t)(unit % heads), col = lane % 16 * 8;
+    const uint64_t unit = (uint64_t)blockIdx.x * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * kTokens;
+    const uint32_t lane = threadIdx.x & 31, h = (uint32_t)(unit % heads), row = lane / LANES, col = lane % LANES * 8;
     if (first >= p.tokens) return;
     const bool here = col < p.head_dim;
-    float mine = 0.f;
+    Raw8<__nv_bfloat16> o[8], d[8];
 #pragma unroll
-    for (uint32_t k = 0; k < 16; k += 8) {
-        Raw8<__nv_bfloat16> o[8], d[8];
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const uint64_t at = min(first + 2 * (k + j) + lane / 16, p.tokens - 1);
-            o[j].load(p.o + at * p.o_ld + h * p.head_dim + (here ? col : 0));
-            d[j].load(p.d_o + at * p.do_ld + h * p.head_dim + (here ? col : 0));
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            float a[8], b[8], sum = 0.f;
-            o[j].get(a);
-            d[j].get(b);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sum = fmaf(a[c], b[c], sum);
-            sum = here ? sum : 0.f;
-#pragma unroll
-            for (int c = 8; c; c >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, c);
-            if (lane % 16 == k + j) mine = sum;
-        }
+    for (uint32_t j = 0; j < 8; ++j) {
+        const uint64_t at = min(first + kRows * j + row, p.tokens - 1);
+        o[j].load(p.o + at * p.o_ld + h * p.head_dim + (here ? col : 0));
+        d[j].load(p.d_o + at * p.do_ld + h * p.head_dim + (here ? col : 0));
     }
-    const uint64_t token = first + 2 * (lane % 16) + lane / 16;
-    if (token < p.tokens) p.delta[h * p.tokens + token] = mine;
+    float mine = 0.f;                  // of token kRows * (lane % LANES) + row, for the first eight of a row's lanes
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+        float a[8], b[8], sum = 0.f;
+        o[j].get(a);
+        d[j].get(b);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum = fmaf(a[c], b[c], sum);
+        sum = here ? sum : 0.f;
+#pragma unroll
+        for (uint32_t c = LANES / 2; c; c >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, c);
+        if (lane % LANES == j) mine = sum;
+    }
+    const uint64_t token = first + kRows * (lane % LANES) + row;
+    if (lane % LANES < 8 && token < p.tokens) p.delta[h * p.tokens + token] = mine;
 }
 
 // ---- dq -------------------------------------------------------------------------------------------------------
@@ -304,11 +312,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 if (lane == 0) mbar_arrive(bar(kDpRead));
 #pragma unroll
                 for (int j = 0; j < (int)kHalf; ++j) z[j] *= d[j] - delta;
-                if (t + 1 == n) {             // on the diagonal: columns up to `last`; a query that sees one key has a constant weight
-                    const int last = row == 0 ? -1 : (int)r - (int)(half * kHalf);
-#pragma unroll
-                    for (int j = 0; j < (int)kHalf; ++j) z[j] = j > last ? 0.f : z[j];
-                }
+                if (t + 1 == n) keep_columns(z, 0, row == 0 ? 0 : (int)r - (int)(half * kHalf) + 1);      // a query that sees one key has a constant weight
                 if ((t + 1) * kAttTile > it.len)              // keys past the sequence
                     clear_rows(smem + (2 + g % kRing3) * kTileBytes, chunks, it.len - t * kAttTile, threadIdx.x - 128, 256);
                 store_half(s_at, z);
@@ -566,7 +570,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             for (uint32_t j = 0; j < f.n; ++j, ++g) {
                 const uint32_t first = t * kAttTile + half * kHalf;       // query of this thread's first column
                 const bool edge = t == f.tile || (t + 1) * kAttTile > f.len;
-                const int low = (int)(f.tile * kAttTile + r) - (int)first, high = (int)f.len - (int)first;      // columns [low, high) are seen
+                const bool tail = (t + 1) * kAttTile > f.len;
                 const float4* lse = reinterpret_cast<const float4*>(&s_stat[g & 1][0][half * kHalf]);
                 const float4* delta = reinterpret_cast<const float4*>(&s_stat[g & 1][1][half * kHalf]);
                 if (!wait(kStatFull + (g & 1), g >> 1 & 1) || !wait(kSFull, g & 1)) break;
@@ -580,9 +584,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     z[4 * c + 2] = exp2_fast(fmaf(z[4 * c + 2], p.k2, l.z));
                     z[4 * c + 3] = exp2_fast(fmaf(z[4 * c + 3], p.k2, l.w));
                 }
-                if (edge) {                   // on the diagonal, or past the sequence
-#pragma unroll
-                    for (int c = 0; c < (int)kHalf; ++c) z[c] = c < low || c >= high ? 0.f : z[c];
+                if (edge) {                   // on the diagonal, or past the sequence: columns [low, high) are seen
+                    const int low = (int)(f.tile * kAttTile + r) - (int)first, high = (int)f.len - (int)first;
+                    keep_columns(z, low, high);
                 }
                 if ((t + 1) * kAttTile > f.len) {             // rows past the sequence, of q and of dout
                     if (!wait(kDoFull + g % kRing2, g / kRing2 & 1)) break;
@@ -602,11 +606,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     z[4 * c + 2] *= d[4 * c + 2] + l.z;
                     z[4 * c + 3] *= d[4 * c + 3] + l.w;
                 }
-                if (edge) {                   // 0 * what lies past the sequence; a query that sees one key has a constant weight
-                    const int from = first == 0 && low < 1 ? 1 : low;
-#pragma unroll
-                    for (int c = 0; c < (int)kHalf; ++c) z[c] = c < from || c >= high ? 0.f : z[c];
-                }
+                // 0 * what lies past the sequence; a query that sees one key has a constant weight
+                if (tail) keep_columns(z, 0, (int)f.len - (int)first);
+                if (first == 0) z[0] = 0.f;
                 store_half(d_at, z);
                 if (lane == 0) {
                     mbar_arrive(bar(kDsFull));
@@ -662,8 +664,11 @@ dte_status launch_attention_backward(const AttParams& params, const dte_matrix* 
     p.sectors = sectors(p.dq, p.dq_ld) && sectors(p.dk, p.dk_ld) && sectors(p.dv, p.dv_ld);
     auto grid = [&] { return (unsigned)(tiles * p.units < (uint64_t)sms ? tiles * p.units : sms); };
     const uint32_t heads = (uint32_t)(q->cols / p.head_dim);
-    const uint64_t warps = (p.tokens + 31) / 32 * heads, per_cta = kDeltaThreads / 32;
-    att_delta_kernel<<<(unsigned)((warps + per_cta - 1) / per_cta), kDeltaThreads, 0, st>>>(p, heads);
+    const bool narrow = p.head_dim <= 64;
+    const uint64_t tokens_per_warp = narrow ? 32 : 16, warps = (p.tokens + tokens_per_warp - 1) / tokens_per_warp * heads, per_cta = kDeltaThreads / 32;
+    const unsigned delta_grid = (unsigned)((warps + per_cta - 1) / per_cta);
+    if (narrow) att_delta_kernel<8><<<delta_grid, kDeltaThreads, 0, st>>>(p, heads);
+    else att_delta_kernel<16><<<delta_grid, kDeltaThreads, 0, st>>>(p, heads);
     DTE_CUDA(cudaGetLastError());
     p.units = (uint32_t)(k->cols / p.head_dim);
     DTE_CUDA(launch_after(att_dkv_kernel, dim3(grid()), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
