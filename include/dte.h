@@ -604,7 +604,8 @@ DTE_API dte_status dte_attention_forward(const dte_matrix* q, const dte_matrix* 
  *   dv = p^T dout,  dz = p (dout v^T - delta),  dq = scale * dz k,  dk = scale * dz^T q
  * dk and dv are sums over the query heads of a key head.  p and dz are rounded to BF16, the operand type of the products they enter, out
  * is taken as it was rounded, and sums are fp32; a query that sees one key has dz = 0.  The scores are made again, twice: once for dk and
- * dv, once for dq, so that every sum has one owner and a fixed order.  workspace: delta and two counters. */
+ * dv, once for dq, so that every sum has a fixed order.  Where a batch has few key tiles, the query heads of a key head are cut into parts,
+ * as the lengths alone say, whose sums of dk and dv are added up in the end.  workspace: delta, counters and these sums (74 MB at most). */
 DTE_API uint64_t dte_attention_backward_workspace_bytes(uint64_t tokens, uint64_t heads);
 DTE_API dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
                                           const dte_matrix* out, const float* lse, const dte_matrix* dout, const void* plan,

@@ -32,10 +32,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     __shared__ uint32_t s_at[2][kPlanLevels];        // tiles of a level, then where the next one of it goes
     __shared__ uint32_t s_warp[2][kPlanThreads / 32];
     __shared__ uint32_t s_bad;
+    __shared__ unsigned long long s_steps;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     PlanHead* head = reinterpret_cast<PlanHead*>(p.plan);
     for (uint32_t i = threadIdx.x; i < kPlanLevels; i += kPlanThreads) s_at[0][i] = s_at[1][i] = 0;
-    if (threadIdx.x == 0) s_bad = 0;
+    if (threadIdx.x == 0) {
+        s_bad = 0;
+        s_steps = 0;
+    }
     __syncthreads();
     bool bad = false;
     for (uint32_t i = threadIdx.x; i <= p.n; i += kPlanThreads) {
@@ -46,7 +50,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     __syncthreads();
     if (s_bad) {
         if (threadIdx.x == 0) {
-            *head = PlanHead{kPlanMagic, p.tokens, 0, 0, p.pairs_at};
+            *head = PlanHead{kPlanMagic, p.tokens, 0, 0, p.pairs_at, 0};
             if (p.flags) atomicOr((unsigned long long*)p.flags, (unsigned long long)DTE_DEV_BOUNDS);
         }
         return;
@@ -54,7 +58,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
     for (int round = 0; round < 2; ++round) {
         for (uint32_t i = warp; i < p.n; i += kPlanThreads / 32) {
             const uint32_t start = (uint32_t)load_id(p.starts, p.starts_dtype, i);
-            const uint32_t len = (uint32_t)load_id(p.starts, p.starts_dtype, i + 1) - start;
+            const uint32_t len = (uint32_t)load_id(p.starts, p.starts_dtype, i + 1) - start, tiles = (len + kAttTile - 1) / kAttTile;
+            if (round == 0 && lane == 0) atomicAdd(&s_steps, (unsigned long long)tiles * (tiles + 1) / 2);
             for (uint32_t which = 0; which < 2; ++which) {
                 const uint32_t rows = kAttTile << which;
                 PlanItem* list = reinterpret_cast<PlanItem*>(p.plan + (which ? p.pairs_at : kPlanHeader));
@@ -94,7 +99,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) 
                 before[which] += count;
             }
         }
-        if (threadIdx.x == 0) *head = PlanHead{kPlanMagic, p.tokens, all[0], all[1], p.pairs_at};
+        if (threadIdx.x == 0) *head = PlanHead{kPlanMagic, p.tokens, all[0], all[1], p.pairs_at, s_steps};
         __syncthreads();
     }
 }
@@ -553,9 +558,24 @@ extern "C" dte_status dte_attention_forward(const dte_matrix* q, const dte_matri
     return DTE_OK;
 }
 
+// Where everything lies in the backward pass's workspace: delta, the counters, and what cut groups need.
+struct BackwardLayout {
+    uint64_t next, parts_done, parts, total;
+};
+
+static BackwardLayout backward_layout(uint64_t tokens, uint64_t heads) {
+    BackwardLayout l;
+    const uint64_t most = tokens * heads < kMostParts ? tokens * heads : kMostParts;
+    l.next = align_up(tokens * heads * sizeof(float), kWorkspaceAlign);
+    l.parts_done = l.next + kWorkspaceAlign;
+    l.parts = l.parts_done + align_up(most * 8 * sizeof(uint32_t), kWorkspaceAlign);
+    l.total = l.parts + most * kPartFloats * sizeof(float);
+    return l;
+}
+
 extern "C" uint64_t dte_attention_backward_workspace_bytes(uint64_t tokens, uint64_t heads) {
     if (tokens > kMaxAttTokens || heads > 65535) return UINT64_MAX;
-    return align_up(tokens * heads * sizeof(float), kWorkspaceAlign) + kWorkspaceAlign;      // delta and the counter
+    return backward_layout(tokens, heads).total;
 }
 
 extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim,
@@ -593,6 +613,10 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     p.dv_ld = dv->ld;
     p.lse_in = lse;
     p.delta = static_cast<float*>(workspace);
-    p.next = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + align_up(q->rows * heads * sizeof(float), kWorkspaceAlign));
+    const BackwardLayout l = backward_layout(q->rows, heads);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.next = reinterpret_cast<uint32_t*>(ws + l.next);
+    p.parts_done = reinterpret_cast<uint32_t*>(ws + l.parts_done);
+    p.parts = reinterpret_cast<float*>(ws + l.parts);
     return launch_attention_backward(p, q, k, v, dout, tiles, device, sms, (cudaStream_t)cuda_stream);
 }

@@ -12,6 +12,9 @@ constexpr uint32_t kMaxAttDim = 128;
 constexpr uint64_t kPlanMagic = 0x6474652d61747431ull;
 constexpr uint64_t kMaxAttTokens = 1ull << 24, kMaxSequences = 1ull << 20;
 constexpr uint64_t kPlanHeader = 256;
+constexpr uint32_t kSms = 148;                   // for rules that choose an order of sums, which is the same on every device
+constexpr uint32_t kMostParts = 4 * kSms;        // pieces that the gradient's first pass may cut its work into
+constexpr uint32_t kPartFloats = 8 * 2 * 2 * 32 * 32;      // of a piece: score warps, dv and dk, groups of 32 columns, columns, rows
 constexpr double kLog2eD = 1.44269504088896340736;
 
 // One tile of one sequence.
@@ -25,6 +28,7 @@ struct PlanHead {
     uint64_t magic, tokens;
     uint32_t tiles, pairs;     // tiles of kAttTile rows, tiles of twice as many
     uint64_t pairs_at;         // where in the plan the second list starts; the first follows the header
+    uint64_t steps;            // pairs of a tile of queries and one of keys that it sees
 };
 static_assert(sizeof(PlanItem) == 16 && sizeof(PlanHead) <= kPlanHeader, "");
 
@@ -44,7 +48,10 @@ struct AttParams {
     __nv_bfloat16 *out, *dq, *dk, *dv;
     uint64_t out_ld, dq_ld, dk_ld, dv_ld;
     float *lse, *delta;
-    uint32_t* next;            // backwards: the next piece of work of the two passes
+    // backwards
+    uint32_t* next;            // the next piece of work of the two passes; then the exponent of how many parts the first one cuts a key head's group into
+    uint32_t* parts_done;      // per key tile and score warp, where groups are cut
+    float* parts;              // what a part's score warps leave
     const float* lse_in;
     uint64_t* flags;
     bool sectors;              // every 16 columns of the outputs are a whole sector of 32 bytes

@@ -1,12 +1,11 @@
 // Gradient of causal attention over packed sequences, in two passes over the scores that share nothing but delta, so that
-// every sum has one owner and its order is fixed (one pass would have to add dq up across CTAs):
+// the order of every sum is fixed (one pass would have to add dq up across CTAs):
 //   att_delta_kernel  delta = sum over a head's columns of dout * out
 //   att_dkv_kernel    a tile of 128 keys of one key head against the queries of its group that see them:  dk, dv
 //   att_dq_kernel     a tile of 128 queries of one head against its keys:  dq
 // With p = exp(z - lse), dz = p (dout v^T - delta): dq = scale dz k, dk = scale dz^T q, dv = p^T dout.  The first pass has four products
-// per pair of tiles, the second three, where one pass would have five.  Both draw their tiles, the
-// largest first, from a counter, and the second one starts on the SMs that the first one leaves: few, unequal key tiles leave
-// most SMs early.
+// per pair of tiles, the second three, where one pass would have five.  Both draw their tiles, the largest first, from a counter,
+// and the second one starts on the SMs that the first one leaves: few, unequal key tiles leave most SMs early.
 //
 // Both: one CTA per SM, a warp that loads, two that issue products, eight that turn scores into operands, each thread half a
 // row.  The first pass works on the transposed scores (rows are keys), so that p and dz are, as they come out of the
@@ -72,14 +71,43 @@ __device__ __forceinline__ void keep_columns(float (&z)[kHalf], int low, int hig
 // ---- delta ------------------------------------------------------------------------------------------------------
 constexpr uint32_t kDeltaThreads = 256;
 
-// A warp takes eight times LANES' share of 32 rows of a head: LANES lanes a row, 8 columns each.  Also sets the counters of the two
-// passes to zero.
+// Into how many parts, a power of two whose exponent is given, the first pass cuts the query heads of each key head, so that one key
+// tile's work need not run on alone.  One where the largest key tile takes no longer than 1.5 times what every SM has to do on average in
+// both passes, whose steps take about 3 to 2; else so many that it takes at most 1.25 times that, with at least 6 steps in the largest piece and
+// kMostParts pieces in all.  A part leaves its sums of dk and dv in the workspace, 128 KB that are written and read again,
+// and the last part of a tile to finish adds all of them up.  Whole backward pass, uncut and cut, from a cold L2, one sequence: 300 tokens,
+// 32 heads on 4: 72 and 47 us, 1024: 139 and 82, 2048: 260 and 182; 2048, 32 on 1: 932 and 188; 4096, 32 on 1 of 64: 1590 and 400.  Uncut
+// by this rule: 2048, 32 on 8, 156 us, cut 199.
+__device__ __forceinline__ uint32_t group_cut(const AttParams& p, uint32_t heads) {
+    if (p.group == 1 || !plan_ok(p)) return 0;
+    const PlanHead* h = reinterpret_cast<const PlanHead*>(p.plan);
+    const uint64_t kv_heads = heads / p.group, pieces = h->tiles * kv_heads;
+    if (pieces == 0) return 0;
+    // of the largest key tile: steps of a query head, and its time as a share of the average SM's
+    const uint64_t tiles = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)->tile + 1;
+    const float share = 3.f * kSms * (float)tiles / (5.f * (float)h->steps * (float)kv_heads);
+    uint32_t cut = 0;
+    while ((p.group >> cut) % 2 == 0 && pieces << (cut + 1) <= kMostParts && tiles * (p.group >> cut) >= 12 &&
+           share > (cut ? 1.25f * (1 << cut) : 1.5f))
+        ++cut;
+    return cut;
+}
+
+// A warp takes eight times LANES' share of 32 rows of a head: LANES lanes a row, 8 columns each.  The first CTA sets up the counters of the
+// two passes instead.
 template <uint32_t LANES>
 __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttParams p, uint32_t heads) {
     constexpr uint32_t kRows = 32 / LANES, kTokens = 8 * kRows;
     let_next_start();
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.next[0] = p.next[1] = 0;
-    const uint64_t unit = (uint64_t)blockIdx.x * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * kTokens;
+    if (blockIdx.x == 0) {
+        for (uint64_t i = threadIdx.x; i < min((uint64_t)kMostParts, p.tokens * heads) * 8 && p.group > 1; i += kDeltaThreads) p.parts_done[i] = 0;
+        if (threadIdx.x == 0) {
+            p.next[0] = p.next[1] = 0;
+            p.next[2] = group_cut(p, heads);
+        }
+        return;
+    }
+    const uint64_t unit = (uint64_t)(blockIdx.x - 1) * (kDeltaThreads / 32) + threadIdx.x / 32, first = unit / heads * kTokens;
     const uint32_t lane = threadIdx.x & 31, h = (uint32_t)(unit % heads), row = lane / LANES, col = lane % LANES * 8;
     if (first >= p.tokens) return;
     const bool here = col < p.head_dim;
@@ -362,18 +390,82 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 // A key tile's work: for each query head of the group, the query tiles from its own to the sequence's last.
 struct DkvWork {
     uint32_t start, len, kv_head, tile, tiles, n;     // tiles: of queries per head; n: in all
+    uint32_t head, heads;                             // the first query head, and how many
+    uint32_t piece;                                   // where the group is cut: which of all pieces
 };
 
-// it: an item of the list, which falls in the number of tiles in front: taken from the other end, in the number of tiles behind.
-__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, const PlanItem& it, uint32_t kv_head) {
+// it: an item of the list, which falls in the number of tiles in front: taken from the other end, in the number of tiles behind.  A
+// group cut into 1 << cut parts is that many pieces of work, one behind the other.  unit: which part of the tile's work, and, where groups
+// are cut, 65536 times which of all pieces.
+__device__ __forceinline__ DkvWork dkv_work(const AttParams& p, const PlanItem& it, uint32_t unit, uint32_t cut) {
     DkvWork f;
-    f.kv_head = kv_head;
+    f.piece = unit >> 16;
+    f.heads = p.group >> cut;
+    f.head = (unit & 0xFFFF) * f.heads;
+    f.kv_head = (unit & 0xFFFF) >> cut;
     f.start = it.start;
     f.len = it.len;
     f.tiles = it.tile + 1;
     f.tile = (it.len + kAttTile - 1) / kAttTile - f.tiles;
-    f.n = f.tiles * p.group;
+    f.n = f.tiles * f.heads;
     return f;
+}
+
+// The end of a piece whose group is cut, by one score warp for its 32 rows and its groups of 32 columns: leaves its sums in the workspace;
+// the last part's warp adds up those of all parts, in their order, whichever came last.
+__device__ __forceinline__ void add_parts(const AttParams& p, const DkvWork& f, uint32_t cut, uint32_t mine, __nv_bfloat16* dv, __nv_bfloat16* dk,
+                                          uint32_t half, bool valid) {
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32 - 4;
+    // four columns of all rows side by side
+    auto place = [&](uint32_t piece, uint32_t which, uint32_t c) {
+        return p.parts + (uint64_t)piece * kPartFloats + ((warp * 2 + which) * 2 + c / 64) * 1024 + lane * 4;
+    };
+    for (uint32_t which = 0; which < 2; ++which)
+        for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
+            uint32_t v[32];
+            tmem_load32(mine + (which ? 384 : 256) + c, v);
+            tmem_load_wait(v);
+            uint4* to = reinterpret_cast<uint4*>(place(f.piece, which, c));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[32 * i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+    __threadfence();
+    __syncwarp();
+    const uint32_t parts = 1u << cut, first = f.piece >> cut << cut;
+    const uint32_t before = __shfl_sync(0xFFFFFFFFu, lane == 0 ? atomicAdd(p.parts_done + (f.piece >> cut) * 8 + warp, 1u) : 0u, 0);
+    if (before + 1 != parts) return;
+    __threadfence();
+    for (uint32_t which = 0; which < 2; ++which)
+        for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
+            float sum[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum[i] = 0.f;
+#pragma unroll 2
+            for (uint32_t k = 0; k < parts; ++k) {
+                const float4* from = reinterpret_cast<const float4*>(place(first + k, which, c));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 x = __ldcg(from + 32 * i);
+                    sum[4 * i] += x.x;
+                    sum[4 * i + 1] += x.y;
+                    sum[4 * i + 2] += x.z;
+                    sum[4 * i + 3] += x.w;
+                }
+            }
+            if (valid) {
+                const float by = which ? p.scale : 1.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (c + 8 * i >= p.head_dim) break;
+                    float o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = sum[8 * i + k] * by;
+                    Raw8<__nv_bfloat16> x;
+                    x.set(o);
+                    x.store((which ? dk : dv) + c + 8 * i);
+                }
+            }
+        }
 }
 
 // Tensor memory: transposed S at column 0 (p over it), transposed dP at 128 (dz over it), dv at 256, dk at 384.  While dz is made
@@ -416,7 +508,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     volatile uint32_t* gave_up = &s_gave_up;
     wait_for_earlier();        // delta is there,
     let_next_start();          // for the second pass, too
-    const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
+    const uint32_t cut = p.next[2];
+    const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * (p.units << cut) : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
     // The next piece of work, by a whole warp; false at the end, or where the wait runs out.
@@ -426,7 +519,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kWorkEmpty + (n & 1)));
         ++n;
-        f = dkv_work(p, PlanItem{w.x, w.y, w.z, 0}, w.w);
+        f = dkv_work(p, PlanItem{w.x, w.y, w.z, 0}, w.w, cut);
         return w.z != kNone;
     };
 
@@ -445,7 +538,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     load_rows(k0, &map_k, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
                     load_rows(v0, &map_v, chunks, f.kv_head, f.start + f.tile * kAttTile, bar(kKvFull));
                     ++kv_issued;
-                    for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
+                    for (uint32_t h = f.head; h < f.head + f.heads && ok; ++h)
                         for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t) {
                             if (!(ok = mbar_wait(bar(kQEmpty + qa.i), qa.phase ^ 1, p.wait_limit, gave_up))) break;
                             mbar_expect_tx(bar(kQFull + qa.i), tile_bytes);
@@ -530,8 +623,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             auto draw = [&]() {
                 const uint32_t w = __shfl_sync(0xFFFFFFFFu, lane == 0 ? atomicAdd(p.next, 1u) : 0u, 0);
                 if (w >= total) return make_uint4(0, 0, kNone, 0);
-                const PlanItem it = list[w / p.units];
-                return make_uint4(it.start, it.len, it.tile, w % p.units);
+                const PlanItem it = list[w / (p.units << cut)];
+                return make_uint4(it.start, it.len, it.tile, w % (p.units << cut) | (cut ? w << 16 : 0));
             };
             auto publish = [&](const uint4& w) {
                 if (!(ok = warp_wait(bar(kWorkEmpty + (works & 1)), (works >> 1 & 1) ^ 1, p.wait_limit, gave_up))) return;
@@ -547,9 +640,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                 const uint4 next = draw();
                 publish(next);
                 if (!ok) break;
-                const DkvWork f = dkv_work(p, PlanItem{now.x, now.y, now.z, 0}, now.w);
+                const DkvWork f = dkv_work(p, PlanItem{now.x, now.y, now.z, 0}, now.w, cut);
                 now = next;
-                for (uint32_t h = f.kv_head * p.group; h < (f.kv_head + 1) * p.group && ok; ++h)
+                for (uint32_t h = f.head; h < f.head + f.heads && ok; ++h)
                     for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
                         const uint32_t row = t * kAttTile + lane * 4;
                         const uint64_t at = h * p.tokens + f.start + row;
@@ -631,9 +724,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             if (!ok || !wait(kAccFull, done++ & 1)) break;
             const uint32_t row = f.tile * kAttTile + r;
             const uint64_t at = (uint64_t)f.start + row;
-            for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
-                store_columns(p.dv + at * p.dv_ld + f.kv_head * p.head_dim, mine + 256, c, p.head_dim, 1.f, row < f.len, p.sectors);
-                store_columns(p.dk + at * p.dk_ld + f.kv_head * p.head_dim, mine + 384, c, p.head_dim, p.scale, row < f.len, p.sectors);
+            __nv_bfloat16 *dv = p.dv + at * p.dv_ld + f.kv_head * p.head_dim, *dk = p.dk + at * p.dk_ld + f.kv_head * p.head_dim;
+            if (cut == 0) {
+                for (uint32_t c = half * 32; c < p.head_dim; c += 64) {
+                    store_columns(dv, mine + 256, c, p.head_dim, 1.f, row < f.len, p.sectors);
+                    store_columns(dk, mine + 384, c, p.head_dim, p.scale, row < f.len, p.sectors);
+                }
+            } else {
+                add_parts(p, f, cut, mine, dv, dk, half, row < f.len);
             }
             tc_fence_before();
         }
@@ -674,18 +772,18 @@ dte_status launch_attention_backward(const AttParams& params, const dte_matrix* 
     AttParams p = params;
     auto sectors = [&](const __nv_bfloat16* x, uint64_t ld) { return !(((uintptr_t)x | ld * 2 | p.head_dim * 2u) & 31u); };
     p.sectors = sectors(p.dq, p.dq_ld) && sectors(p.dk, p.dk_ld) && sectors(p.dv, p.dv_ld);
-    auto grid = [&] { return (unsigned)(tiles * p.units < (uint64_t)sms ? tiles * p.units : sms); };
     const uint32_t heads = (uint32_t)(q->cols / p.head_dim);
     const bool narrow = p.head_dim <= 64;
     const uint64_t tokens_per_warp = narrow ? 32 : 16, warps = (p.tokens + tokens_per_warp - 1) / tokens_per_warp * heads, per_cta = kDeltaThreads / 32;
-    const unsigned delta_grid = (unsigned)((warps + per_cta - 1) / per_cta);
+    const unsigned delta_grid = (unsigned)(1 + (warps + per_cta - 1) / per_cta);
+    const unsigned grid = (unsigned)(tiles * heads < (uint64_t)sms ? tiles * heads : sms);      // of the first pass, too, whose groups may be cut
     if (narrow) att_delta_kernel<8><<<delta_grid, kDeltaThreads, 0, st>>>(p, heads);
     else att_delta_kernel<16><<<delta_grid, kDeltaThreads, 0, st>>>(p, heads);
     DTE_CUDA(cudaGetLastError());
     p.units = (uint32_t)(k->cols / p.head_dim);
-    DTE_CUDA(launch_after(att_dkv_kernel, dim3(grid()), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
+    DTE_CUDA(launch_after(att_dkv_kernel, dim3(grid), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
     p.units = heads;
-    DTE_CUDA(launch_after(att_dq_kernel, dim3(grid()), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
+    DTE_CUDA(launch_after(att_dq_kernel, dim3(grid), kBwdThreads, kBwdSmem, st, mq, mk, mv, md, p));
     return DTE_OK;
 }
 

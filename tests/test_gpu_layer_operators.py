@@ -267,6 +267,49 @@ def test_attention_heads_and_widths(dim, hq, hk, fused):
     b.check_backward()
 
 
+# Few key tiles of many query heads: the heads of a key head are cut into parts, whose sums are added up.
+@pytest.mark.parametrize("lengths,hq,hk,dim", [([300], 8, 1, 128), ([129], 64, 1, 72), ([700, 20], 24, 2, 64), ([512], 32, 4, 40), ([1025, 0, 3, 1], 16, 1, 104),
+                                               ([900], 12, 1, 128), ([128, 128], 32, 1, 96), ([2050], 32, 1, 128)])
+def test_attention_of_few_sequences_and_many_heads(lengths, hq, hk, dim):
+    b = Batch(lengths, hq, hk, dim, front=1, behind=130, fused=True)
+    b.forward()
+    b.backward()
+    b.check_backward()
+    first = [t.clone() for t in b.grads]
+    ws = workspace(dte.dte_attention_backward_workspace_bytes(b.tokens, b.hq))
+    for _ in range(3):                                     # whichever part comes last, with what an earlier call left
+        b.backward(None, ws)
+        for t, w in zip(b.grads, first):
+            assert same_bits(t, w)
+
+
+def test_attention_replayed_where_heads_are_cut_and_where_not():
+    long, short = Batch([640, 0, 0, 0], 16, 1, 64), Batch([160] * 4, 16, 1, 64, seed=50)
+    work = Batch([640, 0, 0, 0], 16, 1, 64, seed=70)
+    ws = workspace(dte.dte_attention_backward_workspace_bytes(640, 16))
+
+    def step():
+        dte.dte_attention_plan(work.starts, 640, work.plan)
+        work.forward()
+        work.backward(None, ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for other in (long, short, long):
+        work.starts.copy_(other.starts)
+        for name in ("q", "k", "v", "dout"):
+            getattr(work, name).copy_(getattr(other, name))
+        graph.replay()
+        other.forward()
+        other.backward()
+        for t, w in zip(work.grads, other.grads):
+            assert same_bits(t, w)
+        other.check_backward()
+
+
 @pytest.mark.parametrize("std,scale", [(6.0, None), (1.0, 3.0), (0.05, None), (1.0, 1e-3), (3.0, 0.7)])
 def test_attention_of_peaked_and_flat_scores(std, scale):
     b = Batch([300, 140], 4, 2, 128, std=std, scale=scale)
