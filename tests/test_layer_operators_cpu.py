@@ -115,7 +115,7 @@ def forward(q=matrix(300, 512), k=matrix(300, 128), v=matrix(300, 128), dim=64, 
 
 
 def backward(out=matrix(300, 512), lse=4096, dout=matrix(300, 512), dq=matrix(300, 512), dk=matrix(300, 128), dv=matrix(300, 128), ws=4096,
-             size=1 << 20, device=-1):
+             size=1 << 27, device=-1):
     return dte.lib().dte_attention_backward(matrix(300, 512), matrix(300, 128), matrix(300, 128), 64, out, lse, dout, 4096, 1 << 20, 0.125,
                                             dq, dk, dv, ws, size, None, device, None)
 
@@ -176,6 +176,9 @@ def test_attention_plan_refuses_and_its_size():
     assert dte.dte_attention_plan_bytes(2 ** 24 + 1, 1) == dte.dte_attention_plan_bytes(1, 2 ** 20 + 1) == UNFIT
     assert dte.dte_attention_backward_workspace_bytes(2 ** 24 + 1, 1) == dte.dte_attention_backward_workspace_bytes(1, 65536) == UNFIT
     assert dte.dte_attention_backward_workspace_bytes(300, 8) >= 300 * 8 * 4
+    # beside delta never more than the sums of all parts
+    assert dte.dte_attention_backward_workspace_bytes(2 ** 24, 64) <= 2 ** 24 * 64 * 4 + (75 << 20)
+    assert backward(size=dte.dte_attention_backward_workspace_bytes(300, 8) - 1) == 3
 
 
 def test_gradient_norm_and_clipping_refuse():
