@@ -16,8 +16,8 @@
 // to bf16 is 1.7e-3.  dz as two bf16 numbers makes the first two 2.2e-3 and 1.9e-3 and the passes 16 % slower, so it is not kept so.
 //
 // Measured, heads of 128, all three kernels: 16384 tokens, 32 heads on 8: 6.7 ms in a loop at the power limit (0.82 PFLOP/s of the five
-// products that the formulas need, 1.15 of the seven that are made); 8192 tokens in 19 sequences, 32 heads on 4: 300 us; 4001 tokens in 57
-// sequences, 16 heads of 64: 72 us.  A step takes 3300 cycles in the first pass, 2048 of them the tensor cores', and 2200 in the second,
+// products that the formulas need, 1.15 of the seven that are made); 8192 tokens in 19 sequences, 32 heads on 4: 296 us; 4001 tokens in 57
+// sequences, 16 heads of 64: 70 us.  A step takes 3300 cycles in the first pass, 2048 of them the tensor cores', and 2200 in the second,
 // 1536: the chain of p (1500 and 1250 cycles, 1024 of which the special function unit needs) and of the products that wait for it sets the
 // pace.  A piece of work costs 4000 to 7000 cycles beside its steps.  Tried and left: sixteen score warps (dk / dv 3.6 to 3.8 ms), p in
 // shared memory so that the next S need not wait for dv (7.2 ms against 6.7: operands of products in shared memory cost its bandwidth), p in
@@ -72,24 +72,22 @@ __device__ __forceinline__ void keep_columns(float (&z)[kHalf], int low, int hig
 constexpr uint32_t kDeltaThreads = 256;
 
 // Into how many parts, a power of two whose exponent is given, the first pass cuts the query heads of each key head, so that one key
-// tile's work need not run on alone.  One where the largest key tile takes no longer than 1.5 times what every SM has to do on average in
-// both passes, whose steps take about 3 to 2; else so many that it takes at most 1.25 times that, with at least 6 steps in the largest piece and
-// kMostParts pieces in all.  A part leaves its sums of dk and dv in the workspace, 128 KB that are written and read again,
-// and the last part of a tile to finish adds all of them up.  Whole backward pass, uncut and cut, from a cold L2, one sequence: 300 tokens,
-// 32 heads on 4: 72 and 47 us, 1024: 139 and 82, 2048: 260 and 182; 2048, 32 on 1: 932 and 188; 4096, 32 on 1 of 64: 1590 and 400.  Uncut
-// by this rule: 2048, 32 on 8, 156 us, cut 199.
+// tile's work need not run on alone.  A part leaves its sums of dk and dv in the workspace, 128 KB that are written and read again, and
+// the last part of a tile to finish adds all of them up.  So groups are halved while that saves more than it costs, in steps of the first pass: the
+// longest piece becomes half as long, which is of use down to what every SM has to do on average (in both passes, whose steps take about 3 to 2),
+// and every piece on an SM costs about ten steps, and the waiting for the last part two.  Whole backward pass, uncut and cut, from a cold L2, one
+// sequence: 300 tokens, 32 heads on 4: 73 and 44 us, 1024: 140 and 67, 2048: 265 and 157, 4096: 515 and 422; 2048, 32 on 1: 960 and 165; 4096,
+// 32 on 1 of 64: 1590 and 370.  Uncut by this rule: 2048, 32 on 8, 150 us, cut 157.
 __device__ __forceinline__ uint32_t group_cut(const AttParams& p, uint32_t heads) {
     if (p.group == 1 || !plan_ok(p)) return 0;
     const PlanHead* h = reinterpret_cast<const PlanHead*>(p.plan);
     const uint64_t kv_heads = heads / p.group, pieces = h->tiles * kv_heads;
     if (pieces == 0) return 0;
-    // of the largest key tile: steps of a query head, and its time as a share of the average SM's
-    const uint64_t tiles = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)->tile + 1;
-    const float share = 3.f * kSms * (float)tiles / (5.f * (float)h->steps * (float)kv_heads);
+    float longest = (float)((reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader)->tile + 1) * p.group);
+    const float average = 5.f / 3.f * (float)h->steps * (float)heads / kSms;
     uint32_t cut = 0;
-    while ((p.group >> cut) % 2 == 0 && pieces << (cut + 1) <= kMostParts && tiles * (p.group >> cut) >= 12 &&
-           share > (cut ? 1.25f * (1 << cut) : 1.5f))
-        ++cut;
+    for (; (p.group >> cut) % 2 == 0 && pieces << (cut + 1) <= kMostParts; ++cut, longest /= 2)
+        if (longest - fmaxf(longest / 2, average) <= 2.f + 10.f * (float)(pieces << (cut + 1)) / kSms) break;
     return cut;
 }
 
@@ -297,16 +295,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             if (lane == 0) s_taken[1] = g;
         } else if (lane == 0) {
             // ---- work: tiles of queries in falling order of their keys, from the counter that all CTAs share ----
-            uint32_t w = atomicAdd(p.next + 1, 1u);
             for (uint32_t n = 0;; ++n) {
+                if (!mbar_wait(bar(kWorkEmpty + (n & 1)), (n >> 1 & 1) ^ 1, p.wait_limit, gave_up)) break;
+                const uint32_t w = atomicAdd(p.next + 1, 1u);
                 const bool more = w < total;
                 uint4 v = make_uint4(0, 0, kNone, 0);
                 if (more) {
                     const PlanItem it = list[w / p.units];
                     v = make_uint4(it.start, it.len, it.tile, w % p.units);
-                    w = atomicAdd(p.next + 1, 1u);
                 }
-                if (!mbar_wait(bar(kWorkEmpty + (n & 1)), (n >> 1 & 1) ^ 1, p.wait_limit, gave_up)) break;
                 s_work[n & 1] = v;
                 mbar_arrive(bar(kWorkFull + (n & 1)));
                 if (!more) break;
@@ -637,16 +634,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             uint4 now = draw();
             publish(now);
             while (ok && now.z != kNone) {
-                const uint4 next = draw();
-                publish(next);
-                if (!ok) break;
                 const DkvWork f = dkv_work(p, PlanItem{now.x, now.y, now.z, 0}, now.w, cut);
-                now = next;
+                uint32_t left = f.n;
                 for (uint32_t h = f.head; h < f.head + f.heads && ok; ++h)
                     for (uint32_t t = f.tile; t < f.tile + f.tiles; ++t, ++g) {
                         const uint32_t row = t * kAttTile + lane * 4;
                         const uint64_t at = h * p.tokens + f.start + row;
                         float l[4], d[4];
+                        // The next piece is drawn when this one's last loads are about to be issued: drawn earlier, a large piece would keep
+                        // a second one waiting behind it while other CTAs have none.
+                        if (left == min(f.n, 3u)) {
+                            publish(now = draw());
+                            if (!ok) break;
+                        }
+                        --left;
 #pragma unroll
                         for (uint32_t j = 0; j < 4; ++j) {
                             l[j] = row + j < f.len ? p.lse_in[at + j] * -(float)kLog2eD : 0.f;
