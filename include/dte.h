@@ -636,7 +636,8 @@ DTE_API dte_status dte_grad_sum_squares(const dte_tensor* tensors, uint64_t n_te
 /* norm = sqrt(*sum_squares), to *norm (DEVICE, fp32, may be NULL); every element times max_norm / norm where norm > max_norm, unchanged
  * otherwise and where the norm is not finite (a step to be skipped: the caller sees it in *norm).  outs: HOST array, n_tensors
  * entries with the tensors' sizes and types of their own, or NULL for in place; an entry may be its tensor itself
- * (same data and dtype), else it overlaps no tensor.  In place with nothing to clip, nothing is read or written.  max_norm > 0. */
+ * (same data and dtype), else it overlaps no tensor.  What is written, in place too, overlaps no other entry: a tensor that appears twice
+ * in place is a race.  In place with nothing to clip, nothing is read or written.  max_norm > 0. */
 DTE_API dte_status dte_grad_clip(const dte_tensor* tensors, uint64_t n_tensors, const double* sum_squares, double max_norm,
                                  const dte_tensor* outs, float* norm, int device, void* cuda_stream);
 
