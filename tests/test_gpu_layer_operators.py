@@ -674,6 +674,44 @@ def test_a_wait_that_runs_out_sets_the_flag_and_leaves_the_device_usable():
         b.check_backward()
 
 
+def test_a_gradient_of_cut_heads_that_gave_up_leaves_nothing_for_the_next_one():
+    b = Batch([640], 16, 1, 64)
+    ws = workspace(dte.dte_attention_backward_workspace_bytes(b.tokens, 16))
+    b.forward()
+    b.backward(None, ws)
+    want = [g.clone() for g in b.grads]
+    dte.lib().dte_attention_set_wait_limit(1)
+    try:
+        flags = torch.zeros(1, dtype=torch.int64, device=DEV)
+        dte.dte_attention_backward(b.q, b.k, b.v, b.out, b.lse, b.dout, b.plan, *(torch.empty_like(g) for g in b.grads), ws, flags=flags)
+        torch.cuda.synchronize()
+    finally:
+        dte.lib().dte_attention_set_wait_limit(0)
+    assert flags.tolist() == [dte.DTE_DEV_TIMEOUT]
+    b.backward(None, ws)
+    for g, w in zip(b.grads, want):
+        assert same_bits(g, w)
+
+
+def test_gradients_of_cut_heads_on_two_streams():
+    batches = [Batch([900, 30], 32, 1, 128, seed=s) for s in (1, 60)]
+    spaces = [workspace(dte.dte_attention_backward_workspace_bytes(930, 32)) for _ in batches]
+    want = []
+    for b, ws in zip(batches, spaces):
+        b.forward()
+        b.backward(None, ws)
+        want.append([g.clone() for g in b.grads])
+    streams = [torch.cuda.Stream() for _ in batches]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for b, s, ws in zip(batches, streams, spaces):
+            b.backward(s, ws)
+    torch.cuda.synchronize()
+    for b, w in zip(batches, want):
+        for g, x in zip(b.grads, w):
+            assert same_bits(g, x)
+
+
 def test_attention_on_two_streams_with_one_plan():
     a, b = Batch([500, 300], 4, 2, 128), Batch([500, 300], 4, 2, 128, seed=40)
     b.plan = a.plan
