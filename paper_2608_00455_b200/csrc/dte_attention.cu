@@ -15,6 +15,8 @@ namespace dte {
 
 constexpr uint32_t kPlanThreads = 1024;
 constexpr uint32_t kPlanLevels = 4096;
+// the gradient's groups are cut by the longest tile, the list's first: its place is certain wherever so few tiles are cut
+static_assert(kPlanLevels > kMostParts, "");
 
 struct PlanParams {
     const void* starts;
