@@ -157,6 +157,9 @@ def receiver_loss(b, shards, vocab, hidden, ids, targets):
 
 
 def run(steps=40, vocab=8192, hidden=512, tokens=4096, lr=2e-2, seed=0, say=print, heads=0, clip=0.0):
+    # two query heads to a key head, and each of the two receivers holds key heads of its own
+    if heads < 0 or heads % 4:
+        raise ValueError("heads must be a multiple of 4 (0: no attention)")
     gen = torch.Generator("cuda").manual_seed(seed)
     successors = torch.randint(0, vocab, (vocab, 4), generator=gen, device="cuda")
     hp = dict(lr=lr, wd=0.01, eps=1e-8)
@@ -226,7 +229,8 @@ def run(steps=40, vocab=8192, hidden=512, tokens=4096, lr=2e-2, seed=0, say=prin
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    for name, default in (("steps", 40), ("vocab", 8192), ("hidden", 512), ("tokens", 4096), ("heads", 0)):
+    for name, default in (("steps", 40), ("vocab", 8192), ("hidden", 512), ("tokens", 4096)):
         ap.add_argument(f"--{name}", type=int, default=default)
+    ap.add_argument("--heads", type=int, default=0, help="query heads of the attention layer, a multiple of 4 (0: no attention)")
     ap.add_argument("--clip", type=float, default=0.0)
     run(**vars(ap.parse_args()))
