@@ -341,14 +341,18 @@ class Layout:
                 _ptr_table(v, torch.float32, self.device))
 
     def shard_table(self, shards):
-        tabs = []
-        for s in shards:
-            assert s is None or s.dtype in (torch.bfloat16, torch.int16)
-            tabs.append(s)
+        """Pointers of the plan's shards, one tensor (or None: held elsewhere) per shard.  The kernels write wherever the plan's
+        sizes allow, so a table that is shorter than the plan, or a tensor that is smaller than its shard, is refused."""
+        tabs = list(shards)
+        if len(tabs) < len(self.shard_numels):
+            raise ValueError(f"{len(tabs)} tensors for a plan of {len(self.shard_numels)} shards")
         arr = (C.c_void_p * max(1, len(tabs)))()
         for i, t in enumerate(tabs):
-            arr[i] = None if t is None else t.data_ptr()
+            assert t is None or t.dtype in (torch.bfloat16, torch.int16)
             assert t is None or (t.is_contiguous() and t.device == self.device)
+            if t is not None and i < len(self.shard_numels) and t.numel() < self.shard_numels[i]:
+                raise ValueError(f"shard {i} has {self.shard_numels[i]} elements, its tensor {t.numel()}")
+            arr[i] = None if t is None else t.data_ptr()
         return arr
 
 

@@ -1,4 +1,4 @@
-"""The example's arguments, and the buffers that updates are scattered into: refused before anything runs on a GPU."""
+"""The example's arguments: refused before anything runs on a GPU."""
 import os
 import sys
 
