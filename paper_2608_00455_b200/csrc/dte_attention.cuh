@@ -49,7 +49,8 @@ struct AttParams {
     uint64_t out_ld, dq_ld, dk_ld, dv_ld;
     float *lse, *delta;
     // backwards
-    uint32_t* next;            // the next piece of work of the two passes; then the exponent of how many parts the first one cuts a key head's group into
+    uint32_t* next;            // the next piece of work of the two passes; then the exponent of how many parts the first one cuts a key head's group into;
+                               // then the counter that hands memory on to the second one
     uint32_t* parts_done;      // per key tile and score warp, where groups are cut
     float* parts;              // what a part's score warps leave
     const float* lse_in;

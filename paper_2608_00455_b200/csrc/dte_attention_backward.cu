@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttParam
     if (blockIdx.x == 0) {
         for (uint64_t i = threadIdx.x; i < min((uint64_t)kMostParts, p.tokens * heads) * 8 && p.group > 1; i += kDeltaThreads) p.parts_done[i] = 0;
         if (threadIdx.x == 0) {
-            p.next[0] = p.next[1] = 0;
+            p.next[0] = p.next[1] = p.next[3] = 0;
             p.next[2] = group_cut(p, heads);
         }
         return;
@@ -143,6 +143,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
            kWorkFull, kWorkEmpty = kWorkFull + 2, kLast = kWorkEmpty + 2, kBars };
     __shared__ __align__(8) uint64_t s_bar[kBars];
     __shared__ uint32_t s_tmem, s_gave_up, s_issued[3], s_taken[3];         // loads of K, V, and Q with dout
+    __shared__ bool s_seen;
     __shared__ uint4 s_work[2];            // start, length, tile and head of the next pieces of work; no tile: the end
     const uint32_t q0 = smem_addr(smem), do0 = q0 + kTileBytes, kt0 = q0 + 2 * kTileBytes, vt0 = kt0 + kRing3 * kTileBytes;
     auto bar = [bar0 = smem_addr(s_bar)](uint32_t i) { return bar0 + 8 * i; };
@@ -163,12 +164,17 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<1>(smem_addr(&s_tmem), 512);
+    // The first pass runs on; delta, the counters and the inputs are there, as it has seen.
+    if (threadIdx.x == 96) s_seen = seen_earlier(p.next + 3, p.wait_limit);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("fence.proxy.async;" ::: "memory");          // for the loads of tiles, too
     const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);
     volatile uint32_t* gave_up = &s_gave_up;
-    const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
+    const bool seen = s_seen;
+    if (!seen) *gave_up = 1;
+    const uint32_t total = seen && plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * p.units : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);
     const uint32_t chunks = (p.head_dim + 63) / 64, tile_bytes = chunks * kChunkBytes;
     // The next piece of work, by a whole warp; false at the end, or where the wait runs out.
@@ -503,8 +509,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     tc_fence_after();
     const uint32_t tmem = uniform(*(volatile uint32_t*)&s_tmem);
     volatile uint32_t* gave_up = &s_gave_up;
-    wait_for_earlier();        // delta is there,
-    let_next_start();          // for the second pass, too
+    wait_for_earlier();        // for delta
+    if (threadIdx.x == 0) {    // the second pass needs no more than this one has now
+        pass_on(p.next + 3);
+        let_next_start();
+    }
     const uint32_t cut = p.next[2];
     const uint32_t total = plan_ok(p) ? reinterpret_cast<const PlanHead*>(p.plan)->tiles * (p.units << cut) : 0;
     const PlanItem* list = reinterpret_cast<const PlanItem*>(p.plan + kPlanHeader);

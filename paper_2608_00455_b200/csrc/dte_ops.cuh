@@ -144,10 +144,21 @@ dte_status launch_sorted_sum(const SortedSum& p, int vec, void* workspace, bool 
 // ---- dependent launches ------------------------------------------------------------------------------
 // A kernel launched with launch_after may start while the one before it in the stream still runs (its launch
 // costs nothing then); it calls wait_for_earlier before it touches memory, which returns when all earlier
-// work is complete and visible.  Used only inside a call, between its own kernels.
+// work is complete and visible.  Used only inside a call, between its own kernels.  A kernel that works beside the one in front of
+// it instead, on what came before that, calls seen_earlier first and wait_for_earlier before it ends; the one in front calls
+// pass_on between its own wait and let_next_start.
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Lets the kernel behind this one start now, as far as there is room.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Being started says nothing about memory, so what the kernel in front has seen by its own wait is handed on through a counter,
+// which still earlier work has set to zero: released by one there, acquired by the other here.  Both sides update the counter, so that
+// none of them can find a value of an earlier call.
+__device__ __forceinline__ void pass_on(uint32_t* counter) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory"); }
+__device__ __forceinline__ bool seen_earlier(uint32_t* counter, uint32_t limit) {
+    uint32_t passed = 0;
+    for (uint32_t i = 0; i < limit && !passed; ++i) asm volatile("atom.acquire.gpu.global.add.u32 %0, [%1], 0;" : "=r"(passed) : "l"(counter) : "memory");
+    return passed != 0;
+}
 
 template <typename... KernelArgs, typename... Args>
 inline cudaError_t launch_after(void (*kernel)(KernelArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
