@@ -581,7 +581,8 @@ DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t h
 /* Causal attention over packed sequences.  Rows starts[s] .. starts[s + 1] - 1 are sequence s; a query sees the keys of
  * its sequence up to its own row:
  *   z = scale * q . k^T over those keys,  lse = log sum exp z,  out = sum exp(z - lse) v
- * Query head h reads key head h / (query heads / key heads).  All matrices BF16; head_dim a multiple of 8 up to 128;
+ * Query head h reads key head h / (query heads / key heads).  All matrices BF16; head_dim a multiple of 8 up to 128; scale > 0, a
+ * normal number in fp32 and, times log2(e), finite there;
  * data 16-byte aligned, ld >= cols and a multiple of 8 (rows go through the tensor memory accelerator).  lse: fp32,
  * heads x tokens.  Rows that belong to no sequence (in front of starts[0], behind the last one) are left as they
  * were in every output, and what they hold in the inputs, NaN included, reaches no result; nor does what one sequence

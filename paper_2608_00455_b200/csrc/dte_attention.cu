@@ -454,8 +454,9 @@ static dte_status check_attention(const dte_matrix* q, const dte_matrix* k, cons
     if (q->cols / head_dim > 65535) return op_fail(DTE_ERR_INVALID_ARG, "at most 65535 heads");
     if (tiles_most(plan_bytes, q->rows) * (q->cols / head_dim) >= (1ull << 31) || (q->rows / kAttTile + 1) * (q->cols / head_dim) >= (1ull << 31))
         return op_fail(DTE_ERR_INVALID_ARG, "tiles x heads are too many for one call");
-    if (!(scale > 0) || !std::isfinite((float)(scale * kLog2eD)))
-        return op_fail(DTE_ERR_INVALID_ARG, "scale must be > 0 and, times log2(e), finite in fp32");
+    // a scale that fp32 holds as zero would make NaN of hidden scores (0 * infinity), a subnormal one has lost bits
+    if (!(scale > 0) || !std::isnormal((float)scale) || !std::isfinite((float)(scale * kLog2eD)))
+        return op_fail(DTE_ERR_INVALID_ARG, "scale must be > 0, a normal number in fp32 and, times log2(e), finite there");
     if ((uintptr_t)flags & 7u) return op_fail(DTE_ERR_INVALID_ARG, "flags must be 8-byte aligned");
     if (!plan || ((uintptr_t)plan & (kWorkspaceAlign - 1)) || plan_bytes < kPlanHeader)
         return op_fail(DTE_ERR_INVALID_ARG, "plan is null, not 256-byte aligned or too small");
