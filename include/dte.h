@@ -635,7 +635,7 @@ DTE_API dte_status dte_grad_sum_squares(const dte_tensor* tensors, uint64_t n_te
                                         void* workspace, uint64_t workspace_bytes, int device, void* cuda_stream);
 
 /* norm = sqrt(*sum_squares), to *norm (DEVICE, fp32, may be NULL); every element times max_norm / norm where norm > max_norm, unchanged
- * otherwise and where the norm is not finite (a step to be skipped: the caller sees it in *norm).  outs: HOST array, n_tensors
+ * otherwise and where the norm is not finite in fp32 (a step to be skipped: the caller sees it in *norm).  outs: HOST array, n_tensors
  * entries with the tensors' sizes and types of their own, or NULL for in place; an entry may be its tensor itself
  * (same data and dtype), else it overlaps no tensor.  What is written, in place too, overlaps no other entry: a tensor that appears twice
  * in place is a race.  In place with nothing to clip, nothing is read or written.  max_norm > 0. */

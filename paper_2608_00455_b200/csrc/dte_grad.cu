@@ -174,9 +174,10 @@ template <uint32_t N>
 __global__ void __launch_bounds__(kGradThreads) clip_kernel(const __grid_constant__ ClipParams<N> p) {
     const GradList<N>& l = p.list;
     const double norm = sqrt(*p.sum_squares);
-    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
-    // a norm that is not finite leaves everything as it is
-    const float factor = norm > p.max_norm && norm <= 0x1.fffffffffffffp1023 ? (float)(p.max_norm / norm) : 1.f;
+    const float shown = (float)norm;
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = shown;
+    // a norm that is not finite, as the caller sees it, leaves everything as it is
+    const float factor = norm > p.max_norm && shown <= 0x1.fffffep127f ? (float)(p.max_norm / norm) : 1.f;
     for (uint32_t c = blockIdx.x; c < l.first[l.n]; c += gridDim.x) {
         const uint32_t t = tensor_of(l, c);
         const bool in16 = l.numel[t] & kInBf16, out16 = l.numel[t] & kOutBf16;

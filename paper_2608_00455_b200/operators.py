@@ -422,7 +422,7 @@ def dte_grad_sum_squares(tensors: Sequence[torch.Tensor], sum_squares: torch.Ten
 
 def dte_grad_clip(tensors: Sequence[torch.Tensor], sum_squares: torch.Tensor, max_norm: float, norm: Optional[torch.Tensor] = None,
                   outs: Optional[Sequence[torch.Tensor]] = None, stream=None) -> None:
-    """Every element times max_norm / norm where norm = sqrt(sum_squares) is finite and larger; into outs, or in place."""
+    """Every element times max_norm / norm where norm = sqrt(sum_squares) is larger, and finite in float32; into outs, or in place."""
     device = _device(sum_squares, "sum_squares")
     if outs is not None and len(outs) != len(tensors):
         _refuse("outs must have one tensor per tensor")
