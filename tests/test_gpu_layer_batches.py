@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2608_00455_b200 as dte
-from test_gpu_layer_operators import BF16, DEV, F32, Batch, norm_of, normal, same_bits, squares, workspace
+from test_gpu_layer_operators import BF16, DEV, E, F32, F64, U, Batch, assert_within, norm_of, normal, same_bits, squares, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,21 @@ def test_a_norm_beyond_fp32_is_shown_as_infinite_and_leaves_the_gradients(dtype,
     assert math.isfinite(total) and norm == math.inf
     for t, o, b in zip(g, g if outs is None else outs, before):
         assert same_bits(t, b) and same_bits(o, b.to(o.dtype))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("into", [None, F32, BF16])
+@pytest.mark.parametrize("ratio", [0.7, 2.0 ** -125, 1e-38, 2.0 ** -126, 1e-40, 1e-44, 1e-50, 1e-70])
+def test_clipping_by_any_factor(dtype, into, ratio):
+    # gradients of all sizes beside some that are as large as the norm
+    g = [normal(5, (40001,), 1e35, dtype), normal(6, (3,), 1e36, dtype), normal(7, (9000,), 1.0, dtype)]
+    before = [t.clone() for t in g]
+    outs = None if into is None else [torch.empty(t.shape, dtype=into, device=DEV) for t in g]
+    max_norm = math.sqrt(squares(g)) * ratio
+    total, norm = norm_of(g, max_norm, outs)
+    assert math.isfinite(norm)
+    for t, o, b in zip(g, g if outs is None else outs, before):
+        w = b.to(F64) * (max_norm / math.sqrt(total))
+        # the quotient and the product in fp32, the output's rounding; below 2^-126 in steps of 2^-149 (fp32) or 2^-133 (bf16)
+        step = 2.0 ** -149 if o.dtype == F32 else 2.0 ** -133
+        assert_within(o, w, (U[o.dtype] + 3 * E) * w.abs() + 0.51 * step + 2.0 ** -149, f"{ratio}")
