@@ -293,6 +293,8 @@ def _heads(t: torch.Tensor, name: str, device: int):
     if t.dim() != 3:
         _refuse(f"{name} must be tokens x heads x head_dim")
     tokens, heads, dim = t.shape
+    if dim == 0:
+        _refuse(f"{name}: head_dim must not be 0")
     ld, step, unit = t.stride()
     if (unit != 1 and dim != 1) or (step != dim and heads != 1):
         _refuse(f"{name}: the heads of a token must lie side by side")

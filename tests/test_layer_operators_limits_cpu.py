@@ -1,7 +1,9 @@
 """Arguments of rotary positions, attention and clipping at the ends of what their types hold: refused, or answered right, without a GPU."""
 import pytest
+import torch
 
 import paper_2608_00455_b200 as dte
+from paper_2608_00455_b200 import operators as ops
 from test_layer_operators_cpu import forward, refused
 
 SMALLEST = 2.0 ** -126          # of fp32's normal numbers; half a step below it, 2^-126 - 2^-150, is a tie that rounds up to it
@@ -15,3 +17,19 @@ def test_attention_refuses_a_scale_that_fp32_cannot_hold(scale):
 @pytest.mark.parametrize("scale", [SMALLEST, SMALLEST * (1 - 2.0 ** -24), 1e-3, 2e38])
 def test_attention_takes_every_scale_that_fp32_holds(scale):
     refused(forward(scale=scale), "device")          # everything else is in order
+
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    """Tensors on the CPU pass for a device's (ordinal -1, which the library refuses last of all): the binding's own checks alone."""
+    monkeypatch.setattr(ops, "_device", lambda t, name: -1)
+    monkeypatch.setattr(ops, "_stream", lambda stream, device: None)
+
+
+def test_heads_without_columns_are_refused(on_the_host):
+    x, t, f, b = torch.zeros(4, 1, 0), torch.zeros(4, dtype=torch.int64), torch.ones(4, dtype=torch.float64), torch.zeros(4096, dtype=torch.uint8)
+    for call in (lambda: dte.dte_rope(x, None, t, f), lambda: dte.dte_attention_forward(x, x, x, b, x, None),
+                 lambda: dte.dte_attention_backward(x, x, x, x, torch.zeros(1, 4), x, b, x, x, x, b)):
+        with pytest.raises(dte.DteError, match="head_dim") as e:
+            call()
+        assert e.value.status == 1
