@@ -317,14 +317,22 @@ def dte_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor
     """Turns the first 2 * len(frequencies) columns of every head of q and k (tokens, heads, head_dim) by positions * frequencies,
     in place where no output is given; inverse: the gradient."""
     device = _device(q, "q")
-    m, _, _, dim = _heads(q, "q", device)
-    o = m if q_out is None else _heads(q_out, "q_out", device)[0]
+    m, rows, heads, dim = _heads(q, "q", device)
+    o = m
+    if q_out is not None:
+        o, *shape = _heads(q_out, "q_out", device)
+        if shape != [rows, heads, dim]:
+            _refuse("q_out must have its input's shape")
     mk = ok = None
     if k is not None:
-        mk, _, _, dim_k = _heads(k, "k", device)
+        mk, rows, heads, dim_k = _heads(k, "k", device)
         if dim_k != dim:
             _refuse("q and k must have one head_dim")
-        ok = mk if k_out is None else _heads(k_out, "k_out", device)[0]
+        ok = mk
+        if k_out is not None:
+            ok, *shape = _heads(k_out, "k_out", device)
+            if shape != [rows, heads, dim]:
+                _refuse("k_out must have its input's shape")
     elif k_out is not None:
         _refuse("k_out without k")
     p, _ = _ids(positions, "positions", device)

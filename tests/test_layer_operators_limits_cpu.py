@@ -33,3 +33,15 @@ def test_heads_without_columns_are_refused(on_the_host):
         with pytest.raises(dte.DteError, match="head_dim") as e:
             call()
         assert e.value.status == 1
+
+
+def test_outputs_of_rotary_positions_have_their_inputs_shapes(on_the_host):
+    # two heads of 8 columns have the columns of one head of 16, and are something else
+    q, k, t, f = torch.zeros(4, 2, 8), torch.zeros(4, 4, 8), torch.zeros(4, dtype=torch.int64), torch.ones(4, dtype=torch.float64)
+    for outs, word in (((torch.zeros(4, 1, 16), None), "q_out"), ((torch.zeros(4, 4, 4), None), "q_out"), ((None, torch.zeros(4, 2, 16)), "k_out"),
+                       ((torch.zeros(2, 4, 8), None), "q_out")):
+        with pytest.raises(dte.DteError, match=f"{word} must have") as e:
+            dte.dte_rope(q, k, t, f, *outs)
+        assert e.value.status == 1
+    with pytest.raises(dte.DteError, match="device"):          # everything else is in order
+        dte.dte_rope(q, k, t, f, torch.zeros(4, 2, 8), torch.zeros(4, 4, 8))
