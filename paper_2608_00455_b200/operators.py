@@ -320,8 +320,8 @@ def dte_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor
     m, rows, heads, dim = _heads(q, "q", device)
     o = m
     if q_out is not None:
-        o, *shape = _heads(q_out, "q_out", device)
-        if shape != [rows, heads, dim]:
+        o, r, h, d = _heads(q_out, "q_out", device)
+        if d != dim or h != heads or r != rows:
             _refuse("q_out must have its input's shape")
     mk = ok = None
     if k is not None:
@@ -330,8 +330,8 @@ def dte_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor
             _refuse("q and k must have one head_dim")
         ok = mk
         if k_out is not None:
-            ok, *shape = _heads(k_out, "k_out", device)
-            if shape != [rows, heads, dim]:
+            ok, r, h, d = _heads(k_out, "k_out", device)
+            if d != dim or h != heads or r != rows:
                 _refuse("k_out must have its input's shape")
     elif k_out is not None:
         _refuse("k_out without k")
