@@ -184,19 +184,21 @@ extern "C" dte_status dte_rope_frequencies(uint32_t rot, double base, uint32_t s
     if (!frequencies || !amplitude) return op_fail(DTE_ERR_INVALID_ARG, "frequencies or amplitude is null");
     if (scaling == DTE_ROPE_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
     double lo = 0, hi = 0;
+    bool slow = false;         // even the first pair turns fewer than slow_turns times
     if (scaling == DTE_ROPE_RAMP) {
         // index of the pair that turns n times over the original positions: base^(-2 i / rot) * positions = 2 pi n
         const double two_pi = 6.28318530717958647693;
         auto index = [&](double n) { return rot * std::log(original_positions / (n * two_pi)) / (2 * std::log(base)); };
         lo = std::fmax(0.0, std::floor(index(fast_turns)));
         hi = std::fmin(rot - 1.0, std::ceil(index(slow_turns)));
+        slow = index(slow_turns) < 0;
     }
     for (uint32_t i = 0; i < rot / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / rot);
         if (scaling == DTE_ROPE_LINEAR) {
             frequencies[i] = f / factor;
         } else if (scaling == DTE_ROPE_RAMP) {
-            const double ramp = std::fmin(1.0, std::fmax(0.0, (i - lo) / std::fmax(hi - lo, 1e-3)));
+            const double ramp = slow ? 1.0 : std::fmin(1.0, std::fmax(0.0, (i - lo) / std::fmax(hi - lo, 1e-3)));
             frequencies[i] = f * (1.0 - ramp) + f / factor * ramp;
         } else {
             frequencies[i] = f;

@@ -1,4 +1,6 @@
 """Arguments of rotary positions, attention and clipping at the ends of what their types hold: refused, or answered right, without a GPU."""
+import math
+
 import pytest
 import torch
 
@@ -45,3 +47,18 @@ def test_outputs_of_rotary_positions_have_their_inputs_shapes(on_the_host):
         assert e.value.status == 1
     with pytest.raises(dte.DteError, match="device"):          # everything else is in order
         dte.dte_rope(q, k, t, f, torch.zeros(4, 2, 8), torch.zeros(4, 4, 8))
+
+
+@pytest.mark.parametrize("rot,base,positions", [(128, 1e6, 6.0), (128, 1e6, 2.0), (2, 1e4, 1.0), (64, 1e4, 6.28)])
+def test_a_ramp_where_no_pair_turns_once(rot, base, positions):
+    # the fastest pair turns positions / (2 pi) times, fewer than slow_turns = 1: every pair is squeezed, the fastest too
+    plain, _ = dte.dte_rope_frequencies(rot, base)
+    f, _ = dte.dte_rope_frequencies(rot, base, dte.DTE_ROPE_RAMP, 4.0, positions)
+    assert positions / (2 * math.pi) < 1
+    assert torch.equal(f, plain / 4)
+
+
+def test_a_ramp_where_every_pair_turns_often():
+    plain, _ = dte.dte_rope_frequencies(8, 10.0)
+    f, _ = dte.dte_rope_frequencies(8, 10.0, dte.DTE_ROPE_RAMP, 4.0, 1e9)
+    assert torch.equal(f, plain)
