@@ -183,6 +183,7 @@ extern "C" dte_status dte_rope_frequencies(uint32_t rot, double base, uint32_t s
         return op_fail(DTE_ERR_INVALID_ARG, "the ramp needs original_positions > 0 and fast_turns >= slow_turns > 0");
     if (!frequencies || !amplitude) return op_fail(DTE_ERR_INVALID_ARG, "frequencies or amplitude is null");
     if (scaling == DTE_ROPE_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+    if (!std::isfinite(base)) return op_fail(DTE_ERR_INVALID_ARG, "base times the factor's power is beyond fp64");
     double lo = 0, hi = 0;
     bool slow = false;         // even the first pair turns fewer than slow_turns times
     if (scaling == DTE_ROPE_RAMP) {

@@ -62,3 +62,10 @@ def test_a_ramp_where_every_pair_turns_often():
     plain, _ = dte.dte_rope_frequencies(8, 10.0)
     f, _ = dte.dte_rope_frequencies(8, 10.0, dte.DTE_ROPE_RAMP, 4.0, 1e9)
     assert torch.equal(f, plain)
+
+
+@pytest.mark.parametrize("args", [(4, 1e200, dte.DTE_ROPE_BASE, 1e60), (128, 1e308, dte.DTE_ROPE_BASE, 4.0)])
+def test_a_changed_base_beyond_fp64_is_refused(args):
+    with pytest.raises(dte.DteError, match="base") as e:
+        dte.dte_rope_frequencies(*args)
+    assert e.value.status == 1
