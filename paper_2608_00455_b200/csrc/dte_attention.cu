@@ -472,8 +472,8 @@ dte_status encode_heads(CUtensorMap* map, const dte_matrix* m, uint32_t head_dim
     return encode_3d(map, m->data, {head_dim, m->cols / head_dim, m->rows}, {head_dim * 2ull, ld * 2}, {64, 1, kAttTile});
 }
 
-static AttParams att_params(const dte_matrix* q, const dte_matrix* k, const dte_matrix* v, uint32_t head_dim, const void* plan, uint64_t plan_bytes,
-                            double scale, uint64_t* flags) {
+static AttParams att_params(const dte_matrix* q, const dte_matrix* k, uint32_t head_dim, const void* plan, uint64_t plan_bytes, double scale,
+                            uint64_t* flags) {
     AttParams p = {};
     p.plan_bytes = plan_bytes;
     p.plan = static_cast<const uint8_t*>(plan);
@@ -483,12 +483,6 @@ static AttParams att_params(const dte_matrix* q, const dte_matrix* k, const dte_
     p.scale = (float)scale;
     p.k2 = (float)(scale * kLog2eD);
     p.wait_limit = g_att_wait_limit.load(std::memory_order_relaxed);
-    p.q = static_cast<const __nv_bfloat16*>(q->data);
-    p.k = static_cast<const __nv_bfloat16*>(k->data);
-    p.v = static_cast<const __nv_bfloat16*>(v->data);
-    p.q_ld = q->ld;
-    p.k_ld = k->ld;
-    p.v_ld = v->ld;
     p.flags = flags;
     return p;
 }
@@ -542,7 +536,7 @@ extern "C" dte_status dte_attention_forward(const dte_matrix* q, const dte_matri
     OpDeviceGuard g;
     int sms = 0;
     if ((s = g.enter(device, &sms)) != DTE_OK) return s;
-    AttParams p = att_params(q, k, v, head_dim, plan, plan_bytes, scale, flags);
+    AttParams p = att_params(q, k, head_dim, plan, plan_bytes, scale, flags);
     p.out = static_cast<__nv_bfloat16*>(out->data);
     p.out_ld = out->ld;
     p.lse = lse;
@@ -603,7 +597,7 @@ extern "C" dte_status dte_attention_backward(const dte_matrix* q, const dte_matr
     OpDeviceGuard g;
     int sms = 0;
     if ((s = g.enter(device, &sms)) != DTE_OK) return s;
-    AttParams p = att_params(q, k, v, head_dim, plan, plan_bytes, scale, flags);
+    AttParams p = att_params(q, k, head_dim, plan, plan_bytes, scale, flags);
     p.o = static_cast<const __nv_bfloat16*>(out->data);
     p.d_o = static_cast<const __nv_bfloat16*>(dout->data);
     p.o_ld = out->ld;

@@ -43,8 +43,8 @@ struct AttParams {
     bool pair_heads;
     uint32_t wait_limit;       // tries of a wait inside the kernel
     float scale, k2;           // k2: scale * log2(e)
-    const __nv_bfloat16 *q, *k, *v, *o, *d_o;
-    uint64_t q_ld, k_ld, v_ld, o_ld, do_ld;
+    const __nv_bfloat16 *o, *d_o;          // q, k, v and d_o as operands of products come through tensor maps
+    uint64_t o_ld, do_ld;
     __nv_bfloat16 *out, *dq, *dk, *dv;
     uint64_t out_ld, dq_ld, dk_ld, dv_ld;
     float *lse, *delta;
@@ -124,13 +124,13 @@ __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uin
     }
 }
 
-// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head; steps FROM to TO of 16 along K.  HALF: columns of tensor memory
-// from A's first 64 bf16 to the other 64.
-template <uint32_t HALF, uint32_t FROM = 0, uint32_t TO = kAttTile / 16>
+// D (+)= A B: A 128 x 128 in tensor memory, B 128 rows of a head.  HALF: columns of tensor memory from A's first 64 bf16 to the
+// other 64.
+template <uint32_t HALF>
 __device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
     const uint64_t db = operand_desc(b, kChunkBytes);
 #pragma unroll
-    for (uint32_t i = FROM; i < TO; ++i) mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, db + (i * 2048 >> 4), desc, add || i != 0);
+    for (uint32_t i = 0; i < kAttTile / 16; ++i) mma_bf16_tmem(d, a + (i / 4) * HALF + (i % 4) * 8, db + (i * 2048 >> 4), desc, add || i != 0);
 }
 
 // Columns c .. c + 31 of this thread's row in tensor memory, times by, as bf16.  Every lane writes to another row: whole sectors where
