@@ -629,7 +629,7 @@ typedef struct dte_tensor {
 
 /* *sum_squares (DEVICE, fp64) = sum of the squares of all elements, added to what it holds if accumulate != 0.  Ranks that
  * hold parts of the gradients add their sums before clipping.  Squares that fp32 would overflow or lose are
- * formed in fp64; sums of 32 to 64 squares in fp32, everything beyond in fp64, in an order that does not depend on the device. */
+ * formed in fp64; sums of at most 32 squares in fp32, everything beyond in fp64, in an order that does not depend on the device. */
 DTE_API uint64_t dte_grad_sum_squares_workspace_bytes(uint64_t n_tensors);
 DTE_API dte_status dte_grad_sum_squares(const dte_tensor* tensors, uint64_t n_tensors, int accumulate, double* sum_squares,
                                         void* workspace, uint64_t workspace_bytes, int device, void* cuda_stream);

@@ -1,5 +1,5 @@
-// Shared by the operators at the two ends of the model (embedding, norm, linear cross entropy):
-// argument checks on the host, typed vector access and reductions on the device, and the sorted-token
+// Shared by the operators of the model and its training step (embedding, norm, rotary positions, attention, linear cross entropy,
+// gradient norm and clipping): argument checks on the host, typed vector access and reductions on the device, and the sorted-token
 // sum that the embedding gradient and the head's gradient both need.
 #pragma once
 
