@@ -138,9 +138,10 @@ __global__ void __launch_bounds__(kGradThreads) join_squares_kernel(const double
     if (threadIdx.x == 0) *out = accumulate ? *out + sum : sum;
 }
 
-// y = x * factor * power; power, a power of two, is for factors that fp32 would hold as subnormal numbers (see clip_kernel).
-template <typename In, typename Out>
-__device__ void chunk_scale(const In* x, Out* y, uint32_t n, float factor, float power) {
+constexpr float kTinyUnit = 0x1p-126f;
+// y = x * factor; TINY: times kTinyUnit, for factors that fp32 would hold as subnormal numbers (see clip_kernel).
+template <bool TINY, typename In, typename Out>
+__device__ void chunk_scale(const In* x, Out* y, uint32_t n, float factor) {
     uint32_t at = 0;
     if (!(((uintptr_t)x | (uintptr_t)y) & 15u)) {
         auto finish = [&](const Raw8<In>& r, uint32_t i) {
@@ -148,7 +149,7 @@ __device__ void chunk_scale(const In* x, Out* y, uint32_t n, float factor, float
             float f[8];
             r.get(f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = f[j] * factor * power;
+            for (int j = 0; j < 8; ++j) f[j] = TINY ? f[j] * factor * kTinyUnit : f[j] * factor;
             o.set(f);
             o.store(y + i);
         };
@@ -168,12 +169,31 @@ __device__ void chunk_scale(const In* x, Out* y, uint32_t n, float factor, float
         }
         at = n / 8 * 8;
     }
-    for (uint32_t i = at + threadIdx.x; i < n; i += kGradThreads) y[i] = from_f<Out>(to_f(x[i]) * factor * power);
+    for (uint32_t i = at + threadIdx.x; i < n; i += kGradThreads) y[i] = from_f<Out>(TINY ? to_f(x[i]) * factor * kTinyUnit : to_f(x[i]) * factor);
+}
+
+// This CTA's chunks of all tensors.
+template <bool TINY, uint32_t N>
+__device__ __forceinline__ void scale_chunks(const GradList<N>& l, float factor) {
+    for (uint32_t c = blockIdx.x; c < l.first[l.n]; c += gridDim.x) {
+        const uint32_t t = tensor_of(l, c);
+        const bool in16 = l.numel[t] & kInBf16, out16 = l.numel[t] & kOutBf16;
+        if (!TINY && factor == 1.f && l.in[t] == l.out[t]) continue;
+        const uint64_t numel = l.numel[t] & ~(kInBf16 | kOutBf16), at = (uint64_t)(c - l.first[t]) * kGradChunk;
+        const uint32_t n = (uint32_t)(numel - at < kGradChunk ? numel - at : kGradChunk);
+        const __nv_bfloat16* x16 = static_cast<const __nv_bfloat16*>(l.in[t]) + at;
+        const float* x32 = static_cast<const float*>(l.in[t]) + at;
+        __nv_bfloat16* y16 = static_cast<__nv_bfloat16*>(l.out[t]) + at;
+        float* y32 = static_cast<float*>(l.out[t]) + at;
+        if (in16 && out16) chunk_scale<TINY>(x16, y16, n, factor);
+        else if (in16) chunk_scale<TINY>(x16, y32, n, factor);
+        else if (out16) chunk_scale<TINY>(x32, y16, n, factor);
+        else chunk_scale<TINY>(x32, y32, n, factor);
+    }
 }
 
 template <uint32_t N>
 __global__ void __launch_bounds__(kGradThreads) clip_kernel(const __grid_constant__ ClipParams<N> p) {
-    const GradList<N>& l = p.list;
     const double norm = sqrt(*p.sum_squares);
     const float shown = (float)norm;
     if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = shown;
@@ -181,23 +201,8 @@ __global__ void __launch_bounds__(kGradThreads) clip_kernel(const __grid_constan
     const double quotient = norm > p.max_norm && shown <= 0x1.fffffep127f ? p.max_norm / norm : 1.0;
     // Below fp32's normal numbers the quotient would lose bits that a large element's product can hold: it is brought up by 2^126,
     // and the product down again, which is exact unless the product is itself subnormal.
-    const bool tiny = quotient < 0x1p-126;
-    const float power = tiny ? 0x1p-126f : 1.f, factor = (float)(tiny ? quotient * 0x1p126 : quotient);
-    for (uint32_t c = blockIdx.x; c < l.first[l.n]; c += gridDim.x) {
-        const uint32_t t = tensor_of(l, c);
-        const bool in16 = l.numel[t] & kInBf16, out16 = l.numel[t] & kOutBf16;
-        if (factor == 1.f && power == 1.f && l.in[t] == l.out[t]) continue;
-        const uint64_t numel = l.numel[t] & ~(kInBf16 | kOutBf16), at = (uint64_t)(c - l.first[t]) * kGradChunk;
-        const uint32_t n = (uint32_t)(numel - at < kGradChunk ? numel - at : kGradChunk);
-        const __nv_bfloat16* x16 = static_cast<const __nv_bfloat16*>(l.in[t]) + at;
-        const float* x32 = static_cast<const float*>(l.in[t]) + at;
-        __nv_bfloat16* y16 = static_cast<__nv_bfloat16*>(l.out[t]) + at;
-        float* y32 = static_cast<float*>(l.out[t]) + at;
-        if (in16 && out16) chunk_scale(x16, y16, n, factor, power);
-        else if (in16) chunk_scale(x16, y32, n, factor, power);
-        else if (out16) chunk_scale(x32, y16, n, factor, power);
-        else chunk_scale(x32, y32, n, factor, power);
-    }
+    if (quotient < (double)kTinyUnit) scale_chunks<true>(p.list, (float)(quotient / (double)kTinyUnit));
+    else scale_chunks<false>(p.list, (float)quotient);
 }
 
 static dte_status check_tensors(const dte_tensor* t, uint64_t n) {
