@@ -33,6 +33,10 @@ constexpr uint32_t kBwdWarps = 8;                 // that work on scores
 constexpr int kFewRegs = 72, kManyRegs = 208;     // 128 * (72 + 2 * 208) = 62464 of the 384 * 168 = 64512 at launch
 constexpr uint32_t kRing3 = 3, kRing2 = 2;         // tiles in flight of the two streams, a ring each: every barrier has one reader in order
 constexpr uint32_t kBwdSmem = (2 + kRing3 + kRing2) * kTileBytes;
+// The score warps count their steps to where places and phases of both rings repeat: a CTA may take more than 2^32 of them.
+constexpr uint32_t kSteps = 4 * kRing3;
+static_assert(kSteps % (2 * kRing2) == 0, "");
+__device__ __forceinline__ uint32_t next_step(uint32_t g) { return g + 1 == kSteps ? 0 : g + 1; }
 constexpr uint32_t kHalf = kAttTile / 2;          // columns of a tile that a thread works on
 // In tensor memory a tile of scores takes 128 columns.  The bf16 operand made of it lies over it, each half over the
 // columns that the same threads have read.
@@ -277,7 +281,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t desc_s = mma_desc(kAttTile, kAttTile, false, false), steps = (p.head_dim + 15) / 16;
             uint32_t q_taken = 0, works = 0, g = 0;
             RingAt<kRing2> va;
-            bool ok = true;
+            bool ok = true, begun = false;           // begun: there is a dP in front whose reading has to be waited for
             auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(bar(b), parity, p.wait_limit, gave_up); };
             PlanItem it;
             uint32_t h;
@@ -289,7 +293,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
                     const uint32_t v = uniform(vt0 + va.i * kTileBytes), release = uniform(bar(kVEmpty + va.i));
                     va.next();
                     ++g;
-                    if (g > 1 && !wait(kDpRead, g & 1)) break;
+                    if (begun && !wait(kDpRead, g & 1)) break;
+                    begun = true;
                     if (elect_lane()) {
                         mma_rows(tmem + 256, do0, v, steps, desc_s);
                         mma_commit<1>(bar(kDpFull));
@@ -339,7 +344,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             const uint32_t n = it.tile + 1, row = it.tile * kAttTile + r;
             const uint64_t stat = h * p.tokens + it.start + min(row, it.len - 1);
             const float lse2 = p.lse_in[stat] * -(float)kLog2eD, delta = p.delta[stat];
-            for (uint32_t t = 0; t < n; ++t, ++g) {
+            for (uint32_t t = 0; t < n; ++t, g = next_step(g)) {
                 const uint32_t s_at = mine + (g & 1) * 128 + half * kHalf;
                 if (!wait(kSFull + (g & 1), g >> 1 & 1)) break;
                 float z[kHalf];
@@ -682,7 +687,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         DkvWork f;
         while (ok && take_work(works, f)) {
             uint32_t t = f.tile;
-            for (uint32_t j = 0; j < f.n; ++j, ++g) {
+            for (uint32_t j = 0; j < f.n; ++j, g = next_step(g)) {
                 const uint32_t first = t * kAttTile + half * kHalf;       // query of this thread's first column
                 const bool edge = t == f.tile || (t + 1) * kAttTile > f.len;
                 const bool tail = (t + 1) * kAttTile > f.len;
