@@ -560,7 +560,7 @@ DTE_API void dte_linear_ce_set_wait_limit(uint32_t tries);
  *   DTE_ROPE_RAMP    f_i where a pair turns more than fast_turns times over original_positions, f_i / factor where
  *                    fewer than slow_turns, in between a ramp over the pair's index (its ends rounded outwards to
  *                    whole indices, inside [0, rot - 1]); amplitude 0.1 ln(factor) + 1 (as YaRN defines them)
- * The amplitude of the others is 1.  base > 1, factor >= 1, rot even, 2 <= rot <= 1024.  Host only. */
+ * The amplitude of the others is 1.  base > 1 and finite, a changed one too; factor >= 1, rot even, 2 <= rot <= 1024.  Host only. */
 #define DTE_ROPE_PLAIN 0u
 #define DTE_ROPE_LINEAR 1u
 #define DTE_ROPE_BASE 2u
@@ -593,7 +593,7 @@ DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t h
  * allowed) once per packed batch and leaves in `plan` (DEVICE, 256-byte aligned) the order of work that the calls on
  * batches with these starts take, in every layer, forwards and backwards.  Starts that decrease or leave the range set
  * DTE_DEV_BOUNDS and give a plan without work; a call whose token count differs from its plan's sets DTE_DEV_BOUNDS and
- * writes nothing.  plan_bytes of the calls: the size of the plan's buffer.  At most 2^24 tokens and 2^20 sequences. */
+ * writes nothing.  A plan of other sequences with the same number of tokens is not noticed.  plan_bytes of the calls: the size of the plan's buffer.  At most 2^24 tokens and 2^20 sequences. */
 DTE_API uint64_t dte_attention_plan_bytes(uint64_t tokens, uint64_t n_sequences);
 DTE_API dte_status dte_attention_plan(const dte_ids* starts, uint64_t tokens, void* plan, uint64_t plan_bytes, uint64_t* flags,
                                       int device, void* cuda_stream);

@@ -5,7 +5,8 @@
 // Bound by the tensor cores (4 head_dim operations per head and pair of a query and a key that it sees) for long sequences, by what a
 // tile costs beside its products for short ones.  Measured, heads of 128: 32768 tokens, 32 heads on 8: 8.1 ms in a loop, 1.09 PFLOP/s
 // at the power limit, and 7.1 to 7.4 ms = 1.2 PFLOP/s over ten calls (a bf16 library product: 1.39 and 1.69); 8192 tokens in 19
-// sequences, 32 heads on 4: 84 us (0.57 PFLOP/s); 77 tokens: 8.4 us.  A step of two slots takes 3600 cycles of which the tensor cores
+// sequences, 32 heads on 4: 81 to 84 us (0.58 PFLOP/s); 77 tokens: 8.3 us; heads of 64, 32 on 8: 32768 tokens 6.0 ms (0.73 PFLOP/s: half the
+// products for the same exponentials), 8192 in 19 sequences 69 us.  A step of two slots takes 3600 cycles of which the tensor cores
 // work 2048; a slot's own chain is 1750 of softmax, 1024 of products, and 600 of barriers and waiting for its turn.
 #include <atomic>
 
@@ -29,7 +30,8 @@ struct PlanParams {
 };
 
 // Lists the tiles of all sequences, and the pairs of tiles that an odd group of heads takes, the ones with the most keys in front of them
-// first: CTAs that take them in turn finish together.  Tiles from kPlanLevels on count as equally long.  One CTA.
+// first: CTAs that take them in turn finish together.  Tiles from kPlanLevels on count as equally long.  One CTA, a warp per sequence,
+// bound by the latency of the starts' loads: 6 us for 19 sequences, 53 for 1000, 4.7 ms for 100000.
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanParams p) {
     __shared__ uint32_t s_at[2][kPlanLevels];        // tiles of a level, then where the next one of it goes
     __shared__ uint32_t s_warp[2][kPlanThreads / 32];

@@ -13,11 +13,11 @@
 //
 // p and dz are rounded to bf16, the operand type of the products they enter, and delta is made of out as it was rounded; sums are fp32.  For
 // random inputs dq, dk and dv are then 2.7e-3 to 3.0e-3, 2.4e-3 to 2.6e-3 and 2.3e-3 off (relative, rms), of which their own rounding
-// to bf16 is 1.7e-3.  dz as two bf16 numbers makes the first two 2.2e-3 and 1.9e-3 and the passes 16 % slower, so it is not kept so.
+// to bf16 is 1.7e-3; where sequences have few tokens, dout v^T - delta cancels more, and dq is up to 4.1e-3, dk 3.6e-3 off.  dz as two bf16 numbers makes the first two 2.2e-3 and 1.9e-3 and the passes 16 % slower, so it is not kept so.
 //
 // Measured, heads of 128, all three kernels: 16384 tokens, 32 heads on 8: 6.7 ms in a loop at the power limit (0.82 PFLOP/s of the five
-// products that the formulas need, 1.15 of the seven that are made); 8192 tokens in 19 sequences, 32 heads on 4: 296 us; 4001 tokens in 57
-// sequences, 16 heads of 64: 70 us.  A step takes 3300 cycles in the first pass, 2048 of them the tensor cores', and 2200 in the second,
+// products that the formulas need, 1.15 of the seven that are made); 8192 tokens in 19 sequences, 32 heads on 4: 299 us; 4001 tokens in 57
+// sequences, 16 heads of 64: 72 us.  A step takes 3300 cycles in the first pass, 2048 of them the tensor cores', and 2200 in the second,
 // 1536: the chain of p (1500 and 1250 cycles, 1024 of which the special function unit needs) and of the products that wait for it sets the
 // pace.  A piece of work costs 4000 to 7000 cycles beside its steps.  Tried and left: sixteen score warps (dk / dv 3.6 to 3.8 ms), p in
 // shared memory so that the next S need not wait for dv (7.2 ms against 6.7: operands of products in shared memory cost its bandwidth), p in

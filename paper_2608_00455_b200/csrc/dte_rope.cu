@@ -3,6 +3,7 @@
 // Bound by memory: every element is read once and written once.  Angles cost two 64-bit multiplications and one sine and
 // cosine per token and pair, shared by all heads of the token through shared memory.  Measured: 16384 tokens, 32 + 8 heads of 128 in bf16:
 // 60 us = 5.6 TB/s; 8191 tokens, 32 + 4 heads of 128 in fp32, half of each turned, interleaved: 48 us = 6.2 TB/s (a copy: 6.46); 8 tokens: 2.5 us.
+// Halves that are no multiple of 8 columns take 4-byte accesses: 16384 tokens, 32 + 8 heads of 72 in bf16: 60 us = 3.2 TB/s, 36 of 96 columns 116 us.
 #include "dte_ops.cuh"
 
 namespace dte {
