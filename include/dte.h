@@ -593,7 +593,8 @@ DTE_API dte_status dte_rope(const dte_matrix* q, const dte_matrix* k, uint32_t h
  * allowed) once per packed batch and leaves in `plan` (DEVICE, 256-byte aligned) the order of work that the calls on
  * batches with these starts take, in every layer, forwards and backwards.  Starts that decrease or leave the range set
  * DTE_DEV_BOUNDS and give a plan without work; a call whose token count differs from its plan's sets DTE_DEV_BOUNDS and
- * writes nothing.  A plan of other sequences with the same number of tokens is not noticed.  plan_bytes of the calls: the size of the plan's buffer.  At most 2^24 tokens and 2^20 sequences. */
+ * writes nothing.  A plan of other sequences with the same number of tokens is not noticed.  plan_bytes of the calls: the
+ * size of the plan's buffer.  At most 2^24 tokens and 2^20 sequences. */
 DTE_API uint64_t dte_attention_plan_bytes(uint64_t tokens, uint64_t n_sequences);
 DTE_API dte_status dte_attention_plan(const dte_ids* starts, uint64_t tokens, void* plan, uint64_t plan_bytes, uint64_t* flags,
                                       int device, void* cuda_stream);

@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         const uint32_t s = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = quarter * 32 << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
         const float k2 = p.k2;
-        uint32_t tiles = 0, items_done = 0, loads = 0;      // loads: tiles of keys and values of the work so far, as far as the ring's place and phase go
+        uint32_t tiles = 0, items_done = 0, loads = 0;      // loads: tiles of keys and values of the work so far, modulo the ring's period
         bool ok = true;
         auto wait = [&](uint32_t b, uint32_t parity) { return ok = ok && warp_wait(b, parity, p.wait_limit, gave_up); };
         for (Turns work(list, total, p.units); work.more() && ok;) {

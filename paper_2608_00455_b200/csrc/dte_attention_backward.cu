@@ -13,7 +13,8 @@
 //
 // p and dz are rounded to bf16, the operand type of the products they enter, and delta is made of out as it was rounded; sums are fp32.  For
 // random inputs dq, dk and dv are then 2.7e-3 to 3.0e-3, 2.4e-3 to 2.6e-3 and 2.3e-3 off (relative, rms), of which their own rounding
-// to bf16 is 1.7e-3; where sequences have few tokens, dout v^T - delta cancels more, and dq is up to 4.1e-3, dk 3.6e-3 off.  dz as two bf16 numbers makes the first two 2.2e-3 and 1.9e-3 and the passes 16 % slower, so it is not kept so.
+// to bf16 is 1.7e-3; where sequences have few tokens, dout v^T - delta cancels more, and dq is up to 4.1e-3, dk 3.6e-3 off.  dz as two
+// bf16 numbers makes the first two 2.2e-3 and 1.9e-3 and the passes 16 % slower, so it is not kept so.
 //
 // Measured, heads of 128, all three kernels: 16384 tokens, 32 heads on 8: 6.7 ms in a loop at the power limit (0.82 PFLOP/s of the five
 // products that the formulas need, 1.15 of the seven that are made); 8192 tokens in 19 sequences, 32 heads on 4: 299 us; 4001 tokens in 57

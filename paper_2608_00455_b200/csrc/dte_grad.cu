@@ -2,8 +2,8 @@
 //
 // Both kernels are streams bound by memory: the norm reads every element once, clipping reads and writes every
 // element once.  Measured: sum of 965 M bf16 300 us = 6.4 TB/s, of 75 M fp32 51 us; clipping them into fp32 985 us = 5.9 TB/s and 97 us =
-// 6.2 TB/s (a copy: 6.46), in place 614 us = 6.3 TB/s and 108 us = 5.5 TB/s; six tensors of 2 M elements 3 + 2 + 4.5 us.  The list of tensors travels in the launch's parameters, so a call
-// needs no copy to the device and can be captured; a CTA finds the tensor of its next chunk by bisection.
+// 6.2 TB/s (a copy: 6.46), in place 614 us = 6.3 TB/s and 108 us = 5.5 TB/s; six tensors of 2 M elements 3 + 2 + 4.5 us.  The list of
+// tensors travels in the launch's parameters, so a call needs no copy to the device and can be captured; a CTA finds the tensor of its next chunk by bisection.
 #include "dte_ops.cuh"
 
 namespace dte {

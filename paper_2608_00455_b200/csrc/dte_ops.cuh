@@ -145,8 +145,9 @@ dte_status launch_sorted_sum(const SortedSum& p, int vec, void* workspace, bool 
 // A kernel launched with launch_after may start while the one before it in the stream still runs (its launch
 // costs nothing then); it calls wait_for_earlier before it touches memory, which returns when all earlier
 // work is complete and visible.  Used only inside a call, between its own kernels.  A kernel that works beside the one in front of
-// it instead, on what came before that, calls seen_earlier first and wait_for_earlier before it ends; the one in front calls
-// pass_on between its own wait and let_next_start.
+// it instead waits before it ends, so that what follows finds both done.  It touches what the caller passed and no kernel in front
+// of it in this call uses; where it needs what an earlier kernel of the call has written, it calls seen_earlier first, and the one in
+// front calls pass_on between its own wait and let_next_start.
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Lets the kernel behind this one start now, as far as there is room.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
